@@ -390,8 +390,97 @@ SALICACHE_API int salicache_attend(salicache_ctx* ctx, const void* d_q, const sa
 SALICACHE_API int salicache_attend_gqa(salicache_ctx* ctx, const void* d_q, int q_per_kv, const salicache_pools* pools,
                                        const int64_t* d_fill, float* d_out, void* cuda_stream);
 
-/* Synchronises `cuda_stream`, returns the deferred device status (0, E_CAPACITY or
- * E_NOCONVERGE; E_CUDA if the stream reports an error) and clears it. */
+/*
+ * Paged cache (the same quantisers, Sec. IV-B, for tokens that arrive a few at a time and for many sequences at once:
+ * questions, answers, the visual tokens of new frames).  One layer's keys and values live in pages of `page` token
+ * positions; a table names the pages of every sequence.  The caller owns all memory, one salicache_pages per layer.
+ *   d_data   [n_pages][2][heads][page][head_dim]  (0 = K, 1 = V): 16-bit elements (format SALICACHE_FP16), int8 codes
+ *            (SALICACHE_INT8), or int4 codes, two per byte, element 2j in the low nibble (SALICACHE_INT4)
+ *   d_scale  INT8: [n_pages][2][heads][page], INT4: [n_pages][2][heads][page][2] = (scale, zero), in the 16-bit type of
+ *            `dtype`; not used by SALICACHE_FP16
+ * One quantisation group is one head of one token (head_dim elements).
+ * Supported: page 16, 32, 64 or 128; head_dim 64 or 128; heads 1 .. 256; dtype SALICACHE_F16 or SALICACHE_BF16.  The
+ * context supplies the device and the status word; its frame size, L, heads, head_dim and group play no part here. */
+#define SALICACHE_F16  0
+#define SALICACHE_BF16 1
+typedef struct salicache_pages {
+    void* d_data;
+    void* d_scale;
+    int32_t n_pages, page, heads, head_dim;
+    int32_t format;          /* SALICACHE_FP16, SALICACHE_INT8 or SALICACHE_INT4                              */
+    int32_t dtype;           /* SALICACHE_F16 or SALICACHE_BF16: type of the rows, of 16-bit pages, of scales */
+} salicache_pages;
+
+/* A ragged batch of sequences.  Sequence b holds d_len[b] positions; position p lives in slot p % page of page
+ * d_table[b * table_width + p / page].  The n = d_row_start[b+1] - d_row_start[b] rows of the caller's arrays from
+ * d_row_start[b] on are its LAST n positions: row i is position d_len[b] - n + i (write first, attend to the same batch
+ * after).  n may be 0; rows with a negative position (n > d_len[b]) exist in no page.  Rows from d_row_start[n_seqs] on
+ * belong to nobody and are left as they are.  d_row_start is non-decreasing, within [0, n_rows].
+ * Positions at or past table_width * page, and positions whose table entry lies outside [0, n_pages), are in no page: a
+ * call that has to touch one records E_CAPACITY in the status word and treats it as stated with the call.  Table entries
+ * of positions that no row has to touch are never used: they may be stale.
+ * The offsets are read on the device: calls can be captured and replayed with other lengths of the same n_rows. */
+typedef struct salicache_seqs {
+    int32_t n_seqs, table_width;
+    int32_t n_rows;                /* rows in the caller's arrays                */
+    const int32_t* d_row_start;    /* DEVICE i32 [n_seqs + 1]                    */
+    const int32_t* d_len;          /* DEVICE i32 [n_seqs]: positions, new ones included */
+    const int32_t* d_table;        /* DEVICE i32 [n_seqs][table_width]           */
+} salicache_seqs;
+
+/*
+ * Writes the batch's rows into their pages.  d_K, d_V: DEVICE [n_rows] rows of [heads][head_dim] in the 16-bit type,
+ * k_stride / v_stride elements from row to row (>= heads * head_dim, a multiple of 8; slices of a fused projection
+ * are fine).  FP16 pages hold a copy.  With T the rounding to the 16-bit type and everything else single binary32
+ * operations, to nearest even:
+ *   INT8: s = T(max|x| / 127), 0 -> 1;           q = rint(x * (1/s)) clamped to +-127
+ *   INT4: zero = min x, s = T((max - zero) / 15), 0 -> 1;  q = rint((x - zero) * (1/s)) clamped to 0 .. 15
+ * (an s whose reciprocal overflows binary32 counts as 0).  Rows in no page are dropped (deferred E_CAPACITY for the
+ * reasons above; silently for a negative position).  Two rows of one call must not land in the same slot.
+ * Errors: E_NULL, E_SHAPE, E_ALIGN (16 bytes), E_PARAM (unsupported value; the current device is not the context's),
+ * E_CUDA.
+ */
+SALICACHE_API int salicache_paged_write(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
+                                        const void* d_K, const void* d_V, int64_t k_stride, int64_t v_stride,
+                                        void* cuda_stream);
+
+/*
+ * The inverse: the batch's rows as their pages hold them, T(q * s) and T(q * s + zero) (multiply, then add) or the
+ * copy.  Rows in no page come back as zeros.  To read whole sequences, let d_row_start be the running sum of d_len.
+ * Arguments and errors as for salicache_paged_write; d_K_out, d_V_out are written.
+ */
+SALICACHE_API int salicache_paged_read(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
+                                       void* d_K_out, void* d_V_out, int64_t k_stride, int64_t v_stride, void* cuda_stream);
+
+/*
+ * Attention of the batch's rows over their sequences' pages (Eq. 2 with the dequantisation fused in; the rows' own
+ * K and V have been written before).  Query head hq attends to key/value head hq / q_per_kv.  The row at position p
+ * sees position j when j <= p, j < d_len and (window == 0 or j > p - window or j < sinks): causal, optionally under a
+ * sliding window of `window` positions (its own among them) with the first `sinks` positions visible throughout.
+ *   score_j = softmax_scale * q . K^_j,  out = T(sum_j softmax(score)_j V^_j),  lse = ln sum_j e^score_j
+ * K^, V^ are the values salicache_paged_read returns.  Products are accumulated in binary32; the softmax weights go
+ * through the second product in the 16-bit type.  Positions in no page are left out (deferred E_CAPACITY).  A row that
+ * sees nothing: out = 0, lse = -infinity.  What pages hold at positions that no row of the sequence sees has no effect,
+ * NaN included; at positions that some rows see, V is finite.
+ *   d_q, d_out  DEVICE [n_rows] rows of [heads * q_per_kv][head_dim], q_stride / out_stride elements from row to row
+ *               (>= heads * q_per_kv * head_dim, multiples of 8)
+ *   d_lse       DEVICE f32 [n_rows][heads * q_per_kv], or NULL
+ *   d_work      DEVICE, 16-byte aligned, salicache_paged_work_bytes() of it: partial results of rows whose keys are
+ *               split.  Its content matters only while a call runs; calls that may overlap (other streams, captured
+ *               graphs replayed side by side) need one each.
+ * q_per_kv 1 .. 64; window, sinks >= 0; softmax_scale > 0 and finite.  Errors as for salicache_paged_write; E_SHAPE
+ * also when work_bytes is too small.
+ */
+SALICACHE_API int salicache_paged_attend(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
+                                         const void* d_q, int64_t q_stride, int q_per_kv, float softmax_scale, int window,
+                                         int sinks, void* d_out, int64_t out_stride, float* d_lse, void* d_work,
+                                         int64_t work_bytes, void* cuda_stream);
+
+/* Bytes of d_work for salicache_paged_attend over such pages (any batch), or a negative error. */
+SALICACHE_API int64_t salicache_paged_work_bytes(const salicache_ctx* ctx, const salicache_pages* pages, int q_per_kv);
+
+/* Synchronises `cuda_stream`, returns the deferred device status (0, E_CAPACITY, E_NOCONVERGE or
+ * E_EVICTED; E_CUDA if the stream reports an error) and clears it. */
 SALICACHE_API int salicache_poll_status(salicache_ctx* ctx, void* cuda_stream);
 
 #ifdef __cplusplus

@@ -13,6 +13,8 @@ from . import build as _build
 
 REUSE, PRUNE, INT4, INT8, FP16 = 0, 1, 2, 3, 4
 
+F16, BF16 = 0, 1
+
 E_NULL, E_SHAPE, E_ALIGN, E_PARAM, E_CUDA, E_CAPACITY, E_NOCONVERGE, E_NOMEM, E_EVICTED = -1, -2, -3, -4, -5, -6, -7, -8, -9
 
 
@@ -47,13 +49,29 @@ class Pools(C.Structure):
     ]
 
 
+class Pages(C.Structure):
+    _fields_ = [
+        ("d_data", C.c_void_p), ("d_scale", C.c_void_p),
+        ("n_pages", C.c_int32), ("page", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+        ("format", C.c_int32), ("dtype", C.c_int32),
+    ]
+
+
+class SeqsC(C.Structure):
+    _fields_ = [
+        ("n_seqs", C.c_int32), ("table_width", C.c_int32), ("n_rows", C.c_int32),
+        ("d_row_start", C.c_void_p), ("d_len", C.c_void_p), ("d_table", C.c_void_p),
+    ]
+
+
 EXPORTS = [
     "salicache_default_params", "salicache_create", "salicache_destroy", "salicache_strerror",
     "salicache_tokens_per_frame", "salicache_launch_count", "salicache_flow_score", "salicache_saliency", "salicache_select",
     "salicache_pack_kv", "salicache_unpack_kv", "salicache_poll_status", "salicache_saliency_noalloc",
     "salicache_frame_redundancy", "salicache_source_frames", "salicache_diff_score", "salicache_attend",
     "salicache_select_anchored", "salicache_select_ranked", "salicache_attend_gqa", "salicache_select_anchored_batch",
-    "salicache_frames_resident", "salicache_tokens_live",
+    "salicache_frames_resident", "salicache_tokens_live", "salicache_paged_write", "salicache_paged_read",
+    "salicache_paged_attend", "salicache_paged_work_bytes",
 ]
 
 _lib = None
@@ -95,12 +113,29 @@ def lib():
         _lib.salicache_attend_gqa.argtypes = [vp, vp, i32, C.POINTER(Pools), vp, vp, vp]
         _lib.salicache_saliency_noalloc.argtypes = [C.POINTER(Params), vp, i32, vp, vp, vp]
         _lib.salicache_frames_resident.argtypes = [vp, vp, vp, i32, C.POINTER(Pools), vp, vp]
+        _lib.salicache_paged_write.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, vp, i64, i64, vp]
+        _lib.salicache_paged_read.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, vp, i64, i64, vp]
+        _lib.salicache_paged_attend.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, i64, i32, C.c_float, i32, i32, vp, i64,
+                                                vp, vp, i64, vp]
+        _lib.salicache_paged_work_bytes.argtypes = [vp, C.POINTER(Pages), i32]
+        _lib.salicache_paged_work_bytes.restype = i64
         _lib.salicache_tokens_live.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp]
     return _lib
 
 
 def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
+
+
+def _dptr(t):
+    """As _ptr, for the paged calls: refuses host memory and tensors of another device than the current one, which the C
+    entry points cannot see."""
+    if t is None:
+        return None
+    import torch
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"a tensor on the current CUDA device expected, got one on {t.device}")
+    return C.c_void_p(t.data_ptr())
 
 
 def _stream(stream=None):
@@ -253,6 +288,30 @@ def salicache_tokens_live(ctx: Context, d_src, B: int, first_frame: int, d_resid
                                        _stream(stream)), "salicache_tokens_live")
 
 
+def salicache_paged_write(ctx: Context, pages: Pages, seqs: SeqsC, d_K, d_V, k_stride: int, v_stride: int, stream=None):
+    _check(lib().salicache_paged_write(ctx.handle, C.byref(pages), C.byref(seqs), _dptr(d_K), _dptr(d_V), k_stride, v_stride,
+                                       _stream(stream)), "salicache_paged_write")
+
+
+def salicache_paged_read(ctx: Context, pages: Pages, seqs: SeqsC, d_K_out, d_V_out, k_stride: int, v_stride: int, stream=None):
+    _check(lib().salicache_paged_read(ctx.handle, C.byref(pages), C.byref(seqs), _dptr(d_K_out), _dptr(d_V_out), k_stride, v_stride,
+                                      _stream(stream)), "salicache_paged_read")
+
+
+def salicache_paged_work_bytes(ctx: Context, pages: Pages, q_per_kv: int) -> int:
+    n = int(lib().salicache_paged_work_bytes(ctx.handle, C.byref(pages), q_per_kv))
+    if n < 0:
+        raise SalicacheError(n, "salicache_paged_work_bytes")
+    return n
+
+
+def salicache_paged_attend(ctx: Context, pages: Pages, seqs: SeqsC, d_q, q_stride: int, q_per_kv: int, softmax_scale: float,
+                           window: int, sinks: int, d_out, out_stride: int, d_lse, d_work, work_bytes: int, stream=None):
+    _check(lib().salicache_paged_attend(ctx.handle, C.byref(pages), C.byref(seqs), _dptr(d_q), q_stride, q_per_kv, softmax_scale,
+                                        window, sinks, _dptr(d_out), out_stride, _dptr(d_lse), _dptr(d_work), work_bytes,
+                                        _stream(stream)), "salicache_paged_attend")
+
+
 def salicache_poll_status(ctx: Context, stream=None) -> int:
     return int(lib().salicache_poll_status(ctx.handle, _stream(stream)))
 
@@ -280,3 +339,40 @@ class PoolSet:
     def nbytes(self) -> int:
         return sum(t.numel() * t.element_size() for t in
                    (self.fp16_pool, self.int8_codes, self.int8_scale, self.int4_codes, self.int4_sz))
+
+
+class PageSet:
+    """One layer's pages as torch tensors (memory only) plus the C struct that points at them.  `dtype` is torch.float16
+    or torch.bfloat16; existing tensors of the documented shapes can be given as `data` and `scale`."""
+
+    def __init__(self, n_pages: int, page: int, heads: int, head_dim: int, format: int, dtype, device="cuda", data=None, scale=None):
+        import torch
+        el = {FP16: dtype, INT8: torch.int8, INT4: torch.uint8}[format]
+        shape = (n_pages, 2, heads, page, head_dim // 2 if format == INT4 else head_dim)
+        sshape = {FP16: None, INT8: shape[:4], INT4: shape[:4] + (2,)}[format]
+        self.data = torch.zeros(shape, dtype=el, device=device) if data is None else data
+        self.scale = (None if sshape is None else torch.zeros(sshape, dtype=dtype, device=device)) if scale is None else scale
+        for t, want, ty in ((self.data, shape, el), (self.scale, sshape, dtype)):
+            _dptr(t)
+            if t is not None and (tuple(t.shape) != want or t.dtype != ty or not t.is_contiguous()):
+                raise ValueError(f"pages of shape {want} and type {ty} expected, got {tuple(t.shape)}, {t.dtype}")
+        self.dtype = dtype
+        self.c = Pages(self.data.data_ptr(), None if self.scale is None else self.scale.data_ptr(), n_pages, page, heads, head_dim,
+                       format, {torch.float16: F16, torch.bfloat16: BF16}[dtype])
+
+    def nbytes(self) -> int:
+        return sum(t.numel() * t.element_size() for t in (self.data, self.scale) if t is not None)
+
+
+class Seqs:
+    """A ragged batch: keeps the three int32 device tensors alive beside the C struct that points at them."""
+
+    def __init__(self, row_start, length, table, n_rows: int):
+        import torch
+        n = table.shape[0]
+        for t, want in ((row_start, (n + 1,)), (length, (n,)), (table, tuple(table.shape))):
+            _dptr(t)
+            if t.dtype != torch.int32 or tuple(t.shape) != want or not t.is_contiguous():
+                raise ValueError(f"int32 tensor of shape {want} expected, got {tuple(t.shape)}, {t.dtype}")
+        self.row_start, self.length, self.table = row_start, length, table
+        self.c = SeqsC(n, table.shape[1], n_rows, row_start.data_ptr(), length.data_ptr(), table.data_ptr())

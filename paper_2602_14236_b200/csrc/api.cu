@@ -113,6 +113,7 @@ int salicache_create(salicache_ctx** out, const salicache_params* p) {
         return SALICACHE_E_CUDA;
     }
     c->sm_count = prop.multiProcessorCount;
+    c->device = dev;
     const size_t P0 = (size_t)p->H * p->W;
     const size_t slots = (size_t)2 * c->chunk;   // independent pairs need prev and cur; a video needs chunk+1
     const int words = (p->W + 31) / 32;
@@ -404,6 +405,98 @@ int salicache_attend_gqa(salicache_ctx* c, const void* d_q, int q_per_kv, const 
     if (rc != SALICACHE_OK) return rc;
     if (!aligned16(d_q) || !aligned16(d_out)) return SALICACHE_E_ALIGN;
     return sc_attend(c, d_q, q_per_kv, pools, d_fill, d_out, (cudaStream_t)cuda_stream);
+}
+
+// The context comes last in these checks: arguments are refused for what they are, with or without a device.
+static int check_pages(const salicache_pages* p) {
+    if (!p || !p->d_data) return SALICACHE_E_NULL;
+    if (p->format != SALICACHE_FP16 && p->format != SALICACHE_INT8 && p->format != SALICACHE_INT4) return SALICACHE_E_PARAM;
+    if (p->format != SALICACHE_FP16 && !p->d_scale) return SALICACHE_E_NULL;
+    if (p->dtype != SALICACHE_F16 && p->dtype != SALICACHE_BF16) return SALICACHE_E_PARAM;
+    if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) return SALICACHE_E_PARAM;
+    if (p->head_dim != 64 && p->head_dim != 128) return SALICACHE_E_PARAM;
+    if (p->heads < 1 || p->heads > 256) return SALICACHE_E_PARAM;
+    if (p->n_pages < 1) return SALICACHE_E_SHAPE;
+    if (!aligned16(p->d_data) || !aligned16(p->d_scale)) return SALICACHE_E_ALIGN;
+    return SALICACHE_OK;
+}
+
+static int check_seqs(const salicache_seqs* q) {
+    if (!q) return SALICACHE_E_NULL;
+    if (q->n_seqs < 0 || q->n_rows < 0 || q->table_width < 1) return SALICACHE_E_SHAPE;
+    if (q->n_seqs > 0 && (!q->d_row_start || !q->d_len || !q->d_table)) return SALICACHE_E_NULL;
+    if ((reinterpret_cast<uintptr_t>(q->d_row_start) | reinterpret_cast<uintptr_t>(q->d_len) |
+         reinterpret_cast<uintptr_t>(q->d_table)) & 3u)
+        return SALICACHE_E_ALIGN;
+    return SALICACHE_OK;
+}
+
+// Rows of `width` elements `stride` apart.
+static int check_rows(const void* p, int64_t stride, int64_t width) {
+    if (!p) return SALICACHE_E_NULL;
+    if (stride < width || stride % 8 != 0) return SALICACHE_E_SHAPE;
+    return aligned16(p) ? SALICACHE_OK : SALICACHE_E_ALIGN;
+}
+
+static int check_device(const salicache_ctx* c) {
+    if (!c) return SALICACHE_E_NULL;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SALICACHE_E_CUDA;
+    return dev == c->device ? SALICACHE_OK : SALICACHE_E_PARAM;
+}
+
+static int paged_move(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, void* d_K, void* d_V,
+                      int64_t k_stride, int64_t v_stride, bool write, void* cuda_stream) {
+    int rc = check_pages(pg);
+    if (rc == SALICACHE_OK) rc = check_seqs(sq);
+    if (rc == SALICACHE_OK) rc = check_rows(d_K, k_stride, (int64_t)pg->heads * pg->head_dim);
+    if (rc == SALICACHE_OK) rc = check_rows(d_V, v_stride, (int64_t)pg->heads * pg->head_dim);
+    if (rc == SALICACHE_OK) rc = check_device(c);
+    if (rc != SALICACHE_OK) return rc;
+    if (sq->n_seqs == 0 || sq->n_rows == 0) return SALICACHE_OK;
+    return sc_paged_move(c, pg, sq, d_K, d_V, k_stride, v_stride, write, (cudaStream_t)cuda_stream);
+}
+
+int salicache_paged_write(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, const void* d_K,
+                          const void* d_V, int64_t k_stride, int64_t v_stride, void* cuda_stream) {
+    Range range__("salicache_paged_write");
+    return paged_move(c, pages, seqs, const_cast<void*>(d_K), const_cast<void*>(d_V), k_stride, v_stride, true, cuda_stream);
+}
+
+int salicache_paged_read(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, void* d_K_out, void* d_V_out,
+                         int64_t k_stride, int64_t v_stride, void* cuda_stream) {
+    Range range__("salicache_paged_read");
+    return paged_move(c, pages, seqs, d_K_out, d_V_out, k_stride, v_stride, false, cuda_stream);
+}
+
+int64_t salicache_paged_work_bytes(const salicache_ctx* c, const salicache_pages* pages, int q_per_kv) {
+    int rc = check_pages(pages);
+    if (rc != SALICACHE_OK) return rc;
+    if (q_per_kv < 1 || q_per_kv > 64) return SALICACHE_E_PARAM;
+    if (!c) return SALICACHE_E_NULL;
+    return sc_paged_work_bytes(c, pages->head_dim);
+}
+
+int salicache_paged_attend(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, const void* d_q,
+                           int64_t q_stride, int q_per_kv, float softmax_scale, int window, int sinks, void* d_out,
+                           int64_t out_stride, float* d_lse, void* d_work, int64_t work_bytes, void* cuda_stream) {
+    Range range__("salicache_paged_attend");
+    int rc = check_pages(pages);
+    if (rc == SALICACHE_OK) rc = check_seqs(seqs);
+    if (rc != SALICACHE_OK) return rc;
+    if (q_per_kv < 1 || q_per_kv > 64 || window < 0 || sinks < 0 || !(softmax_scale > 0.0f) || !(softmax_scale < INFINITY))
+        return SALICACHE_E_PARAM;
+    const int64_t width = (int64_t)pages->heads * q_per_kv * pages->head_dim;
+    rc = check_rows(d_q, q_stride, width);
+    if (rc == SALICACHE_OK) rc = check_rows(d_out, out_stride, width);
+    if (rc == SALICACHE_OK && !d_work) rc = SALICACHE_E_NULL;
+    if (rc == SALICACHE_OK && (!aligned16(d_work) || (reinterpret_cast<uintptr_t>(d_lse) & 3u))) rc = SALICACHE_E_ALIGN;
+    if (rc == SALICACHE_OK) rc = check_device(c);
+    if (rc != SALICACHE_OK) return rc;
+    if (work_bytes < sc_paged_work_bytes(c, pages->head_dim)) return SALICACHE_E_SHAPE;
+    if (seqs->n_seqs == 0 || seqs->n_rows == 0) return SALICACHE_OK;
+    return sc_paged_attend(c, pages, seqs, d_q, q_stride, q_per_kv, softmax_scale, window, sinks, d_out, out_stride, d_lse,
+                           d_work, (cudaStream_t)cuda_stream);
 }
 
 int salicache_poll_status(salicache_ctx* c, void* cuda_stream) {

@@ -52,6 +52,7 @@ struct salicache_ctx {
     float* attend_ws;          // partial attention results [L][max(heads, 64)][128][head_dim + 2]
     int* d_status;             // deferred status word
     int sm_count;
+    int device;                // the CUDA device the context was created on
     long long launches;        // kernels launched through this context so far
 };
 
@@ -88,6 +89,13 @@ int sc_select_anchored(salicache_ctx* c, const uint8_t* d_frames, const float* d
 size_t sc_attend_workspace_bytes(int L, int H);
 int sc_attend(salicache_ctx* c, const void* d_q, int q_per_kv, const salicache_pools* pools, const int64_t* d_fill, float* d_out,
               cudaStream_t st);
+// paged.cu, paged_attend.cu: arguments are checked by the entry points
+int sc_paged_move(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, void* d_K, void* d_V, int64_t k_stride,
+                  int64_t v_stride, bool write, cudaStream_t st);
+int64_t sc_paged_work_bytes(const salicache_ctx* c, int head_dim);
+int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, const void* d_q, int64_t q_stride,
+                    int q_per_kv, float softmax_scale, int window, int sinks, void* d_out, int64_t out_stride, float* d_lse,
+                    void* d_work, cudaStream_t st);
 // kv.cu
 int sc_pack(salicache_ctx* c, const void* d_K, const void* d_V, int64_t frame_stride, const int32_t* d_idx,
             const int32_t* d_counts, const int64_t* d_row_offset, int B, const salicache_pools* pools, cudaStream_t st);

@@ -1,0 +1,87 @@
+// Device-side view of the paged cache, shared by its store (paged.cu) and its attention (paged_attend*.cu).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+// The 16-bit types.  Both kinds of arithmetic below are the plain IEEE operations of the type.
+struct TypeF16 {
+    using pair = __half2;
+    static __device__ __forceinline__ float lo(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu))); }
+    static __device__ __forceinline__ float hi(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {           // (a, b) rounded, a in the low half
+        __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ uint16_t round(float a) { return __half_as_ushort(__float2half_rn(a)); }
+    static constexpr uint32_t ONE = 0x3c00u;
+};
+struct TypeBF16 {
+    using pair = __nv_bfloat162;
+    static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
+    static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ uint16_t round(float a) { return __bfloat16_as_ushort(__float2bfloat16_rn(a)); }
+    static constexpr uint32_t ONE = 0x3f80u;
+};
+template <typename T>
+__device__ __forceinline__ typename T::pair as_pair(uint32_t w) { return *reinterpret_cast<typename T::pair*>(&w); }
+template <typename P>
+__device__ __forceinline__ uint32_t as_word(P p) { return *reinterpret_cast<uint32_t*>(&p); }
+
+constexpr int PF_16 = 0, PF_I8 = 1, PF_I4 = 2;      // page formats as template arguments
+
+struct PgCache {
+    uint8_t* data;
+    uint8_t* scale;
+    int n_pages, page_shift, heads;
+};
+struct PgSeqs {
+    const int* start;
+    const int* len;
+    const int* table;
+    int n_seqs, width, n_rows;
+};
+
+inline PgCache pg_cache(const salicache_pages* p) {
+    int shift = 4;
+    while ((1 << shift) < p->page) ++shift;
+    return PgCache{(uint8_t*)p->d_data, (uint8_t*)p->d_scale, p->n_pages, shift, p->heads};
+}
+inline PgSeqs pg_seqs(const salicache_seqs* q) {
+    return PgSeqs{q->d_row_start, q->d_len, q->d_table, q->n_seqs, q->table_width, q->n_rows};
+}
+
+// Bytes of one token's head in the pages, and of its scale (and zero).
+template <int FMT, int D> __host__ __device__ constexpr int pg_row_bytes() { return FMT == PF_16 ? 2 * D : FMT == PF_I8 ? D : D / 2; }
+template <int FMT> __host__ __device__ constexpr int pg_meta_bytes() { return FMT == PF_16 ? 0 : FMT == PF_I8 ? 2 : 4; }
+
+// Slot index of (page id, K or V, head, slot): times pg_row_bytes it is the byte offset in `data`, times pg_meta_bytes in
+// `scale`.  64 bits: a long cache passes 2^32 bytes.
+__device__ __forceinline__ size_t pg_slot(const PgCache& c, int pid, int kv, int head, int slot) {
+    return (((size_t)pid * 2 + kv) * c.heads + head << c.page_shift) + slot;
+}
+
+// Rows and positions of a sequence, clamped so that no offset the device finds reaches outside the caller's arrays.
+struct PgSeq {
+    int row0, n;        // first row in the caller's arrays, rows
+    int pos0;           // position of row 0 (may be negative)
+    int len;            // positions held, without those past the table
+    bool cut;           // some lie past the table
+};
+__device__ __forceinline__ PgSeq pg_seq(const PgSeqs& s, const PgCache& c, int b) {
+    PgSeq r;
+    const int a = min(max(s.start[b], 0), s.n_rows), e = min(max(s.start[b + 1], a), s.n_rows);
+    const int len = max(s.len[b], 0);
+    const long long cap = (long long)s.width << c.page_shift;
+    r.row0 = a;
+    r.n = e - a;
+    r.pos0 = len - r.n;
+    r.cut = len > cap;
+    r.len = (int)min((long long)len, cap);
+    return r;
+}
