@@ -1,0 +1,199 @@
+// How the attention kernels over the paged cache share their work, and how split results are joined.
+//
+// An item is (sequence, key/value head, tile of rows); rows are numbered i * G + g (new token i, query head g of the
+// group), so that all query heads of a group meet a key in one tile.  An item's work is the tiles of 128 positions that
+// any of its rows may see: tiles of the first `sinks` positions and those from the window's edge on.  All items' tiles
+// stand in one line, and block c of C takes the c-th equal stretch of it, wherever items begin and end: a batch of very
+// different lengths, or one long sequence, loads every SM alike, and the split follows the lengths on the device, so
+// that a captured call adapts to new ones.
+// A stretch that covers an item from its first to its last tile writes the output.  Else the block leaves unnormalised
+// sums, running maxima and denominators in the caller's workspace: at most one item that began in an earlier block
+// ("head") and one that goes on in a later block ("tail").  A second kernel joins tail and heads in the order of the
+// blocks, so results do not depend on timing.
+#pragma once
+#include "paged.cuh"
+
+constexpr int PT_KEYS = 128;                 // positions per tile
+constexpr float PT_NONE = -3.0e38f;          // running maximum of a row that has seen nothing
+constexpr float PT_LOG2E = 1.4426950408889634f, PT_LN2 = 0.6931471805599453f;
+
+struct PtArgs {
+    PgCache pc;
+    PgSeqs sq;
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;
+    long long q_stride, out_stride;
+    int G, window, sinks;
+    float scale;                             // softmax scale * log2(e): the kernels work in powers of two
+    float* part;                             // [2 * blocks][rows of a tile][D], tail records after head records of a block
+    float2* stat;                            // [2 * blocks][rows of a tile]: running maximum (powers of two), denominator
+    int4* head;                              // [blocks]: head record (0 none, 1 the item goes on, 2 it ends); tail record: 1 + head or 0, b, rt
+    int* status;
+};
+
+// The tiles an item's rows may see.
+struct PtSpan {
+    int n;                                   // tiles
+    int sink_tiles, first;                   // tile k is k below sink_tiles, first + k - sink_tiles from there on
+    int lo, hi;                              // [lo, hi): positions inside some row's window; below `sinks` seen by all
+    int all_lo, all_hi;                      // positions in [all_lo, all_hi) or below min(sinks, all_hi) are seen by every row
+    __device__ __forceinline__ int tile(int k) const { return k < sink_tiles ? k : first + (k - sink_tiles); }
+};
+__device__ __forceinline__ PtSpan pt_span(const PgSeq& s, int G, int r0, int r1, int window, int sinks) {
+    PtSpan p;
+    const int p0 = s.pos0 + r0 / G, p1 = s.pos0 + (r1 - 1) / G;      // first and last row's position
+    p.hi = max(0, min(p1 + 1, s.len));
+    p.all_hi = max(0, min(p0 + 1, s.len));
+    p.lo = window ? max(0, p0 - window + 1) : 0;
+    p.all_lo = window ? max(0, p1 - window + 1) : 0;
+    p.first = p.lo / PT_KEYS;
+    p.sink_tiles = min(p.first, (min(window ? sinks : 0, p.hi) + PT_KEYS - 1) / PT_KEYS);
+    p.n = p.sink_tiles + max(0, (p.hi + PT_KEYS - 1) / PT_KEYS - p.first);
+    return p;
+}
+// Whether the row at position `pos` sees position j (j < len is the caller's to check).
+__device__ __forceinline__ bool pt_sees(int pos, int j, int window, int sinks) {
+    return j <= pos && (window == 0 || j > pos - window || j < sinks);
+}
+
+template <int RT>
+__device__ __forceinline__ int pt_row_tiles(const PgSeq& s, int G) { return (int)(((long long)s.n * G + RT - 1) / RT); }
+template <int RT>
+__device__ __forceinline__ PtSpan pt_item(const PgSeq& s, const PtArgs& a, int rt) {
+    const int r0 = rt * RT, r1 = (int)min((long long)r0 + RT, (long long)s.n * a.G);
+    return pt_span(s, a.G, r0, r1, a.window, a.sinks);
+}
+
+// A block's place in the line of tiles.
+struct PtWalk {
+    long long left;                          // tiles still to do
+    int b, h, rt, k;                         // the next one: item and tile within it
+};
+
+// Every thread gets the same walk.  One thread per sequence sums its tiles; block-wide scans find the block's start.
+template <int RT, int THREADS>
+__device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int blocks) {
+    __shared__ long long wsum[THREADS / 32];
+    __shared__ PtWalk found;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    auto weight = [&](int b) -> long long {
+        if (b >= a.sq.n_seqs) return 0;
+        const PgSeq s = pg_seq(a.sq, a.pc, b);
+        const int R = pt_row_tiles<RT>(s, a.G);
+        long long w = 0;
+        for (int rt = 0; rt < R; ++rt) w += max(1, pt_item<RT>(s, a, rt).n);
+        return w * a.pc.heads;
+    };
+    auto block_sum = [&](long long v) -> long long {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == 0) wsum[wid] = v;
+        __syncthreads();
+        long long t = 0;
+#pragma unroll
+        for (int i = 0; i < THREADS / 32; ++i) t += wsum[i];
+        __syncthreads();
+        return t;
+    };
+    const long long w0 = weight(threadIdx.x);
+    long long mine = w0;
+    for (int b = threadIdx.x + THREADS; b < a.sq.n_seqs; b += THREADS) mine += weight(b);
+    const long long total = block_sum(mine);
+    const long long beg = total * block / blocks, end = total * (block + 1) / blocks;
+    if (threadIdx.x == 0) found.left = 0;
+    __syncthreads();
+    if (beg == end) return found;
+    long long before = 0;                    // tiles of the sequences before this round's
+    for (int b0 = 0; b0 < a.sq.n_seqs; b0 += THREADS) {
+        const int b = b0 + threadIdx.x;
+        const long long w = b0 == 0 ? w0 : weight(b);
+        long long incl = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        if (lane == 31) wsum[wid] = incl;
+        __syncthreads();
+        long long off = before;
+        for (int i = 0; i < wid; ++i) off += wsum[i];
+        const long long at = beg - (off + incl - w);
+        if (at >= 0 && at < w) {             // this thread's sequence holds the start
+            const PgSeq s = pg_seq(a.sq, a.pc, b);
+            const long long per_head = w / a.pc.heads;
+            long long rem = at % per_head;
+            int rt = 0;
+            for (;; ++rt) {
+                const int n = max(1, pt_item<RT>(s, a, rt).n);
+                if (rem < n) break;
+                rem -= n;
+            }
+            found = PtWalk{end - beg, b, (int)(at / per_head), rt, (int)rem};
+        }
+        for (int i = 0; i < THREADS / 32; ++i) before += wsum[i];
+        __syncthreads();
+        if (before > beg) break;
+    }
+    return found;
+}
+
+// On to the next item: row tiles, then heads, then sequences with rows.
+template <int RT>
+__device__ __forceinline__ void pt_next(PtWalk& w, PgSeq& s, const PtArgs& a) {
+    w.k = 0;
+    if (++w.rt < pt_row_tiles<RT>(s, a.G)) return;
+    w.rt = 0;
+    if (++w.h < a.pc.heads) return;
+    w.h = 0;
+    do {
+        ++w.b;
+        if (w.b >= a.sq.n_seqs) return;      // cannot happen while tiles are left
+        s = pg_seq(a.sq, a.pc, w.b);
+    } while (s.n == 0);
+}
+
+// Joins the records of the item that block blockIdx.x left as its tail.  grid.y: groups of 8 rows, one warp per row.
+template <typename T, int RT, int D>
+__global__ void __launch_bounds__(256)
+k_paged_join(PtArgs a, int blocks) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    constexpr int N = D / 32;
+    const int4 hd = a.head[blockIdx.x];
+    if (hd.y == 0) return;
+    const int lane = threadIdx.x & 31, row = blockIdx.y * 8 + (threadIdx.x >> 5);
+    const int b = hd.z, h = hd.y - 1, rt = hd.w;
+    const PgSeq s = pg_seq(a.sq, a.pc, b);
+    const long long r = (long long)rt * RT + row;
+    if (r >= (long long)s.n * a.G) return;
+    // the item's records: this block's tail, then later blocks' heads until one ends
+    const size_t t0 = (size_t)(2 * blockIdx.x + 1) * RT + row;
+    float M = a.stat[t0].x;
+    int last = blockIdx.x;
+    for (int c = blockIdx.x + 1; c < blocks; ++c) {
+        const int f = a.head[c].x;
+        if (f == 0) continue;
+        M = fmaxf(M, a.stat[(size_t)(2 * c) * RT + row].x);
+        last = c;
+        if (f == 2) break;
+    }
+    float o[N], l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = 0.0f;
+    for (int c = blockIdx.x; c <= last; ++c) {
+        if (c != blockIdx.x && a.head[c].x == 0) continue;
+        const size_t t = c == blockIdx.x ? t0 : (size_t)(2 * c) * RT + row;
+        const float2 st = a.stat[t];
+        const float e = exp2f(st.x - M);
+        l += e * st.y;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] += e * a.part[t * D + lane * N + i];
+    }
+    const int hq = h * a.G + (int)(r % a.G);
+    const long long tok = s.row0 + r / a.G;
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    uint16_t* dst = a.out + tok * a.out_stride + (long long)hq * D + lane * N;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = T::pack(o[i] * inv, o[i + 1] * inv);
+    if (a.lse && lane == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (M + log2f(l)) * PT_LN2 : -INFINITY;
+}

@@ -72,6 +72,10 @@ def test_attention_arguments_are_checked(args, want):
     assert _attend(_pages(), _seqs(), **args) == want
 
 
+def test_too_many_rows_for_one_attention_call():
+    assert _attend(_pages(), _seqs(n_rows=1 << 29), g=2) == sc.E_SHAPE
+
+
 @pytest.mark.parametrize("call", CALLS)
 def test_sound_arguments_still_need_a_context(call):
     assert call(_pages(), _seqs()) == sc.E_NULL
