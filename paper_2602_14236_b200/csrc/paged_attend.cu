@@ -38,12 +38,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
     return d;
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 template <int W>
 __device__ __forceinline__ void ld_words(uint32_t* d, const uint8_t* p) {
     if (W == 4) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3]) : "l"(p));
@@ -100,45 +94,6 @@ struct VTile {
         }
     }
 };
-
-// (a & b) | c in one instruction.
-__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t d;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-// Codes to the 16-bit type: OR-ed into the mantissa of a power of two whose last place is 1 (f16: 1024, bf16: 128; for a
-// nibble one place up, f16: 64), a code adds exactly its value; the power is then subtracted.
-template <typename T>
-struct Codes;
-template <>
-struct Codes<TypeF16> {
-    using P = __half2;
-    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) { return as_word(__hsub2(as_pair<TypeF16>(a), as_pair<TypeF16>(b))); }
-    // the two signed bytes in the low bytes of the halves of h (whatever is above them)
-    static __device__ __forceinline__ uint32_t bytes(uint32_t w, uint32_t sel) {
-        return sub(__byte_perm(w ^ 0x80808080u, 0x64646464u, sel), 0x64806480u);
-    }
-    static __device__ __forceinline__ uint32_t nib_lo(uint32_t x) { return sub(and_or(x, 0x000f000fu, 0x64006400u), 0x64006400u); }
-    static __device__ __forceinline__ uint32_t nib_hi(uint32_t x) { return sub(and_or(x, 0x00f000f0u, 0x54005400u), 0x54005400u); }
-};
-template <>
-struct Codes<TypeBF16> {
-    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) { return as_word(__hsub2(as_pair<TypeBF16>(a), as_pair<TypeBF16>(b))); }
-    // seven bits fit the mantissa of 128; the sign bit (-128) goes into the other operand, 256 instead of 128
-    static __device__ __forceinline__ uint32_t bytes(uint32_t w, uint32_t sel) {
-        const uint32_t h = __byte_perm(w, 0u, sel);
-        return sub(and_or(h, 0x007f007fu, 0x43004300u), and_or(h, 0x00800080u, 0x43004300u));
-    }
-    static __device__ __forceinline__ uint32_t nib_lo(uint32_t x) { return sub(and_or(x, 0x000f000fu, 0x43004300u), 0x43004300u); }
-    static __device__ __forceinline__ uint32_t nib_hi(uint32_t x) { return nib_lo(x >> 4); }
-};
-template <typename T>
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t s) { return as_word(__hmul2(as_pair<T>(a), as_pair<T>(s))); }
-template <typename T>
-__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t s, uint32_t z) { return as_word(__hfma2(as_pair<T>(a), as_pair<T>(s), as_pair<T>(z))); }
-__device__ __forceinline__ uint32_t dup_lo(uint32_t w) { return __byte_perm(w, 0, 0x1010); }
-__device__ __forceinline__ uint32_t dup_hi(uint32_t w) { return __byte_perm(w, 0, 0x3232); }
 
 // K fragments of matrix instruction st: registers (a0, a2) of one key row.
 template <typename T, int FMT, int D>
@@ -470,6 +425,7 @@ int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache
     a.scale = softmax_scale * PT_LOG2E;
     a.status = c->d_status;
     char* work = (char*)d_work;
+    if ((long long)a.sq.n_rows * a.G > 16ll * a.sq.n_seqs) return sc_paged_chunk(c, a, pg, work, st);
 #define GO(T, F, D) return launch_attend<T, F, D>(c, a, work, st)
 #define GO_FORMAT(T, D)                                      \
     do {                                                     \

@@ -32,6 +32,9 @@ struct PtArgs {
     int* status;
 };
 
+// paged_chunk.cu
+int sc_paged_chunk(salicache_ctx* c, const PtArgs& a, const salicache_pages* pg, char* work, cudaStream_t st);
+
 // The tiles an item's rows may see.
 struct PtSpan {
     int n;                                   // tiles
