@@ -399,7 +399,8 @@ SALICACHE_API int salicache_attend_gqa(salicache_ctx* ctx, const void* d_q, int 
  *   d_scale  INT8: [n_pages][2][heads][page], INT4: [n_pages][2][heads][page][2] = (scale, zero), in the 16-bit type of
  *            `dtype`; not used by SALICACHE_FP16
  * One quantisation group is one head of one token (head_dim elements).
- * Supported: page 16, 32, 64 or 128; head_dim 64 or 128; heads 1 .. 256; dtype SALICACHE_F16 or SALICACHE_BF16.  The
+ * Supported: page 16, 32, 64 or 128; head_dim 64 or 128; heads 1 .. 256; n_pages * 2 * heads * page below 2^31 (550 GB of
+ * 128-element 16-bit rows; byte offsets have 64 bits); dtype SALICACHE_F16 or SALICACHE_BF16.  The
  * context supplies the device and the status word; its frame size, L, heads, head_dim and group play no part here. */
 #define SALICACHE_F16  0
 #define SALICACHE_BF16 1

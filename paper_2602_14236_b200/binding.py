@@ -127,15 +127,27 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-def _dptr(t):
-    """As _ptr, for the paged calls: refuses host memory and tensors of another device than the current one, which the C
-    entry points cannot see."""
+def _here():
+    """The current device and its current stream, the way the paged calls ask for them: once per call."""
+    global _torch_c
+    if _torch_c is None:
+        import torch
+        torch.cuda.current_stream()
+        _torch_c = torch._C
+    dev = _torch_c._cuda_getDevice()
+    return dev, _torch_c._cuda_getCurrentRawStream(dev)
+
+
+_torch_c = None
+
+
+def _dptr(t, dev):
+    """The address of a tensor on device `dev`: the C entry points cannot tell host memory or another device's from their own."""
     if t is None:
         return None
-    import torch
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"a tensor on the current CUDA device expected, got one on {t.device}")
-    return C.c_void_p(t.data_ptr())
+    if t.get_device() != dev:
+        raise ValueError(f"a tensor on cuda:{dev}, the current device, expected, got one on {t.device}")
+    return t.data_ptr()
 
 
 def _stream(stream=None):
@@ -288,14 +300,20 @@ def salicache_tokens_live(ctx: Context, d_src, B: int, first_frame: int, d_resid
                                        _stream(stream)), "salicache_tokens_live")
 
 
+def _paged_move(name: str, ctx: Context, pages: Pages, seqs: SeqsC, d_K, d_V, k_stride: int, v_stride: int, stream):
+    dev, st = _here()
+    rc = getattr(lib(), name)(ctx.handle, pages, seqs, _dptr(d_K, dev), _dptr(d_V, dev), k_stride, v_stride,
+                              st if stream is None else stream.cuda_stream)
+    if rc:
+        raise SalicacheError(rc, name)
+
+
 def salicache_paged_write(ctx: Context, pages: Pages, seqs: SeqsC, d_K, d_V, k_stride: int, v_stride: int, stream=None):
-    _check(lib().salicache_paged_write(ctx.handle, C.byref(pages), C.byref(seqs), _dptr(d_K), _dptr(d_V), k_stride, v_stride,
-                                       _stream(stream)), "salicache_paged_write")
+    _paged_move("salicache_paged_write", ctx, pages, seqs, d_K, d_V, k_stride, v_stride, stream)
 
 
 def salicache_paged_read(ctx: Context, pages: Pages, seqs: SeqsC, d_K_out, d_V_out, k_stride: int, v_stride: int, stream=None):
-    _check(lib().salicache_paged_read(ctx.handle, C.byref(pages), C.byref(seqs), _dptr(d_K_out), _dptr(d_V_out), k_stride, v_stride,
-                                      _stream(stream)), "salicache_paged_read")
+    _paged_move("salicache_paged_read", ctx, pages, seqs, d_K_out, d_V_out, k_stride, v_stride, stream)
 
 
 def salicache_paged_work_bytes(ctx: Context, pages: Pages, q_per_kv: int) -> int:
@@ -307,9 +325,12 @@ def salicache_paged_work_bytes(ctx: Context, pages: Pages, q_per_kv: int) -> int
 
 def salicache_paged_attend(ctx: Context, pages: Pages, seqs: SeqsC, d_q, q_stride: int, q_per_kv: int, softmax_scale: float,
                            window: int, sinks: int, d_out, out_stride: int, d_lse, d_work, work_bytes: int, stream=None):
-    _check(lib().salicache_paged_attend(ctx.handle, C.byref(pages), C.byref(seqs), _dptr(d_q), q_stride, q_per_kv, softmax_scale,
-                                        window, sinks, _dptr(d_out), out_stride, _dptr(d_lse), _dptr(d_work), work_bytes,
-                                        _stream(stream)), "salicache_paged_attend")
+    dev, st = _here()
+    rc = lib().salicache_paged_attend(ctx.handle, pages, seqs, _dptr(d_q, dev), q_stride, q_per_kv, softmax_scale, window, sinks,
+                                      _dptr(d_out, dev), out_stride, _dptr(d_lse, dev), _dptr(d_work, dev), work_bytes,
+                                      st if stream is None else stream.cuda_stream)
+    if rc:
+        raise SalicacheError(rc, "salicache_paged_attend")
 
 
 def salicache_poll_status(ctx: Context, stream=None) -> int:
@@ -353,7 +374,8 @@ class PageSet:
         self.data = torch.zeros(shape, dtype=el, device=device) if data is None else data
         self.scale = (None if sshape is None else torch.zeros(sshape, dtype=dtype, device=device)) if scale is None else scale
         for t, want, ty in ((self.data, shape, el), (self.scale, sshape, dtype)):
-            _dptr(t)
+            if t is not None and not t.is_cuda:
+                raise ValueError(f"pages on a CUDA device expected, got {t.device}")
             if t is not None and (tuple(t.shape) != want or t.dtype != ty or not t.is_contiguous()):
                 raise ValueError(f"pages of shape {want} and type {ty} expected, got {tuple(t.shape)}, {t.dtype}")
         self.dtype = dtype
@@ -371,7 +393,8 @@ class Seqs:
         import torch
         n = table.shape[0]
         for t, want in ((row_start, (n + 1,)), (length, (n,)), (table, tuple(table.shape))):
-            _dptr(t)
+            if not t.is_cuda or t.device != table.device:
+                raise ValueError(f"tensors on one CUDA device expected, got {t.device}")
             if t.dtype != torch.int32 or tuple(t.shape) != want or not t.is_contiguous():
                 raise ValueError(f"int32 tensor of shape {want} expected, got {tuple(t.shape)}, {t.dtype}")
         self.row_start, self.length, self.table = row_start, length, table

@@ -416,7 +416,7 @@ static int check_pages(const salicache_pages* p) {
     if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) return SALICACHE_E_PARAM;
     if (p->head_dim != 64 && p->head_dim != 128) return SALICACHE_E_PARAM;
     if (p->heads < 1 || p->heads > 256) return SALICACHE_E_PARAM;
-    if (p->n_pages < 1) return SALICACHE_E_SHAPE;
+    if (p->n_pages < 1 || (int64_t)p->n_pages * 2 * p->heads * p->page >= (1ll << 31)) return SALICACHE_E_SHAPE;
     if (!aligned16(p->d_data) || !aligned16(p->d_scale)) return SALICACHE_E_ALIGN;
     return SALICACHE_OK;
 }

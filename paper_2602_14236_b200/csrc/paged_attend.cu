@@ -378,7 +378,7 @@ int launch_step(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     constexpr int RT = 8 * NT;
     // no more blocks than there can be tiles of work: rows of q times heads times the table's tiles
     const long long most = (long long)a.sq.n_rows * a.pc.heads * ((((long long)a.sq.width << a.pc.page_shift) + PT_KEYS - 1) / PT_KEYS);
-    const int blocks = (int)max(1ll, min(most, (long long)c->sm_count * st_blocks<FMT, D, NT>()));
+    const int blocks = (int)max(1ll, min(min(most, (long long)PT_MAX_BLOCKS), (long long)c->sm_count * st_blocks<FMT, D, NT>()));
     a.part = reinterpret_cast<float*>(work);
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * RT * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * RT);

@@ -6,9 +6,10 @@
 // Roles by warp group:
 //   0, 1   one thread per row of half 0 / 1: maximum over the row's 128 scores, weights, row sum; P overwrites S as the
 //          16-bit operand of the second product; also Q into shared memory before an item and the output after it
-//   2      K and V of the next tiles into a ring of shared-memory stages: 16-bit pages by asynchronous copies, codes
-//          through registers (the next stage's codes are requested before the present ones are expanded)
-//   3      one thread issues the matrix instructions
+//   2      codes from a ring of raw stages to 16-bit operands; of 16-bit pages only the V tiles that hold positions no
+//          row sees, which are stored as zeros whatever the page holds there
+//   3      one thread issues the matrix instructions; one warp feeds the rings with bulk copies, a lane per page: tensor
+//          copies straight into the operand stages (16-bit pages), plain ones of codes and scales into the raw stages
 // While one half's weights are formed, the tensor core works for the other: the products of a half are issued as
 // P(t) V(t), then Q K(t+1).  Instructions of one thread run in order there, so S may be overwritten right behind the
 // product that read P from the same columns, and whoever sees the scores of tile t knows the sums of tile t-1 complete.
@@ -19,6 +20,7 @@
 // dimension contiguous; V has it across rows, which the instruction descriptor's transpose bit covers, so neither is
 // transposed in memory.  INT4 codes come out of their words in the order 0 4 1 5 2 6 3 7; Q is permuted alike when it is
 // staged and the output back when it is written.
+#include <cuda.h>
 #include <math.h>
 
 #include "paged_plan.cuh"
@@ -33,6 +35,19 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)_
 // ---- mbarriers
 __device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {          // one arrival, and bytes to come
+    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+                 "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+                 "l"(map), "r"(bar), "r"(x), "r"(y)
+                 : "memory");
+}
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2, %3; selp.b32 %0, 1, 0, p; }"
@@ -118,17 +133,22 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uin
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+constexpr int CH_RAW = 4;                    // raw stages at most
 struct ChBars {
-    uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], q_ready[2], s_full[2], p_ready[2], o_done[2];
+    uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_ready[2], s_full[2], p_ready[2], o_done[2];
     uint32_t tmem;
     int gave_up;
-    uint32_t pages[4];                       // per tile (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
+    uint32_t pages[8];                       // per tile (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
 };
 
-template <int D>
+template <int FMT, int D>
 struct ChSmem {
     static constexpr int TILE = 128 * D * 2;         // bytes of an operand tile
-    static constexpr int Q = 0, KV = 2 * TILE, BARS = KV + CH_STAGES * TILE, BYTES = BARS + (int)sizeof(ChBars) + 1024;
+    static constexpr int RAW_CODES = 128 * pg_row_bytes<FMT, D>(), RAW = RAW_CODES + 128 * pg_meta_bytes<FMT>();
+    static constexpr int N_RAW = FMT == PF_16 ? 0 : D == 64 ? 4 : FMT == PF_I4 ? 3 : 2;      // what 227 KB leave room for
+    static constexpr int Q = 0, KV = 2 * TILE, RAWS = KV + CH_STAGES * TILE, BARS = RAWS + N_RAW * RAW;
+    static constexpr int BYTES = BARS + (int)sizeof(ChBars) + 1024;
+    static_assert(BYTES <= 227 * 1024, "shared memory");
 };
 
 // A walk over a block's segments that every role repeats for itself.
@@ -142,20 +162,24 @@ struct ChSeg {
         rows = min(CH_ROWS, s.n * a.G - w.rt * CH_ROWS);
         tiles = sp.n == 0 ? 0 : k1 - k0;
     }
-};
-
-// What a loader thread holds of a stage of codes: PASSES rows, 16 bytes of each.
-template <int FMT, int D>
-struct CodeRegs {
-    static constexpr int LPR = pg_row_bytes<FMT, D>() / 16 > 0 ? pg_row_bytes<FMT, D>() / 16 : 1;      // lanes per row = passes
-    uint4 c[LPR];
-    uint32_t s[LPR];
+    // Page of keys 16 grp .. of tile k: -2 no row sees them (or grp > 7), -1 there is no such page.
+    __device__ __forceinline__ int page_of(const PtArgs& a, const PtWalk& w, int k, int grp) const {
+        const int j = sp.tile(k) * PT_KEYS + grp * 16;
+        if (grp > 7 || j >= sp.hi || (j + 16 <= sp.lo && j >= a.sinks)) return -2;
+        const int p = a.sq.table[(size_t)w.b * a.sq.width + (j >> a.pc.page_shift)];
+        return p >= 0 && p < a.pc.n_pages ? p : -1;
+    }
+    // Whether some row sees each key of tile k (pages permitting).
+    __device__ __forceinline__ bool clean(const PtArgs& a, int k) const {
+        const int j0 = sp.tile(k) * PT_KEYS;
+        return j0 + PT_KEYS <= sp.hi && (j0 >= sp.lo || j0 + PT_KEYS <= a.sinks);
+    }
 };
 
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(CH_THREADS, 1)
-k_paged_chunk(PtArgs a, int blocks) {
-    using SM = ChSmem<D>;
+k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
+    using SM = ChSmem<FMT, D>;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     ChBars& bars = *reinterpret_cast<ChBars*>(raw + (base - smem_u32(raw)) + SM::BARS);
@@ -164,8 +188,12 @@ k_paged_chunk(PtArgs a, int blocks) {
 
     if (tid == 0) {
         for (int i = 0; i < CH_STAGES; ++i) {
-            bar_init(smem_u32(&bars.kv_full[i]), 128);
+            bar_init(smem_u32(&bars.kv_full[i]), FMT == PF_16 ? 5 : 4);      // the four warps of group 2, and the feeder
             bar_init(smem_u32(&bars.kv_empty[i]), 1);
+        }
+        for (int i = 0; i < CH_RAW; ++i) {
+            bar_init(smem_u32(&bars.raw_full[i]), 1);
+            bar_init(smem_u32(&bars.raw_empty[i]), 4);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_u32(&bars.q_ready[i]), 128);
@@ -246,7 +274,7 @@ k_paged_chunk(PtArgs a, int blocks) {
                         tc_ld32(x + 96, S + 96);
                         tc_wait_ld();
                         const int j0 = g.sp.tile(k) * PT_KEYS;
-                        const uint32_t pages = *(volatile uint32_t*)&bars.pages[n_tile & 3];
+                        const uint32_t pages = *(volatile uint32_t*)&bars.pages[n_tile & 7];
                         if (!(j0 + PT_KEYS <= hs.all_hi && (j0 >= hs.all_lo || j0 + PT_KEYS <= a.sinks) && pages == 0xffu)) {
                             const int hi = vis_hi - j0, lo = vis_lo - j0, sk = a.sinks - j0;
 #pragma unroll
@@ -348,129 +376,89 @@ k_paged_chunk(PtArgs a, int blocks) {
         }
         if (tid == 0) a.head[blockIdx.x] = hd;
     } else if (wid < 12) {
-        // ---------------- loaders
+        // ---------------- operands
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         const int lw = wid - 8;                              // this warp's rows: 32 lw .. 32 lw + 31 of a tile
-        uint32_t n_stage = 0, n_tile = 0, n_arrived = 0;
+        uint32_t n_stage = 0;
         bool ok = true;
         while (w.left > 0 && ok) {
             g.set(a, w, s);
-            const int* table = a.sq.table + (size_t)w.b * a.sq.width;
-            // pages of this warp's two groups of 16 keys of tile k: -2 no row sees them, -1 there is no such page
-            auto page_of = [&](int k, int grp) -> int {
-                if (k >= g.k1) return -2;
-                const int j = g.sp.tile(k) * PT_KEYS + lw * 32 + grp * 16;
-                if (j >= g.sp.hi || (j + 16 <= g.sp.lo && j >= a.sinks)) return -2;
-                const int p = table[j >> a.pc.page_shift];
-                return p >= 0 && p < a.pc.n_pages ? p : -1;
-            };
-            const int tiles_end = g.k0 + g.tiles;
-            int pg0 = -2, pg1 = -2;
-            if (g.tiles > 0) {
-                pg0 = page_of(g.k0, 0);
-                pg1 = page_of(g.k0, 1);
-            }
-            for (int k = g.k0; k < tiles_end && ok; ++k, ++n_tile) {
-                const int nx0 = page_of(k + 1, 0), nx1 = page_of(k + 1, 1);
-                const int j0 = g.sp.tile(k) * PT_KEYS + lw * 32;
-                if ((pg0 == -1 || pg1 == -1) && lane == 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
-                // which of the tile's keys any row sees: others are stored as zeros, whatever the page holds
-                auto want = [&](int r) -> int {              // r: row of this warp's 32; page id or -1
-                    const int j = j0 + r, p = r < 16 ? pg0 : pg1;
-                    return p >= 0 && j < g.sp.hi && (j >= g.sp.lo || j < a.sinks) ? p : -1;
+            for (int k = g.k0; k < g.k0 + g.tiles && ok; ++k) {
+                const int j0 = g.sp.tile(k) * PT_KEYS;
+                const int pid = g.page_of(a, w, k, lane);
+                const uint32_t bad = __ballot_sync(0xffffffffu, pid == -1);
+                const bool clean = g.clean(a, k) && bad == 0;
+                // whether some row sees key r of this warp's 32
+                auto seen = [&](int r) -> bool {
+                    const int j = j0 + lw * 32 + r;
+                    return j < g.sp.hi && (j >= g.sp.lo || j < a.sinks) && !(bad >> (lw * 2 + (r >> 4)) & 1u);
                 };
+                const int pg0 = __shfl_sync(0xffffffffu, pid, lw * 2), pg1 = __shfl_sync(0xffffffffu, pid, lw * 2 + 1);
                 for (int kv = 0; kv < 2 && ok; ++kv, ++n_stage) {
                     const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE;
+                    if (n_stage >= CH_STAGES)
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up));
+                    if (!ok) break;
                     if (FMT == PF_16) {
-                        if (n_stage >= CH_STAGES) ok = bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
-                        if (!ok) break;
-                        constexpr int LPR = D / 8, RPP = 32 / LPR;
-                        const int c = lane % LPR;
-#pragma unroll
-                        for (int p = 0; p < 32 / RPP; ++p) {
-                            const int r = p * RPP + lane / LPR;
-                            const int pid = want(r);
-                            const size_t slot = pg_slot(a.pc, max(pid, 0), kv, w.h, (j0 + r) & ((1 << a.pc.page_shift) - 1));
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + swz(lw * 32 + r, c)),
-                                         "l"(a.pc.data + slot * (2 * D) + c * 16), "r"(pid >= 0 ? 16 : 0)
-                                         : "memory");
-                        }
-                        asm volatile("cp.async.commit_group;" ::: "memory");
-                    } else {
-                        constexpr int LPR = CodeRegs<FMT, D>::LPR, RPP = 32 / LPR;
-                        CodeRegs<FMT, D> cr;
-                        const int c = lane % LPR;
-#pragma unroll
-                        for (int p = 0; p < LPR; ++p) {
-                            const int r = p * RPP + lane / LPR, pid = want(r);
-                            const size_t slot = pg_slot(a.pc, max(pid, 0), kv, w.h, (j0 + r) & ((1 << a.pc.page_shift) - 1));
-                            cr.c[p] = make_uint4(0, 0, 0, 0);
-                            cr.s[p] = 0;
-                            if (pid >= 0) {
-                                cr.c[p] = __ldg(reinterpret_cast<const uint4*>(a.pc.data + slot * pg_row_bytes<FMT, D>()) + c);
-                                cr.s[p] = FMT == PF_I8 ? __ldg(reinterpret_cast<const uint16_t*>(a.pc.scale) + slot)
-                                                       : __ldg(reinterpret_cast<const uint32_t*>(a.pc.scale) + slot);
+                        if (kv == 1 && !clean) {
+                            constexpr int LPR = D / 8, RPP = 32 / LPR;
+                            const int c = lane % LPR;
+                            for (int p = 0; p < 32 / RPP; ++p) {
+                                const int r = p * RPP + lane / LPR, page = r < 16 ? pg0 : pg1;
+                                const bool get = seen(r) && page >= 0;
+                                const size_t slot = pg_slot(a.pc, get ? page : 0, 1, w.h, (j0 + lw * 32 + r) & ((1 << a.pc.page_shift) - 1));
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + swz(lw * 32 + r, c)),
+                                             "l"(a.pc.data + slot * (2 * D) + c * 16), "r"(get ? 16 : 0)
+                                             : "memory");
                             }
+                            asm volatile("cp.async.wait_all;" ::: "memory");
+                            fence_async();
+                            __syncwarp();
                         }
-                        if (n_stage >= CH_STAGES) ok = bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
+                    } else {
+                        constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
+                        constexpr int LPR = pg_row_bytes<FMT, D>() >= 16 ? pg_row_bytes<FMT, D>() / 16 : 1, RPP = 32 / LPR;
+                        const uint32_t rs = n_stage % N_RAW, raw0 = base + SM::RAWS + rs * SM::RAW;
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&bars.raw_full[rs]), (n_stage / N_RAW) & 1, gave_up));
                         if (!ok) break;
+                        const int c = lane % LPR;
 #pragma unroll
                         for (int p = 0; p < LPR; ++p) {
-                            const int r = lw * 32 + p * RPP + lane / LPR;
-                            const uint32_t words[4] = {cr.c[p].x, cr.c[p].y, cr.c[p].z, cr.c[p].w};
-                            const uint32_t s2 = dup_lo(cr.s[p]), z2 = dup_hi(cr.s[p]);
+                            const int r = p * RPP + lane / LPR, row = lw * 32 + r;
+                            uint32_t words[4], meta;
+                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(words[0]), "=r"(words[1]), "=r"(words[2]), "=r"(words[3])
+                                         : "r"(raw0 + row * pg_row_bytes<FMT, D>() + c * 16));
+                            if (FMT == PF_I8) {
+                                uint16_t s16;
+                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(s16) : "r"(raw0 + SM::RAW_CODES + row * 2));
+                                meta = s16;
+                            } else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(meta) : "r"(raw0 + SM::RAW_CODES + row * 4));
+                            if (!clean && !seen(r)) meta = 0;             // scale and zero 0: the row becomes zeros
+                            const uint32_t s2 = dup_lo(meta), z2 = dup_hi(meta);
                             if (FMT == PF_I8) {
 #pragma unroll
                                 for (int i = 0; i < 2; ++i)
-                                    sts16(dst + swz(r, 2 * c + i), mul2<T>(Codes<T>::bytes(words[2 * i], 0x5140), s2),
+                                    sts16(dst + swz(row, 2 * c + i), mul2<T>(Codes<T>::bytes(words[2 * i], 0x5140), s2),
                                           mul2<T>(Codes<T>::bytes(words[2 * i], 0x5342), s2), mul2<T>(Codes<T>::bytes(words[2 * i + 1], 0x5140), s2),
                                           mul2<T>(Codes<T>::bytes(words[2 * i + 1], 0x5342), s2));
                             } else {
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     const uint32_t y = words[i] >> 8;
-                                    sts16(dst + swz(r, 4 * c + i), fma2<T>(Codes<T>::nib_lo(words[i]), s2, z2), fma2<T>(Codes<T>::nib_hi(words[i]), s2, z2),
+                                    sts16(dst + swz(row, 4 * c + i), fma2<T>(Codes<T>::nib_lo(words[i]), s2, z2), fma2<T>(Codes<T>::nib_hi(words[i]), s2, z2),
                                           fma2<T>(Codes<T>::nib_lo(y), s2, z2), fma2<T>(Codes<T>::nib_hi(y), s2, z2));
                                 }
                             }
                         }
-                    }
-                    // which pages exist: read by the rows of this tile, whose scores come after this stage
-                    if (kv == 0 && tid == 8 * 32) {
-                        uint32_t mask = 0;
-                        for (int i = 0; i < 8; ++i) {
-                            const int j = g.sp.tile(k) * PT_KEYS + i * 16;
-                            bool there = true;
-                            if (j < g.sp.hi && !(j + 16 <= g.sp.lo && j >= a.sinks)) {
-                                const int p = table[j >> a.pc.page_shift];
-                                there = p >= 0 && p < a.pc.n_pages;
-                            }
-                            mask |= (there ? 1u : 0u) << i;
-                        }
-                        *(volatile uint32_t*)&bars.pages[n_tile & 3] = mask;
-                    }
-                    if (FMT == PF_16) {
-                        // the copies of two stages may still be under way
-                        if (n_stage >= 2) {
-                            asm volatile("cp.async.wait_group 2;" ::: "memory");
-                            fence_async();
-                            bar_arrive(smem_u32(&bars.kv_full[n_arrived++ % CH_STAGES]));
-                        }
-                    } else {
                         fence_async();
-                        bar_arrive(smem_u32(&bars.kv_full[stage]));
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_u32(&bars.raw_empty[rs]));
                     }
+                    if (lane == 0) bar_arrive(smem_u32(&bars.kv_full[stage]));
                 }
-                pg0 = nx0;
-                pg1 = nx1;
             }
             w.left -= g.k1 - g.k0;
             if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
-        }
-        if (FMT == PF_16) {
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_async();
-            while (n_arrived < n_stage) bar_arrive(smem_u32(&bars.kv_full[n_arrived++ % CH_STAGES]));
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -523,12 +511,81 @@ k_paged_chunk(PtArgs a, int blocks) {
                     }
                     if (t < g.tiles) {
                         tc_commit(smem_u32(&bars.kv_empty[ks % CH_STAGES]));
-                        if (t == 0) ++n_stage;
-                        else ++n_stage;
+                        ++n_stage;
                     }
                 }
                 w.left -= g.k1 - g.k0;
                 if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
+            }
+        }
+        if (wid == 13) {
+            // ---------------- feeder: lane i < 128 / page copies page i of a tile
+            uint32_t n_stage = 0, n_tile = 0;
+            bool ok = true;
+            const int per_page = 1 << a.pc.page_shift, n_pages = PT_KEYS >> a.pc.page_shift;
+            if (FMT == PF_16 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+            while (w.left > 0 && ok) {
+                g.set(a, w, s);
+                int pid16 = g.tiles > 0 ? g.page_of(a, w, g.k0, lane) : -2;
+                for (int k = g.k0; k < g.k0 + g.tiles && ok; ++k, ++n_tile) {
+                    const int pid16n = k + 1 < g.k0 + g.tiles ? g.page_of(a, w, k + 1, lane) : -2;
+                    const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), need = __ballot_sync(0xffffffffu, pid16 >= 0);
+                    const bool clean = g.clean(a, k) && bad == 0;
+                    if (bad != 0 && lane == 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
+                    // the first group of 16 keys of this lane's page that is needed names the page
+                    const uint32_t mine = lane < n_pages ? need >> (lane << (a.pc.page_shift - 4)) & ((1u << (per_page >> 4)) - 1u) : 0u;
+                    const int from = mine ? (lane << (a.pc.page_shift - 4)) + __ffs(mine) - 1 : 0;
+                    const int pid = __shfl_sync(0xffffffffu, pid16, from);
+                    const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine != 0));
+                    for (int kv = 0; kv < 2 && ok; ++kv, ++n_stage) {
+                        const size_t slot = pg_slot(a.pc, mine ? pid : 0, kv, w.h, 0);
+                        if (FMT == PF_16) {
+                            const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE, bar = smem_u32(&bars.kv_full[stage]);
+                            if (n_stage >= CH_STAGES)
+                                ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up));
+                            if (!ok) break;
+                            const bool copy = kv == 0 || clean;          // group 2 stores the others
+                            if (lane == 0) {
+                                if (kv == 0) *(volatile uint32_t*)&bars.pages[n_tile & 7] = ~bad & 0xffu;
+                                if (copy) bar_expect(bar, copies * (uint32_t)(per_page * D * 2));
+                                else bar_arrive(bar);
+                            }
+                            __syncwarp();
+                            if (copy && mine) {
+#pragma unroll
+                                for (int x = 0; x < D; x += 64) tensor_copy(dst + x * 256 + lane * per_page * 128, &map, x, (int)slot, bar);
+                            }
+                        } else {
+                            constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
+                            const uint32_t rs = n_stage % N_RAW, dst = base + SM::RAWS + rs * SM::RAW, bar = smem_u32(&bars.raw_full[rs]);
+                            if (n_stage >= N_RAW)
+                                ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&bars.raw_empty[rs]), (n_stage / N_RAW - 1) & 1, gave_up));
+                            if (!ok) break;
+                            constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
+                            if (lane == 0) {
+                                if (kv == 0) *(volatile uint32_t*)&bars.pages[n_tile & 7] = ~bad & 0xffu;
+                                bar_expect(bar, copies * per_page * (RB + MB));
+                            }
+                            __syncwarp();
+                            if (mine) {
+                                bulk_copy(dst + lane * per_page * RB, a.pc.data + slot * RB, per_page * RB, bar);
+                                bulk_copy(dst + SM::RAW_CODES + lane * per_page * MB, a.pc.scale + slot * MB, per_page * MB, bar);
+                            }
+                        }
+                    }
+                    pid16 = pid16n;
+                }
+                w.left -= g.k1 - g.k0;
+                if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
+            }
+            // copies in flight end before the block does: their stages have been waited for by those who used them; after
+            // an early leave, wait here
+            if (!ok) {
+                const uint32_t n = FMT == PF_16 ? CH_STAGES : (SM::N_RAW > 0 ? SM::N_RAW : 1);
+                for (uint32_t i = n_stage > n ? n_stage - n : 0; i < n_stage; ++i) {
+                    const uint32_t bar = FMT == PF_16 ? smem_u32(&bars.kv_full[i % n]) : smem_u32(&bars.raw_full[i % n]);
+                    for (int t = 0; t < (1 << 16) && !bar_try(bar, (i / n) & 1); ++t) {}
+                }
             }
         }
         __syncwarp();
@@ -550,73 +607,95 @@ k_paged_chunk(PtArgs a, int blocks) {
     }
 }
 
-// Joins the records of the item that block blockIdx.x left as its tail: a thread per row, grid.y over 32 dimensions each.
+// Joins split items: a thread per row, grid.y over CH_JOIN dimensions each.
+constexpr int CH_JOIN = 8;
 template <typename T, int D>
 __global__ void __launch_bounds__(CH_ROWS)
 k_paged_join_chunk(PtArgs a, int blocks) {
+    __shared__ int list[PT_MAX_BLOCKS + 1];
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    constexpr int N = CH_JOIN / 4;
     const int4 hd = a.head[blockIdx.x];
     if (hd.y == 0) return;
+    const int n = pt_records(a, blockIdx.x, blocks, list);
     const int row = threadIdx.x, b = hd.z, h = hd.y - 1, rt = hd.w;
     const PgSeq s = pg_seq(a.sq, a.pc, b);
     const int rr = rt * CH_ROWS + row;
     if (rr >= s.n * a.G) return;
-    const size_t t0 = 2 * (size_t)blockIdx.x + 1;
-    float M = a.stat[t0 * CH_ROWS + row].x;
-    int last = blockIdx.x;
-    for (int c = blockIdx.x + 1; c < blocks; ++c) {
-        const int f = a.head[c].x;
-        if (f == 0) continue;
-        M = fmaxf(M, a.stat[(size_t)(2 * c) * CH_ROWS + row].x);
-        last = c;
-        if (f == 2) break;
-    }
-    float4 o[8];
-    float l = 0.0f;
+    // the maximum moves along with the records: one pass over them
+    float M = PT_NONE, l = 0.0f;
+    float4 o[N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int c = blockIdx.x; c <= last; ++c) {
-        if (c != blockIdx.x && a.head[c].x == 0) continue;
-        const size_t t = c == blockIdx.x ? t0 : 2 * (size_t)c;
-        const float2 st = a.stat[t * CH_ROWS + row];
-        const float e = ex2(st.x - M);
-        l += e * st.y;
-        const float4* src = reinterpret_cast<const float4*>(a.part) + (t * (D / 4) + blockIdx.y * 8) * CH_ROWS + row;
+    for (int i = 0; i < N; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const size_t t = (size_t)list[i];
+        const float2 st = __ldg(a.stat + t * CH_ROWS + row);
+        const float4* src = reinterpret_cast<const float4*>(a.part) + (t * (D / 4) + blockIdx.y * N) * CH_ROWS + row;
+        const float nm = fmaxf(M, st.x), f = ex2(M - nm), e = ex2(st.x - nm);
+        M = nm;
+        l = l * f + e * st.y;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 v = __ldcs(src + i * CH_ROWS);
-            o[i].x += e * v.x;
-            o[i].y += e * v.y;
-            o[i].z += e * v.z;
-            o[i].w += e * v.w;
+        for (int x = 0; x < N; ++x) {
+            const float4 v = __ldcs(src + x * CH_ROWS);
+            o[x].x = o[x].x * f + e * v.x;
+            o[x].y = o[x].y * f + e * v.y;
+            o[x].z = o[x].z * f + e * v.z;
+            o[x].w = o[x].w * f + e * v.w;
         }
     }
     const int hq = h * a.G + rr % a.G;
     const long long tok = s.row0 + rr / a.G;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    uint4* dst = reinterpret_cast<uint4*>(a.out + tok * a.out_stride + (long long)hq * D + blockIdx.y * 32);
+    uint4* dst = reinterpret_cast<uint4*>(a.out + tok * a.out_stride + (long long)hq * D + blockIdx.y * CH_JOIN);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < N / 2; ++i)
         dst[i] = make_uint4(T::pack(o[2 * i].x * inv, o[2 * i].y * inv), T::pack(o[2 * i].z * inv, o[2 * i].w * inv),
                             T::pack(o[2 * i + 1].x * inv, o[2 * i + 1].y * inv), T::pack(o[2 * i + 1].z * inv, o[2 * i + 1].w * inv));
     if (a.lse && blockIdx.y == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (M + log2f(l)) * PT_LN2 : -INFINITY;
 }
 
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                 CUtensorMapFloatOOBfill);
+// The driver's encoder, looked up once (the library does not link against the driver).
+EncodeTiled tensor_encoder() {
+    static EncodeTiled fn = []() -> EncodeTiled {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess) return nullptr;
+        return found == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(p) : nullptr;
+    }();
+    return fn;
+}
+// All 16-bit pages as rows of D elements; a copy takes one page of one head, 64 elements wide, 128-byte swizzled.
+bool page_map(CUtensorMap* map, const PgCache& pc, int D, bool bf16) {
+    const EncodeTiled fn = tensor_encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)D, ((cuuint64_t)pc.n_pages * 2 * pc.heads) << pc.page_shift}, strides[1] = {(cuuint64_t)D * 2};
+    const cuuint32_t box[2] = {64, 1u << pc.page_shift}, step[2] = {1, 1};
+    return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, pc.data, dims, strides, box, step,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int FMT, int D>
 int launch_chunk(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
-    constexpr int BYTES = ChSmem<D>::BYTES;
+    constexpr int BYTES = ChSmem<FMT, D>::BYTES;
+    CUtensorMap map{};
+    if (FMT == PF_16 && !page_map(&map, a.pc, D, T::ONE == TypeBF16::ONE)) return SALICACHE_E_CUDA;
     SC_CHECK(cudaFuncSetAttribute(k_paged_chunk<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
-    const int blocks = c->sm_count;
+    const int blocks = min(c->sm_count, PT_MAX_BLOCKS);
     a.part = reinterpret_cast<float*>(work);
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * CH_ROWS * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * CH_ROWS);
-    k_paged_chunk<T, FMT, D><<<blocks, CH_THREADS, BYTES, st>>>(a, blocks);
+    k_paged_chunk<T, FMT, D><<<blocks, CH_THREADS, BYTES, st>>>(a, map, blocks);
     SC_CHECK(cudaGetLastError());
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(blocks, D / 32);
+    cfg.gridDim = dim3(blocks, D / CH_JOIN);
     cfg.blockDim = dim3(CH_ROWS);
     cfg.stream = st;
     cfg.attrs = &at;

@@ -74,43 +74,55 @@ struct PtWalk {
     int b, h, rt, k;                         // the next one: item and tile within it
 };
 
-// Every thread gets the same walk.  One thread per sequence sums its tiles; block-wide scans find the block's start.
+// Every thread gets the same walk.  One thread per sequence sums its tiles, a warp together where there are many row
+// tiles; block-wide scans find the block's start.
 template <int RT, int THREADS>
 __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int blocks) {
+    constexpr int ALONE = 2;                 // row tiles that a thread sums by itself
     __shared__ long long wsum[THREADS / 32];
     __shared__ PtWalk found;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    auto weight = [&](int b) -> long long {
-        if (b >= a.sq.n_seqs) return 0;
-        const PgSeq s = pg_seq(a.sq, a.pc, b);
+    // tiles of one head of sequence b; called by whole warps
+    auto per_head = [&](int b) -> long long {
+        PgSeq s{};
+        if (b < a.sq.n_seqs) s = pg_seq(a.sq, a.pc, b);
         const int R = pt_row_tiles<RT>(s, a.G);
         long long w = 0;
-        for (int rt = 0; rt < R; ++rt) w += max(1, pt_item<RT>(s, a, rt).n);
-        return w * a.pc.heads;
-    };
-    auto block_sum = [&](long long v) -> long long {
+        if (R <= ALONE)
+            for (int rt = 0; rt < R; ++rt) w += max(1, pt_item<RT>(s, a, rt).n);
+        for (uint32_t many = __ballot_sync(0xffffffffu, R > ALONE); many; many &= many - 1) {
+            const int from = __ffs(many) - 1;
+            PgSeq o{};
+            o.n = __shfl_sync(0xffffffffu, s.n, from);
+            o.pos0 = __shfl_sync(0xffffffffu, s.pos0, from);
+            o.len = __shfl_sync(0xffffffffu, s.len, from);
+            const int Ro = pt_row_tiles<RT>(o, a.G);
+            long long x = 0;
+            for (int rt = lane; rt < Ro; rt += 32) x += max(1, pt_item<RT>(o, a, rt).n);
 #pragma unroll
-        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0) wsum[wid] = v;
-        __syncthreads();
-        long long t = 0;
-#pragma unroll
-        for (int i = 0; i < THREADS / 32; ++i) t += wsum[i];
-        __syncthreads();
-        return t;
+            for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            if (lane == from) w = x;
+        }
+        return w;
     };
-    const long long w0 = weight(threadIdx.x);
+    const long long w0 = per_head(threadIdx.x) * a.pc.heads;
     long long mine = w0;
-    for (int b = threadIdx.x + THREADS; b < a.sq.n_seqs; b += THREADS) mine += weight(b);
-    const long long total = block_sum(mine);
-    const long long beg = total * block / blocks, end = total * (block + 1) / blocks;
+    for (int b0 = THREADS; b0 < a.sq.n_seqs; b0 += THREADS) mine += per_head(b0 + threadIdx.x) * a.pc.heads;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (lane == 0) wsum[wid] = mine;
     if (threadIdx.x == 0) found.left = 0;
     __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) total += wsum[i];
+    __syncthreads();
+    const long long beg = total * block / blocks, end = total * (block + 1) / blocks;
     if (beg == end) return found;
     long long before = 0;                    // tiles of the sequences before this round's
     for (int b0 = 0; b0 < a.sq.n_seqs; b0 += THREADS) {
         const int b = b0 + threadIdx.x;
-        const long long w = b0 == 0 ? w0 : weight(b);
+        const long long w = b0 == 0 ? w0 : per_head(b) * a.pc.heads;
         long long incl = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -122,22 +134,43 @@ __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int block
         long long off = before;
         for (int i = 0; i < wid; ++i) off += wsum[i];
         const long long at = beg - (off + incl - w);
-        if (at >= 0 && at < w) {             // this thread's sequence holds the start
-            const PgSeq s = pg_seq(a.sq, a.pc, b);
-            const long long per_head = w / a.pc.heads;
-            long long rem = at % per_head;
-            int rt = 0;
-            for (;; ++rt) {
-                const int n = max(1, pt_item<RT>(s, a, rt).n);
-                if (rem < n) break;
-                rem -= n;
-            }
-            found = PtWalk{end - beg, b, (int)(at / per_head), rt, (int)rem};
+        if (at >= 0 && at < w) {             // this thread's sequence holds the start: its head, and tiles into the head
+            const long long ph = w / a.pc.heads;
+            found.left = at % ph;
+            found.b = b;
+            found.h = (int)(at / ph);
         }
         for (int i = 0; i < THREADS / 32; ++i) before += wsum[i];
         __syncthreads();
         if (before > beg) break;
     }
+    if (wid == 0) {                          // the row tile and the tile in it
+        const PgSeq s = pg_seq(a.sq, a.pc, found.b);
+        const int R = pt_row_tiles<RT>(s, a.G);
+        long long rem = found.left;
+        for (int r0 = 0;; r0 += 32) {
+            const int n = r0 + lane < R ? max(1, pt_item<RT>(s, a, r0 + lane).n) : 0;
+            long long incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long t = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += t;
+            }
+            const uint32_t hit = __ballot_sync(0xffffffffu, rem >= incl - n && rem < incl);
+            if (hit || r0 + 32 >= R) {
+                const int from = hit ? __ffs(hit) - 1 : 0;
+                if (lane == from) {
+                    found.rt = r0 + lane;
+                    found.k = (int)(rem - (incl - n));
+                }
+                break;
+            }
+            rem -= __shfl_sync(0xffffffffu, incl, 31);
+        }
+        __syncwarp();
+        if (lane == 0) found.left = end - beg;
+    }
+    __syncthreads();
     return found;
 }
 
@@ -156,43 +189,62 @@ __device__ __forceinline__ void pt_next(PtWalk& w, PgSeq& s, const PtArgs& a) {
     } while (s.n == 0);
 }
 
-// Joins the records of the item that block blockIdx.x left as its tail.  grid.y: groups of 8 rows, one warp per row.
+// The record slots of the item that block c left as its tail: its tail, then later blocks' heads until one ends.  All
+// threads of the block get the count.
+__device__ __forceinline__ int pt_records(const PtArgs& a, int c, int blocks, int* list) {
+    __shared__ int count;
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        int n = 1;
+        if (lane == 0) list[0] = 2 * c + 1;
+        for (int c0 = c + 1; c0 < blocks; c0 += 32) {
+            const int f = c0 + lane < blocks ? a.head[c0 + lane].x : 0;
+            const uint32_t ends = __ballot_sync(0xffffffffu, f == 2);
+            const uint32_t upto = ends ? (2u << (__ffs(ends) - 1)) - 1u : 0xffffffffu;       // lanes up to the first that ends
+            const uint32_t has = __ballot_sync(0xffffffffu, f != 0) & upto;
+            if (has >> lane & 1u) list[n + __popc(has & ((1u << lane) - 1u))] = 2 * (c0 + lane);
+            n += __popc(has);
+            if (ends) break;
+        }
+        if (lane == 0) count = n;
+    }
+    __syncthreads();
+    return count;
+}
+constexpr int PT_MAX_BLOCKS = 1024;          // of the attention kernels
+
+// Joins split items.  grid.x: blocks of the first kernel, grid.y: groups of 8 rows, one warp per row.
 template <typename T, int RT, int D>
 __global__ void __launch_bounds__(256)
 k_paged_join(PtArgs a, int blocks) {
+    __shared__ int list[PT_MAX_BLOCKS + 1];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int N = D / 32;
     const int4 hd = a.head[blockIdx.x];
     if (hd.y == 0) return;
+    const int n = pt_records(a, blockIdx.x, blocks, list);
     const int lane = threadIdx.x & 31, row = blockIdx.y * 8 + (threadIdx.x >> 5);
     const int b = hd.z, h = hd.y - 1, rt = hd.w;
     const PgSeq s = pg_seq(a.sq, a.pc, b);
-    const long long r = (long long)rt * RT + row;
-    if (r >= (long long)s.n * a.G) return;
-    // the item's records: this block's tail, then later blocks' heads until one ends
-    const size_t t0 = (size_t)(2 * blockIdx.x + 1) * RT + row;
-    float M = a.stat[t0].x;
-    int last = blockIdx.x;
-    for (int c = blockIdx.x + 1; c < blocks; ++c) {
-        const int f = a.head[c].x;
-        if (f == 0) continue;
-        M = fmaxf(M, a.stat[(size_t)(2 * c) * RT + row].x);
-        last = c;
-        if (f == 2) break;
-    }
+    const int r = rt * RT + row;
+    if (r >= s.n * a.G) return;
+    float M = PT_NONE;
+    for (int i = lane; i < n; i += 32) M = fmaxf(M, a.stat[(size_t)list[i] * RT + row].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
     float o[N], l = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = 0.0f;
-    for (int c = blockIdx.x; c <= last; ++c) {
-        if (c != blockIdx.x && a.head[c].x == 0) continue;
-        const size_t t = c == blockIdx.x ? t0 : (size_t)(2 * c) * RT + row;
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+        const size_t t = (size_t)list[i] * RT + row;
         const float2 st = a.stat[t];
-        const float e = exp2f(st.x - M);
+        const float e = ex2(st.x - M);
         l += e * st.y;
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i] += e * a.part[t * D + lane * N + i];
+        for (int x = 0; x < N; ++x) o[x] += e * a.part[t * D + lane * N + x];
     }
-    const int hq = h * a.G + (int)(r % a.G);
+    const int hq = h * a.G + r % a.G;
     const long long tok = s.row0 + r / a.G;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     uint16_t* dst = a.out + tok * a.out_stride + (long long)hq * D + lane * N;

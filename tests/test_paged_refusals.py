@@ -40,7 +40,7 @@ CALLS = [_write, _read, _attend]
     (dict(d_data=None), sc.E_NULL), (dict(d_scale=None), sc.E_NULL), (dict(format=sc.REUSE), sc.E_PARAM), (dict(format=5), sc.E_PARAM),
     (dict(dtype=2), sc.E_PARAM), (dict(page=8), sc.E_PARAM), (dict(page=48), sc.E_PARAM), (dict(page=256), sc.E_PARAM),
     (dict(head_dim=96), sc.E_PARAM), (dict(head_dim=256), sc.E_PARAM), (dict(heads=0), sc.E_PARAM), (dict(heads=257), sc.E_PARAM),
-    (dict(n_pages=0), sc.E_SHAPE), (dict(d_data=A + 8), sc.E_ALIGN), (dict(d_scale=A + 2), sc.E_ALIGN),
+    (dict(n_pages=0), sc.E_SHAPE), (dict(n_pages=2 ** 22, heads=16, page=128), sc.E_SHAPE), (dict(d_data=A + 8), sc.E_ALIGN), (dict(d_scale=A + 2), sc.E_ALIGN),
 ])
 def test_pages_are_checked(call, pages, want):
     assert call(_pages(**pages), _seqs()) == want
