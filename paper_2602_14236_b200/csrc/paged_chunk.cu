@@ -28,7 +28,7 @@
 namespace {
 
 constexpr int CH_ROWS = 256, CH_THREADS = 512, CH_STAGES = 4;
-constexpr int CH_WAIT_LIMIT = 1 << 22;       // tries (each suspends for up to about a microsecond) before a wait gives up
+constexpr int CH_WAIT_LIMIT = 1 << 24;       // tries before a wait gives up (a second or more)
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -50,8 +50,8 @@ __device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2, %3; selp.b32 %0, 1, 0, p; }"
-                 : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2; selp.b32 %0, 1, 0, p; }"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 // False when the wait was given up, here or by another role: the caller leaves its loops.
@@ -101,9 +101,13 @@ __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sy
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Shared-memory operand: 128-byte swizzle; `lead` = bytes between blocks of 64 elements (only where those are the rows of
-// the result), 1024 bytes between groups of eight rows.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead) {
-    return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)((lead >> 4) & 0x3fffu) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+// the result), 1024 bytes between groups of eight rows.  The low word holds the address (16-byte units) and moves.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lead) { return addr >> 4 | (lead >> 4) << 16; }
+__device__ __forceinline__ uint64_t desc(uint32_t lo) { return (uint64_t)((1024u >> 4) | 1u << 14 | 2u << 29) << 32 | lo; }
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.b32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
 }
 // kind::f16, binary32 accumulator, M = 128; `vt`: B has the contracted dimension across its rows.
 template <typename T>
@@ -134,6 +138,9 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uin
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 constexpr int CH_RAW = 4;                    // raw stages at most
+// Bits 0 .. n - 1.
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
 struct ChBars {
     uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_ready[2], s_full[2], p_ready[2], o_done[2];
     uint32_t tmem;
@@ -213,7 +220,6 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     __syncthreads();
     tc_after();
     const uint32_t tmem = bars.tmem;
-    const uint32_t TS[2] = {tmem, tmem + 128}, TO[2] = {tmem + 256, tmem + 256 + 128};
     PgSeq s{};
     if (w.left > 0) s = pg_seq(a.sq, a.pc, w.b);
     ChSeg g;
@@ -223,7 +229,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int half = wid >> 2, row = tid & 127;
         const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
-        const uint32_t S = TS[half] + lane_base, O = TO[half] + lane_base;
+        const uint32_t S = tmem + 128 * half + lane_base, O = tmem + 256 + 128 * half + lane_base;
         const uint32_t q_ready = smem_u32(&bars.q_ready[half]), s_full = smem_u32(&bars.s_full[half]);
         const uint32_t p_ready = smem_u32(&bars.p_ready[half]), o_done = smem_u32(&bars.o_done[half]);
         uint32_t n_s = 0, n_o = 0, n_tile = 0;               // scores, outputs of this half and tiles seen so far
@@ -278,8 +284,13 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         if (!(j0 + PT_KEYS <= hs.all_hi && (j0 >= hs.all_lo || j0 + PT_KEYS <= a.sinks) && pages == 0xffu)) {
                             const int hi = vis_hi - j0, lo = vis_lo - j0, sk = a.sinks - j0;
 #pragma unroll
-                            for (int i = 0; i < 128; ++i)
-                                if (i >= hi || (i < lo && i >= sk) || !(pages >> (i >> 4) & 1u)) x[i] = 0xff800000u;
+                            for (int c = 0; c < 4; ++c) {        // 32 keys at a time as a word of visible ones
+                                const uint32_t there = ((pages >> (2 * c) & 1u) ? 0xffffu : 0u) | ((pages >> (2 * c + 1) & 1u) ? 0xffff0000u : 0u);
+                                const uint32_t vis = below(hi - 32 * c) & (~below(lo - 32 * c) | below(sk - 32 * c)) & there;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (!(vis & 1u << i)) x[32 * c + i] = 0xff800000u;
+                            }
                         }
                         float mx[4] = {__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3])};
 #pragma unroll
@@ -462,57 +473,65 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (wid == 12 && lane == 0) {
-            // ---------------- matrix instructions
+        if (wid == 12) {
+            // ---------------- matrix instructions: the warp stays together (its values are uniform), one lane issues
             constexpr uint32_t ID_S = instr_desc<T>(128, false), ID_O = instr_desc<T>(D, true);
             uint32_t n_stage = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
             bool ok = true;
+            const uint32_t q_lo = desc_lo(base + SM::Q, 16), k_lo = desc_lo(base + SM::KV, 16), v_lo = desc_lo(base + SM::KV, 16384);
+            auto wait = [&](uint64_t& bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, bar_wait(smem_u32(&bar), parity, gave_up)); };
             auto scores = [&](int h, uint32_t st) {
-                const uint32_t qa = base + SM::Q + h * SM::TILE, kb = base + SM::KV + st * SM::TILE;
+                const uint32_t qa = q_lo + h * (SM::TILE >> 4), kb = k_lo + st * (SM::TILE >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
-                    mma_ss(TS[h], smem_desc(qa + off, 16), smem_desc(kb + off, 16), ID_S, i > 0);
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t off = (i >> 2) * 1024 + (i & 3) * 2;
+                        mma_ss(tmem + 128 * h, desc(qa + off), desc(kb + off), ID_S, i > 0);
+                    }
+                    tc_commit(smem_u32(&bars.s_full[h]));
                 }
-                tc_commit(smem_u32(&bars.s_full[h]));
+                __syncwarp();
             };
-            auto sums = [&](int h, uint32_t st, bool add) {
-                const uint32_t vb = base + SM::KV + st * SM::TILE;
+            auto sums = [&](int h, uint32_t st, bool add, bool last) {
+                const uint32_t vb = v_lo + st * (SM::TILE >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int i = 0; i < PT_KEYS / 16; ++i) mma_ts(TO[h], TS[h] + 8 * i, smem_desc(vb + i * 2048, 16384), ID_O, add || i > 0);
+                    for (int i = 0; i < PT_KEYS / 16; ++i) mma_ts(tmem + 256 + 128 * h, tmem + 128 * h + 8 * i, desc(vb + i * 128), ID_O, add || i > 0);
+                    if (last) tc_commit(smem_u32(&bars.o_done[h]));
+                }
+                __syncwarp();
             };
             while (w.left > 0 && ok) {
                 g.set(a, w, s);
                 const int halves = g.rows > 128 ? 2 : 1;
-                for (int h = 0; h < halves && ok && g.tiles > 0; ++h) ok = bar_wait(smem_u32(&bars.q_ready[h]), n_q[h]++ & 1, gave_up);
+                for (int h = 0; h < halves && ok && g.tiles > 0; ++h) ok = wait(bars.q_ready[h], n_q[h]++ & 1);
                 for (int t = 0; t <= g.tiles && ok && g.tiles > 0; ++t) {
                     // stages in order: K(0), V(0), K(1), ...: V(t - 1) then K(t)
                     const uint32_t vs = n_stage, ks = t > 0 ? n_stage + 1 : n_stage;
-                    if (t > 0) ok = bar_wait(smem_u32(&bars.kv_full[vs % CH_STAGES]), (vs / CH_STAGES) & 1, gave_up);
-                    for (int h = 0; h < halves && ok; ++h) {
+                    if (t > 0) ok = wait(bars.kv_full[vs % CH_STAGES], (vs / CH_STAGES) & 1);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (h >= halves || !ok) break;
                         if (t > 0) {
-                            ok = bar_wait(smem_u32(&bars.p_ready[h]), n_p[h]++ & 1, gave_up);
+                            ok = wait(bars.p_ready[h], n_p[h]++ & 1);
                             if (!ok) break;
                             tc_after();
-                            sums(h, vs % CH_STAGES, t > 1);
-                            if (t == g.tiles) tc_commit(smem_u32(&bars.o_done[h]));
+                            sums(h, vs % CH_STAGES, t > 1, t == g.tiles);
                         }
                         if (t < g.tiles) {
-                            if (h == 0) ok = bar_wait(smem_u32(&bars.kv_full[ks % CH_STAGES]), (ks / CH_STAGES) & 1, gave_up);
+                            if (h == 0) ok = wait(bars.kv_full[ks % CH_STAGES], (ks / CH_STAGES) & 1);
                             if (!ok) break;
                             tc_after();
                             scores(h, ks % CH_STAGES);
                         }
                     }
                     if (!ok) break;
-                    if (t > 0) {
-                        tc_commit(smem_u32(&bars.kv_empty[vs % CH_STAGES]));
-                        ++n_stage;
+                    if (elect_one()) {
+                        if (t > 0) tc_commit(smem_u32(&bars.kv_empty[vs % CH_STAGES]));
+                        if (t < g.tiles) tc_commit(smem_u32(&bars.kv_empty[ks % CH_STAGES]));
                     }
-                    if (t < g.tiles) {
-                        tc_commit(smem_u32(&bars.kv_empty[ks % CH_STAGES]));
-                        ++n_stage;
-                    }
+                    __syncwarp();
+                    n_stage += (t > 0) + (t < g.tiles);
                 }
                 w.left -= g.k1 - g.k0;
                 if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
