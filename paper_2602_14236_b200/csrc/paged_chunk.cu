@@ -5,7 +5,8 @@
 // halves of 128 = the lanes of tensor memory; scores S = Q K^T and sums O += P V of both halves stand in all 512 columns.
 // Roles by warp group:
 //   0, 1   one thread per row of half 0 / 1: maximum over the row's 128 scores, weights, row sum; P overwrites S as the
-//          16-bit operand of the second product; also Q into shared memory before an item and the output after it
+//          16-bit operand of the second product, handed on in two parts; also the output, and the next item's Q, which
+//          is under way while the present item ends
 //   2      codes from a ring of raw stages to 16-bit operands; of 16-bit pages only the V tiles that hold positions no
 //          row sees, which are stored as zeros whatever the page holds there
 //   3      one thread issues the matrix instructions; one warp feeds the rings with bulk copies, a lane per page: tensor
@@ -90,6 +91,16 @@ __device__ __forceinline__ void tc_ld16(uint32_t* r, uint32_t addr) {
         : "r"(addr)
         : "memory");
 }
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31])
+        : "memory");
+}
 __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
@@ -97,7 +108,24 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* r) {
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The wait takes the loaded registers along, so that no use of them moves ahead of it.
+__device__ __forceinline__ void tc_wait_ld(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                   "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                   "+r"(r[28]), "+r"(r[29])
+                 :
+                 : "memory");
+    asm volatile("" : "+r"(r[30]), "+r"(r[31]) : : "memory");
+}
+__device__ __forceinline__ void tc_wait_ld16(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Shared-memory operand: 128-byte swizzle; `lead` = bytes between blocks of 64 elements (only where those are the rows of
@@ -135,6 +163,13 @@ __device__ __forceinline__ uint32_t swz(int r, int c) { return (uint32_t)((c >> 
 __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+__device__ __forceinline__ void lds16(uint32_t* v, uint32_t addr) {
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
+}
+// 16 bytes into shared memory behind the thread's back, or zeros.
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool get) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(get ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 constexpr int CH_RAW = 4;                    // raw stages at most
@@ -142,7 +177,7 @@ constexpr int CH_RAW = 4;                    // raw stages at most
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
 struct ChBars {
-    uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_ready[2], s_full[2], p_ready[2], o_done[2];
+    uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_ready[2], s_full[2], p_ready[2][2], o_done[2];
     uint32_t tmem;
     int gave_up;
     uint32_t pages[8];                       // per tile (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
@@ -205,7 +240,8 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_u32(&bars.q_ready[i]), 128);
             bar_init(smem_u32(&bars.s_full[i]), 1);
-            bar_init(smem_u32(&bars.p_ready[i]), 128);
+            bar_init(smem_u32(&bars.p_ready[i][0]), 128);
+            bar_init(smem_u32(&bars.p_ready[i][1]), 128);
             bar_init(smem_u32(&bars.o_done[i]), 1);
         }
         bars.gave_up = 0;
@@ -226,41 +262,66 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
 
     if (wid < 8) {
         // ---------------- rows: softmax, Q, output
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int half = wid >> 2, row = tid & 127;
         const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
         const uint32_t S = tmem + 128 * half + lane_base, O = tmem + 256 + 128 * half + lane_base;
         const uint32_t q_ready = smem_u32(&bars.q_ready[half]), s_full = smem_u32(&bars.s_full[half]);
-        const uint32_t p_ready = smem_u32(&bars.p_ready[half]), o_done = smem_u32(&bars.o_done[half]);
+        const uint32_t p_ready = smem_u32(&bars.p_ready[half][0]), o_done = smem_u32(&bars.o_done[half]);
+        const uint32_t q_tile = base + SM::Q + half * SM::TILE;
         uint32_t n_s = 0, n_o = 0, n_tile = 0;               // scores, outputs of this half and tiles seen so far
         int4 hd = make_int4(0, 0, 0, 0);
         bool ok = true;
+        // Q of an item's rows: a row by D / 8 lanes, asynchronously; each thread works out its own row's address
+        auto fetch_q = [&](const ChSeg& gg, const PtWalk& ww, const PgSeq& ss) {
+            const int rows = min(128, gg.rows - half * 128);
+            if (rows <= 0 || gg.tiles == 0) return;
+            const int x = ww.rt * CH_ROWS + half * 128 + min(row, rows - 1);
+            const long long at = (long long)(ss.row0 + x / a.G) * a.q_stride + (long long)(ww.h * a.G + x % a.G) * D;
+            constexpr int LPR = D / 8, RPP = 32 / LPR;
+#pragma unroll 4
+            for (int p = 0; p < 32 / RPP; ++p) {
+                const int lr = p * RPP + lane / LPR, qr = (wid & 3) * 32 + lr, c = lane % LPR;
+                const long long src = __shfl_sync(0xffffffffu, at, lr);
+                cp16(q_tile + swz(qr, c), a.q + src + c * 8, qr < rows);
+            }
+        };
+        if (w.left > 0) {
+            g.set(a, w, s);
+            fetch_q(g, w, s);
+        }
         while (w.left > 0 && ok) {
             g.set(a, w, s);
             const bool first = g.k0 == 0, lastp = g.k1 == max(g.sp.n, 1), done = first && lastp;
             const int rows = min(128, g.rows - half * 128);  // of this half
             if (tid == 0 && s.cut && s.pos0 + s.n > s.len) atomicMin(a.status, SALICACHE_E_CAPACITY);
+            // the item after this one
+            PtWalk wn = w;
+            PgSeq sn = s;
+            wn.left -= g.k1 - g.k0;
+            if (wn.left > 0) pt_next<CH_ROWS>(wn, sn, a);
+            bool fetched = false;
+            auto fetch_next = [&]() {
+                fetched = true;
+                if (wn.left <= 0) return;
+                ChSeg gn;
+                gn.set(a, wn, sn);
+                fetch_q(gn, wn, sn);
+            };
             if (rows > 0) {
                 const int rr = w.rt * CH_ROWS + half * 128 + row;                 // this thread's row of the item
                 const bool live = row < rows;
                 const int pos = s.pos0 + (live ? rr : 0) / a.G;
                 float m = PT_NONE, l = 0.0f;
                 if (g.tiles > 0) {
-                    // Q: a row by D / 8 lanes, 16 bytes each
-                    constexpr int LPR = D / 8, RPP = 32 / LPR;
-#pragma unroll 4
-                    for (int p = 0; p < 32 / RPP; ++p) {
-                        const int qr = (wid & 3) * 32 + p * RPP + lane / LPR, c = lane % LPR;
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (qr < rows) {
-                            const int x = w.rt * CH_ROWS + half * 128 + qr;
-                            v = __ldg(reinterpret_cast<const uint4*>(a.q + (long long)(s.row0 + x / a.G) * a.q_stride +
-                                                                     (long long)(w.h * a.G + x % a.G) * D) + c);
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    if (FMT == PF_I4) {          // the order in which codes leave their words
+                        __syncwarp();
+                        for (int c = 0; c < D / 8; ++c) {
+                            uint32_t v[4];
+                            lds16(v, q_tile + swz(row, c));
+                            sts16(q_tile + swz(row, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632),
+                                  __byte_perm(v[1], v[3], 0x5410), __byte_perm(v[1], v[3], 0x7632));
                         }
-                        if (FMT == PF_I4)        // the order in which codes leave their words
-                            v = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
-                                           __byte_perm(v.y, v.w, 0x7632));
-                        sts16(base + SM::Q + half * SM::TILE + swz(qr, c), v.x, v.y, v.z, v.w);
                     }
                     fence_async();
                     bar_arrive(q_ready);
@@ -273,62 +334,77 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         ++n_s;
                         if (!ok) break;
                         tc_after();
-                        uint32_t x[128];
-                        tc_ld32(x, S);
-                        tc_ld32(x + 32, S + 32);
-                        tc_ld32(x + 64, S + 64);
-                        tc_ld32(x + 96, S + 96);
-                        tc_wait_ld();
                         const int j0 = g.sp.tile(k) * PT_KEYS;
                         const uint32_t pages = *(volatile uint32_t*)&bars.pages[n_tile & 7];
+                        uint32_t x[2][32];
                         if (!(j0 + PT_KEYS <= hs.all_hi && (j0 >= hs.all_lo || j0 + PT_KEYS <= a.sinks) && pages == 0xffu)) {
                             const int hi = vis_hi - j0, lo = vis_lo - j0, sk = a.sinks - j0;
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < 4; ++c) {        // 32 keys at a time as a word of visible ones
                                 const uint32_t there = ((pages >> (2 * c) & 1u) ? 0xffffu : 0u) | ((pages >> (2 * c + 1) & 1u) ? 0xffff0000u : 0u);
                                 const uint32_t vis = below(hi - 32 * c) & (~below(lo - 32 * c) | below(sk - 32 * c)) & there;
+                                tc_ld32(x[0], S + 32 * c);
+                                tc_wait_ld(x[0]);
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
-                                    if (!(vis & 1u << i)) x[32 * c + i] = 0xff800000u;
+                                    if (!(vis & 1u << i)) x[0][i] = 0xff800000u;
+                                tc_st32(S + 32 * c, x[0]);
                             }
+                            tc_wait_st();
                         }
-                        float mx[4] = {__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3])};
+                        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                        tc_ld32(x[0], S);
+                        tc_wait_ld(x[0]);
 #pragma unroll
-                        for (int i = 4; i < 128; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
+                        for (int c = 0; c < 4; ++c) {
+                            if (c < 3) tc_ld32(x[(c + 1) & 1], S + 32 * (c + 1));
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2)
+                                mx[(i >> 1) & 3] = fmaxf(mx[(i >> 1) & 3], fmaxf(__uint_as_float(x[c & 1][i]), __uint_as_float(x[c & 1][i + 1])));
+                            if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
+                        }
+                        tc_ld32(x[0], S);
                         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
                         if (k == g.k0) m = fmaxf(m, top);
                         else if (__any_sync(0xffffffffu, top > m + 8.0f)) {
                             const float nm = fmaxf(m, top), f = ex2(m - nm);
                             m = nm;
                             l *= f;
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < D; c += 16) {
                                 uint32_t o[16];
                                 tc_ld16(o, O + c);
-                                tc_wait_ld();
+                                tc_wait_ld16(o);
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
                                 tc_st16(O + c, o);
                             }
                         }
-                        float sum[2] = {0.0f, 0.0f};
+                        tc_wait_ld(x[0]);
+                        // P takes half the columns of S: what it overwrites has been read
+                        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
+                            if (c < 3) tc_ld32(x[(c + 1) & 1], S + 32 * (c + 1));
                             uint32_t pk[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
-                                const float p0 = ex2(fmaf(__uint_as_float(x[32 * c + 2 * i]), a.scale, -m));
-                                const float p1 = ex2(fmaf(__uint_as_float(x[32 * c + 2 * i + 1]), a.scale, -m));
-                                sum[0] += p0;
-                                sum[1] += p1;
+                                const float p0 = ex2(fmaf(__uint_as_float(x[c & 1][2 * i]), a.scale, -m));
+                                const float p1 = ex2(fmaf(__uint_as_float(x[c & 1][2 * i + 1]), a.scale, -m));
+                                sum[2 * (i & 1)] += p0;
+                                sum[2 * (i & 1) + 1] += p1;
                                 pk[i] = T::pack(p0, p1);
                             }
+                            if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
                             tc_st16(S + 16 * c, pk);
+                            if (c & 1) {             // half of P: the product may start on it
+                                tc_wait_st();
+                                tc_before();
+                                bar_arrive(p_ready + 8 * (c >> 1));
+                            }
                         }
-                        l += sum[0] + sum[1];
-                        tc_wait_st();
-                        tc_before();
-                        bar_arrive(p_ready);
+                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                        if (k == g.k1 - 1) fetch_next();         // the scores are done with this item's Q
                     }
                     if (ok) {
                         ok = __all_sync(0xffffffffu, bar_wait(o_done, n_o & 1, gave_up));
@@ -344,13 +420,13 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     const long long tok = s.row0 + rr / a.G;
                     uint16_t* dst = a.out + tok * a.out_stride + (long long)hq * D;
                     float4* part = reinterpret_cast<float4*>(a.part) + slot * (D / 4) * CH_ROWS + half * 128 + row;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D; c += 32) {
                         uint32_t o[32];
                         __syncwarp();
                         if (g.tiles > 0) {
                             tc_ld32(o, O + c);
-                            tc_wait_ld();
+                            tc_wait_ld(o);
                         } else {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) o[i] = 0u;
@@ -375,6 +451,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     if (live && !done) a.stat[slot * CH_ROWS + half * 128 + row] = make_float2(m, l);
                 }
             } else n_tile += g.tiles;
+            if (!fetched) fetch_next();
             if (!done) {
                 if (first) {
                     hd.y = w.h + 1;
@@ -382,13 +459,13 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     hd.w = w.rt;
                 } else hd.x = lastp ? 2 : 1;
             }
-            w.left -= g.k1 - g.k0;
-            if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
+            w = wn;
+            s = sn;
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         if (tid == 0) a.head[blockIdx.x] = hd;
     } else if (wid < 12) {
         // ---------------- operands
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         const int lw = wid - 8;                              // this warp's rows: 32 lw .. 32 lw + 31 of a tile
         uint32_t n_stage = 0;
         bool ok = true;
@@ -418,9 +495,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                                 const int r = p * RPP + lane / LPR, page = r < 16 ? pg0 : pg1;
                                 const bool get = seen(r) && page >= 0;
                                 const size_t slot = pg_slot(a.pc, get ? page : 0, 1, w.h, (j0 + lw * 32 + r) & ((1 << a.pc.page_shift) - 1));
-                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + swz(lw * 32 + r, c)),
-                                             "l"(a.pc.data + slot * (2 * D) + c * 16), "r"(get ? 16 : 0)
-                                             : "memory");
+                                cp16(dst + swz(lw * 32 + r, c), a.pc.data + slot * (2 * D) + c * 16, get);
                             }
                             asm volatile("cp.async.wait_all;" ::: "memory");
                             fence_async();
@@ -437,8 +512,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         for (int p = 0; p < LPR; ++p) {
                             const int r = p * RPP + lane / LPR, row = lw * 32 + r;
                             uint32_t words[4], meta;
-                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(words[0]), "=r"(words[1]), "=r"(words[2]), "=r"(words[3])
-                                         : "r"(raw0 + row * pg_row_bytes<FMT, D>() + c * 16));
+                            lds16(words, raw0 + row * pg_row_bytes<FMT, D>() + c * 16);
                             if (FMT == PF_I8) {
                                 uint16_t s16;
                                 asm volatile("ld.shared.u16 %0, [%1];" : "=h"(s16) : "r"(raw0 + SM::RAW_CODES + row * 2));
@@ -472,7 +546,6 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (wid == 12) {
             // ---------------- matrix instructions: the warp stays together (its values are uniform), one lane issues
             constexpr uint32_t ID_S = instr_desc<T>(128, false), ID_O = instr_desc<T>(D, true);
@@ -492,11 +565,11 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 }
                 __syncwarp();
             };
-            auto sums = [&](int h, uint32_t st, bool add, bool last) {
+            auto sums = [&](int h, uint32_t st, int part, bool add, bool last) {         // keys 64 part .. 64 part + 63
                 const uint32_t vb = v_lo + st * (SM::TILE >> 4);
                 if (elect_one()) {
 #pragma unroll
-                    for (int i = 0; i < PT_KEYS / 16; ++i) mma_ts(tmem + 256 + 128 * h, tmem + 128 * h + 8 * i, desc(vb + i * 128), ID_O, add || i > 0);
+                    for (int i = 4 * part; i < 4 * part + 4; ++i) mma_ts(tmem + 256 + 128 * h, tmem + 128 * h + 8 * i, desc(vb + i * 128), ID_O, add || i > 0);
                     if (last) tc_commit(smem_u32(&bars.o_done[h]));
                 }
                 __syncwarp();
@@ -513,10 +586,14 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     for (int h = 0; h < 2; ++h) {
                         if (h >= halves || !ok) break;
                         if (t > 0) {
-                            ok = wait(bars.p_ready[h], n_p[h]++ & 1);
+                            ok = wait(bars.p_ready[h][0], n_p[h] & 1);
                             if (!ok) break;
                             tc_after();
-                            sums(h, vs % CH_STAGES, t > 1, t == g.tiles);
+                            sums(h, vs % CH_STAGES, 0, t > 1, false);
+                            ok = wait(bars.p_ready[h][1], n_p[h]++ & 1);
+                            if (!ok) break;
+                            tc_after();
+                            sums(h, vs % CH_STAGES, 1, true, t == g.tiles);
                         }
                         if (t < g.tiles) {
                             if (h == 0) ok = wait(bars.kv_full[ks % CH_STAGES], (ks / CH_STAGES) & 1);
