@@ -55,15 +55,14 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// False when the wait was given up, here or by another role: the caller leaves its loops.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-    if (bar_try(bar, parity)) return true;
+// A wait that is given up, here or by another role, returns all the same: the roles look at the flag once a tile and leave.
+__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
+    if (bar_try(bar, parity)) return;
     for (int i = 0; i < CH_WAIT_LIMIT; ++i) {
-        if (bar_try(bar, parity)) return true;
-        if (*gave_up) return false;
+        if (bar_try(bar, parity)) return;
+        if (*gave_up) return;
     }
     *gave_up = 1;
-    return false;
 }
 
 // ---- tensor memory and tcgen05
@@ -173,6 +172,47 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool get) {
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 constexpr int CH_RAW = 4;                    // raw stages at most
+// Two binary32 numbers at a time.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2f(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2f(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// 2^y without the special-function unit, which the exponentials alone would keep as busy as the products keep the tensor
+// core: y = n + f with n the nearest integer (by adding 1.5 * 2^23), 2^f by a polynomial of degree 5 fitted here for the
+// least relative error on [-1/2, 1/2] with the value 1 at 0 (1.6e-7 in binary32, as good as the unit's), n added to the
+// exponent.  From -127 down the result is 0, as it has to be for a masked score.
+constexpr int CH_POLY = 5;                   // of 16 pairs of weights
+__device__ __forceinline__ void poly_ex2(uint64_t y, float& p0, float& p1) {
+    float a, b;
+    unpack2(y, a, b);
+    y = pack2(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
+    const uint64_t big = pack2(12582912.0f, 12582912.0f), nbig = pack2(-12582912.0f, -12582912.0f), neg = pack2(-1.0f, -1.0f);
+    const uint64_t t = add2f(y, big), f = fma2f(add2f(t, nbig), neg, y);
+    uint64_t p = pack2(0.001326472731307149f, 0.001326472731307149f);
+    p = fma2f(p, f, pack2(0.009671512991189957f, 0.009671512991189957f));
+    p = fma2f(p, f, pack2(0.05550733581185341f, 0.05550733581185341f));
+    p = fma2f(p, f, pack2(0.24022242426872253f, 0.24022242426872253f));
+    p = fma2f(p, f, pack2(0.6931470036506653f, 0.6931470036506653f));
+    p = fma2f(p, f, pack2(1.0f, 1.0f));
+    float ta, tb;
+    unpack2(t, ta, tb);
+    unpack2(p, p0, p1);
+    p0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(ta) << 23));
+    p1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(tb) << 23));
+}
+
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
@@ -193,16 +233,24 @@ struct ChSmem {
     static_assert(BYTES <= 227 * 1024, "shared memory");
 };
 
-// A walk over a block's segments that every role repeats for itself.
+// A walk over a block's segments that every role repeats for itself.  An item's first CH_ITEM units stand for its fixed
+// cost (Q, output; measured at about three tiles' time), the others are its tiles.
+constexpr int CH_ITEM = 3;
 struct ChSeg {
     PtSpan sp;
-    int k0, k1, rows, tiles;                 // item tiles [k0, k1), rows in it (at most 256), tiles with keys
+    int k0, k1, t0, tiles, rows;             // units [k0, k1), first tile, tiles with keys, rows in the item (at most 256)
+    bool last, real;                         // the item's end is in here; some of its tiles are (an item without keys has one)
     __device__ __forceinline__ void set(const PtArgs& a, const PtWalk& w, const PgSeq& s) {
         sp = pt_item<CH_ROWS>(s, a, w.rt);
+        const int units = CH_ITEM + max(sp.n, 1);
         k0 = w.k;
-        k1 = (int)min((long long)max(sp.n, 1), k0 + w.left);
+        k1 = (int)min((long long)units, k0 + w.left);
         rows = min(CH_ROWS, s.n * a.G - w.rt * CH_ROWS);
-        tiles = sp.n == 0 ? 0 : k1 - k0;
+        t0 = max(0, k0 - CH_ITEM);
+        const int t1 = max(0, k1 - CH_ITEM);
+        last = k1 == units;
+        real = t1 > t0;
+        tiles = sp.n == 0 ? 0 : t1 - t0;
     }
     // Page of keys 16 grp .. of tile k: -2 no row sees them (or grp > 7), -1 there is no such page.
     __device__ __forceinline__ int page_of(const PtArgs& a, const PtWalk& w, int k, int grp) const {
@@ -238,10 +286,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             bar_init(smem_u32(&bars.raw_empty[i]), 4);
         }
         for (int i = 0; i < 2; ++i) {
-            bar_init(smem_u32(&bars.q_ready[i]), 128);
+            bar_init(smem_u32(&bars.q_ready[i]), 4);      // a lane of each of the half's warps
             bar_init(smem_u32(&bars.s_full[i]), 1);
-            bar_init(smem_u32(&bars.p_ready[i][0]), 128);
-            bar_init(smem_u32(&bars.p_ready[i][1]), 128);
+            bar_init(smem_u32(&bars.p_ready[i][0]), 4);
+            bar_init(smem_u32(&bars.p_ready[i][1]), 4);
             bar_init(smem_u32(&bars.o_done[i]), 1);
         }
         bars.gave_up = 0;
@@ -252,7 +300,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_before();
-    PtWalk w = pt_start<CH_ROWS, CH_THREADS>(a, blockIdx.x, blocks);
+    PtWalk w = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks);
     __syncthreads();
     tc_after();
     const uint32_t tmem = bars.tmem;
@@ -285,13 +333,30 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 cp16(q_tile + swz(qr, c), a.q + src + c * 8, qr < rows);
             }
         };
+        // ... and when it has arrived
+        auto hand_q = [&](const ChSeg& gg) {
+            if (gg.rows <= half * 128 || gg.tiles == 0) return;
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
+            if (FMT == PF_I4) {                  // the order in which codes leave their words
+                for (int c = 0; c < D / 8; ++c) {
+                    uint32_t v[4];
+                    lds16(v, q_tile + swz(row, c));
+                    sts16(q_tile + swz(row, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632),
+                          __byte_perm(v[1], v[3], 0x5410), __byte_perm(v[1], v[3], 0x7632));
+                }
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) bar_arrive(q_ready);
+        };
         if (w.left > 0) {
             g.set(a, w, s);
             fetch_q(g, w, s);
+            hand_q(g);
         }
         while (w.left > 0 && ok) {
-            g.set(a, w, s);
-            const bool first = g.k0 == 0, lastp = g.k1 == max(g.sp.n, 1), done = first && lastp;
+            const bool first = g.t0 == 0, lastp = g.last, done = first && lastp;
             const int rows = min(128, g.rows - half * 128);  // of this half
             if (tid == 0 && s.cut && s.pos0 + s.n > s.len) atomicMin(a.status, SALICACHE_E_CAPACITY);
             // the item after this one
@@ -299,42 +364,26 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             PgSeq sn = s;
             wn.left -= g.k1 - g.k0;
             if (wn.left > 0) pt_next<CH_ROWS>(wn, sn, a);
-            bool fetched = false;
-            auto fetch_next = [&]() {
-                fetched = true;
-                if (wn.left <= 0) return;
-                ChSeg gn;
-                gn.set(a, wn, sn);
-                fetch_q(gn, wn, sn);
-            };
+            ChSeg gn;
+            gn.rows = gn.tiles = 0;
+            if (wn.left > 0) gn.set(a, wn, sn);
+            bool handed = false;
             if (rows > 0) {
                 const int rr = w.rt * CH_ROWS + half * 128 + row;                 // this thread's row of the item
                 const bool live = row < rows;
                 const int pos = s.pos0 + (live ? rr : 0) / a.G;
                 float m = PT_NONE, l = 0.0f;
                 if (g.tiles > 0) {
-                    asm volatile("cp.async.wait_all;" ::: "memory");
-                    if (FMT == PF_I4) {          // the order in which codes leave their words
-                        __syncwarp();
-                        for (int c = 0; c < D / 8; ++c) {
-                            uint32_t v[4];
-                            lds16(v, q_tile + swz(row, c));
-                            sts16(q_tile + swz(row, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632),
-                                  __byte_perm(v[1], v[3], 0x5410), __byte_perm(v[1], v[3], 0x7632));
-                        }
-                    }
-                    fence_async();
-                    bar_arrive(q_ready);
                     // positions that every row of this half sees in full tiles need no mask
                     const PtSpan hs = pt_span(s, a.G, w.rt * CH_ROWS + half * 128, w.rt * CH_ROWS + half * 128 + rows, a.window, a.sinks);
                     const int vis_hi = live ? max(0, min(pos + 1, s.len)) : 0;
                     const int vis_lo = a.window ? pos - a.window + 1 : 0;
-                    for (int k = g.k0; k < g.k1 && ok; ++k, ++n_tile) {
-                        ok = __all_sync(0xffffffffu, bar_wait(s_full, n_s & 1, gave_up));
-                        ++n_s;
-                        if (!ok) break;
+                    for (int k = 0; k < g.tiles && ok; ++k, ++n_tile) {
+                        bar_wait(s_full, n_s++ & 1, gave_up);
+                        __syncwarp();
                         tc_after();
-                        const int j0 = g.sp.tile(k) * PT_KEYS;
+                        ok = *gave_up == 0;
+                        const int j0 = g.sp.tile(g.t0 + k) * PT_KEYS;
                         const uint32_t pages = *(volatile uint32_t*)&bars.pages[n_tile & 7];
                         uint32_t x[2][32];
                         if (!(j0 + PT_KEYS <= hs.all_hi && (j0 >= hs.all_lo || j0 + PT_KEYS <= a.sinks) && pages == 0xffu)) {
@@ -365,7 +414,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         }
                         tc_ld32(x[0], S);
                         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
-                        if (k == g.k0) m = fmaxf(m, top);
+                        if (k == 0) m = fmaxf(m, top);
                         else if (__any_sync(0xffffffffu, top > m + 8.0f)) {
                             const float nm = fmaxf(m, top), f = ex2(m - nm);
                             m = nm;
@@ -382,17 +431,23 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         }
                         tc_wait_ld(x[0]);
                         // P takes half the columns of S: what it overwrites has been read
-                        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        const uint64_t scale2 = pack2(a.scale, a.scale), m2 = pack2(-m, -m);
+                        uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             if (c < 3) tc_ld32(x[(c + 1) & 1], S + 32 * (c + 1));
                             uint32_t pk[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
-                                const float p0 = ex2(fmaf(__uint_as_float(x[c & 1][2 * i]), a.scale, -m));
-                                const float p1 = ex2(fmaf(__uint_as_float(x[c & 1][2 * i + 1]), a.scale, -m));
-                                sum[2 * (i & 1)] += p0;
-                                sum[2 * (i & 1) + 1] += p1;
+                                const uint64_t y = fma2f(pack2(__uint_as_float(x[c & 1][2 * i]), __uint_as_float(x[c & 1][2 * i + 1])), scale2, m2);
+                                float p0, p1;
+                                if (i % 16 < CH_POLY) poly_ex2(y, p0, p1);
+                                else {
+                                    unpack2(y, p0, p1);
+                                    p0 = ex2(p0);
+                                    p1 = ex2(p1);
+                                }
+                                sum[i & 1] = add2f(sum[i & 1], pack2(p0, p1));
                                 pk[i] = T::pack(p0, p1);
                             }
                             if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
@@ -400,19 +455,24 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                             if (c & 1) {             // half of P: the product may start on it
                                 tc_wait_st();
                                 tc_before();
-                                bar_arrive(p_ready + 8 * (c >> 1));
+                                __syncwarp();
+                                if (lane == 0) bar_arrive(p_ready + 8 * (c >> 1));
                             }
                         }
-                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                        if (k == g.k1 - 1) fetch_next();         // the scores are done with this item's Q
+                        float s0, s1;
+                        unpack2(add2f(sum[0], sum[1]), s0, s1);
+                        l += s0 + s1;
+                        if (k == g.tiles - 1) fetch_q(gn, wn, sn);           // the scores are done with this item's Q
                     }
                     if (ok) {
-                        ok = __all_sync(0xffffffffu, bar_wait(o_done, n_o & 1, gave_up));
-                        ++n_o;
+                        hand_q(gn);
+                        handed = true;
+                        bar_wait(o_done, n_o++ & 1, gave_up);
+                        __syncwarp();
                         tc_after();
                     }
                 }
-                if (ok) {
+                if (ok && g.real) {
                     // the output, or the partial record: float4 [D / 4][256 rows]
                     const size_t slot = 2 * (size_t)blockIdx.x + (first ? 1 : 0);
                     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
@@ -451,8 +511,11 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     if (live && !done) a.stat[slot * CH_ROWS + half * 128 + row] = make_float2(m, l);
                 }
             } else n_tile += g.tiles;
-            if (!fetched) fetch_next();
-            if (!done) {
+            if (!handed) {
+                fetch_q(gn, wn, sn);
+                hand_q(gn);
+            }
+            if (!done && g.real) {
                 if (first) {
                     hd.y = w.h + 1;
                     hd.z = w.b;
@@ -461,6 +524,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             }
             w = wn;
             s = sn;
+            g = gn;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (tid == 0) a.head[blockIdx.x] = hd;
@@ -471,7 +535,8 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         bool ok = true;
         while (w.left > 0 && ok) {
             g.set(a, w, s);
-            for (int k = g.k0; k < g.k0 + g.tiles && ok; ++k) {
+            for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k) {
+                ok = *gave_up == 0;
                 const int j0 = g.sp.tile(k) * PT_KEYS;
                 const int pid = g.page_of(a, w, k, lane);
                 const uint32_t bad = __ballot_sync(0xffffffffu, pid == -1);
@@ -482,11 +547,11 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     return j < g.sp.hi && (j >= g.sp.lo || j < a.sinks) && !(bad >> (lw * 2 + (r >> 4)) & 1u);
                 };
                 const int pg0 = __shfl_sync(0xffffffffu, pid, lw * 2), pg1 = __shfl_sync(0xffffffffu, pid, lw * 2 + 1);
-                for (int kv = 0; kv < 2 && ok; ++kv, ++n_stage) {
+                for (int kv = 0; kv < 2; ++kv, ++n_stage) {
                     const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE;
                     if (n_stage >= CH_STAGES)
-                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up));
-                    if (!ok) break;
+                        bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
+                    __syncwarp();
                     if (FMT == PF_16) {
                         if (kv == 1 && !clean) {
                             constexpr int LPR = D / 8, RPP = 32 / LPR;
@@ -505,8 +570,8 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
                         constexpr int LPR = pg_row_bytes<FMT, D>() >= 16 ? pg_row_bytes<FMT, D>() / 16 : 1, RPP = 32 / LPR;
                         const uint32_t rs = n_stage % N_RAW, raw0 = base + SM::RAWS + rs * SM::RAW;
-                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&bars.raw_full[rs]), (n_stage / N_RAW) & 1, gave_up));
-                        if (!ok) break;
+                        bar_wait(smem_u32(&bars.raw_full[rs]), (n_stage / N_RAW) & 1, gave_up);
+                        __syncwarp();
                         const int c = lane % LPR;
 #pragma unroll
                         for (int p = 0; p < LPR; ++p) {
@@ -552,7 +617,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             uint32_t n_stage = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
             bool ok = true;
             const uint32_t q_lo = desc_lo(base + SM::Q, 16), k_lo = desc_lo(base + SM::KV, 16), v_lo = desc_lo(base + SM::KV, 16384);
-            auto wait = [&](uint64_t& bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, bar_wait(smem_u32(&bar), parity, gave_up)); };
+            auto wait = [&](uint64_t& bar, uint32_t parity) {
+                bar_wait(smem_u32(&bar), parity, gave_up);
+                __syncwarp();
+            };
             auto scores = [&](int h, uint32_t st) {
                 const uint32_t qa = q_lo + h * (SM::TILE >> 4), kb = k_lo + st * (SM::TILE >> 4);
                 if (elect_one()) {
@@ -577,32 +645,29 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             while (w.left > 0 && ok) {
                 g.set(a, w, s);
                 const int halves = g.rows > 128 ? 2 : 1;
-                for (int h = 0; h < halves && ok && g.tiles > 0; ++h) ok = wait(bars.q_ready[h], n_q[h]++ & 1);
+                for (int h = 0; h < halves && g.tiles > 0; ++h) wait(bars.q_ready[h], n_q[h]++ & 1);
                 for (int t = 0; t <= g.tiles && ok && g.tiles > 0; ++t) {
+                    ok = *gave_up == 0;
                     // stages in order: K(0), V(0), K(1), ...: V(t - 1) then K(t)
                     const uint32_t vs = n_stage, ks = t > 0 ? n_stage + 1 : n_stage;
-                    if (t > 0) ok = wait(bars.kv_full[vs % CH_STAGES], (vs / CH_STAGES) & 1);
+                    if (t > 0) wait(bars.kv_full[vs % CH_STAGES], (vs / CH_STAGES) & 1);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        if (h >= halves || !ok) break;
+                        if (h >= halves) break;
                         if (t > 0) {
-                            ok = wait(bars.p_ready[h][0], n_p[h] & 1);
-                            if (!ok) break;
+                            wait(bars.p_ready[h][0], n_p[h] & 1);
                             tc_after();
                             sums(h, vs % CH_STAGES, 0, t > 1, false);
-                            ok = wait(bars.p_ready[h][1], n_p[h]++ & 1);
-                            if (!ok) break;
+                            wait(bars.p_ready[h][1], n_p[h]++ & 1);
                             tc_after();
                             sums(h, vs % CH_STAGES, 1, true, t == g.tiles);
                         }
                         if (t < g.tiles) {
-                            if (h == 0) ok = wait(bars.kv_full[ks % CH_STAGES], (ks / CH_STAGES) & 1);
-                            if (!ok) break;
+                            if (h == 0) wait(bars.kv_full[ks % CH_STAGES], (ks / CH_STAGES) & 1);
                             tc_after();
                             scores(h, ks % CH_STAGES);
                         }
                     }
-                    if (!ok) break;
                     if (elect_one()) {
                         if (t > 0) tc_commit(smem_u32(&bars.kv_empty[vs % CH_STAGES]));
                         if (t < g.tiles) tc_commit(smem_u32(&bars.kv_empty[ks % CH_STAGES]));
@@ -622,9 +687,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             if (FMT == PF_16 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
             while (w.left > 0 && ok) {
                 g.set(a, w, s);
-                int pid16 = g.tiles > 0 ? g.page_of(a, w, g.k0, lane) : -2;
-                for (int k = g.k0; k < g.k0 + g.tiles && ok; ++k, ++n_tile) {
-                    const int pid16n = k + 1 < g.k0 + g.tiles ? g.page_of(a, w, k + 1, lane) : -2;
+                int pid16 = g.tiles > 0 ? g.page_of(a, w, g.t0, lane) : -2;
+                for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k, ++n_tile) {
+                    ok = *gave_up == 0;
+                    const int pid16n = k + 1 < g.t0 + g.tiles ? g.page_of(a, w, k + 1, lane) : -2;
                     const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), need = __ballot_sync(0xffffffffu, pid16 >= 0);
                     const bool clean = g.clean(a, k) && bad == 0;
                     if (bad != 0 && lane == 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
@@ -633,13 +699,13 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     const int from = mine ? (lane << (a.pc.page_shift - 4)) + __ffs(mine) - 1 : 0;
                     const int pid = __shfl_sync(0xffffffffu, pid16, from);
                     const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine != 0));
-                    for (int kv = 0; kv < 2 && ok; ++kv, ++n_stage) {
+                    for (int kv = 0; kv < 2; ++kv, ++n_stage) {
                         const size_t slot = pg_slot(a.pc, mine ? pid : 0, kv, w.h, 0);
                         if (FMT == PF_16) {
                             const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE, bar = smem_u32(&bars.kv_full[stage]);
                             if (n_stage >= CH_STAGES)
-                                ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up));
-                            if (!ok) break;
+                                bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
+                            __syncwarp();
                             const bool copy = kv == 0 || clean;          // group 2 stores the others
                             if (lane == 0) {
                                 if (kv == 0) *(volatile uint32_t*)&bars.pages[n_tile & 7] = ~bad & 0xffu;
@@ -655,8 +721,8 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                             constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
                             const uint32_t rs = n_stage % N_RAW, dst = base + SM::RAWS + rs * SM::RAW, bar = smem_u32(&bars.raw_full[rs]);
                             if (n_stage >= N_RAW)
-                                ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&bars.raw_empty[rs]), (n_stage / N_RAW - 1) & 1, gave_up));
-                            if (!ok) break;
+                                bar_wait(smem_u32(&bars.raw_empty[rs]), (n_stage / N_RAW - 1) & 1, gave_up);
+                            __syncwarp();
                             constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
                             if (lane == 0) {
                                 if (kv == 0) *(volatile uint32_t*)&bars.pages[n_tile & 7] = ~bad & 0xffu;
@@ -723,7 +789,7 @@ k_paged_join_chunk(PtArgs a, int blocks) {
     float4 o[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < n; ++i) {
         const size_t t = (size_t)list[i];
         const float2 st = __ldg(a.stat + t * CH_ROWS + row);

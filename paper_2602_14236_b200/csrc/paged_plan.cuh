@@ -76,7 +76,8 @@ struct PtWalk {
 
 // Every thread gets the same walk.  One thread per sequence sums its tiles, a warp together where there are many row
 // tiles; block-wide scans find the block's start.
-template <int RT, int THREADS>
+// ITEM: units an item counts beside its tiles, before them.
+template <int RT, int THREADS, int ITEM>
 __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int blocks) {
     constexpr int ALONE = 2;                 // row tiles that a thread sums by itself
     __shared__ long long wsum[THREADS / 32];
@@ -89,7 +90,7 @@ __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int block
         const int R = pt_row_tiles<RT>(s, a.G);
         long long w = 0;
         if (R <= ALONE)
-            for (int rt = 0; rt < R; ++rt) w += max(1, pt_item<RT>(s, a, rt).n);
+            for (int rt = 0; rt < R; ++rt) w += ITEM + max(1, pt_item<RT>(s, a, rt).n);
         for (uint32_t many = __ballot_sync(0xffffffffu, R > ALONE); many; many &= many - 1) {
             const int from = __ffs(many) - 1;
             PgSeq o{};
@@ -98,7 +99,7 @@ __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int block
             o.len = __shfl_sync(0xffffffffu, s.len, from);
             const int Ro = pt_row_tiles<RT>(o, a.G);
             long long x = 0;
-            for (int rt = lane; rt < Ro; rt += 32) x += max(1, pt_item<RT>(o, a, rt).n);
+            for (int rt = lane; rt < Ro; rt += 32) x += ITEM + max(1, pt_item<RT>(o, a, rt).n);
 #pragma unroll
             for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
             if (lane == from) w = x;
@@ -149,7 +150,7 @@ __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int block
         const int R = pt_row_tiles<RT>(s, a.G);
         long long rem = found.left;
         for (int r0 = 0;; r0 += 32) {
-            const int n = r0 + lane < R ? max(1, pt_item<RT>(s, a, r0 + lane).n) : 0;
+            const int n = r0 + lane < R ? ITEM + max(1, pt_item<RT>(s, a, r0 + lane).n) : 0;
             long long incl = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
