@@ -160,8 +160,7 @@ k_paged_step(PtArgs a, int blocks) {
     __shared__ float2 sh_stat[ST_WARPS][8];
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g8 = lane >> 2, c4 = lane & 3;
     const int c = blockIdx.x;
-    __shared__ PtShared sh_plan;
-    PtWalk w = pt_start<RT, ST_THREADS, 0>(a, c, blocks, sh_plan);
+    PtWalk w = pt_start<RT, ST_THREADS, 0>(a, c, blocks);
     int4 hd = make_int4(0, 0, 0, 0);
     PgSeq s;
     if (w.left > 0) s = pg_seq(a.sq, a.pc, w.b);

@@ -4,14 +4,13 @@
 // One block per SM walks its stretch of the line of (256 rows x 128 keys) tiles (paged_plan.cuh).  A tile's rows are two
 // halves of 128 = the lanes of tensor memory; scores S = Q K^T and sums O += P V of both halves stand in all 512 columns.
 // Roles by warp group:
-//   0 .. 3  two threads per row, 64 keys each: maximum over the row's scores (joined through shared memory), weights, row
-//           sums; P overwrites its own part of S as the 16-bit operand of the second product.  Also the output, and the next
-//           item's Q, which is under way while the present item ends.  (With one thread per row and 128 keys a half's round
-//           of products and weights took 3600 clocks, most of it one warp's latencies; the products alone need 2050.)
-//   4       codes from a ring of raw stages to 16-bit operands; of 16-bit pages only the V tiles that hold positions no
-//           row sees, which are stored as zeros whatever the page holds there
-//   5       one thread issues the matrix instructions; one warp feeds the rings with bulk copies, a lane per page: tensor
-//           copies straight into the operand stages (16-bit pages), plain ones of codes and scales into the raw stages
+//   0, 1   one thread per row of half 0 / 1: maximum over the row's 128 scores, weights, row sum; P overwrites S as the
+//          16-bit operand of the second product, handed on in two parts; also the output, and the next item's Q, which
+//          is under way while the present item ends
+//   2      codes from a ring of raw stages to 16-bit operands; of 16-bit pages only the V tiles that hold positions no
+//          row sees, which are stored as zeros whatever the page holds there
+//   3      one thread issues the matrix instructions; one warp feeds the rings with bulk copies, a lane per page: tensor
+//          copies straight into the operand stages (16-bit pages), plain ones of codes and scales into the raw stages
 // While one half's weights are formed, the tensor core works for the other: the products of a half are issued as
 // P(t) V(t), then Q K(t+1).  Instructions of one thread run in order there, so S may be overwritten right behind the
 // product that read P from the same columns, and whoever sees the scores of tile t knows the sums of tile t-1 complete.
@@ -29,7 +28,7 @@
 
 namespace {
 
-constexpr int CH_ROWS = 256, CH_THREADS = 768, CH_STAGES = 4;
+constexpr int CH_ROWS = 256, CH_THREADS = 512, CH_STAGES = 4;
 constexpr int CH_WAIT_LIMIT = 1 << 24;       // tries before a wait gives up (a second or more)
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -64,14 +63,6 @@ __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile
         if (*gave_up) return;
     }
     *gave_up = 1;
-}
-
-// Joins two warps; whether any of their threads says so.
-__device__ __forceinline__ bool pair_any(int id, bool x) {
-    uint32_t r;
-    asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %2, 0; barrier.cta.red.or.pred q, %1, 64, p; selp.b32 %0, 1, 0, q; }"
-                 : "=r"(r) : "r"(id), "r"((uint32_t)x) : "memory");
-    return r != 0;
 }
 
 // ---- tensor memory and tcgen05
@@ -202,7 +193,7 @@ __device__ __forceinline__ uint64_t add2f(uint64_t a, uint64_t b) {
 // core: y = n + f with n the nearest integer (by adding 1.5 * 2^23), 2^f by a polynomial of degree 5 fitted here for the
 // least relative error on [-1/2, 1/2] with the value 1 at 0 (1.6e-7 in binary32, as good as the unit's), n added to the
 // exponent.  From -127 down the result is 0, as it has to be for a masked score.
-constexpr int CH_POLY = 0;                   // of 16 pairs of weights
+constexpr int CH_POLY = 5;                   // of 16 pairs of weights
 __device__ __forceinline__ void poly_ex2(uint64_t y, float& p0, float& p1) {
     float a, b;
     unpack2(y, a, b);
@@ -229,10 +220,6 @@ struct ChBars {
     uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_ready[2], s_full[2], p_ready[2][2], o_done[2];
     uint32_t tmem;
     int gave_up;
-    union {
-        PtShared plan;                       // before the roles part
-        float xch[2][2][128];                // [half][part][row]: a part's maximum, at the end its sum
-    };
     uint32_t pages[8];                       // per tile (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
 };
 
@@ -242,7 +229,7 @@ struct ChSmem {
     static constexpr int RAW_CODES = 128 * pg_row_bytes<FMT, D>(), RAW = RAW_CODES + 128 * pg_meta_bytes<FMT>();
     static constexpr int N_RAW = FMT == PF_16 ? 0 : D == 64 ? 4 : FMT == PF_I4 ? 3 : 2;      // what 227 KB leave room for
     static constexpr int Q = 0, KV = 2 * TILE, RAWS = KV + CH_STAGES * TILE, BARS = RAWS + N_RAW * RAW;
-    static constexpr int BYTES = BARS + (int)sizeof(ChBars);
+    static constexpr int BYTES = BARS + (int)sizeof(ChBars) + 1024;
     static_assert(BYTES <= 227 * 1024, "shared memory");
 };
 
@@ -283,18 +270,11 @@ template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(CH_THREADS, 1)
 k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     using SM = ChSmem<FMT, D>;
-    extern __shared__ __align__(1024) uint8_t raw[];        // the kernel's only shared memory: it starts on an atom
-    const uint32_t base = smem_u32(raw);
-    ChBars& bars = *reinterpret_cast<ChBars*>(raw + SM::BARS);
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    ChBars& bars = *reinterpret_cast<ChBars*>(raw + (base - smem_u32(raw)) + SM::BARS);
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
     volatile int* gave_up = &bars.gave_up;
-    if (base & 1023u) {                      // never so far; nothing below would work
-        if (tid == 0) {
-            atomicMin(a.status, SALICACHE_E_CUDA);
-            a.head[blockIdx.x] = make_int4(0, 0, 0, 0);
-        }
-        return;
-    }
 
     if (tid == 0) {
         for (int i = 0; i < CH_STAGES; ++i) {
@@ -306,7 +286,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             bar_init(smem_u32(&bars.raw_empty[i]), 4);
         }
         for (int i = 0; i < 2; ++i) {
-            bar_init(smem_u32(&bars.q_ready[i]), 8);      // a lane of each of the half's warps
+            bar_init(smem_u32(&bars.q_ready[i]), 4);      // a lane of each of the half's warps
             bar_init(smem_u32(&bars.s_full[i]), 1);
             bar_init(smem_u32(&bars.p_ready[i][0]), 4);
             bar_init(smem_u32(&bars.p_ready[i][1]), 4);
@@ -315,12 +295,12 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         bars.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (wid == 20) {
+    if (wid == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_before();
-    PtWalk w = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks, bars.plan);
+    PtWalk w = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks);
     __syncthreads();
     tc_after();
     const uint32_t tmem = bars.tmem;
@@ -328,33 +308,29 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     if (w.left > 0) s = pg_seq(a.sq, a.pc, w.b);
     ChSeg g;
 
-    if (wid < 16) {
+    if (wid < 8) {
         // ---------------- rows: softmax, Q, output
-        const int half = wid >> 3, part = (wid >> 2) & 1, row = (wid & 3) * 32 + lane;
+        const int half = wid >> 2, row = tid & 127;
         const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
-        const uint32_t S = tmem + 128 * half + 64 * part + lane_base, O = tmem + 256 + 128 * half + part * (D / 2) + lane_base;
+        const uint32_t S = tmem + 128 * half + lane_base, O = tmem + 256 + 128 * half + lane_base;
         const uint32_t q_ready = smem_u32(&bars.q_ready[half]), s_full = smem_u32(&bars.s_full[half]);
-        const uint32_t p_ready = smem_u32(&bars.p_ready[half][part]), o_done = smem_u32(&bars.o_done[half]);
+        const uint32_t p_ready = smem_u32(&bars.p_ready[half][0]), o_done = smem_u32(&bars.o_done[half]);
         const uint32_t q_tile = base + SM::Q + half * SM::TILE;
-        const int pair = 1 + half * 4 + (wid & 3);           // barrier of the two warps that share 32 rows
-        volatile float* mine = &bars.xch[half][part][row];
-        volatile float* other = &bars.xch[half][part ^ 1][row];
         uint32_t n_s = 0, n_o = 0, n_tile = 0;               // scores, outputs of this half and tiles seen so far
         int4 hd = make_int4(0, 0, 0, 0);
         bool ok = true;
-        // Q of an item's rows: 16 rows a warp, a row by D / 8 lanes, asynchronously
-        const int q_row = (wid & 7) * 16;
+        // Q of an item's rows: a row by D / 8 lanes, asynchronously; each thread works out its own row's address
         auto fetch_q = [&](const ChSeg& gg, const PtWalk& ww, const PgSeq& ss) {
             const int rows = min(128, gg.rows - half * 128);
             if (rows <= 0 || gg.tiles == 0) return;
-            const int x = ww.rt * CH_ROWS + half * 128 + min(q_row + (lane & 15), rows - 1);
+            const int x = ww.rt * CH_ROWS + half * 128 + min(row, rows - 1);
             const long long at = (long long)(ss.row0 + x / a.G) * a.q_stride + (long long)(ww.h * a.G + x % a.G) * D;
             constexpr int LPR = D / 8, RPP = 32 / LPR;
-#pragma unroll
-            for (int p = 0; p < 16 / RPP; ++p) {
-                const int lr = p * RPP + lane / LPR, c = lane % LPR;
+#pragma unroll 4
+            for (int p = 0; p < 32 / RPP; ++p) {
+                const int lr = p * RPP + lane / LPR, qr = (wid & 3) * 32 + lr, c = lane % LPR;
                 const long long src = __shfl_sync(0xffffffffu, at, lr);
-                cp16(q_tile + swz(q_row + lr, c), a.q + src + c * 8, q_row + lr < rows);
+                cp16(q_tile + swz(qr, c), a.q + src + c * 8, qr < rows);
             }
         };
         // ... and when it has arrived
@@ -363,11 +339,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();
             if (FMT == PF_I4) {                  // the order in which codes leave their words
-                const int r = q_row + (lane & 15);
-                for (int c = (lane >> 4) * (D / 16); c < (lane >> 4) * (D / 16) + D / 16; ++c) {
+                for (int c = 0; c < D / 8; ++c) {
                     uint32_t v[4];
-                    lds16(v, q_tile + swz(r, c));
-                    sts16(q_tile + swz(r, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632),
+                    lds16(v, q_tile + swz(row, c));
+                    sts16(q_tile + swz(row, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632),
                           __byte_perm(v[1], v[3], 0x5410), __byte_perm(v[1], v[3], 0x7632));
                 }
             }
@@ -381,7 +356,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             hand_q(g);
         }
         while (w.left > 0 && ok) {
-            const bool first = g.t0 == 0, done = first && g.last;
+            const bool first = g.t0 == 0, lastp = g.last, done = first && lastp;
             const int rows = min(128, g.rows - half * 128);  // of this half
             if (tid == 0 && s.cut && s.pos0 + s.n > s.len) atomicMin(a.status, SALICACHE_E_CAPACITY);
             // the item after this one
@@ -403,49 +378,49 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     const PtSpan hs = pt_span(s, a.G, w.rt * CH_ROWS + half * 128, w.rt * CH_ROWS + half * 128 + rows, a.window, a.sinks);
                     const int vis_hi = live ? max(0, min(pos + 1, s.len)) : 0;
                     const int vis_lo = a.window ? pos - a.window + 1 : 0;
-                    for (int k = 0; k < g.tiles; ++k, ++n_tile) {
+                    for (int k = 0; k < g.tiles && ok; ++k, ++n_tile) {
                         bar_wait(s_full, n_s++ & 1, gave_up);
                         __syncwarp();
                         tc_after();
+                        ok = *gave_up == 0;
                         const int j0 = g.sp.tile(g.t0 + k) * PT_KEYS;
                         const uint32_t pages = *(volatile uint32_t*)&bars.pages[n_tile & 7];
-                        uint32_t x[32];
+                        uint32_t x[2][32];
                         if (!(j0 + PT_KEYS <= hs.all_hi && (j0 >= hs.all_lo || j0 + PT_KEYS <= a.sinks) && pages == 0xffu)) {
                             const int hi = vis_hi - j0, lo = vis_lo - j0, sk = a.sinks - j0;
 #pragma unroll 1
-                            for (int c = 2 * part; c < 2 * part + 2; ++c) {       // 32 keys at a time as a word of visible ones
+                            for (int c = 0; c < 4; ++c) {        // 32 keys at a time as a word of visible ones
                                 const uint32_t there = ((pages >> (2 * c) & 1u) ? 0xffffu : 0u) | ((pages >> (2 * c + 1) & 1u) ? 0xffff0000u : 0u);
                                 const uint32_t vis = below(hi - 32 * c) & (~below(lo - 32 * c) | below(sk - 32 * c)) & there;
-                                tc_ld32(x, S + 32 * (c & 1));
-                                tc_wait_ld(x);
+                                tc_ld32(x[0], S + 32 * c);
+                                tc_wait_ld(x[0]);
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
-                                    if (!(vis & 1u << i)) x[i] = 0xff800000u;
-                                tc_st32(S + 32 * (c & 1), x);
+                                    if (!(vis & 1u << i)) x[0][i] = 0xff800000u;
+                                tc_st32(S + 32 * c, x[0]);
                             }
                             tc_wait_st();
                         }
                         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                        tc_ld32(x[0], S);
+                        tc_wait_ld(x[0]);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            tc_ld32(x, S + 32 * c);
-                            tc_wait_ld(x);
+                        for (int c = 0; c < 4; ++c) {
+                            if (c < 3) tc_ld32(x[(c + 1) & 1], S + 32 * (c + 1));
 #pragma unroll
                             for (int i = 0; i < 32; i += 2)
-                                mx[(i >> 1) & 3] = fmaxf(mx[(i >> 1) & 3], fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+                                mx[(i >> 1) & 3] = fmaxf(mx[(i >> 1) & 3], fmaxf(__uint_as_float(x[c & 1][i]), __uint_as_float(x[c & 1][i + 1])));
+                            if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
                         }
-                        float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
-                        *mine = top;
-                        ok = !pair_any(pair, *gave_up != 0);             // (the barrier also orders the exchange)
-                        if (!ok) break;
-                        top = fmaxf(top, *other);
+                        tc_ld32(x[0], S);
+                        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
                         if (k == 0) m = fmaxf(m, top);
-                        else if (__any_sync(0xffffffffu, top > m + 8.0f)) {      // the same for both warps: same rows
+                        else if (__any_sync(0xffffffffu, top > m + 8.0f)) {
                             const float nm = fmaxf(m, top), f = ex2(m - nm);
                             m = nm;
                             l *= f;
 #pragma unroll 1
-                            for (int c = 0; c < D / 2; c += 16) {
+                            for (int c = 0; c < D; c += 16) {
                                 uint32_t o[16];
                                 tc_ld16(o, O + c);
                                 tc_wait_ld16(o);
@@ -453,26 +428,20 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                                 for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
                                 tc_st16(O + c, o);
                             }
-                            tc_wait_st();
-                            tc_ld32(x, S + 32);
-                            tc_wait_ld(x);
-                            pair_any(pair, false);           // either part's weights start a product over all of O
                         }
-                        // P of 32 keys takes the first half of their scores' columns
+                        tc_wait_ld(x[0]);
+                        // P takes half the columns of S: what it overwrites has been read
                         const uint64_t scale2 = pack2(a.scale, a.scale), m2 = pack2(-m, -m);
                         uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-                        for (int c = 1; c >= 0; --c) {
-                            if (c == 0) {                    // (the other chunk is still here from the maximum)
-                                tc_ld32(x, S);
-                                tc_wait_ld(x);
-                            }
+                        for (int c = 0; c < 4; ++c) {
+                            if (c < 3) tc_ld32(x[(c + 1) & 1], S + 32 * (c + 1));
                             uint32_t pk[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
-                                const uint64_t y = fma2f(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), scale2, m2);
+                                const uint64_t y = fma2f(pack2(__uint_as_float(x[c & 1][2 * i]), __uint_as_float(x[c & 1][2 * i + 1])), scale2, m2);
                                 float p0, p1;
-                                if (i < CH_POLY) poly_ex2(y, p0, p1);
+                                if (i % 16 < CH_POLY) poly_ex2(y, p0, p1);
                                 else {
                                     unpack2(y, p0, p1);
                                     p0 = ex2(p0);
@@ -481,12 +450,15 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                                 sum[i & 1] = add2f(sum[i & 1], pack2(p0, p1));
                                 pk[i] = T::pack(p0, p1);
                             }
-                            tc_st16(S + 32 * c, pk);
+                            if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
+                            tc_st16(S + 16 * c, pk);
+                            if (c & 1) {             // half of P: the product may start on it
+                                tc_wait_st();
+                                tc_before();
+                                __syncwarp();
+                                if (lane == 0) bar_arrive(p_ready + 8 * (c >> 1));
+                            }
                         }
-                        tc_wait_st();
-                        tc_before();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(p_ready);
                         float s0, s1;
                         unpack2(add2f(sum[0], sum[1]), s0, s1);
                         l += s0 + s1;
@@ -498,22 +470,18 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         bar_wait(o_done, n_o++ & 1, gave_up);
                         __syncwarp();
                         tc_after();
-                        *mine = l;
-                        ok = !pair_any(pair, *gave_up != 0);
-                        l += *other;
-                        pair_any(pair, false);               // before the next item's maxima
                     }
                 }
                 if (ok && g.real) {
-                    // the output, or the partial record: float4 [D / 4][256 rows]; this thread's half of the dimensions
+                    // the output, or the partial record: float4 [D / 4][256 rows]
                     const size_t slot = 2 * (size_t)blockIdx.x + (first ? 1 : 0);
                     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
                     const int hq = w.h * a.G + rr % a.G;
                     const long long tok = s.row0 + rr / a.G;
-                    uint16_t* dst = a.out + tok * a.out_stride + (long long)hq * D + part * (D / 2);
-                    float4* rec = reinterpret_cast<float4*>(a.part) + (slot * (D / 4) + part * (D / 8)) * CH_ROWS + half * 128 + row;
+                    uint16_t* dst = a.out + tok * a.out_stride + (long long)hq * D;
+                    float4* part = reinterpret_cast<float4*>(a.part) + slot * (D / 4) * CH_ROWS + half * 128 + row;
 #pragma unroll 1
-                    for (int c = 0; c < D / 2; c += 32) {
+                    for (int c = 0; c < D; c += 32) {
                         uint32_t o[32];
                         __syncwarp();
                         if (g.tiles > 0) {
@@ -533,15 +501,14 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                                                      T::pack(f[4] * inv, f[5] * inv), T::pack(f[6] * inv, f[7] * inv));
                                 *reinterpret_cast<uint4*>(dst + c + e) = v;
                             } else if (live) {
-                                rec[(size_t)((c + e) / 4) * CH_ROWS] = make_float4(f[0], f[1], f[2], f[3]);
-                                rec[(size_t)((c + e) / 4 + 1) * CH_ROWS] = make_float4(f[4], f[5], f[6], f[7]);
+                                part[(size_t)((c + e) / 4) * CH_ROWS] = make_float4(f[0], f[1], f[2], f[3]);
+                                part[(size_t)((c + e) / 4 + 1) * CH_ROWS] = make_float4(f[4], f[5], f[6], f[7]);
                             }
                         }
                     }
                     tc_before();
-                    if (part == 0 && live && done && a.lse)
-                        a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (m + log2f(l)) * PT_LN2 : -INFINITY;
-                    if (part == 0 && live && !done) a.stat[slot * CH_ROWS + half * 128 + row] = make_float2(m, l);
+                    if (live && done && a.lse) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (m + log2f(l)) * PT_LN2 : -INFINITY;
+                    if (live && !done) a.stat[slot * CH_ROWS + half * 128 + row] = make_float2(m, l);
                 }
             } else n_tile += g.tiles;
             if (!handed) {
@@ -553,7 +520,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     hd.y = w.h + 1;
                     hd.z = w.b;
                     hd.w = w.rt;
-                } else hd.x = g.last ? 2 : 1;
+                } else hd.x = lastp ? 2 : 1;
             }
             w = wn;
             s = sn;
@@ -561,9 +528,9 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (tid == 0) a.head[blockIdx.x] = hd;
-    } else if (wid < 20) {
+    } else if (wid < 12) {
         // ---------------- operands
-        const int lw = wid - 16;                              // this warp's rows: 32 lw .. 32 lw + 31 of a tile
+        const int lw = wid - 8;                              // this warp's rows: 32 lw .. 32 lw + 31 of a tile
         uint32_t n_stage = 0;
         bool ok = true;
         while (w.left > 0 && ok) {
@@ -606,39 +573,30 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         bar_wait(smem_u32(&bars.raw_full[rs]), (n_stage / N_RAW) & 1, gave_up);
                         __syncwarp();
                         const int c = lane % LPR;
-                        constexpr int BATCH = LPR < 4 ? LPR : 4;             // rows in flight
 #pragma unroll
-                        for (int p0 = 0; p0 < LPR; p0 += BATCH) {
-                            uint32_t words[BATCH][4], meta[BATCH];
+                        for (int p = 0; p < LPR; ++p) {
+                            const int r = p * RPP + lane / LPR, row = lw * 32 + r;
+                            uint32_t words[4], meta;
+                            lds16(words, raw0 + row * pg_row_bytes<FMT, D>() + c * 16);
+                            if (FMT == PF_I8) {
+                                uint16_t s16;
+                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(s16) : "r"(raw0 + SM::RAW_CODES + row * 2));
+                                meta = s16;
+                            } else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(meta) : "r"(raw0 + SM::RAW_CODES + row * 4));
+                            if (!clean && !seen(r)) meta = 0;             // scale and zero 0: the row becomes zeros
+                            const uint32_t s2 = dup_lo(meta), z2 = dup_hi(meta);
+                            if (FMT == PF_I8) {
 #pragma unroll
-                            for (int p = 0; p < BATCH; ++p) {
-                                const int row = lw * 32 + (p0 + p) * RPP + lane / LPR;
-                                lds16(words[p], raw0 + row * pg_row_bytes<FMT, D>() + c * 16);
-                                if (FMT == PF_I8) {
-                                    uint16_t s16;
-                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(s16) : "r"(raw0 + SM::RAW_CODES + row * 2));
-                                    meta[p] = s16;
-                                } else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(meta[p]) : "r"(raw0 + SM::RAW_CODES + row * 4));
-                            }
+                                for (int i = 0; i < 2; ++i)
+                                    sts16(dst + swz(row, 2 * c + i), mul2<T>(Codes<T>::bytes(words[2 * i], 0x5140), s2),
+                                          mul2<T>(Codes<T>::bytes(words[2 * i], 0x5342), s2), mul2<T>(Codes<T>::bytes(words[2 * i + 1], 0x5140), s2),
+                                          mul2<T>(Codes<T>::bytes(words[2 * i + 1], 0x5342), s2));
+                            } else {
 #pragma unroll
-                            for (int p = 0; p < BATCH; ++p) {
-                                const int r = (p0 + p) * RPP + lane / LPR, row = lw * 32 + r;
-                                if (!clean && !seen(r)) meta[p] = 0;      // scale and zero 0: the row becomes zeros
-                                const uint32_t s2 = dup_lo(meta[p]), z2 = dup_hi(meta[p]);
-                                const uint32_t* w4 = words[p];
-                                if (FMT == PF_I8) {
-#pragma unroll
-                                    for (int i = 0; i < 2; ++i)
-                                        sts16(dst + swz(row, 2 * c + i), mul2<T>(Codes<T>::bytes(w4[2 * i], 0x5140), s2),
-                                              mul2<T>(Codes<T>::bytes(w4[2 * i], 0x5342), s2), mul2<T>(Codes<T>::bytes(w4[2 * i + 1], 0x5140), s2),
-                                              mul2<T>(Codes<T>::bytes(w4[2 * i + 1], 0x5342), s2));
-                                } else {
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        const uint32_t y = w4[i] >> 8;
-                                        sts16(dst + swz(row, 4 * c + i), fma2<T>(Codes<T>::nib_lo(w4[i]), s2, z2), fma2<T>(Codes<T>::nib_hi(w4[i]), s2, z2),
-                                              fma2<T>(Codes<T>::nib_lo(y), s2, z2), fma2<T>(Codes<T>::nib_hi(y), s2, z2));
-                                    }
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint32_t y = words[i] >> 8;
+                                    sts16(dst + swz(row, 4 * c + i), fma2<T>(Codes<T>::nib_lo(words[i]), s2, z2), fma2<T>(Codes<T>::nib_hi(words[i]), s2, z2),
+                                          fma2<T>(Codes<T>::nib_lo(y), s2, z2), fma2<T>(Codes<T>::nib_hi(y), s2, z2));
                                 }
                             }
                         }
@@ -653,7 +611,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
         }
     } else {
-        if (wid == 20) {
+        if (wid == 12) {
             // ---------------- matrix instructions: the warp stays together (its values are uniform), one lane issues
             constexpr uint32_t ID_S = instr_desc<T>(128, false), ID_O = instr_desc<T>(D, true);
             uint32_t n_stage = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
@@ -679,7 +637,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 const uint32_t vb = v_lo + st * (SM::TILE >> 4);
                 if (elect_one()) {
 #pragma unroll
-                    for (int i = 4 * part; i < 4 * part + 4; ++i) mma_ts(tmem + 256 + 128 * h, tmem + 128 * h + 32 * (i >> 1) + 8 * (i & 1), desc(vb + i * 128), ID_O, add || i > 0);
+                    for (int i = 4 * part; i < 4 * part + 4; ++i) mma_ts(tmem + 256 + 128 * h, tmem + 128 * h + 8 * i, desc(vb + i * 128), ID_O, add || i > 0);
                     if (last) tc_commit(smem_u32(&bars.o_done[h]));
                 }
                 __syncwarp();
@@ -721,7 +679,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
             }
         }
-        if (wid == 21) {
+        if (wid == 13) {
             // ---------------- feeder: lane i < 128 / page copies page i of a tile
             uint32_t n_stage = 0, n_tile = 0;
             bool ok = true;
@@ -797,7 +755,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     tc_before();
     __syncthreads();
     if (tid == 0 && bars.gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
-    if (wid == 20) {
+    if (wid == 12) {
         if (bars.gave_up) {                  // a role left early: matrix instructions may be under way
             if (lane == 0) {
                 bar_init(smem_u32(&bars.o_done[0]), 1);

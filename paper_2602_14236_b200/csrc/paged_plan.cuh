@@ -77,15 +77,11 @@ struct PtWalk {
 // Every thread gets the same walk.  One thread per sequence sums its tiles, a warp together where there are many row
 // tiles; block-wide scans find the block's start.
 // ITEM: units an item counts beside its tiles, before them.
-struct PtShared {
-    long long wsum[32];
-    PtWalk found;
-};
 template <int RT, int THREADS, int ITEM>
-__device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int blocks, PtShared& sh) {
+__device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int blocks) {
     constexpr int ALONE = 2;                 // row tiles that a thread sums by itself
-    long long* wsum = sh.wsum;
-    PtWalk& found = sh.found;
+    __shared__ long long wsum[THREADS / 32];
+    __shared__ PtWalk found;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     // tiles of one head of sequence b; called by whole warps
     auto per_head = [&](int b) -> long long {
