@@ -189,30 +189,6 @@ __device__ __forceinline__ uint64_t add2f(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-// 2^y without the special-function unit, which the exponentials alone would keep as busy as the products keep the tensor
-// core: y = n + f with n the nearest integer (by adding 1.5 * 2^23), 2^f by a polynomial of degree 5 fitted here for the
-// least relative error on [-1/2, 1/2] with the value 1 at 0 (1.6e-7 in binary32, as good as the unit's), n added to the
-// exponent.  From -127 down the result is 0, as it has to be for a masked score.
-constexpr int CH_POLY = 5;                   // of 16 pairs of weights
-__device__ __forceinline__ void poly_ex2(uint64_t y, float& p0, float& p1) {
-    float a, b;
-    unpack2(y, a, b);
-    y = pack2(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
-    const uint64_t big = pack2(12582912.0f, 12582912.0f), nbig = pack2(-12582912.0f, -12582912.0f), neg = pack2(-1.0f, -1.0f);
-    const uint64_t t = add2f(y, big), f = fma2f(add2f(t, nbig), neg, y);
-    uint64_t p = pack2(0.001326472731307149f, 0.001326472731307149f);
-    p = fma2f(p, f, pack2(0.009671512991189957f, 0.009671512991189957f));
-    p = fma2f(p, f, pack2(0.05550733581185341f, 0.05550733581185341f));
-    p = fma2f(p, f, pack2(0.24022242426872253f, 0.24022242426872253f));
-    p = fma2f(p, f, pack2(0.6931470036506653f, 0.6931470036506653f));
-    p = fma2f(p, f, pack2(1.0f, 1.0f));
-    float ta, tb;
-    unpack2(t, ta, tb);
-    unpack2(p, p0, p1);
-    p0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(ta) << 23));
-    p1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(tb) << 23));
-}
-
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
@@ -441,12 +417,9 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                             for (int i = 0; i < 16; ++i) {
                                 const uint64_t y = fma2f(pack2(__uint_as_float(x[c & 1][2 * i]), __uint_as_float(x[c & 1][2 * i + 1])), scale2, m2);
                                 float p0, p1;
-                                if (i % 16 < CH_POLY) poly_ex2(y, p0, p1);
-                                else {
-                                    unpack2(y, p0, p1);
-                                    p0 = ex2(p0);
-                                    p1 = ex2(p1);
-                                }
+                                unpack2(y, p0, p1);
+                                p0 = ex2(p0);
+                                p1 = ex2(p1);
                                 sum[i & 1] = add2f(sum[i & 1], pack2(p0, p1));
                                 pk[i] = T::pack(p0, p1);
                             }
@@ -573,30 +546,39 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         bar_wait(smem_u32(&bars.raw_full[rs]), (n_stage / N_RAW) & 1, gave_up);
                         __syncwarp();
                         const int c = lane % LPR;
+                        constexpr int BATCH = LPR < 4 ? LPR : 4;             // rows in flight
 #pragma unroll
-                        for (int p = 0; p < LPR; ++p) {
-                            const int r = p * RPP + lane / LPR, row = lw * 32 + r;
-                            uint32_t words[4], meta;
-                            lds16(words, raw0 + row * pg_row_bytes<FMT, D>() + c * 16);
-                            if (FMT == PF_I8) {
-                                uint16_t s16;
-                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(s16) : "r"(raw0 + SM::RAW_CODES + row * 2));
-                                meta = s16;
-                            } else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(meta) : "r"(raw0 + SM::RAW_CODES + row * 4));
-                            if (!clean && !seen(r)) meta = 0;             // scale and zero 0: the row becomes zeros
-                            const uint32_t s2 = dup_lo(meta), z2 = dup_hi(meta);
-                            if (FMT == PF_I8) {
+                        for (int p0 = 0; p0 < LPR; p0 += BATCH) {
+                            uint32_t words[BATCH][4], meta[BATCH];
 #pragma unroll
-                                for (int i = 0; i < 2; ++i)
-                                    sts16(dst + swz(row, 2 * c + i), mul2<T>(Codes<T>::bytes(words[2 * i], 0x5140), s2),
-                                          mul2<T>(Codes<T>::bytes(words[2 * i], 0x5342), s2), mul2<T>(Codes<T>::bytes(words[2 * i + 1], 0x5140), s2),
-                                          mul2<T>(Codes<T>::bytes(words[2 * i + 1], 0x5342), s2));
-                            } else {
+                            for (int p = 0; p < BATCH; ++p) {
+                                const int row = lw * 32 + (p0 + p) * RPP + lane / LPR;
+                                lds16(words[p], raw0 + row * pg_row_bytes<FMT, D>() + c * 16);
+                                if (FMT == PF_I8) {
+                                    uint16_t s16;
+                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(s16) : "r"(raw0 + SM::RAW_CODES + row * 2));
+                                    meta[p] = s16;
+                                } else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(meta[p]) : "r"(raw0 + SM::RAW_CODES + row * 4));
+                            }
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const uint32_t y = words[i] >> 8;
-                                    sts16(dst + swz(row, 4 * c + i), fma2<T>(Codes<T>::nib_lo(words[i]), s2, z2), fma2<T>(Codes<T>::nib_hi(words[i]), s2, z2),
-                                          fma2<T>(Codes<T>::nib_lo(y), s2, z2), fma2<T>(Codes<T>::nib_hi(y), s2, z2));
+                            for (int p = 0; p < BATCH; ++p) {
+                                const int r = (p0 + p) * RPP + lane / LPR, row = lw * 32 + r;
+                                if (!clean && !seen(r)) meta[p] = 0;      // scale and zero 0: the row becomes zeros
+                                const uint32_t s2 = dup_lo(meta[p]), z2 = dup_hi(meta[p]);
+                                const uint32_t* w4 = words[p];
+                                if (FMT == PF_I8) {
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i)
+                                        sts16(dst + swz(row, 2 * c + i), mul2<T>(Codes<T>::bytes(w4[2 * i], 0x5140), s2),
+                                              mul2<T>(Codes<T>::bytes(w4[2 * i], 0x5342), s2), mul2<T>(Codes<T>::bytes(w4[2 * i + 1], 0x5140), s2),
+                                              mul2<T>(Codes<T>::bytes(w4[2 * i + 1], 0x5342), s2));
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        const uint32_t y = w4[i] >> 8;
+                                        sts16(dst + swz(row, 4 * c + i), fma2<T>(Codes<T>::nib_lo(w4[i]), s2, z2), fma2<T>(Codes<T>::nib_hi(w4[i]), s2, z2),
+                                              fma2<T>(Codes<T>::nib_lo(y), s2, z2), fma2<T>(Codes<T>::nib_hi(y), s2, z2));
+                                    }
                                 }
                             }
                         }
@@ -651,6 +633,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     // stages in order: K(0), V(0), K(1), ...: V(t - 1) then K(t)
                     const uint32_t vs = n_stage, ks = t > 0 ? n_stage + 1 : n_stage;
                     if (t > 0) wait(bars.kv_full[vs % CH_STAGES], (vs / CH_STAGES) & 1);
+                    if (t < g.tiles) wait(bars.kv_full[ks % CH_STAGES], (ks / CH_STAGES) & 1);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (h >= halves) break;
@@ -663,7 +646,6 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                             sums(h, vs % CH_STAGES, 1, true, t == g.tiles);
                         }
                         if (t < g.tiles) {
-                            if (h == 0) wait(bars.kv_full[ks % CH_STAGES], (ks / CH_STAGES) & 1);
                             tc_after();
                             scores(h, ks % CH_STAGES);
                         }
