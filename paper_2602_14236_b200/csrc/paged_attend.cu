@@ -7,9 +7,12 @@
 // A warp takes 16 keys of one head at a time, and both products are m16n8k16 matrix instructions with the keys as the
 // long side, since there are few rows: scores = K (16 keys x 16 dimensions) times up to 8 rows of q as columns; values =
 // V transposed (16 dimensions x 16 keys) times the weights, transposed in registers by movmatrix.  Any order of the
-// dimensions that q and K share will do, as will any that V and the output share, so a lane loads 16 contiguous bytes
-// wherever the rows have them, straight into the registers that hold its operands; codes become the 16-bit type there.
-// The next tile's K is requested as soon as this tile's K is used up, V likewise.
+// dimensions that q and K share will do, as will any that V and the output share, and any of the keys: a lane reads up to
+// 16 contiguous bytes wherever the rows have them, straight into the registers that hold its operands; codes become the
+// 16-bit type there.
+// One more warp feeds a ring of tiles in shared memory by bulk copies of whole pages, so that some 130 to 200 KB per SM are
+// under way whatever the registers hold.  (Loading each lane's next operands into registers instead: 32 ragged streams
+// over INT4 pages took 149 us, 0.27 of the copy bandwidth.)
 // The weights' reference maximum moves only when a score exceeds it by 2^8 (in powers of two): until then no lane needs
 // another's, weights stay below 2^8, and the sums are joined across lanes once at the end of an item.
 #include <math.h>
@@ -18,8 +21,22 @@
 
 namespace {
 
-constexpr int ST_WARPS = 8, ST_THREADS = 32 * ST_WARPS;
+constexpr int ST_WARPS = 8, ST_THREADS = 32 * (ST_WARPS + 1);        // eight that compute, one that feeds
+constexpr int ST_ROUND = 4;                  // rows joined across the warps at a time
 static_assert(ST_WARPS * 16 == PT_KEYS, "a warp per 16 keys of a tile");
+
+// A stage of the ring: 128 keys' K and V rows, then their scales.
+template <int FMT, int D, int NT>
+struct StSmem {
+    static constexpr int ROWS = 128 * pg_row_bytes<FMT, D>(), META = 128 * pg_meta_bytes<FMT>(), STAGE = 2 * (ROWS + META);
+    static constexpr int K = 0, V = ROWS, KM = 2 * ROWS, VM = 2 * ROWS + META;
+    static constexpr int ACC = ST_WARPS * ST_ROUND * (D + 4) * 4;
+    // two blocks per SM where a ring of two stages leaves room for them, and the registers of 8 rows do
+    static constexpr int BLOCKS = NT == 1 && 2 * STAGE + ACC <= 110 * 1024 ? 2 : 1;
+    static constexpr int ROOM = (BLOCKS == 2 ? 110 * 1024 : 222 * 1024) - ACC;
+    static constexpr int STAGES = ROOM / STAGE < 8 ? ROOM / STAGE : 8;
+    static constexpr int BYTES = STAGES * STAGE + ACC;
+};
 
 template <typename T>
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
@@ -33,37 +50,41 @@ __device__ __forceinline__ void mma16816<TypeBF16>(float (&d)[4], uint32_t a0, u
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// Joins the computing warps; whether any of their threads says so.
+__device__ __forceinline__ bool any_of(bool x) {
+    uint32_t r;
+    asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %1, 0; barrier.cta.red.or.pred q, 1, %2, p; selp.b32 %0, 1, 0, q; }"
+                 : "=r"(r) : "r"((uint32_t)x), "n"(ST_WARPS * 32) : "memory");
+    return r != 0;
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     uint32_t d;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
     return d;
 }
-template <int W>
-__device__ __forceinline__ void ld_words(uint32_t* d, const uint8_t* p) {
-    if (W == 4) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3]) : "l"(p));
-    if (W == 2) asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(d[0]), "=r"(d[1]) : "l"(p));
-    if (W == 1) asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(d[0]) : "l"(p));
-}
+// Key of row slot r of the fragments: the keys 2 c, 2 c + 1 that a lane multiplies are c and c + 4, which lie in
+// different banks.
+__device__ __forceinline__ int key_of(int g8) { return (g8 >> 1) + 4 * (g8 & 1); }
 
-// What a lane (g8 = lane / 4, c4 = lane % 4) holds of 16 keys: the shares of rows g8 and g8 + 8 of K that make its A
-// fragments, and its share of rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9 of V.
+// What a lane (g8 = lane / 4, c4 = lane % 4) takes of 16 keys: the shares of the keys of slots g8 and g8 + 8 of K that make
+// its A fragments, and its share of slots 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9 of V.
 template <int FMT, int D>
 struct KTile {
     static constexpr int W = pg_row_bytes<FMT, D>() / 16;       // words of a key row per lane
     uint32_t k[2][W];
     uint32_t s[2];                                              // scale, or (scale, zero)
-    __device__ __forceinline__ void load(const PgCache& pc, size_t slot, int g8, int c4) {
-        constexpr int RB = pg_row_bytes<FMT, D>();
+    __device__ __forceinline__ void load(uint32_t rows, uint32_t meta, int g8, int c4) {
+        constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const size_t row = slot + g8 + 8 * r;
-            const uint8_t* p = pc.data + row * RB;
+            const int key = key_of(g8) + 8 * r;
+            const uint32_t p = rows + key * RB;
             if (RB >= 64) {
 #pragma unroll
-                for (int i = 0; i < RB / 64; ++i) ld_words<4>(&k[r][4 * i], p + 64 * i + 16 * c4);
-            } else ld_words<2>(&k[r][0], p + 8 * c4);
-            if (FMT == PF_I8) s[r] = __ldg(reinterpret_cast<const uint16_t*>(pc.scale) + row);
-            if (FMT == PF_I4) s[r] = __ldg(reinterpret_cast<const uint32_t*>(pc.scale) + row);
+                for (int i = 0; i < RB / 64; ++i) lds16(&k[r][4 * i], p + 64 * i + 16 * c4);
+            } else lds_words<2>(&k[r][0], p + 8 * c4);
+            if (FMT == PF_I8) s[r] = lds_u16(meta + key * MB);
+            if (FMT == PF_I4) lds_words<1>(&s[r], meta + key * MB);
         }
     }
 };
@@ -71,25 +92,21 @@ template <int FMT, int D>
 struct VTile {
     static constexpr int W = pg_row_bytes<FMT, D>() / 32;       // words of a value row per lane
     uint32_t v[4][W];
-    uint32_t s[2][FMT == PF_I4 ? 2 : 1];                        // per pair of keys: the scales (and zeros), key order
-    __device__ __forceinline__ void load(const PgCache& pc, size_t slot, int g8, int c4) {
-        constexpr int RB = pg_row_bytes<FMT, D>();
+    uint32_t s[2][FMT == PF_I4 ? 2 : 1];                        // per pair of keys: their scales in one word, or (scale, zero) each
+    __device__ __forceinline__ void load(uint32_t rows, uint32_t meta, int g8, int c4) {
+        constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint8_t* p = pc.data + (slot + 2 * c4 + (j & 1) + 8 * (j >> 1)) * RB;
+            const int key = c4 + 4 * (j & 1) + 8 * (j >> 1);
+            const uint32_t p = rows + key * RB;
             if (W == 8) {
-                ld_words<4>(&v[j][0], p + 16 * g8);
-                ld_words<4>(&v[j][4], p + 128 + 16 * g8);
-            } else ld_words<W == 8 ? 4 : W>(&v[j][0], p + 4 * W * g8);
-        }
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const size_t row = slot + 2 * c4 + 8 * r;
-            if (FMT == PF_I8) s[r][0] = __ldg(reinterpret_cast<const uint32_t*>(pc.scale + row * 2));
-            if (FMT == PF_I4) {
-                const uint2 x = __ldg(reinterpret_cast<const uint2*>(pc.scale + row * 4));
-                s[r][0] = x.x;
-                s[r][FMT == PF_I4 ? 1 : 0] = x.y;
+                lds16(&v[j][0], p + 16 * g8);
+                lds16(&v[j][W == 8 ? 4 : 0], p + 128 + 16 * g8);
+            } else lds_words<W == 8 ? 4 : W>(&v[j][0], p + 4 * W * g8);
+            if (FMT == PF_I4) lds_words<1>(&s[j >> 1][FMT == PF_I4 ? j & 1 : 0], meta + key * MB);
+            if (FMT == PF_I8) {
+                const uint32_t x = lds_u16(meta + key * MB);
+                s[j >> 1][0] = (j & 1) ? s[j >> 1][0] | x << 16 : x;
             }
         }
     }
@@ -148,27 +165,97 @@ __device__ __forceinline__ int value_dim(int t, int half, int g8) {
     return g8 * (D / 8) + half * (D / 16) + t;
 }
 
-// Blocks per SM: two where the registers allow it.
-template <int FMT, int D, int NT> constexpr int st_blocks() { return NT == 1 && !(FMT == PF_16 && D == 128) ? 2 : 1; }
-
 // NT: 8-row column tiles per item.
 template <typename T, int FMT, int D, int NT>
-__global__ void __launch_bounds__(ST_THREADS, st_blocks<FMT, D, NT>())
+__global__ void __launch_bounds__(ST_THREADS, StSmem<FMT, D, NT>::BLOCKS)
 k_paged_step(PtArgs a, int blocks) {
-    constexpr int RT = 8 * NT, KS = D / 16, VS = D / 16;
-    __shared__ float sh_acc[ST_WARPS][8][D + 4];
-    __shared__ float2 sh_stat[ST_WARPS][8];
+    using SM = StSmem<FMT, D, NT>;
+    constexpr int RT = 8 * NT, KS = D / 16, VS = D / 16, STAGES = SM::STAGES;
+    static_assert(STAGES >= 2, "ring");
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ uint64_t full[STAGES], empty[STAGES];
+    __shared__ uint32_t kinds[STAGES];       // per stage: bit g: some row sees keys 16 g .. and their page exists
+    __shared__ float2 sh_stat[ST_WARPS][ST_ROUND];
+    __shared__ PtShared sh_plan;
+    __shared__ int sh_gave_up;
+    float (*sh_acc)[ST_ROUND][D + 4] = reinterpret_cast<float (*)[ST_ROUND][D + 4]>(ring + STAGES * SM::STAGE);
+    volatile int* gave_up = &sh_gave_up;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g8 = lane >> 2, c4 = lane & 3;
     const int c = blockIdx.x;
-    PtWalk w = pt_start<RT, ST_THREADS, 0>(a, c, blocks);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < STAGES; ++i) {
+            bar_init(smem_u32(&full[i]), 1);
+            bar_init(smem_u32(&empty[i]), ST_WARPS);
+        }
+        sh_gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    grid_wait();
+    grid_release();
+    PtWalk w = pt_start<RT, ST_THREADS, 0>(a, c, blocks, sh_plan);
+    __syncthreads();
     int4 hd = make_int4(0, 0, 0, 0);
-    PgSeq s;
+    PgSeq s{};
     if (w.left > 0) s = pg_seq(a.sq, a.pc, w.b);
-    while (w.left > 0) {
+    uint32_t n_stage = 0;
+    bool ok = true;
+
+    if (wid == ST_WARPS) {
+        // ---------------- feeder: a lane per (page of the tile, K rows | V rows | K scales | V scales)
+        const int per_page = 1 << a.pc.page_shift, n_pages = PT_KEYS >> a.pc.page_shift;
+        constexpr int PIECES = FMT == PF_16 ? 2 : 4;
+        const int page = lane / PIECES, piece = lane % PIECES;
+        constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
+        while (w.left > 0 && ok) {
+            const PtSpan sp = pt_item<RT>(s, a, w.rt);
+            const int k0 = w.k, k1 = (int)min((long long)max(sp.n, 1), k0 + w.left);
+            // page of keys 16 grp .. of tile k: -2 no row sees them, -1 there is no such page
+            auto page_of = [&](int k) -> int {
+                const int j = sp.tile(k) * PT_KEYS + lane * 16;
+                if (lane > 7 || k >= k1 || j >= sp.hi || (j + 16 <= sp.lo && j >= a.sinks)) return -2;
+                const int p = a.sq.table[(size_t)w.b * a.sq.width + (j >> a.pc.page_shift)];
+                return p >= 0 && p < a.pc.n_pages ? p : -1;
+            };
+            int next = sp.n > 0 ? page_of(k0) : -2;
+            for (int k = k0; k < k1 && sp.n > 0 && ok; ++k, ++n_stage) {
+                ok = *gave_up == 0;
+                const int pid16 = next;
+                next = page_of(k + 1);
+                const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), need = __ballot_sync(0xffffffffu, pid16 >= 0);
+                if (bad != 0 && lane == 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
+                const uint32_t mine = page < n_pages ? need >> (page << (a.pc.page_shift - 4)) & ((1u << (per_page >> 4)) - 1u) : 0u;
+                const int from = mine ? (page << (a.pc.page_shift - 4)) + __ffs(mine) - 1 : 0;
+                const int pid = __shfl_sync(0xffffffffu, pid16, from);
+                const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine != 0 && piece == 0));
+                const uint32_t st = n_stage % STAGES, bar = smem_u32(&full[st]), dst = smem_u32(ring) + st * SM::STAGE;
+                if (n_stage >= STAGES) bar_wait(smem_u32(&empty[st]), (n_stage / STAGES - 1) & 1, gave_up);
+                __syncwarp();
+                if (lane == 0) {
+                    *(volatile uint32_t*)&kinds[st] = need;
+                    bar_expect(bar, copies * per_page * 2 * (RB + MB));
+                }
+                __syncwarp();
+                if (mine) {
+                    const size_t slot = pg_slot(a.pc, pid, piece & 1, w.h, 0);
+                    const uint32_t at = (uint32_t)(page << a.pc.page_shift);
+                    if (piece < 2) bulk_copy(dst + (piece ? SM::V : SM::K) + at * RB, a.pc.data + slot * RB, per_page * RB, bar);
+                    else bulk_copy(dst + (piece == 3 ? SM::VM : SM::KM) + at * MB, a.pc.scale + slot * MB, per_page * MB, bar);
+                }
+            }
+            w.left -= k1 - k0;
+            if (w.left > 0) pt_next<RT>(w, s, a);
+        }
+        if (!ok) {                           // given up: copies in flight end before the block does
+            for (uint32_t i = n_stage > STAGES ? n_stage - STAGES : 0; i < n_stage; ++i)
+                for (int t = 0; t < (1 << 16) && !bar_try(smem_u32(&full[i % STAGES]), (i / STAGES) & 1); ++t) {}
+        }
+        return;
+    }
+
+    while (w.left > 0 && ok) {
         const PtSpan sp = pt_item<RT>(s, a, w.rt);
         const int k0 = w.k, k1 = (int)min((long long)max(sp.n, 1), k0 + w.left);
         const int rows = min(RT, s.n * a.G - w.rt * RT);
-        const int* table = a.sq.table + (size_t)w.b * a.sq.width;
         if (s.cut && threadIdx.x == 0 && s.pos0 + s.n > s.len) atomicMin(a.status, SALICACHE_E_CAPACITY);
 
         // q as B fragments: column g8 of column tile n is row 8 n + g8
@@ -205,44 +292,37 @@ k_paged_step(PtArgs a, int blocks) {
             for (int t = 0; t < VS; ++t) acc[n][t][0] = acc[n][t][1] = acc[n][t][2] = acc[n][t][3] = 0.0f;
         }
 
-        // page of this warp's 16 keys of tile k: -2 behind the last position, -1 no such page
-        auto page_of = [&](int k) -> int {
-            if (k >= k1 || k >= sp.n) return -2;
-            const int j = sp.tile(k) * PT_KEYS + wid * 16;
-            if (j >= sp.hi || (j + 16 <= sp.lo && j >= a.sinks)) return -2;
-            const int p = table[j >> a.pc.page_shift];
-            return p >= 0 && p < a.pc.n_pages ? p : -1;
-        };
-        auto slot_of = [&](int k, int pid, int kv) -> size_t {
-            const int j = sp.tile(k) * PT_KEYS + wid * 16;
-            return pg_slot(a.pc, pid, kv, w.h, j & ((1 << a.pc.page_shift) - 1));
-        };
-        KTile<FMT, D> kt;
-        VTile<FMT, D> vt;
-        int pid = page_of(k0), pid1 = page_of(k0 + 1);
-        if (pid >= 0) {
-            kt.load(a.pc, slot_of(k0, pid, 0), g8, c4);
-            vt.load(a.pc, slot_of(k0, pid, 1), g8, c4);
-        }
-        for (int k = k0; k < k1; ++k) {
-            const int pid2 = page_of(k + 2);
+        for (int k = k0; k < k1 && sp.n > 0; ++k, ++n_stage) {
+            const uint32_t st = n_stage % STAGES, src = smem_u32(ring) + st * SM::STAGE;
+            bar_wait(smem_u32(&full[st]), (n_stage / STAGES) & 1, gave_up);
+            __syncwarp();
             const int j0 = sp.tile(k) * PT_KEYS + wid * 16;
+            if (!(*(volatile uint32_t*)&kinds[st] >> wid & 1u)) {
+                if (lane == 0) bar_arrive(smem_u32(&empty[st]));
+                continue;
+            }
+            constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
             float sc[NT][4];
-            if (pid >= 0) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
+            for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
+            {
+                KTile<FMT, D> kt;
+                kt.load(src + SM::K + wid * 16 * RB, src + SM::KM + wid * 16 * MB, g8, c4);
 #pragma unroll
-                for (int st = 0; st < KS; ++st) {
+                for (int i = 0; i < KS; ++i) {
                     uint32_t a0, a1, a2, a3;
-                    key_frag<T, FMT, D>(kt.k[0], kt.s[0], st, a0, a2);
-                    key_frag<T, FMT, D>(kt.k[1], kt.s[1], st, a1, a3);
+                    key_frag<T, FMT, D>(kt.k[0], kt.s[0], i, a0, a2);
+                    key_frag<T, FMT, D>(kt.k[1], kt.s[1], i, a1, a3);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma16816<T>(sc[n], a0, a1, a2, a3, qf[n][st][0], qf[n][st][1]);
+                    for (int n = 0; n < NT; ++n) mma16816<T>(sc[n], a0, a1, a2, a3, qf[n][i][0], qf[n][i][1]);
                 }
-            } else if (pid == -1 && lane == 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
-            if (pid1 >= 0) kt.load(a.pc, slot_of(k + 1, pid1, 0), g8, c4);
-            if (pid >= 0) {
-                // scores in powers of two; sc[n][i]: key g8 + 8 (i >> 1), row 8 n + 2 c4 + (i & 1)
+            }
+            VTile<FMT, D> vt;
+            vt.load(src + SM::V + wid * 16 * RB, src + SM::VM + wid * 16 * MB, g8, c4);
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_u32(&empty[st]));
+            {
+                // scores in powers of two; sc[n][i]: key key_of(g8) + 8 (i >> 1), row 8 n + 2 c4 + (i & 1)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -253,13 +333,13 @@ k_paged_step(PtArgs a, int blocks) {
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const int j = j0 + g8 + 8 * (i >> 1), rr = w.rt * RT + 8 * n + 2 * c4 + (i & 1);
+                            const int j = j0 + key_of(g8) + 8 * (i >> 1), rr = w.rt * RT + 8 * n + 2 * c4 + (i & 1);
                             if (j >= s.len || !pt_sees(s.pos0 + rr / a.G, j, a.window, a.sinks)) sc[n][i] = -INFINITY;
                         }
                     // values that no row sees may be anything: keep them out of the product
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const int j = j0 + 2 * c4 + (x & 1) + 8 * (x >> 1);
+                        const int j = j0 + c4 + 4 * (x & 1) + 8 * (x >> 1);
                         if (j >= sp.hi || (j < sp.lo && j >= a.sinks)) {
 #pragma unroll
                             for (int i = 0; i < VTile<FMT, D>::W; ++i) vt.v[x][i] = 0u;
@@ -305,60 +385,65 @@ k_paged_step(PtArgs a, int blocks) {
                     for (int n = 0; n < NT; ++n) mma16816<T>(acc[n][t], a0, a1, a2, a3, pf[n][0], pf[n][1]);
                 }
             }
-            if (pid1 >= 0) vt.load(a.pc, slot_of(k + 1, pid1, 1), g8, c4);
-            pid = pid1;
-            pid1 = pid2;
         }
 
         // join the warps: acc[n][t][i] is dimension value_dim(t, i >> 1), row 8 n + 2 c4 + (i & 1)
         const bool first = k0 == 0, lastp = k1 == max(sp.n, 1), done = first && lastp;
         const size_t slot = 2 * (size_t)c + (first ? 1 : 0);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], o);
-            if (g8 == 0) {
-                sh_stat[wid][2 * c4] = make_float2(m[n][0], l[n][0]);
-                sh_stat[wid][2 * c4 + 1] = make_float2(m[n][1], l[n][1]);
+        for (int r0 = 0; r0 < rows && ok; r0 += ST_ROUND) {          // rows r0 .. r0 + 3: columns of lanes c4 = (r0 & 7) / 2 and + 1
+            const bool holds = (c4 >> 1) == ((r0 >> 2) & 1);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (n != r0 >> 3 || !holds) continue;
+                const int lr = 2 * (c4 & 1);
+                if (g8 == 0) {
+                    sh_stat[wid][lr] = make_float2(m[n][0], l[n][0]);
+                    sh_stat[wid][lr + 1] = make_float2(m[n][1], l[n][1]);
+                }
+#pragma unroll
+                for (int t = 0; t < VS; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sh_acc[wid][lr + (i & 1)][value_dim<FMT, D>(t, i >> 1, g8)] = acc[n][t][i];
             }
+            ok = !any_of(*gave_up != 0);
+            const int r = r0 + (wid >> 1), d0 = (wid & 1) * (D / 2) + lane * (D / 64);        // two warps per row
+            if (r < rows && ok) {
+                float M = PT_NONE, L = 0.0f, o[D / 64];
+                const int lr = wid >> 1;
 #pragma unroll
-            for (int t = 0; t < VS; ++t)
+                for (int x = 0; x < ST_WARPS; ++x) M = fmaxf(M, sh_stat[x][lr].x);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sh_acc[wid][2 * c4 + (i & 1)][value_dim<FMT, D>(t, i >> 1, g8)] = acc[n][t][i];
-            __syncthreads();
-            const int r = 8 * n + wid;                  // a warp per row
-            if (r < rows) {
-                float M = PT_NONE, L = 0.0f, o[D / 32];
-#pragma unroll
-                for (int x = 0; x < ST_WARPS; ++x) M = fmaxf(M, sh_stat[x][wid].x);
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) o[i] = 0.0f;
+                for (int i = 0; i < D / 64; ++i) o[i] = 0.0f;
 #pragma unroll
                 for (int x = 0; x < ST_WARPS; ++x) {
-                    const float2 st = sh_stat[x][wid];
+                    const float2 st = sh_stat[x][lr];
                     const float f = ex2(st.x - M);
                     L += f * st.y;
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) o[i] += f * sh_acc[x][wid][lane * (D / 32) + i];
+                    for (int i = 0; i < D / 64; ++i) o[i] += f * sh_acc[x][lr][d0 + i];
                 }
                 if (done) {
                     const int rr = w.rt * RT + r, hq = w.h * a.G + rr % a.G;
                     const long long tok = s.row0 + rr / a.G;
                     const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-                    uint16_t* dst = a.out + tok * a.out_stride + (long long)hq * D + lane * (D / 32);
-#pragma unroll
-                    for (int i = 0; i < D / 32; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = T::pack(o[i] * inv, o[i + 1] * inv);
-                    if (a.lse && lane == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = L > 0.0f ? (M + log2f(L)) * PT_LN2 : -INFINITY;
+                    uint16_t* dst = a.out + tok * a.out_stride + (long long)hq * D + d0;
+                    if (D == 128) *reinterpret_cast<uint32_t*>(dst) = T::pack(o[0] * inv, o[D / 64 - 1] * inv);
+                    else *dst = T::round(o[0] * inv);
+                    if (a.lse && lane == 0 && (wid & 1) == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = L > 0.0f ? (M + log2f(L)) * PT_LN2 : -INFINITY;
                 } else {
-                    float* dst = a.part + (slot * RT + r) * D + lane * (D / 32);
+                    float* dst = a.part + (slot * RT + r) * D + d0;
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) dst[i] = o[i];
-                    if (lane == 0) a.stat[slot * RT + r] = make_float2(M, L);
+                    for (int i = 0; i < D / 64; ++i) dst[i] = o[i];
+                    if (lane == 0 && (wid & 1) == 0) a.stat[slot * RT + r] = make_float2(M, L);
                 }
             }
-            __syncthreads();
+            any_of(false);
         }
         if (!done) {
             if (first) {
@@ -370,29 +455,25 @@ k_paged_step(PtArgs a, int blocks) {
         w.left -= k1 - k0;
         if (w.left > 0) pt_next<RT>(w, s, a);
     }
-    if (threadIdx.x == 0) a.head[c] = hd;
+    if (threadIdx.x == 0) {
+        a.head[c] = hd;
+        if (sh_gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
+    }
 }
 
 template <typename T, int FMT, int D, int NT>
 int launch_step(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
+    using SM = StSmem<FMT, D, NT>;
     constexpr int RT = 8 * NT;
+    SC_CHECK(cudaFuncSetAttribute(k_paged_step<T, FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::BYTES));
     // no more blocks than there can be tiles of work: rows of q times heads times the table's tiles
     const long long most = (long long)a.sq.n_rows * a.pc.heads * ((((long long)a.sq.width << a.pc.page_shift) + PT_KEYS - 1) / PT_KEYS);
-    const int blocks = (int)max(1ll, min(min(most, (long long)PT_MAX_BLOCKS), (long long)c->sm_count * st_blocks<FMT, D, NT>()));
+    const int blocks = (int)max(1ll, min(min(most, (long long)PT_MAX_BLOCKS), (long long)c->sm_count * SM::BLOCKS));
     a.part = reinterpret_cast<float*>(work);
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * RT * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * RT);
-    k_paged_step<T, FMT, D, NT><<<blocks, ST_THREADS, 0, st>>>(a, blocks);
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(blocks, NT);
-    cfg.blockDim = dim3(256);
-    cfg.stream = st;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    SC_CHECK(cudaLaunchKernelEx(&cfg, k_paged_join<T, RT, D>, a, blocks));
+    SC_CHECK(pt_launch(k_paged_step<T, FMT, D, NT>, dim3(blocks), ST_THREADS, SM::BYTES, st, a, blocks));
+    SC_CHECK(pt_launch(k_paged_join<T, RT, D>, dim3(blocks, NT), 256, 0, st, a, blocks));
     c->launches += 2;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;

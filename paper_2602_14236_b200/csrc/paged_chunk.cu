@@ -24,48 +24,19 @@
 #include <cuda.h>
 #include <math.h>
 
+#include "paged_async.cuh"
 #include "paged_plan.cuh"
 
 namespace {
 
 constexpr int CH_ROWS = 256, CH_THREADS = 512, CH_STAGES = 4;
-constexpr int CH_WAIT_LIMIT = 1 << 24;       // tries before a wait gives up (a second or more)
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-// ---- mbarriers
-__device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
-__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {          // one arrival, and bytes to come
-    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
-                 "r"(bar)
-                 : "memory");
-}
+// ---- tensor memory and tcgen05
 __device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
                  "l"(map), "r"(bar), "r"(x), "r"(y)
                  : "memory");
 }
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2; selp.b32 %0, 1, 0, p; }"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-// A wait that is given up, here or by another role, returns all the same: the roles look at the flag once a tile and leave.
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-    if (bar_try(bar, parity)) return;
-    for (int i = 0; i < CH_WAIT_LIMIT; ++i) {
-        if (bar_try(bar, parity)) return;
-        if (*gave_up) return;
-    }
-    *gave_up = 1;
-}
-
-// ---- tensor memory and tcgen05
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
@@ -162,9 +133,6 @@ __device__ __forceinline__ uint32_t swz(int r, int c) { return (uint32_t)((c >> 
 __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ void lds16(uint32_t* v, uint32_t addr) {
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
-}
 // 16 bytes into shared memory behind the thread's back, or zeros.
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool get) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(get ? 16 : 0) : "memory");
@@ -247,6 +215,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1)
 k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     using SM = ChSmem<FMT, D>;
     extern __shared__ uint8_t raw[];
+    __shared__ PtShared plan;
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     ChBars& bars = *reinterpret_cast<ChBars*>(raw + (base - smem_u32(raw)) + SM::BARS);
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
@@ -275,8 +244,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    grid_wait();
+    grid_release();
     tc_before();
-    PtWalk w = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks);
+    PtWalk w = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks, plan);
     __syncthreads();
     tc_after();
     const uint32_t tmem = bars.tmem;
@@ -742,7 +713,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             if (lane == 0) {
                 bar_init(smem_u32(&bars.o_done[0]), 1);
                 tc_commit(smem_u32(&bars.o_done[0]));
-                for (int i = 0; i < CH_WAIT_LIMIT && !bar_try(smem_u32(&bars.o_done[0]), 0); ++i) {}
+                for (int i = 0; i < WAIT_LIMIT && !bar_try(smem_u32(&bars.o_done[0]), 0); ++i) {}
             }
             __syncwarp();
         }
@@ -757,7 +728,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(CH_ROWS)
 k_paged_join_chunk(PtArgs a, int blocks) {
     __shared__ int list[PT_MAX_BLOCKS + 1];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    grid_wait();
     constexpr int N = CH_JOIN / 4;
     const int4 hd = a.head[blockIdx.x];
     if (hd.y == 0) return;
@@ -833,18 +804,8 @@ int launch_chunk(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     a.part = reinterpret_cast<float*>(work);
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * CH_ROWS * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * CH_ROWS);
-    k_paged_chunk<T, FMT, D><<<blocks, CH_THREADS, BYTES, st>>>(a, map, blocks);
-    SC_CHECK(cudaGetLastError());
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(blocks, D / CH_JOIN);
-    cfg.blockDim = dim3(CH_ROWS);
-    cfg.stream = st;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    SC_CHECK(cudaLaunchKernelEx(&cfg, k_paged_join_chunk<T, D>, a, blocks));
+    SC_CHECK(pt_launch(k_paged_chunk<T, FMT, D>, dim3(blocks), CH_THREADS, BYTES, st, a, map, blocks));
+    SC_CHECK(pt_launch(k_paged_join_chunk<T, D>, dim3(blocks, D / CH_JOIN), CH_ROWS, 0, st, a, blocks));
     c->launches += 2;
     return SALICACHE_OK;
 }

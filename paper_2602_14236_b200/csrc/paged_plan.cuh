@@ -12,6 +12,7 @@
 // blocks, so results do not depend on timing.
 #pragma once
 #include "paged.cuh"
+#include "paged_async.cuh"
 
 constexpr int PT_KEYS = 128;                 // positions per tile
 constexpr float PT_NONE = -3.0e38f;          // running maximum of a row that has seen nothing
@@ -77,11 +78,15 @@ struct PtWalk {
 // Every thread gets the same walk.  One thread per sequence sums its tiles, a warp together where there are many row
 // tiles; block-wide scans find the block's start.
 // ITEM: units an item counts beside its tiles, before them.
+struct PtShared {
+    long long wsum[32];
+    PtWalk found;
+};
 template <int RT, int THREADS, int ITEM>
-__device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int blocks) {
+__device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int blocks, PtShared& sh) {
     constexpr int ALONE = 2;                 // row tiles that a thread sums by itself
-    __shared__ long long wsum[THREADS / 32];
-    __shared__ PtWalk found;
+    long long* wsum = sh.wsum;
+    PtWalk& found = sh.found;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     // tiles of one head of sequence b; called by whole warps
     auto per_head = [&](int b) -> long long {
@@ -219,7 +224,7 @@ template <typename T, int RT, int D>
 __global__ void __launch_bounds__(256)
 k_paged_join(PtArgs a, int blocks) {
     __shared__ int list[PT_MAX_BLOCKS + 1];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    grid_wait();
     constexpr int N = D / 32;
     const int4 hd = a.head[blockIdx.x];
     if (hd.y == 0) return;
@@ -252,4 +257,20 @@ k_paged_join(PtArgs a, int blocks) {
 #pragma unroll
     for (int i = 0; i < N; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = T::pack(o[i] * inv, o[i + 1] * inv);
     if (a.lse && lane == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (M + log2f(l)) * PT_LN2 : -INFINITY;
+}
+
+// A launch that may begin while the kernel before it in the stream ends (each of these kernels waits for that one first).
+template <typename... P, typename... A>
+cudaError_t pt_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
