@@ -2,9 +2,13 @@
 //
 // Bound by memory: a row is read once and its codes written once.  A CTA takes a tile of consecutive rows of the caller's
 // arrays and a share of the (K|V, head) pairs; for a pair, groups of head_dim / 8 lanes take one row each (16 bytes a
-// lane), so that the group's extremes need only a few shuffles, and the rows of a tile fill neighbouring slots of a page
-// (their codes and their 2- or 4-byte scales meet in whole sectors).  Several pairs are loaded before the first is
-// quantised.
+// lane), and the rows of a tile fill neighbouring slots of a page (their codes and their 2- or 4-byte scales meet in whole
+// sectors).  Four pairs are under way at a time, the first four before the rows' places are known: looking those up takes
+// three dependent loads.
+// Issue slots come next: at the copy bandwidth an SM has 28 clocks for 512 bytes of rows.  So the four pairs' extremes go
+// through one transposing butterfly (5 exchanges instead of 16), after which a quarter of the lanes each divides for one of
+// the four, and integers are found in the mantissa bits of 1.5 * 2^23 + x instead of by the conversion unit.
+#include "paged_async.cuh"
 #include "paged.cuh"
 
 namespace {
@@ -14,7 +18,7 @@ constexpr int PM_AHEAD = 4;          // (K|V, head) pairs in flight per lane
 
 __device__ __forceinline__ uint4 ld16(const uint8_t* p) {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 
@@ -62,86 +66,100 @@ __device__ __forceinline__ void map_rows(RowMap<ROWS>& m, const PgSeqs& sq, cons
     }
 }
 
-// The largest value of both halves over the LPG lanes of a group.
-template <typename T, int LPG>
-__device__ __forceinline__ uint32_t group_max2(uint32_t w) {
-#pragma unroll
-    for (int o = LPG / 2; o; o >>= 1) w = as_word(__hmax2(as_pair<T>(w), as_pair<T>(__shfl_xor_sync(0xffffffffu, w, o))));
-    return w;
-}
-
-// Nearest integer (ties to even) of the product, as bits: |product| < 2^22.
+// Nearest integer (ties to even) of the product, as bits on top of those of 1.5 * 2^23: |product| < 2^22.
 __device__ __forceinline__ uint32_t rint_bits(float d, float inv) {
     return __float_as_uint(__fadd_rn(__fmul_rn(d, inv), 12582912.0f));
 }
-
-// The reciprocal of a stored scale; a scale whose reciprocal is not finite, zero among them, becomes 1.
 template <typename T>
-__device__ __forceinline__ float scale_inv(uint16_t& s16) {
-    float inv = __fdiv_rn(1.0f, T::lo(s16));
-    if (!(inv < INFINITY)) {
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) { return as_word(__hmax2(as_pair<T>(a), as_pair<T>(b))); }
+template <typename T>
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) { return as_word(__hmin2(as_pair<T>(a), as_pair<T>(b))); }
+
+// Four words per lane, each the two halves' maximum to be taken over a group of LPG lanes: quarter u of the group's lanes
+// (lane / (LPG / 4)) gets word u's.
+template <typename T, int LPG>
+__device__ __forceinline__ uint32_t quarter_max(const uint32_t (&w)[4], int gl) {
+    const bool up = gl & (LPG / 2), up2 = gl & (LPG / 4);
+    const uint32_t x0 = max2<T>(up ? w[2] : w[0], __shfl_xor_sync(0xffffffffu, up ? w[0] : w[2], LPG / 2));
+    const uint32_t x1 = max2<T>(up ? w[3] : w[1], __shfl_xor_sync(0xffffffffu, up ? w[1] : w[3], LPG / 2));
+    uint32_t y = max2<T>(up2 ? x1 : x0, __shfl_xor_sync(0xffffffffu, up2 ? x0 : x1, LPG / 4));
+#pragma unroll
+    for (int o = LPG / 8; o; o >>= 1) y = max2<T>(y, __shfl_xor_sync(0xffffffffu, y, o));
+    return y;
+}
+
+// A lane's 8 elements of four groups (pairs p0 .. p0 + 3 of a row, those below p1) -> codes and scales in the pages.
+template <typename T, int FMT, int D>
+__device__ __forceinline__ void store_groups(const uint4 (&v)[PM_AHEAD], const PgCache& pc, int pid, int slot, int p0, int p1, int gl, bool live) {
+    constexpr int LPG = D / 8, Q = LPG / 4;
+    auto place = [&](int u) -> size_t {
+        const int p = min(p0 + u, p1 - 1), kv = p >= pc.heads;
+        return pg_slot(pc, max(pid, 0), kv, p - (kv ? pc.heads : 0), max(slot, 0));
+    };
+    if (FMT == PF_16) {
+#pragma unroll
+        for (int u = 0; u < PM_AHEAD; ++u)
+            if (live && p0 + u < p1) reinterpret_cast<uint4*>(pc.data + place(u) * pg_row_bytes<FMT, D>())[gl] = v[u];
+        return;
+    }
+    uint32_t e[PM_AHEAD];
+#pragma unroll
+    for (int u = 0; u < PM_AHEAD; ++u) {
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        if (FMT == PF_I8) {
+            const uint32_t m = max2<T>(max2<T>(as_word(__habs2(as_pair<T>(w[0]))), as_word(__habs2(as_pair<T>(w[1])))),
+                                       max2<T>(as_word(__habs2(as_pair<T>(w[2]))), as_word(__habs2(as_pair<T>(w[3])))));
+            e[u] = m;
+        } else {                             // (maximum, -minimum)
+            const uint32_t hi = max2<T>(max2<T>(w[0], w[1]), max2<T>(w[2], w[3]));
+            const uint32_t lo = as_word(__hneg2(as_pair<T>(min2<T>(min2<T>(w[0], w[1]), min2<T>(w[2], w[3])))));
+            e[u] = max2<T>(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
+        }
+    }
+    const uint32_t x = quarter_max<T, LPG>(e, gl);
+    const int mine = gl / Q;                 // the group whose scale this lane forms
+    const float zero = FMT == PF_I4 ? -T::hi(x) : 0.0f;
+    const float span = FMT == PF_I4 ? __fsub_rn(T::lo(x), zero) : fmaxf(T::lo(x), T::hi(x));
+    uint16_t s16 = T::round(__fdiv_rn(span, FMT == PF_I4 ? 15.0f : 127.0f));
+    float inv = __frcp_rn(T::lo(s16));
+    if (!(inv < INFINITY)) {                 // zero, and what has no reciprocal in binary32
         s16 = (uint16_t)T::ONE;
         inv = 1.0f;
     }
-    return inv;
-}
-
-// One lane's 8 elements of a group -> codes and scale in the pages.
-template <typename T, int FMT, int D>
-__device__ __forceinline__ void store_group(const uint4& v, const PgCache& pc, size_t slot, int gl, bool put) {
-    constexpr int LPG = D / 8;
-    uint8_t* dst = pc.data + slot * pg_row_bytes<FMT, D>();
-    if (FMT == PF_16) {
-        if (put) reinterpret_cast<uint4*>(dst)[gl] = v;
-        return;
+    if (live && gl % Q == 0 && p0 + mine < p1) {
+        const size_t at = place(mine);
+        if (FMT == PF_I8) reinterpret_cast<uint16_t*>(pc.scale)[at] = s16;
+        else reinterpret_cast<uint32_t*>(pc.scale)[at] = (uint32_t)s16 | (uint32_t)T::round(zero) << 16;
     }
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    if (FMT == PF_I8) {
-        uint32_t m = as_word(__hmax2(__hmax2(__habs2(as_pair<T>(w[0])), __habs2(as_pair<T>(w[1]))),
-                                     __hmax2(__habs2(as_pair<T>(w[2])), __habs2(as_pair<T>(w[3])))));
-        m = group_max2<T, LPG>(m);
-        uint16_t s16 = T::round(__fdiv_rn(fmaxf(T::lo(m), T::hi(m)), 127.0f));
-        const float inv = scale_inv<T>(s16);
+    // A normal scale is within half a step of the quotient, so no code can leave its range; a subnormal one has fewer bits.
+    const bool clamp = __any_sync(0xffffffffu, (s16 & 0x7fffu) < T::NORMAL);
+    const int first = (threadIdx.x & 31) - gl;
+#pragma unroll
+    for (int u = 0; u < PM_AHEAD; ++u) {
+        const float iu = __shfl_sync(0xffffffffu, inv, first + u * Q);
+        const float zu = FMT == PF_I4 ? __shfl_sync(0xffffffffu, zero, first + u * Q) : 0.0f;
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
         uint32_t q[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {       // a scale rounded down may put the extreme half a step past 127: clamp
-            q[2 * i] = rint_bits(T::lo(w[i]), inv);
-            q[2 * i + 1] = rint_bits(T::hi(w[i]), inv);
-        }
-        uint32_t o[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t b = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = min(127, max(-127, (int)q[4 * i + j] - 0x4B400000));
-                b |= (uint32_t)(c & 0xff) << (8 * j);
-            }
-            o[i] = b;
-        }
-        if (put) {
-            reinterpret_cast<uint2*>(dst)[gl] = make_uint2(o[0], o[1]);
-            if (gl == 0) reinterpret_cast<uint16_t*>(pc.scale)[slot] = s16;
-        }
-    } else {
-        const uint32_t hi2 = as_word(__hmax2(__hmax2(as_pair<T>(w[0]), as_pair<T>(w[1])), __hmax2(as_pair<T>(w[2]), as_pair<T>(w[3]))));
-        const uint32_t lo2 = as_word(__hmin2(__hmin2(as_pair<T>(w[0]), as_pair<T>(w[1])), __hmin2(as_pair<T>(w[2]), as_pair<T>(w[3]))));
-        const uint32_t a = as_word(__hmax2(as_pair<T>(hi2), as_pair<T>(__byte_perm(hi2, 0, 0x1032))));       // max in both halves
-        const uint32_t n = as_word(__hneg2(__hmin2(as_pair<T>(lo2), as_pair<T>(__byte_perm(lo2, 0, 0x1032)))));
-        const uint32_t e = group_max2<T, LPG>((a & 0xffffu) | (n << 16));                                    // (max, -min)
-        const float z = -T::hi(e);
-        uint16_t s16 = T::round(__fdiv_rn(__fsub_rn(T::lo(e), z), 15.0f));
-        const float inv = scale_inv<T>(s16);
-        uint32_t o = 0;
-#pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int q0 = min(15, (int)rint_bits(__fsub_rn(T::lo(w[i]), z), inv) - 0x4B400000);
-            const int q1 = min(15, (int)rint_bits(__fsub_rn(T::hi(w[i]), z), inv) - 0x4B400000);
-            o |= (uint32_t)(q0 | q1 << 4) << (8 * i);
+            q[2 * i] = rint_bits(FMT == PF_I4 ? __fsub_rn(T::lo(w[i]), zu) : T::lo(w[i]), iu);
+            q[2 * i + 1] = rint_bits(FMT == PF_I4 ? __fsub_rn(T::hi(w[i]), zu) : T::hi(w[i]), iu);
         }
-        if (put) {
-            reinterpret_cast<uint32_t*>(dst)[gl] = o;
-            if (gl == 0) reinterpret_cast<uint32_t*>(pc.scale)[slot] = (uint32_t)s16 | (uint32_t)T::round(z) << 16;
+        if (clamp) {
+            constexpr int TOP = FMT == PF_I4 ? 15 : 127, LOW = FMT == PF_I4 ? 0 : -127;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = (uint32_t)max(LOW, min(TOP, (int)q[i] - 0x4B400000));
+        }
+        const bool put = live && p0 + u < p1;
+        uint8_t* dst = pc.data + place(u) * pg_row_bytes<FMT, D>();
+        if (FMT == PF_I8) {
+            const uint32_t a = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+            const uint32_t b = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+            if (put) reinterpret_cast<uint2*>(dst)[gl] = make_uint2(a, b);
+        } else {
+            const uint32_t b0 = q[0] + (q[1] << 4), b1 = q[2] + (q[3] << 4), b2 = q[4] + (q[5] << 4), b3 = q[6] + (q[7] << 4);
+            const uint32_t o = __byte_perm(__byte_perm(b0, b1, 0x0040), __byte_perm(b2, b3, 0x0040), 0x5410);
+            if (put) reinterpret_cast<uint32_t*>(dst)[gl] = o;
         }
     }
 }
@@ -169,23 +187,33 @@ __device__ __forceinline__ void fetch_group(Fetched<FMT>& f, const PgCache& pc, 
         f.meta = reinterpret_cast<const uint32_t*>(pc.scale)[slot];
     }
 }
+// Codes to numbers by putting them into the mantissa of 2^23.  A nibble i places up stands for 16^i times its value, which
+// the scale, divided by the same power of two, makes good exactly; the offset is taken off in the same fused step, whose
+// exact result q * s fits binary32, so that nothing is rounded before the zero is added.
 template <typename T, int FMT>
 __device__ __forceinline__ uint4 expand_group(const Fetched<FMT>& f) {
     if (FMT == PF_16) return f.c;
     uint32_t o[4];
     const float s = T::lo(f.meta), z = T::hi(f.meta);
+    if (FMT == PF_I8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float a, b;
-        if (FMT == PF_I8) {
-            const uint32_t w = i < 2 ? f.c.x : f.c.y;
-            a = __fmul_rn((float)(int8_t)(w >> (16 * (i & 1))), s);
-            b = __fmul_rn((float)(int8_t)(w >> (16 * (i & 1) + 8)), s);
-        } else {
-            a = __fadd_rn(__fmul_rn((float)((f.c.x >> (8 * i)) & 15u), s), z);
-            b = __fadd_rn(__fmul_rn((float)((f.c.x >> (8 * i + 4)) & 15u), s), z);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = (i < 2 ? f.c.x : f.c.y) ^ 0x80808080u;
+            const float a = __uint_as_float(__byte_perm(w, 0x4B000000u, (i & 1) ? 0x7442 : 0x7440)) - 8388736.0f;
+            const float b = __uint_as_float(__byte_perm(w, 0x4B000000u, (i & 1) ? 0x7443 : 0x7441)) - 8388736.0f;
+            o[i] = T::pack(__fmul_rn(a, s), __fmul_rn(b, s));
         }
-        o[i] = T::pack(a, b);
+    } else {
+        float x[8];
+        const uint32_t w1 = f.c.x >> 16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float si = s * (1.0f / (float)(1 << (4 * (i & 3))));
+            const uint32_t b = and_or(i < 4 ? f.c.x : w1, 15u << (4 * (i & 3)), 0x4B000000u);
+            x[i] = __fadd_rn(__fmaf_rn(__uint_as_float(b), si, -8388608.0f * si), z);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = T::pack(x[2 * i], x[2 * i + 1]);
     }
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
@@ -193,44 +221,60 @@ __device__ __forceinline__ uint4 expand_group(const Fetched<FMT>& f) {
 // grid.x: tiles of rows; grid.y: shares of `per` consecutive (K|V, head) pairs (pair = kv * heads + head).
 template <typename T, int FMT, int D, bool WRITE>
 __global__ void __launch_bounds__(PM_THREADS)
-k_paged_move(PgCache pc, PgSeqs sq, uint16_t* __restrict__ K, uint16_t* __restrict__ V, long long ks, long long vs, int per,
-             int* __restrict__ status) {
+k_paged_move(PgCache pc, PgSeqs sq, uint16_t* K, uint16_t* V, long long ks, long long vs, int per,
+             int* status) {
     constexpr int LPG = D / 8, ROWS = PM_THREADS / LPG;
     __shared__ RowMap<ROWS> map;
-    map_rows<ROWS>(map, sq, pc, blockIdx.x * ROWS, status);
-    __syncthreads();
     const int row = threadIdx.x / LPG, gl = threadIdx.x % LPG;
-    const int pid = map.pid[row], slot = map.slot[row];
     const long long r = (long long)blockIdx.x * ROWS + row;
     const int p1 = min(2 * pc.heads, (int)(blockIdx.y + 1) * per);
-    const bool live = slot >= 0;                       // the row has a place in the pages
-    for (int p0 = blockIdx.y * per; p0 < p1; p0 += PM_AHEAD) {
-        if (WRITE) {
-            uint4 v[PM_AHEAD];
+    grid_wait();
+    grid_release();
+    if (WRITE) {
+        auto load = [&](uint4 (&v)[PM_AHEAD], int p0) {
 #pragma unroll
             for (int u = 0; u < PM_AHEAD; ++u) {
                 const int p = p0 + u, kv = p >= pc.heads, h = p - (kv ? pc.heads : 0);
                 v[u] = make_uint4(0, 0, 0, 0);
-                if (live && p < p1) v[u] = ld16(reinterpret_cast<const uint8_t*>((kv ? V + r * vs : K + r * ks) + h * D + gl * 8));
+                if (r < sq.n_rows && p < p1) v[u] = ld16(reinterpret_cast<const uint8_t*>((kv ? V + r * vs : K + r * ks) + h * D + gl * 8));
             }
+        };
+        uint4 v[PM_AHEAD], next[PM_AHEAD];
+        int p0 = blockIdx.y * per;
+        load(v, p0);
+        map_rows<ROWS>(map, sq, pc, blockIdx.x * ROWS, status);
+        __syncthreads();
+        const int pid = map.pid[row], slot = map.slot[row];
+        for (; p0 < p1; p0 += PM_AHEAD) {
+            load(next, p0 + PM_AHEAD);
+            store_groups<T, FMT, D>(v, pc, pid, slot, p0, p1, gl, slot >= 0);
+#pragma unroll
+            for (int u = 0; u < PM_AHEAD; ++u) v[u] = next[u];
+        }
+    } else {
+        map_rows<ROWS>(map, sq, pc, blockIdx.x * ROWS, status);
+        __syncthreads();
+        const int pid = map.pid[row], slot = map.slot[row];
+        Fetched<FMT> f[PM_AHEAD], next[PM_AHEAD];
+        auto load = [&](Fetched<FMT> (&x)[PM_AHEAD], int p0) {
 #pragma unroll
             for (int u = 0; u < PM_AHEAD; ++u) {
-                const int p = p0 + u, kv = p >= pc.heads, h = p - (kv ? pc.heads : 0);
-                store_group<T, FMT, D>(v[u], pc, pg_slot(pc, max(pid, 0), kv, h, max(slot, 0)), gl, live && p < p1);
+                const int p = min(p0 + u, p1 - 1), kv = p >= pc.heads;
+                fetch_group<FMT, D>(x[u], pc, pg_slot(pc, max(pid, 0), kv, p - (kv ? pc.heads : 0), max(slot, 0)), gl, slot >= 0 && p0 + u < p1);
             }
-        } else {
-            Fetched<FMT> f[PM_AHEAD];
-#pragma unroll
-            for (int u = 0; u < PM_AHEAD; ++u) {
-                const int p = p0 + u, kv = p >= pc.heads, h = p - (kv ? pc.heads : 0);
-                fetch_group<FMT, D>(f[u], pc, pg_slot(pc, max(pid, 0), kv, h, max(slot, 0)), gl, live && p < p1);
-            }
+        };
+        int p0 = blockIdx.y * per;
+        load(f, p0);
+        for (; p0 < p1; p0 += PM_AHEAD) {
+            load(next, p0 + PM_AHEAD);
 #pragma unroll
             for (int u = 0; u < PM_AHEAD; ++u) {
                 const int p = p0 + u, kv = p >= pc.heads, h = p - (kv ? pc.heads : 0);
                 if (slot >= -1 && p < p1)               // rows in no page come back as zeros, rows of no sequence stay
                     __stcs(reinterpret_cast<uint4*>((kv ? V + r * vs : K + r * ks) + h * D + gl * 8), expand_group<T, FMT>(f[u]));
             }
+#pragma unroll
+            for (int u = 0; u < PM_AHEAD; ++u) f[u] = next[u];
         }
     }
 }
@@ -243,9 +287,10 @@ int launch_move(salicache_ctx* c, const PgCache& pc, const PgSeqs& sq, void* K, 
     const int pairs = 2 * pc.heads;
     int per = pairs;
     while (per > PM_AHEAD && tiles * ((pairs + per - 1) / per) < 8ll * c->sm_count) per = (per + 1) / 2;
+    per = (per + PM_AHEAD - 1) / PM_AHEAD * PM_AHEAD;
     const dim3 grid((unsigned)tiles, (unsigned)((pairs + per - 1) / per));
-    if (write) k_paged_move<T, FMT, D, true><<<grid, PM_THREADS, 0, st>>>(pc, sq, (uint16_t*)K, (uint16_t*)V, ks, vs, per, c->d_status);
-    else k_paged_move<T, FMT, D, false><<<grid, PM_THREADS, 0, st>>>(pc, sq, (uint16_t*)K, (uint16_t*)V, ks, vs, per, c->d_status);
+    if (write) SC_CHECK(pt_launch(k_paged_move<T, FMT, D, true>, grid, PM_THREADS, 0, st, pc, sq, (uint16_t*)K, (uint16_t*)V, (long long)ks, (long long)vs, per, c->d_status));
+    else SC_CHECK(pt_launch(k_paged_move<T, FMT, D, false>, grid, PM_THREADS, 0, st, pc, sq, (uint16_t*)K, (uint16_t*)V, (long long)ks, (long long)vs, per, c->d_status));
     c->launches++;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;

@@ -745,7 +745,7 @@ k_paged_join_chunk(PtArgs a, int blocks) {
 #pragma unroll 8
     for (int i = 0; i < n; ++i) {
         const size_t t = (size_t)list[i];
-        const float2 st = __ldg(a.stat + t * CH_ROWS + row);
+        const float2 st = a.stat[t * CH_ROWS + row];
         const float4* src = reinterpret_cast<const float4*>(a.part) + (t * (D / 4) + blockIdx.y * N) * CH_ROWS + row;
         const float nm = fmaxf(M, st.x), f = ex2(M - nm), e = ex2(st.x - nm);
         M = nm;
