@@ -88,18 +88,27 @@ __device__ __forceinline__ uint32_t quarter_max(const uint32_t (&w)[4], int gl) 
     return y;
 }
 
+// Where a row's codes (this lane's share) and scales lie for pair 0; a pair is one page's worth of slots further on.
+struct RowPlace {
+    uint8_t* data;
+    uint8_t* scale;
+    uint32_t data_step, scale_step;
+};
+template <int FMT, int D>
+__device__ __forceinline__ RowPlace row_place(const PgCache& pc, int pid, int slot, int gl) {
+    constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>(), LPG = D / 8;
+    const size_t at = pg_slot(pc, max(pid, 0), 0, 0, max(slot, 0));
+    return RowPlace{pc.data + at * RB + gl * (RB / LPG), pc.scale + at * MB, (uint32_t)RB << pc.page_shift, (uint32_t)MB << pc.page_shift};
+}
+
 // A lane's 8 elements of four groups (pairs p0 .. p0 + 3 of a row, those below p1) -> codes and scales in the pages.
 template <typename T, int FMT, int D>
-__device__ __forceinline__ void store_groups(const uint4 (&v)[PM_AHEAD], const PgCache& pc, int pid, int slot, int p0, int p1, int gl, bool live) {
+__device__ __forceinline__ void store_groups(const uint4 (&v)[PM_AHEAD], const RowPlace& rp, int p0, int p1, int gl, bool live) {
     constexpr int LPG = D / 8, Q = LPG / 4;
-    auto place = [&](int u) -> size_t {
-        const int p = min(p0 + u, p1 - 1), kv = p >= pc.heads;
-        return pg_slot(pc, max(pid, 0), kv, p - (kv ? pc.heads : 0), max(slot, 0));
-    };
     if (FMT == PF_16) {
 #pragma unroll
         for (int u = 0; u < PM_AHEAD; ++u)
-            if (live && p0 + u < p1) reinterpret_cast<uint4*>(pc.data + place(u) * pg_row_bytes<FMT, D>())[gl] = v[u];
+            if (live && p0 + u < p1) *reinterpret_cast<uint4*>(rp.data + (p0 + u) * rp.data_step) = v[u];
         return;
     }
     uint32_t e[PM_AHEAD];
@@ -127,9 +136,9 @@ __device__ __forceinline__ void store_groups(const uint4 (&v)[PM_AHEAD], const P
         inv = 1.0f;
     }
     if (live && gl % Q == 0 && p0 + mine < p1) {
-        const size_t at = place(mine);
-        if (FMT == PF_I8) reinterpret_cast<uint16_t*>(pc.scale)[at] = s16;
-        else reinterpret_cast<uint32_t*>(pc.scale)[at] = (uint32_t)s16 | (uint32_t)T::round(zero) << 16;
+        uint8_t* at = rp.scale + (p0 + mine) * rp.scale_step;
+        if (FMT == PF_I8) *reinterpret_cast<uint16_t*>(at) = s16;
+        else *reinterpret_cast<uint32_t*>(at) = (uint32_t)s16 | (uint32_t)T::round(zero) << 16;
     }
     // A normal scale is within half a step of the quotient, so no code can leave its range; a subnormal one has fewer bits.
     const bool clamp = __any_sync(0xffffffffu, (s16 & 0x7fffu) < T::NORMAL);
@@ -151,15 +160,15 @@ __device__ __forceinline__ void store_groups(const uint4 (&v)[PM_AHEAD], const P
             for (int i = 0; i < 8; ++i) q[i] = (uint32_t)max(LOW, min(TOP, (int)q[i] - 0x4B400000));
         }
         const bool put = live && p0 + u < p1;
-        uint8_t* dst = pc.data + place(u) * pg_row_bytes<FMT, D>();
+        uint8_t* dst = rp.data + (p0 + u) * rp.data_step;
         if (FMT == PF_I8) {
             const uint32_t a = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
             const uint32_t b = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-            if (put) reinterpret_cast<uint2*>(dst)[gl] = make_uint2(a, b);
+            if (put) *reinterpret_cast<uint2*>(dst) = make_uint2(a, b);
         } else {
             const uint32_t b0 = q[0] + (q[1] << 4), b1 = q[2] + (q[3] << 4), b2 = q[4] + (q[5] << 4), b3 = q[6] + (q[7] << 4);
             const uint32_t o = __byte_perm(__byte_perm(b0, b1, 0x0040), __byte_perm(b2, b3, 0x0040), 0x5410);
-            if (put) reinterpret_cast<uint32_t*>(dst)[gl] = o;
+            if (put) *reinterpret_cast<uint32_t*>(dst) = o;
         }
     }
 }
@@ -170,21 +179,22 @@ struct Fetched {
     uint4 c;
     uint32_t meta;
 };
-template <int FMT, int D>
-__device__ __forceinline__ void fetch_group(Fetched<FMT>& f, const PgCache& pc, size_t slot, int gl, bool get) {
-    const uint8_t* src = pc.data + slot * pg_row_bytes<FMT, D>();
+template <int FMT>
+__device__ __forceinline__ void fetch_group(Fetched<FMT>& f, const RowPlace& rp, int p, bool get) {
+    const uint8_t* src = rp.data + p * rp.data_step;
+    const uint8_t* meta = rp.scale + p * rp.scale_step;
     f.c = make_uint4(0, 0, 0, 0);
     f.meta = 0;
     if (!get) return;
-    if (FMT == PF_16) f.c = __ldcs(reinterpret_cast<const uint4*>(src) + gl);
+    if (FMT == PF_16) f.c = __ldcs(reinterpret_cast<const uint4*>(src));
     else if (FMT == PF_I8) {
-        const uint2 x = __ldcs(reinterpret_cast<const uint2*>(src) + gl);
+        const uint2 x = __ldcs(reinterpret_cast<const uint2*>(src));
         f.c.x = x.x;
         f.c.y = x.y;
-        f.meta = reinterpret_cast<const uint16_t*>(pc.scale)[slot];
+        f.meta = *reinterpret_cast<const uint16_t*>(meta);
     } else {
-        f.c.x = __ldcs(reinterpret_cast<const uint32_t*>(src) + gl);
-        f.meta = reinterpret_cast<const uint32_t*>(pc.scale)[slot];
+        f.c.x = __ldcs(reinterpret_cast<const uint32_t*>(src));
+        f.meta = *reinterpret_cast<const uint32_t*>(meta);
     }
 }
 // Codes to numbers by putting them into the mantissa of 2^23.  A nibble i places up stands for 16^i times its value, which
@@ -230,49 +240,46 @@ k_paged_move(PgCache pc, PgSeqs sq, uint16_t* K, uint16_t* V, long long ks, long
     const int p1 = min(2 * pc.heads, (int)(blockIdx.y + 1) * per);
     grid_wait();
     grid_release();
+    // this lane's share of pair p: K's or V's row, the latter from pair `heads` on
+    uint16_t* const k0 = K + r * ks + gl * 8;
+    uint16_t* const v0 = V + r * vs + gl * 8 - (long long)pc.heads * D;
+    auto dense = [&](int p) -> uint4* { return reinterpret_cast<uint4*>((p >= pc.heads ? v0 : k0) + p * D); };
+    int p0 = blockIdx.y * per;
     if (WRITE) {
-        auto load = [&](uint4 (&v)[PM_AHEAD], int p0) {
+        auto load = [&](uint4 (&v)[PM_AHEAD], int q0) {
 #pragma unroll
             for (int u = 0; u < PM_AHEAD; ++u) {
-                const int p = p0 + u, kv = p >= pc.heads, h = p - (kv ? pc.heads : 0);
                 v[u] = make_uint4(0, 0, 0, 0);
-                if (r < sq.n_rows && p < p1) v[u] = ld16(reinterpret_cast<const uint8_t*>((kv ? V + r * vs : K + r * ks) + h * D + gl * 8));
+                if (r < sq.n_rows && q0 + u < p1) v[u] = ld16(reinterpret_cast<const uint8_t*>(dense(q0 + u)));
             }
         };
         uint4 v[PM_AHEAD], next[PM_AHEAD];
-        int p0 = blockIdx.y * per;
         load(v, p0);
         map_rows<ROWS>(map, sq, pc, blockIdx.x * ROWS, status);
         __syncthreads();
-        const int pid = map.pid[row], slot = map.slot[row];
+        const bool live = map.slot[row] >= 0;
+        const RowPlace rp = row_place<FMT, D>(pc, map.pid[row], map.slot[row], gl);
         for (; p0 < p1; p0 += PM_AHEAD) {
             load(next, p0 + PM_AHEAD);
-            store_groups<T, FMT, D>(v, pc, pid, slot, p0, p1, gl, slot >= 0);
+            store_groups<T, FMT, D>(v, rp, p0, p1, gl, live);
 #pragma unroll
             for (int u = 0; u < PM_AHEAD; ++u) v[u] = next[u];
         }
     } else {
         map_rows<ROWS>(map, sq, pc, blockIdx.x * ROWS, status);
         __syncthreads();
-        const int pid = map.pid[row], slot = map.slot[row];
+        const int slot = map.slot[row];
+        const RowPlace rp = row_place<FMT, D>(pc, map.pid[row], slot, gl);
         Fetched<FMT> f[PM_AHEAD], next[PM_AHEAD];
-        auto load = [&](Fetched<FMT> (&x)[PM_AHEAD], int p0) {
 #pragma unroll
-            for (int u = 0; u < PM_AHEAD; ++u) {
-                const int p = min(p0 + u, p1 - 1), kv = p >= pc.heads;
-                fetch_group<FMT, D>(x[u], pc, pg_slot(pc, max(pid, 0), kv, p - (kv ? pc.heads : 0), max(slot, 0)), gl, slot >= 0 && p0 + u < p1);
-            }
-        };
-        int p0 = blockIdx.y * per;
-        load(f, p0);
+        for (int u = 0; u < PM_AHEAD; ++u) fetch_group(f[u], rp, p0 + u, slot >= 0 && p0 + u < p1);
         for (; p0 < p1; p0 += PM_AHEAD) {
-            load(next, p0 + PM_AHEAD);
 #pragma unroll
-            for (int u = 0; u < PM_AHEAD; ++u) {
-                const int p = p0 + u, kv = p >= pc.heads, h = p - (kv ? pc.heads : 0);
-                if (slot >= -1 && p < p1)               // rows in no page come back as zeros, rows of no sequence stay
-                    __stcs(reinterpret_cast<uint4*>((kv ? V + r * vs : K + r * ks) + h * D + gl * 8), expand_group<T, FMT>(f[u]));
-            }
+            for (int u = 0; u < PM_AHEAD; ++u) fetch_group(next[u], rp, p0 + PM_AHEAD + u, slot >= 0 && p0 + PM_AHEAD + u < p1);
+#pragma unroll
+            for (int u = 0; u < PM_AHEAD; ++u)
+                if (slot >= -1 && p0 + u < p1)          // rows in no page come back as zeros, rows of no sequence stay
+                    __stcs(dense(p0 + u), expand_group<T, FMT>(f[u]));
 #pragma unroll
             for (int u = 0; u < PM_AHEAD; ++u) f[u] = next[u];
         }
