@@ -30,12 +30,14 @@ template <int FMT, int D, int NT>
 struct StSmem {
     static constexpr int ROWS = 128 * pg_row_bytes<FMT, D>(), META = 128 * pg_meta_bytes<FMT>(), STAGE = 2 * (ROWS + META);
     static constexpr int K = 0, V = ROWS, KM = 2 * ROWS, VM = 2 * ROWS + META;
-    static constexpr int ACC = ST_WARPS * ST_ROUND * (D + 4) * 4;
+    static constexpr int ACC = ST_WARPS * ST_ROUND * (D + 4) * 4, Q = 8 * NT * D * 2;       // Q: rows of an item
     // two blocks per SM where a ring of two stages leaves room for them, and the registers of 8 rows do
-    static constexpr int BLOCKS = NT == 1 && 2 * STAGE + ACC <= 110 * 1024 ? 2 : 1;
-    static constexpr int ROOM = (BLOCKS == 2 ? 110 * 1024 : 222 * 1024) - ACC;
+    static constexpr int BLOCKS = NT == 1 && 2 * STAGE + ACC + 2 * Q <= 110 * 1024 ? 2 : 1;
+    static constexpr int ROOM = (BLOCKS == 2 ? 110 * 1024 : 222 * 1024) - ACC - 2 * Q;
     static constexpr int STAGES = ROOM / STAGE < 8 ? ROOM / STAGE : 8;
-    static constexpr int BYTES = STAGES * STAGE + ACC;
+    static constexpr int BYTES = STAGES * STAGE + ACC + 2 * Q;
+    // an item's fixed cost (its rows of q, joining the warps, the output) in tiles' time, as measured
+    static constexpr int ITEM = FMT == PF_16 ? 1 : FMT == PF_I8 ? 2 : 3;
 };
 
 template <typename T>
@@ -173,11 +175,13 @@ k_paged_step(PtArgs a, int blocks) {
     constexpr int RT = 8 * NT, KS = D / 16, VS = D / 16, STAGES = SM::STAGES;
     static_assert(STAGES >= 2, "ring");
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ uint64_t full[STAGES], empty[STAGES];
+    __shared__ uint64_t full[STAGES], empty[STAGES], q_full[2], q_empty[2];
     __shared__ uint32_t kinds[STAGES];       // per stage: bit g: some row sees keys 16 g .. and their page exists
     __shared__ float2 sh_stat[ST_WARPS][ST_ROUND];
     __shared__ PtShared sh_plan;
     __shared__ int sh_gave_up;
+    using Seg = PtSeg<RT, SM::ITEM>;
+    const uint32_t q_ring = smem_u32(ring) + STAGES * SM::STAGE + SM::ACC;
     float (*sh_acc)[ST_ROUND][D + 4] = reinterpret_cast<float (*)[ST_ROUND][D + 4]>(ring + STAGES * SM::STAGE);
     volatile int* gave_up = &sh_gave_up;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g8 = lane >> 2, c4 = lane & 3;
@@ -187,18 +191,23 @@ k_paged_step(PtArgs a, int blocks) {
             bar_init(smem_u32(&full[i]), 1);
             bar_init(smem_u32(&empty[i]), ST_WARPS);
         }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_u32(&q_full[i]), 1);
+            bar_init(smem_u32(&q_empty[i]), ST_WARPS);
+        }
         sh_gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     grid_wait();
     grid_release();
-    PtWalk w = pt_start<RT, ST_THREADS, 0>(a, c, blocks, sh_plan);
+    PtWalk w = pt_start<RT, ST_THREADS, SM::ITEM>(a, c, blocks, sh_plan);
     __syncthreads();
     int4 hd = make_int4(0, 0, 0, 0);
     PgSeq s{};
     if (w.left > 0) s = pg_seq(a.sq, a.pc, w.b);
-    uint32_t n_stage = 0;
+    uint32_t n_stage = 0, n_q = 0;
     bool ok = true;
+    Seg g;
 
     if (wid == ST_WARPS) {
         // ---------------- feeder: a lane per (page of the tile, K rows | V rows | K scales | V scales)
@@ -207,20 +216,25 @@ k_paged_step(PtArgs a, int blocks) {
         const int page = lane / PIECES, piece = lane % PIECES;
         constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
         while (w.left > 0 && ok) {
-            const PtSpan sp = pt_item<RT>(s, a, w.rt);
-            const int k0 = w.k, k1 = (int)min((long long)max(sp.n, 1), k0 + w.left);
-            // page of keys 16 grp .. of tile k: -2 no row sees them, -1 there is no such page
-            auto page_of = [&](int k) -> int {
-                const int j = sp.tile(k) * PT_KEYS + lane * 16;
-                if (lane > 7 || k >= k1 || j >= sp.hi || (j + 16 <= sp.lo && j >= a.sinks)) return -2;
-                const int p = a.sq.table[(size_t)w.b * a.sq.width + (j >> a.pc.page_shift)];
-                return p >= 0 && p < a.pc.n_pages ? p : -1;
-            };
-            int next = sp.n > 0 ? page_of(k0) : -2;
-            for (int k = k0; k < k1 && sp.n > 0 && ok; ++k, ++n_stage) {
+            g.set(a, w, s);
+            if (g.tiles > 0) {               // the item's rows of q, a lane per row
+                const uint32_t qb = n_q & 1, bar = smem_u32(&q_full[qb]);
+                if (n_q >= 2) bar_wait(smem_u32(&q_empty[qb]), (n_q / 2 - 1) & 1, gave_up);
+                __syncwarp();
+                if (lane == 0) bar_expect(bar, (uint32_t)g.rows * (D * 2));
+                __syncwarp();
+                if (lane < g.rows) {
+                    const int rr = w.rt * RT + lane;
+                    bulk_copy(q_ring + qb * SM::Q + lane * (D * 2),
+                              a.q + (long long)(s.row0 + rr / a.G) * a.q_stride + (long long)(w.h * a.G + rr % a.G) * D, D * 2, bar);
+                }
+                ++n_q;
+            }
+            int next = g.tiles > 0 ? g.page_of(a, w, g.t0, lane) : -2;
+            for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k, ++n_stage) {
                 ok = *gave_up == 0;
                 const int pid16 = next;
-                next = page_of(k + 1);
+                next = k + 1 < g.t0 + g.tiles ? g.page_of(a, w, k + 1, lane) : -2;
                 const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), need = __ballot_sync(0xffffffffu, pid16 >= 0);
                 if (bad != 0 && lane == 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
                 const uint32_t mine = page < n_pages ? need >> (page << (a.pc.page_shift - 4)) & ((1u << (per_page >> 4)) - 1u) : 0u;
@@ -242,46 +256,50 @@ k_paged_step(PtArgs a, int blocks) {
                     else bulk_copy(dst + (piece == 3 ? SM::VM : SM::KM) + at * MB, a.pc.scale + slot * MB, per_page * MB, bar);
                 }
             }
-            w.left -= k1 - k0;
+            w.left -= g.k1 - g.k0;
             if (w.left > 0) pt_next<RT>(w, s, a);
         }
         if (!ok) {                           // given up: copies in flight end before the block does
             for (uint32_t i = n_stage > STAGES ? n_stage - STAGES : 0; i < n_stage; ++i)
                 for (int t = 0; t < (1 << 16) && !bar_try(smem_u32(&full[i % STAGES]), (i / STAGES) & 1); ++t) {}
+            for (uint32_t i = n_q > 2 ? n_q - 2 : 0; i < n_q; ++i)
+                for (int t = 0; t < (1 << 16) && !bar_try(smem_u32(&q_full[i & 1]), (i / 2) & 1); ++t) {}
         }
         return;
     }
 
     while (w.left > 0 && ok) {
-        const PtSpan sp = pt_item<RT>(s, a, w.rt);
-        const int k0 = w.k, k1 = (int)min((long long)max(sp.n, 1), k0 + w.left);
-        const int rows = min(RT, s.n * a.G - w.rt * RT);
+        g.set(a, w, s);
+        const PtSpan& sp = g.sp;
+        const int rows = g.rows;
         if (s.cut && threadIdx.x == 0 && s.pos0 + s.n > s.len) atomicMin(a.status, SALICACHE_E_CAPACITY);
 
         // q as B fragments: column g8 of column tile n is row 8 n + g8
         uint32_t qf[NT][KS][2];
+        if (g.tiles > 0) {
+            const uint32_t qb = n_q & 1;
+            bar_wait(smem_u32(&q_full[qb]), (n_q / 2) & 1, gave_up);
+            __syncwarp();
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int r = 8 * n + g8, rr = w.rt * RT + r;
-            const bool in = r < rows;
-            const uint16_t* src = a.q + (long long)(s.row0 + (in ? rr / a.G : 0)) * a.q_stride + (long long)(w.h * a.G + (in ? rr % a.G : 0)) * D;
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t src = q_ring + qb * SM::Q + (8 * n + g8) * (D * 2);
+                const bool in = 8 * n + g8 < rows;
 #pragma unroll
-            for (int st = 0; st < KS; ++st) {
-                int d[4];
-                q_dims<FMT>(st, c4, D, d);
-                uint32_t x0 = 0, x1 = 0;
-                if (in) {
-                    if (FMT == PF_I4) {
-                        x0 = src[d[0]] | (uint32_t)src[d[1]] << 16;
-                        x1 = src[d[2]] | (uint32_t)src[d[3]] << 16;
-                    } else {
-                        x0 = *reinterpret_cast<const uint32_t*>(src + d[0]);
-                        x1 = *reinterpret_cast<const uint32_t*>(src + d[2]);
+                for (int st = 0; st < KS; ++st) {
+                    int d[4];
+                    q_dims<FMT>(st, c4, D, d);
+                    uint32_t x0 = 0, x1 = 0;
+                    if (in) {                // (b, b + 1) and (b + 2, b + 3), or (b, b + 4) and (b + 1, b + 5)
+                        lds_words<1>(&x0, src + 2 * d[0]);
+                        lds_words<1>(&x1, src + 2 * (FMT == PF_I4 ? d[1] : d[2]));
                     }
+                    qf[n][st][0] = FMT == PF_I4 ? __byte_perm(x0, x1, 0x5410) : x0;
+                    qf[n][st][1] = FMT == PF_I4 ? __byte_perm(x0, x1, 0x7632) : x1;
                 }
-                qf[n][st][0] = x0;
-                qf[n][st][1] = x1;
             }
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_u32(&q_empty[qb]));
+            ++n_q;
         }
         float acc[NT][VS][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -292,7 +310,7 @@ k_paged_step(PtArgs a, int blocks) {
             for (int t = 0; t < VS; ++t) acc[n][t][0] = acc[n][t][1] = acc[n][t][2] = acc[n][t][3] = 0.0f;
         }
 
-        for (int k = k0; k < k1 && sp.n > 0; ++k, ++n_stage) {
+        for (int k = g.t0; k < g.t0 + g.tiles; ++k, ++n_stage) {
             const uint32_t st = n_stage % STAGES, src = smem_u32(ring) + st * SM::STAGE;
             bar_wait(smem_u32(&full[st]), (n_stage / STAGES) & 1, gave_up);
             __syncwarp();
@@ -388,7 +406,7 @@ k_paged_step(PtArgs a, int blocks) {
         }
 
         // join the warps: acc[n][t][i] is dimension value_dim(t, i >> 1), row 8 n + 2 c4 + (i & 1)
-        const bool first = k0 == 0, lastp = k1 == max(sp.n, 1), done = first && lastp;
+        const bool first = g.t0 == 0, done = first && g.last;
         const size_t slot = 2 * (size_t)c + (first ? 1 : 0);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -396,7 +414,7 @@ k_paged_step(PtArgs a, int blocks) {
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], o);
-        for (int r0 = 0; r0 < rows && ok; r0 += ST_ROUND) {          // rows r0 .. r0 + 3: columns of lanes c4 = (r0 & 7) / 2 and + 1
+        for (int r0 = 0; r0 < rows && ok && g.real; r0 += ST_ROUND) {          // rows r0 .. r0 + 3: columns of lanes c4 = (r0 & 7) / 2 and + 1
             const bool holds = (c4 >> 1) == ((r0 >> 2) & 1);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -445,14 +463,14 @@ k_paged_step(PtArgs a, int blocks) {
             }
             any_of(false);
         }
-        if (!done) {
+        if (!done && g.real) {
             if (first) {
                 hd.y = w.h + 1;
                 hd.z = w.b;
                 hd.w = w.rt;
-            } else hd.x = lastp ? 2 : 1;
+            } else hd.x = g.last ? 2 : 1;
         }
-        w.left -= k1 - k0;
+        w.left -= g.k1 - g.k0;
         if (w.left > 0) pt_next<RT>(w, s, a);
     }
     if (threadIdx.x == 0) {

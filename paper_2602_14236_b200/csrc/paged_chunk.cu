@@ -177,38 +177,9 @@ struct ChSmem {
     static_assert(BYTES <= 227 * 1024, "shared memory");
 };
 
-// A walk over a block's segments that every role repeats for itself.  An item's first CH_ITEM units stand for its fixed
-// cost (Q, output; measured at about three tiles' time), the others are its tiles.
+// An item's fixed cost (Q, output) in tiles' time, as measured.
 constexpr int CH_ITEM = 3;
-struct ChSeg {
-    PtSpan sp;
-    int k0, k1, t0, tiles, rows;             // units [k0, k1), first tile, tiles with keys, rows in the item (at most 256)
-    bool last, real;                         // the item's end is in here; some of its tiles are (an item without keys has one)
-    __device__ __forceinline__ void set(const PtArgs& a, const PtWalk& w, const PgSeq& s) {
-        sp = pt_item<CH_ROWS>(s, a, w.rt);
-        const int units = CH_ITEM + max(sp.n, 1);
-        k0 = w.k;
-        k1 = (int)min((long long)units, k0 + w.left);
-        rows = min(CH_ROWS, s.n * a.G - w.rt * CH_ROWS);
-        t0 = max(0, k0 - CH_ITEM);
-        const int t1 = max(0, k1 - CH_ITEM);
-        last = k1 == units;
-        real = t1 > t0;
-        tiles = sp.n == 0 ? 0 : t1 - t0;
-    }
-    // Page of keys 16 grp .. of tile k: -2 no row sees them (or grp > 7), -1 there is no such page.
-    __device__ __forceinline__ int page_of(const PtArgs& a, const PtWalk& w, int k, int grp) const {
-        const int j = sp.tile(k) * PT_KEYS + grp * 16;
-        if (grp > 7 || j >= sp.hi || (j + 16 <= sp.lo && j >= a.sinks)) return -2;
-        const int p = a.sq.table[(size_t)w.b * a.sq.width + (j >> a.pc.page_shift)];
-        return p >= 0 && p < a.pc.n_pages ? p : -1;
-    }
-    // Whether some row sees each key of tile k (pages permitting).
-    __device__ __forceinline__ bool clean(const PtArgs& a, int k) const {
-        const int j0 = sp.tile(k) * PT_KEYS;
-        return j0 + PT_KEYS <= sp.hi && (j0 >= sp.lo || j0 + PT_KEYS <= a.sinks);
-    }
-};
+using ChSeg = PtSeg<CH_ROWS, CH_ITEM>;
 
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(CH_THREADS, 1)

@@ -75,9 +75,41 @@ struct PtWalk {
     int b, h, rt, k;                         // the next one: item and tile within it
 };
 
+// A block's share of one item, which every role of a block works out for itself.  An item counts ITEM units before its
+// tiles' for its fixed cost, so that a stretch of many short items is not longer than one long item's.
+template <int RT, int ITEM>
+struct PtSeg {
+    PtSpan sp;
+    int k0, k1, t0, tiles, rows;             // units [k0, k1), first tile, tiles with keys, rows in the item
+    bool last, real;                         // the item's end is in here; some of its tiles are (an item without keys has one)
+    __device__ __forceinline__ void set(const PtArgs& a, const PtWalk& w, const PgSeq& s) {
+        sp = pt_item<RT>(s, a, w.rt);
+        const int units = ITEM + max(sp.n, 1);
+        k0 = w.k;
+        k1 = (int)min((long long)units, k0 + w.left);
+        rows = min(RT, s.n * a.G - w.rt * RT);
+        t0 = max(0, k0 - ITEM);
+        const int t1 = max(0, k1 - ITEM);
+        last = k1 == units;
+        real = t1 > t0;
+        tiles = sp.n == 0 ? 0 : t1 - t0;
+    }
+    // Page of keys 16 grp .. of tile k: -2 no row sees them (or grp > 7), -1 there is no such page.
+    __device__ __forceinline__ int page_of(const PtArgs& a, const PtWalk& w, int k, int grp) const {
+        const int j = sp.tile(k) * PT_KEYS + grp * 16;
+        if (grp > 7 || j >= sp.hi || (j + 16 <= sp.lo && j >= a.sinks)) return -2;
+        const int p = a.sq.table[(size_t)w.b * a.sq.width + (j >> a.pc.page_shift)];
+        return p >= 0 && p < a.pc.n_pages ? p : -1;
+    }
+    // Whether some row sees each key of tile k (pages permitting).
+    __device__ __forceinline__ bool clean(const PtArgs& a, int k) const {
+        const int j0 = sp.tile(k) * PT_KEYS;
+        return j0 + PT_KEYS <= sp.hi && (j0 >= sp.lo || j0 + PT_KEYS <= a.sinks);
+    }
+};
+
 // Every thread gets the same walk.  One thread per sequence sums its tiles, a warp together where there are many row
 // tiles; block-wide scans find the block's start.
-// ITEM: units an item counts beside its tiles, before them.
 struct PtShared {
     long long wsum[32];
     PtWalk found;
