@@ -215,11 +215,12 @@ __device__ __forceinline__ uint4 expand_group(const Fetched<FMT>& f) {
         }
     } else {
         float x[8];
-        const uint32_t w1 = f.c.x >> 16;
+        const uint32_t w1 = f.c.x >> 16, big = held<0x4B000000u>();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float si = s * (1.0f / (float)(1 << (4 * (i & 3))));
-            const uint32_t b = and_or(i < 4 ? f.c.x : w1, 15u << (4 * (i & 3)), 0x4B000000u);
+            const uint32_t w = i < 4 ? f.c.x : w1;
+            const uint32_t b = (i & 3) == 0 ? and_or<0xfu>(w, big) : (i & 3) == 1 ? and_or<0xf0u>(w, big) : (i & 3) == 2 ? and_or<0xf00u>(w, big) : and_or<0xf000u>(w, big);
             x[i] = __fadd_rn(__fmaf_rn(__uint_as_float(b), si, -8388608.0f * si), z);
         }
 #pragma unroll

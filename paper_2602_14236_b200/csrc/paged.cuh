@@ -86,10 +86,18 @@ __device__ __forceinline__ PgSeq pg_seq(const PgSeqs& s, const PgCache& c, int b
     return r;
 }
 
-// (a & b) | c in one instruction.
-__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
+// (a & B) | c in one instruction, which takes one literal: c has to be in a register.
+template <uint32_t B>
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t c) {
     uint32_t d;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "n"(B), "r"(c));
+    return d;
+}
+// A constant that the compiler does not know, so that it stays in its register.
+template <uint32_t C>
+__device__ __forceinline__ uint32_t held() {
+    uint32_t d;
+    asm volatile("mov.b32 %0, %1;" : "=r"(d) : "n"(C));
     return d;
 }
 // Codes to the 16-bit type: OR-ed into the mantissa of a power of two whose last place is 1 (f16: 1024, bf16: 128; for a
@@ -98,24 +106,26 @@ template <typename T>
 struct Codes;
 template <>
 struct Codes<TypeF16> {
+    uint32_t k1024 = held<0x64006400u>(), k64 = held<0x54005400u>(), k1152 = held<0x64806480u>();
     static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) { return as_word(__hsub2(as_pair<TypeF16>(a), as_pair<TypeF16>(b))); }
-    // the two signed bytes in the low bytes of the halves of h (whatever is above them)
-    static __device__ __forceinline__ uint32_t bytes(uint32_t w, uint32_t sel) {
-        return sub(__byte_perm(w ^ 0x80808080u, 0x64646464u, sel), 0x64806480u);
+    // two signed bytes of w (whose places PRMT's selector names, with the constant's byte above each)
+    __device__ __forceinline__ uint32_t bytes(uint32_t w, uint32_t sel) const {
+        return sub(__byte_perm(w ^ 0x80808080u, 0x64646464u, sel), k1152);
     }
-    static __device__ __forceinline__ uint32_t nib_lo(uint32_t x) { return sub(and_or(x, 0x000f000fu, 0x64006400u), 0x64006400u); }
-    static __device__ __forceinline__ uint32_t nib_hi(uint32_t x) { return sub(and_or(x, 0x00f000f0u, 0x54005400u), 0x54005400u); }
+    __device__ __forceinline__ uint32_t nib_lo(uint32_t x) const { return sub(and_or<0x000f000fu>(x, k1024), k1024); }
+    __device__ __forceinline__ uint32_t nib_hi(uint32_t x) const { return sub(and_or<0x00f000f0u>(x, k64), k64); }
 };
 template <>
 struct Codes<TypeBF16> {
+    uint32_t k128 = held<0x43004300u>();
     static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) { return as_word(__hsub2(as_pair<TypeBF16>(a), as_pair<TypeBF16>(b))); }
     // seven bits fit the mantissa of 128; the sign bit (-128) goes into the other operand, 256 instead of 128
-    static __device__ __forceinline__ uint32_t bytes(uint32_t w, uint32_t sel) {
+    __device__ __forceinline__ uint32_t bytes(uint32_t w, uint32_t sel) const {
         const uint32_t h = __byte_perm(w, 0u, sel);
-        return sub(and_or(h, 0x007f007fu, 0x43004300u), and_or(h, 0x00800080u, 0x43004300u));
+        return sub(and_or<0x007f007fu>(h, k128), and_or<0x00800080u>(h, k128));
     }
-    static __device__ __forceinline__ uint32_t nib_lo(uint32_t x) { return sub(and_or(x, 0x000f000fu, 0x43004300u), 0x43004300u); }
-    static __device__ __forceinline__ uint32_t nib_hi(uint32_t x) { return nib_lo(x >> 4); }
+    __device__ __forceinline__ uint32_t nib_lo(uint32_t x) const { return sub(and_or<0x000f000fu>(x, k128), k128); }
+    __device__ __forceinline__ uint32_t nib_hi(uint32_t x) const { return nib_lo(x >> 4); }
 };
 template <typename T>
 __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t s) { return as_word(__hmul2(as_pair<T>(a), as_pair<T>(s))); }

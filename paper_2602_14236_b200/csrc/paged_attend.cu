@@ -37,7 +37,7 @@ struct StSmem {
     static constexpr int STAGES = ROOM / STAGE < 8 ? ROOM / STAGE : 8;
     static constexpr int BYTES = STAGES * STAGE + ACC + 2 * Q;
     // an item's fixed cost (its rows of q, joining the warps, the output) in tiles' time, as measured
-    static constexpr int ITEM = FMT == PF_16 ? 1 : FMT == PF_I8 ? 2 : 3;
+    static constexpr int ITEM = FMT == PF_I4 ? 2 : 1;
 };
 
 template <typename T>
@@ -116,18 +116,18 @@ struct VTile {
 
 // K fragments of matrix instruction st: registers (a0, a2) of one key row.
 template <typename T, int FMT, int D>
-__device__ __forceinline__ void key_frag(const uint32_t (&k)[KTile<FMT, D>::W], uint32_t s, int st, uint32_t& x, uint32_t& y) {
+__device__ __forceinline__ void key_frag(const Codes<T>& cd, const uint32_t (&k)[KTile<FMT, D>::W], uint32_t s, int st, uint32_t& x, uint32_t& y) {
     if (FMT == PF_16) {
         x = k[2 * st];
         y = k[2 * st + 1];
     } else if (FMT == PF_I8) {
         const uint32_t s2 = dup_lo(s);
-        x = mul2<T>(Codes<T>::bytes(k[st], 0x5140), s2);
-        y = mul2<T>(Codes<T>::bytes(k[st], 0x5342), s2);
+        x = mul2<T>(cd.bytes(k[st], 0x5140), s2);
+        y = mul2<T>(cd.bytes(k[st], 0x5342), s2);
     } else {
         const uint32_t s2 = dup_lo(s), z2 = dup_hi(s), w = k[st >> 1] >> (8 * (st & 1));
-        x = fma2<T>(Codes<T>::nib_lo(w), s2, z2);
-        y = fma2<T>(Codes<T>::nib_hi(w), s2, z2);
+        x = fma2<T>(cd.nib_lo(w), s2, z2);
+        y = fma2<T>(cd.nib_hi(w), s2, z2);
     }
 }
 // The dimension pairs that instruction st multiplies in a lane's registers b0 and b1.
@@ -146,20 +146,20 @@ __device__ __forceinline__ void q_dims(int st, int c4, int D, int (&d)[4]) {
 }
 // V fragments of dimension tile t: rows g8 (half 0) and g8 + 8 (half 1) of V transposed, key pairs 0 and 1.
 template <typename T, int FMT, int D>
-__device__ __forceinline__ uint32_t value_frag(const VTile<FMT, D>& v, int t, int half, int pair) {
+__device__ __forceinline__ uint32_t value_frag(const Codes<T>& cd, const VTile<FMT, D>& v, int t, int half, int pair) {
     constexpr int NT = D / 16;
     const int x = half * NT + t;                        // which of the lane's D / 8 dimensions
     const uint32_t *A = v.v[2 * pair], *B = v.v[2 * pair + 1];
     if (FMT == PF_16) return __byte_perm(A[x >> 1], B[x >> 1], (x & 1) ? 0x7632 : 0x5410);
     if (FMT == PF_I8) {
         const uint32_t ab = __byte_perm(A[x >> 2], B[x >> 2], (x & 2) ? 0x7632 : 0x5410);      // bytes A, A+1, B, B+1
-        return mul2<T>(Codes<T>::bytes(ab, (x & 1) ? 0x5341 : 0x5240), v.s[pair][0]);
+        return mul2<T>(cd.bytes(ab, (x & 1) ? 0x5341 : 0x5240), v.s[pair][0]);
     }
     const uint32_t ab = __byte_perm(A[x >> 3], B[x >> 3], (x & 4) ? 0x7632 : 0x5410);          // 4 nibbles of A, 4 of B
     const uint32_t w = (x & 2) ? ab >> 8 : ab;
     const uint32_t s2 = __byte_perm(v.s[pair][0], v.s[pair][FMT == PF_I4 ? 1 : 0], 0x5410);
     const uint32_t z2 = __byte_perm(v.s[pair][0], v.s[pair][FMT == PF_I4 ? 1 : 0], 0x7632);
-    return fma2<T>((x & 1) ? Codes<T>::nib_hi(w) : Codes<T>::nib_lo(w), s2, z2);
+    return fma2<T>((x & 1) ? cd.nib_hi(w) : cd.nib_lo(w), s2, z2);
 }
 template <int FMT, int D>
 __device__ __forceinline__ int value_dim(int t, int half, int g8) {
@@ -268,6 +268,7 @@ k_paged_step(PtArgs a, int blocks) {
         return;
     }
 
+    const Codes<T> cd;
     while (w.left > 0 && ok) {
         g.set(a, w, s);
         const PtSpan& sp = g.sp;
@@ -329,8 +330,8 @@ k_paged_step(PtArgs a, int blocks) {
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
                     uint32_t a0, a1, a2, a3;
-                    key_frag<T, FMT, D>(kt.k[0], kt.s[0], i, a0, a2);
-                    key_frag<T, FMT, D>(kt.k[1], kt.s[1], i, a1, a3);
+                    key_frag<T, FMT, D>(cd, kt.k[0], kt.s[0], i, a0, a2);
+                    key_frag<T, FMT, D>(cd, kt.k[1], kt.s[1], i, a1, a3);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma16816<T>(sc[n], a0, a1, a2, a3, qf[n][i][0], qf[n][i][1]);
                 }
@@ -340,11 +341,7 @@ k_paged_step(PtArgs a, int blocks) {
             __syncwarp();
             if (lane == 0) bar_arrive(smem_u32(&empty[st]));
             {
-                // scores in powers of two; sc[n][i]: key key_of(g8) + 8 (i >> 1), row 8 n + 2 c4 + (i & 1)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[n][i] *= a.scale;
+                // sc[n][i]: key key_of(g8) + 8 (i >> 1), row 8 n + 2 c4 + (i & 1)
                 const bool whole = j0 + 16 <= sp.all_hi && (j0 >= sp.all_lo || j0 + 16 <= a.sinks);
                 if (!whole) {
 #pragma unroll
@@ -369,27 +366,30 @@ k_paged_step(PtArgs a, int blocks) {
                 uint32_t pf[NT][2];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const float x0 = fmaxf(sc[n][0], sc[n][2]), x1 = fmaxf(sc[n][1], sc[n][3]);
-                    if (__any_sync(0xffffffffu, x0 > m[n][0] + 8.0f || x1 > m[n][1] + 8.0f)) {
-                        float y[2] = {x0, x1};
+                    float p[4];                              // in powers of two, less the reference
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] = fmaf(sc[n][i], a.scale, -m[n][i & 1]);
+                    if (__any_sync(0xffffffffu, fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])) > 8.0f)) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
+                            float y = fmaxf(sc[n][i], sc[n][2 + i]) * a.scale;
 #pragma unroll
-                            for (int o = 4; o < 32; o <<= 1) y[i] = fmaxf(y[i], __shfl_xor_sync(0xffffffffu, y[i], o));
-                            y[i] = fmaxf(y[i], m[n][i]);
-                            const float f = ex2(m[n][i] - y[i]);
-                            m[n][i] = y[i];
+                            for (int o = 4; o < 32; o <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, o));
+                            y = fmaxf(y, m[n][i]);
+                            const float f = ex2(m[n][i] - y);
+                            m[n][i] = y;
                             l[n][i] *= f;
 #pragma unroll
                             for (int t = 0; t < VS; ++t) {
                                 acc[n][t][i] *= f;
                                 acc[n][t][2 + i] *= f;
                             }
+                            p[i] = fmaf(sc[n][i], a.scale, -y);
+                            p[2 + i] = fmaf(sc[n][2 + i], a.scale, -y);
                         }
                     }
-                    float p[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[i] = ex2(sc[n][i] - m[n][i & 1]);
+                    for (int i = 0; i < 4; ++i) p[i] = ex2(p[i]);
                     l[n][0] += p[0] + p[2];
                     l[n][1] += p[1] + p[3];
                     pf[n][0] = transpose8(T::pack(p[0], p[1]));
@@ -397,8 +397,8 @@ k_paged_step(PtArgs a, int blocks) {
                 }
 #pragma unroll
                 for (int t = 0; t < VS; ++t) {
-                    const uint32_t a0 = value_frag<T, FMT, D>(vt, t, 0, 0), a1 = value_frag<T, FMT, D>(vt, t, 1, 0);
-                    const uint32_t a2 = value_frag<T, FMT, D>(vt, t, 0, 1), a3 = value_frag<T, FMT, D>(vt, t, 1, 1);
+                    const uint32_t a0 = value_frag<T, FMT, D>(cd, vt, t, 0, 0), a1 = value_frag<T, FMT, D>(cd, vt, t, 1, 0);
+                    const uint32_t a2 = value_frag<T, FMT, D>(cd, vt, t, 0, 1), a3 = value_frag<T, FMT, D>(cd, vt, t, 1, 1);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma16816<T>(acc[n][t], a0, a1, a2, a3, pf[n][0], pf[n][1]);
                 }

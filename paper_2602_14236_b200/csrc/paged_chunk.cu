@@ -445,6 +445,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         if (tid == 0) a.head[blockIdx.x] = hd;
     } else if (wid < 12) {
         // ---------------- operands
+        const Codes<T> cd;
         const int lw = wid - 8;                              // this warp's rows: 32 lw .. 32 lw + 31 of a tile
         uint32_t n_stage = 0;
         bool ok = true;
@@ -511,15 +512,15 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                                 if (FMT == PF_I8) {
 #pragma unroll
                                     for (int i = 0; i < 2; ++i)
-                                        sts16(dst + swz(row, 2 * c + i), mul2<T>(Codes<T>::bytes(w4[2 * i], 0x5140), s2),
-                                              mul2<T>(Codes<T>::bytes(w4[2 * i], 0x5342), s2), mul2<T>(Codes<T>::bytes(w4[2 * i + 1], 0x5140), s2),
-                                              mul2<T>(Codes<T>::bytes(w4[2 * i + 1], 0x5342), s2));
+                                        sts16(dst + swz(row, 2 * c + i), mul2<T>(cd.bytes(w4[2 * i], 0x5140), s2),
+                                              mul2<T>(cd.bytes(w4[2 * i], 0x5342), s2), mul2<T>(cd.bytes(w4[2 * i + 1], 0x5140), s2),
+                                              mul2<T>(cd.bytes(w4[2 * i + 1], 0x5342), s2));
                                 } else {
 #pragma unroll
                                     for (int i = 0; i < 4; ++i) {
                                         const uint32_t y = w4[i] >> 8;
-                                        sts16(dst + swz(row, 4 * c + i), fma2<T>(Codes<T>::nib_lo(w4[i]), s2, z2), fma2<T>(Codes<T>::nib_hi(w4[i]), s2, z2),
-                                              fma2<T>(Codes<T>::nib_lo(y), s2, z2), fma2<T>(Codes<T>::nib_hi(y), s2, z2));
+                                        sts16(dst + swz(row, 4 * c + i), fma2<T>(cd.nib_lo(w4[i]), s2, z2), fma2<T>(cd.nib_hi(w4[i]), s2, z2),
+                                              fma2<T>(cd.nib_lo(y), s2, z2), fma2<T>(cd.nib_hi(y), s2, z2));
                                     }
                                 }
                             }

@@ -155,7 +155,11 @@ __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int block
 #pragma unroll
     for (int i = 0; i < THREADS / 32; ++i) total += wsum[i];
     __syncthreads();
-    const long long beg = total * block / blocks, end = total * (block + 1) / blocks;
+    // shares of the total: 32-bit divisions unless it needs more
+    const long long each = total >> 32 ? total / blocks : (long long)((uint32_t)total / (uint32_t)blocks);
+    const uint32_t over = (uint32_t)(total - each * blocks);
+    const long long beg = each * block + over * (uint32_t)block / (uint32_t)blocks;
+    const long long end = each * (block + 1) + over * (uint32_t)(block + 1) / (uint32_t)blocks;
     if (beg == end) return found;
     long long before = 0;                    // tiles of the sequences before this round's
     for (int b0 = 0; b0 < a.sq.n_seqs; b0 += THREADS) {
@@ -173,10 +177,16 @@ __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int block
         for (int i = 0; i < wid; ++i) off += wsum[i];
         const long long at = beg - (off + incl - w);
         if (at >= 0 && at < w) {             // this thread's sequence holds the start: its head, and tiles into the head
-            const long long ph = w / a.pc.heads;
-            found.left = at % ph;
             found.b = b;
-            found.h = (int)(at / ph);
+            if (w >> 32) {
+                const long long ph = w / a.pc.heads;
+                found.h = (int)(at / ph);
+                found.left = at - found.h * ph;
+            } else {
+                const uint32_t ph = (uint32_t)w / (uint32_t)a.pc.heads;
+                found.h = (int)((uint32_t)at / ph);
+                found.left = (uint32_t)at - found.h * ph;
+            }
         }
         for (int i = 0; i < THREADS / 32; ++i) before += wsum[i];
         __syncthreads();
