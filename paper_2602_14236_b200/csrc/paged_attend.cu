@@ -200,11 +200,10 @@ k_paged_step(PtArgs a, int blocks) {
     }
     grid_wait();
     grid_release();
-    PtWalk w = pt_start<RT, ST_THREADS, SM::ITEM>(a, c, blocks, sh_plan);
+    PgSeq s;
+    PtWalk w = pt_start<RT, ST_THREADS, SM::ITEM>(a, c, blocks, sh_plan, s);
     __syncthreads();
     int4 hd = make_int4(0, 0, 0, 0);
-    PgSeq s{};
-    if (w.left > 0) s = pg_seq(a.sq, a.pc, w.b);
     uint32_t n_stage = 0, n_q = 0;
     bool ok = true;
     Seg g;

@@ -218,12 +218,11 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     grid_wait();
     grid_release();
     tc_before();
-    PtWalk w = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks, plan);
+    PgSeq s;
+    PtWalk w = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks, plan, s);
     __syncthreads();
     tc_after();
     const uint32_t tmem = bars.tmem;
-    PgSeq s{};
-    if (w.left > 0) s = pg_seq(a.sq, a.pc, w.b);
     ChSeg g;
 
     if (wid < 8) {
@@ -704,31 +703,47 @@ k_paged_join_chunk(PtArgs a, int blocks) {
     constexpr int N = CH_JOIN / 4;
     const int4 hd = a.head[blockIdx.x];
     if (hd.y == 0) return;
-    const int n = pt_records(a, blockIdx.x, blocks, list);
     const int row = threadIdx.x, b = hd.z, h = hd.y - 1, rt = hd.w;
     const PgSeq s = pg_seq(a.sq, a.pc, b);
+    const int n = pt_records(a, blockIdx.x, blocks, list);
     const int rr = rt * CH_ROWS + row;
     if (rr >= s.n * a.G) return;
-    // the maximum moves along with the records: one pass over them
+    // the maximum moves along with the records: one pass over them, eight under way at a time
+    constexpr int AHEAD = 8;
     float M = PT_NONE, l = 0.0f;
     float4 o[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-        const size_t t = (size_t)list[i];
-        const float2 st = a.stat[t * CH_ROWS + row];
-        const float4* src = reinterpret_cast<const float4*>(a.part) + (t * (D / 4) + blockIdx.y * N) * CH_ROWS + row;
-        const float nm = fmaxf(M, st.x), f = ex2(M - nm), e = ex2(st.x - nm);
-        M = nm;
-        l = l * f + e * st.y;
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        float2 st[AHEAD];
+        float4 v[AHEAD][N];
 #pragma unroll
-        for (int x = 0; x < N; ++x) {
-            const float4 v = __ldcs(src + x * CH_ROWS);
-            o[x].x = o[x].x * f + e * v.x;
-            o[x].y = o[x].y * f + e * v.y;
-            o[x].z = o[x].z * f + e * v.z;
-            o[x].w = o[x].w * f + e * v.w;
+        for (int u = 0; u < AHEAD; ++u) {
+            const size_t t = (size_t)list[min(i0 + u, n - 1)];
+            const float4* src = reinterpret_cast<const float4*>(a.part) + (t * (D / 4) + blockIdx.y * N) * CH_ROWS + row;
+            st[u] = a.stat[t * CH_ROWS + row];
+#pragma unroll
+            for (int x = 0; x < N; ++x) v[u][x] = __ldcs(src + x * CH_ROWS);
+        }
+        float nm = M;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) nm = fmaxf(nm, st[u].x);
+        const float f = ex2(M - nm);
+        M = nm;
+        l *= f;
+#pragma unroll
+        for (int x = 0; x < N; ++x) o[x] = make_float4(o[x].x * f, o[x].y * f, o[x].z * f, o[x].w * f);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const float e = i0 + u < n ? ex2(st[u].x - M) : 0.0f;
+            l += e * st[u].y;
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                o[x].x += e * v[u][x].x;
+                o[x].y += e * v[u][x].y;
+                o[x].z += e * v[u][x].z;
+                o[x].w += e * v[u][x].w;
+            }
         }
     }
     const int hq = h * a.G + rr % a.G;
