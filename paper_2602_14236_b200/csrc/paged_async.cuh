@@ -24,13 +24,19 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 }
 // A wait that is given up, here or by another role, returns all the same: the roles look at the flag once a tile and leave.
 __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-    if (bar_try(bar, parity)) return;
+#pragma unroll 1
     for (int i = 0; i < WAIT_LIMIT; ++i) {
         if (bar_try(bar, parity)) return;
         if (*gave_up) return;
     }
     *gave_up = 1;
 }
+// The same with its loop in a function, for kernels with many waits and few values that live across them.
+static __device__ __noinline__ void bar_wait_long(uint32_t bar, uint32_t parity, volatile int* gave_up) { bar_wait(bar, parity, gave_up); }
+__device__ __forceinline__ void bar_wait_far(uint32_t bar, uint32_t parity, volatile int* gave_up) {
+    if (!bar_try(bar, parity)) bar_wait_long(bar, parity, gave_up);
+}
+
 __device__ __forceinline__ void lds16(uint32_t* v, uint32_t addr) {
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
 }

@@ -200,8 +200,9 @@ k_paged_step(PtArgs a, int blocks) {
     }
     grid_wait();
     grid_release();
-    PgSeq s;
-    PtWalk w = pt_start<RT, ST_THREADS, SM::ITEM>(a, c, blocks, sh_plan, s);
+    const PtPlace start = pt_start<RT, ST_THREADS, SM::ITEM>(a, c, blocks, sh_plan);
+    PtWalk w = start.w;
+    PgSeq s = start.s;
     __syncthreads();
     int4 hd = make_int4(0, 0, 0, 0);
     uint32_t n_stage = 0, n_q = 0;

@@ -181,6 +181,40 @@ struct ChSmem {
 constexpr int CH_ITEM = 3;
 using ChSeg = PtSeg<CH_ROWS, CH_ITEM>;
 
+// Q of a half's rows x0 .. of an item: a row by D / 8 lanes, asynchronously; each thread works out its own row's address.
+template <int D>
+__device__ __noinline__ void fetch_rows(const PtArgs& a, uint32_t q_tile, int x0, int rows, int head, int row0) {
+    const int row = threadIdx.x & 127, lane = row & 31, r0 = row & ~31;
+    const int x = x0 + min(row, rows - 1);
+    const long long at = (long long)(row0 + x / a.G) * a.q_stride + (long long)(head * a.G + x % a.G) * D;
+    constexpr int LPR = D / 8, RPP = 32 / LPR;
+#pragma unroll 4
+    for (int p = 0; p < 32 / RPP; ++p) {
+        const int lr = p * RPP + lane / LPR, c = lane % LPR;
+        const long long src = __shfl_sync(0xffffffffu, at, lr);
+        cp16(q_tile + swz(r0 + lr, c), a.q + src + c * 8, r0 + lr < rows);
+    }
+}
+// ... and when they have arrived
+template <int FMT, int D>
+__device__ __noinline__ void hand_rows(uint32_t q_tile, uint32_t q_ready) {
+    const int row = threadIdx.x & 127;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+    if (FMT == PF_I4) {                          // the order in which codes leave their words
+#pragma unroll 2
+        for (int c = 0; c < D / 8; ++c) {
+            uint32_t v[4];
+            lds16(v, q_tile + swz(row, c));
+            sts16(q_tile + swz(row, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632), __byte_perm(v[1], v[3], 0x5410),
+                  __byte_perm(v[1], v[3], 0x7632));
+        }
+    }
+    fence_async();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(q_ready);
+}
+
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(CH_THREADS, 1)
 k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
@@ -218,8 +252,9 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     grid_wait();
     grid_release();
     tc_before();
-    PgSeq s;
-    PtWalk w = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks, plan, s);
+    const PtPlace start = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks, plan);
+    PtWalk w = start.w;
+    PgSeq s = start.s;
     __syncthreads();
     tc_after();
     const uint32_t tmem = bars.tmem;
@@ -236,39 +271,15 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         uint32_t n_s = 0, n_o = 0, n_tile = 0;               // scores, outputs of this half and tiles seen so far
         int4 hd = make_int4(0, 0, 0, 0);
         bool ok = true;
-        // Q of an item's rows: a row by D / 8 lanes, asynchronously; each thread works out its own row's address
         auto fetch_q = [&](const ChSeg& gg, const PtWalk& ww, const PgSeq& ss) {
             const int rows = min(128, gg.rows - half * 128);
-            if (rows <= 0 || gg.tiles == 0) return;
-            const int x = ww.rt * CH_ROWS + half * 128 + min(row, rows - 1);
-            const long long at = (long long)(ss.row0 + x / a.G) * a.q_stride + (long long)(ww.h * a.G + x % a.G) * D;
-            constexpr int LPR = D / 8, RPP = 32 / LPR;
-#pragma unroll 4
-            for (int p = 0; p < 32 / RPP; ++p) {
-                const int lr = p * RPP + lane / LPR, qr = (wid & 3) * 32 + lr, c = lane % LPR;
-                const long long src = __shfl_sync(0xffffffffu, at, lr);
-                cp16(q_tile + swz(qr, c), a.q + src + c * 8, qr < rows);
-            }
+            if (rows > 0 && gg.tiles > 0) fetch_rows<D>(a, q_tile, ww.rt * CH_ROWS + half * 128, rows, ww.h, ss.row0);
         };
-        // ... and when it has arrived
         auto hand_q = [&](const ChSeg& gg) {
-            if (gg.rows <= half * 128 || gg.tiles == 0) return;
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            __syncwarp();
-            if (FMT == PF_I4) {                  // the order in which codes leave their words
-                for (int c = 0; c < D / 8; ++c) {
-                    uint32_t v[4];
-                    lds16(v, q_tile + swz(row, c));
-                    sts16(q_tile + swz(row, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632),
-                          __byte_perm(v[1], v[3], 0x5410), __byte_perm(v[1], v[3], 0x7632));
-                }
-            }
-            fence_async();
-            __syncwarp();
-            if (lane == 0) bar_arrive(q_ready);
+            if (gg.rows > half * 128 && gg.tiles > 0) hand_rows<FMT, D>(q_tile, q_ready);
         };
         if (w.left > 0) {
-            g.set(a, w, s);
+            g = ChSeg::of(a, w, s);
             fetch_q(g, w, s);
             hand_q(g);
         }
@@ -280,10 +291,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             PtWalk wn = w;
             PgSeq sn = s;
             wn.left -= g.k1 - g.k0;
-            if (wn.left > 0) pt_next<CH_ROWS>(wn, sn, a);
+            if (wn.left > 0) pt_next_far<CH_ROWS>(wn, sn, a);
             ChSeg gn;
             gn.rows = gn.tiles = 0;
-            if (wn.left > 0) gn.set(a, wn, sn);
+            if (wn.left > 0) gn = ChSeg::of(a, wn, sn);
             bool handed = false;
             if (rows > 0) {
                 const int rr = w.rt * CH_ROWS + half * 128 + row;                 // this thread's row of the item
@@ -296,7 +307,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     const int vis_hi = live ? max(0, min(pos + 1, s.len)) : 0;
                     const int vis_lo = a.window ? pos - a.window + 1 : 0;
                     for (int k = 0; k < g.tiles && ok; ++k, ++n_tile) {
-                        bar_wait(s_full, n_s++ & 1, gave_up);
+                        bar_wait_far(s_full, n_s++ & 1, gave_up);
                         __syncwarp();
                         tc_after();
                         ok = *gave_up == 0;
@@ -381,7 +392,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     if (ok) {
                         hand_q(gn);
                         handed = true;
-                        bar_wait(o_done, n_o++ & 1, gave_up);
+                        bar_wait_far(o_done, n_o++ & 1, gave_up);
                         __syncwarp();
                         tc_after();
                     }
@@ -449,7 +460,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         uint32_t n_stage = 0;
         bool ok = true;
         while (w.left > 0 && ok) {
-            g.set(a, w, s);
+            g = ChSeg::of(a, w, s);
             for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k) {
                 ok = *gave_up == 0;
                 const int j0 = g.sp.tile(k) * PT_KEYS;
@@ -465,7 +476,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 for (int kv = 0; kv < 2; ++kv, ++n_stage) {
                     const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE;
                     if (n_stage >= CH_STAGES)
-                        bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
+                        bar_wait_far(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
                     __syncwarp();
                     if (FMT == PF_16) {
                         if (kv == 1 && !clean) {
@@ -485,7 +496,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
                         constexpr int LPR = pg_row_bytes<FMT, D>() >= 16 ? pg_row_bytes<FMT, D>() / 16 : 1, RPP = 32 / LPR;
                         const uint32_t rs = n_stage % N_RAW, raw0 = base + SM::RAWS + rs * SM::RAW;
-                        bar_wait(smem_u32(&bars.raw_full[rs]), (n_stage / N_RAW) & 1, gave_up);
+                        bar_wait_far(smem_u32(&bars.raw_full[rs]), (n_stage / N_RAW) & 1, gave_up);
                         __syncwarp();
                         const int c = lane % LPR;
                         constexpr int BATCH = LPR < 4 ? LPR : 4;             // rows in flight
@@ -532,7 +543,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 }
             }
             w.left -= g.k1 - g.k0;
-            if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
+            if (w.left > 0) pt_next_far<CH_ROWS>(w, s, a);
         }
     } else {
         if (wid == 12) {
@@ -542,7 +553,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             bool ok = true;
             const uint32_t q_lo = desc_lo(base + SM::Q, 16), k_lo = desc_lo(base + SM::KV, 16), v_lo = desc_lo(base + SM::KV, 16384);
             auto wait = [&](uint64_t& bar, uint32_t parity) {
-                bar_wait(smem_u32(&bar), parity, gave_up);
+                bar_wait_far(smem_u32(&bar), parity, gave_up);
                 __syncwarp();
             };
             auto scores = [&](int h, uint32_t st) {
@@ -567,7 +578,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 __syncwarp();
             };
             while (w.left > 0 && ok) {
-                g.set(a, w, s);
+                g = ChSeg::of(a, w, s);
                 const int halves = g.rows > 128 ? 2 : 1;
                 for (int h = 0; h < halves && g.tiles > 0; ++h) wait(bars.q_ready[h], n_q[h]++ & 1);
                 for (int t = 0; t <= g.tiles && ok && g.tiles > 0; ++t) {
@@ -600,7 +611,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     n_stage += (t > 0) + (t < g.tiles);
                 }
                 w.left -= g.k1 - g.k0;
-                if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
+                if (w.left > 0) pt_next_far<CH_ROWS>(w, s, a);
             }
         }
         if (wid == 13) {
@@ -610,7 +621,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             const int per_page = 1 << a.pc.page_shift, n_pages = PT_KEYS >> a.pc.page_shift;
             if (FMT == PF_16 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
             while (w.left > 0 && ok) {
-                g.set(a, w, s);
+                g = ChSeg::of(a, w, s);
                 int pid16 = g.tiles > 0 ? g.page_of(a, w, g.t0, lane) : -2;
                 for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k, ++n_tile) {
                     ok = *gave_up == 0;
@@ -628,7 +639,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         if (FMT == PF_16) {
                             const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE, bar = smem_u32(&bars.kv_full[stage]);
                             if (n_stage >= CH_STAGES)
-                                bar_wait(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
+                                bar_wait_far(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
                             __syncwarp();
                             const bool copy = kv == 0 || clean;          // group 2 stores the others
                             if (lane == 0) {
@@ -645,7 +656,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                             constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
                             const uint32_t rs = n_stage % N_RAW, dst = base + SM::RAWS + rs * SM::RAW, bar = smem_u32(&bars.raw_full[rs]);
                             if (n_stage >= N_RAW)
-                                bar_wait(smem_u32(&bars.raw_empty[rs]), (n_stage / N_RAW - 1) & 1, gave_up);
+                                bar_wait_far(smem_u32(&bars.raw_empty[rs]), (n_stage / N_RAW - 1) & 1, gave_up);
                             __syncwarp();
                             constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
                             if (lane == 0) {
@@ -662,7 +673,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     pid16 = pid16n;
                 }
                 w.left -= g.k1 - g.k0;
-                if (w.left > 0) pt_next<CH_ROWS>(w, s, a);
+                if (w.left > 0) pt_next_far<CH_ROWS>(w, s, a);
             }
             // copies in flight end before the block does: their stages have been waited for by those who used them; after
             // an early leave, wait here

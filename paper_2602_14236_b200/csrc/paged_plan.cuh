@@ -74,6 +74,11 @@ struct PtWalk {
     long long left;                          // tiles still to do
     int b, h, rt, k;                         // the next one: item and tile within it
 };
+// ... and the sequence it is in.
+struct PtPlace {
+    PtWalk w;
+    PgSeq s;
+};
 
 // A block's share of one item, which every role of a block works out for itself.  An item counts ITEM units before its
 // tiles' for its fixed cost, so that a stretch of many short items is not longer than one long item's.
@@ -82,6 +87,11 @@ struct PtSeg {
     PtSpan sp;
     int k0, k1, t0, tiles, rows;             // units [k0, k1), first tile, tiles with keys, rows in the item
     bool last, real;                         // the item's end is in here; some of its tiles are (an item without keys has one)
+    static __device__ __noinline__ PtSeg of(const PtArgs& a, PtWalk w, PgSeq s) {
+        PtSeg g;
+        g.set(a, w, s);
+        return g;
+    }
     __device__ __forceinline__ void set(const PtArgs& a, const PtWalk& w, const PgSeq& s) {
         sp = pt_item<RT>(s, a, w.rt);
         const int units = ITEM + max(sp.n, 1);
@@ -111,11 +121,12 @@ struct PtSeg {
 // Tiles (and fixed costs) of one head of the sequence that each lane of a warp has; a lane sums a few row tiles by itself,
 // the warp sums them together where there are many.
 template <int RT, int ITEM>
-__device__ __forceinline__ long long pt_per_head(const PtArgs& a, const PgSeq& s) {
+__device__ __forceinline__ long long pt_per_head(const PtArgs& a, PgSeq s) {
     constexpr int ALONE = 2;
     const int lane = threadIdx.x & 31, R = pt_row_tiles<RT>(s, a.G);
     long long w = 0;
     if (R <= ALONE)
+#pragma unroll 1
         for (int rt = 0; rt < R; ++rt) w += ITEM + max(1, pt_item<RT>(s, a, rt).n);
     for (uint32_t many = __ballot_sync(0xffffffffu, R > ALONE); many; many &= many - 1) {
         const int from = __ffs(many) - 1;
@@ -125,6 +136,7 @@ __device__ __forceinline__ long long pt_per_head(const PtArgs& a, const PgSeq& s
         o.len = __shfl_sync(0xffffffffu, s.len, from);
         const int Ro = pt_row_tiles<RT>(o, a.G);
         long long x = 0;
+#pragma unroll 1
         for (int rt = lane; rt < Ro; rt += 32) x += ITEM + max(1, pt_item<RT>(o, a, rt).n);
 #pragma unroll
         for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
@@ -159,7 +171,7 @@ __device__ __forceinline__ void pt_share(long long total, int block, int blocks,
 }
 // `at` units into sequence `s` (w units): head, row tile and unit within it.  Called by whole warps.
 template <int RT, int ITEM>
-__device__ __forceinline__ void pt_find(const PtArgs& a, const PgSeq& s, long long w, long long at, PtWalk& walk) {
+__device__ __forceinline__ PtWalk pt_find(const PtArgs& a, PgSeq s, long long w, long long at, PtWalk walk) {
     const int lane = threadIdx.x & 31, R = pt_row_tiles<RT>(s, a.G);
     long long rem;
     if (w >> 32) {
@@ -171,6 +183,7 @@ __device__ __forceinline__ void pt_find(const PtArgs& a, const PgSeq& s, long lo
         walk.h = (int)((uint32_t)at / ph);
         rem = (uint32_t)at - walk.h * ph;
     }
+#pragma unroll 1
     for (int r0 = 0;; r0 += 32) {
         const int n = r0 + lane < R ? ITEM + max(1, pt_item<RT>(s, a, r0 + lane).n) : 0;
         const long long incl = pt_scan(n);
@@ -179,7 +192,7 @@ __device__ __forceinline__ void pt_find(const PtArgs& a, const PgSeq& s, long lo
             const int from = hit ? __ffs(hit) - 1 : 0;
             walk.rt = r0 + from;
             walk.k = __shfl_sync(0xffffffffu, (int)(rem - (incl - n)), from);
-            return;
+            return walk;
         }
         rem -= __shfl_sync(0xffffffffu, incl, 31);
     }
@@ -195,24 +208,25 @@ struct PtShared {
     PgSeq s;
 };
 template <int RT, int THREADS, int ITEM>
-__device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int blocks, PtShared& sh, PgSeq& seq) {
+__device__ __forceinline__ PtPlace pt_start(const PtArgs& a, int block, int blocks, PtShared& sh) {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    PtWalk walk{};
-    seq = PgSeq{};
+    PtPlace place{};
+    PtWalk& walk = place.w;
+    PgSeq& seq = place.s;
     long long beg, end;
     if (a.sq.n_seqs <= 32) {
         PgSeq s{};
         if (lane < a.sq.n_seqs) s = pg_seq(a.sq, a.pc, lane);
         const long long w = pt_per_head<RT, ITEM>(a, s) * a.pc.heads, incl = pt_scan(w);
         pt_share(__shfl_sync(0xffffffffu, incl, 31), block, blocks, beg, end);
-        if (beg == end) return walk;
+        if (beg == end) return place;
         const uint32_t hit = __ballot_sync(0xffffffffu, beg >= incl - w && beg < incl);
         const int from = __ffs(hit) - 1;
         seq = pt_seq_of(s, from);
         walk.b = from;
         walk.left = end - beg;
-        pt_find<RT, ITEM>(a, seq, __shfl_sync(0xffffffffu, w, from), __shfl_sync(0xffffffffu, beg - (incl - w), from), walk);
-        return walk;
+        walk = pt_find<RT, ITEM>(a, seq, __shfl_sync(0xffffffffu, w, from), __shfl_sync(0xffffffffu, beg - (incl - w), from), walk);
+        return place;
     }
     auto units = [&](int b, PgSeq& s) -> long long {
         s = PgSeq{};
@@ -232,7 +246,7 @@ __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int block
     for (int i = 0; i < THREADS / 32; ++i) total += sh.wsum[i];
     __syncthreads();
     pt_share(total, block, blocks, beg, end);
-    if (beg == end) return walk;
+    if (beg == end) return place;
     long long before = 0;                    // units of the sequences before this round's
     for (int b0 = 0; b0 < a.sq.n_seqs; b0 += THREADS) {
         const int b = b0 + threadIdx.x;
@@ -257,8 +271,8 @@ __device__ __forceinline__ PtWalk pt_start(const PtArgs& a, int block, int block
     seq = sh.s;
     walk.b = sh.b;
     walk.left = end - beg;
-    pt_find<RT, ITEM>(a, seq, sh.w, sh.at, walk);
-    return walk;
+    walk = pt_find<RT, ITEM>(a, seq, sh.w, sh.at, walk);
+    return place;
 }
 
 // On to the next item: row tiles, then heads, then sequences with rows.
@@ -269,11 +283,25 @@ __device__ __forceinline__ void pt_next(PtWalk& w, PgSeq& s, const PtArgs& a) {
     w.rt = 0;
     if (++w.h < a.pc.heads) return;
     w.h = 0;
+#pragma unroll 1
     do {
         ++w.b;
         if (w.b >= a.sq.n_seqs) return;      // cannot happen while tiles are left
         s = pg_seq(a.sq, a.pc, w.b);
     } while (s.n == 0);
+}
+// The same in a function, for a kernel of many roles: with a copy of all this at each call it had grown past the
+// instruction cache (170 KB).
+template <int RT>
+__device__ __noinline__ PtPlace pt_after(const PtArgs& a, PtPlace p) {
+    pt_next<RT>(p.w, p.s, a);
+    return p;
+}
+template <int RT>
+__device__ __forceinline__ void pt_next_far(PtWalk& w, PgSeq& s, const PtArgs& a) {
+    const PtPlace p = pt_after<RT>(a, PtPlace{w, s});
+    w = p.w;
+    s = p.s;
 }
 
 // The record slots of the item that block c left as its tail: its tail, then later blocks' heads until one ends.  All
