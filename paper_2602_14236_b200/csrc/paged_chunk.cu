@@ -617,12 +617,14 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         if (wid == 13) {
             // ---------------- feeder: lane i < 128 / page copies page i of a tile
             uint32_t n_stage = 0, n_tile = 0;
+            int first_rows = 0;
             bool ok = true;
             const int per_page = 1 << a.pc.page_shift, n_pages = PT_KEYS >> a.pc.page_shift;
             if (FMT == PF_16 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
             while (w.left > 0 && ok) {
                 g = ChSeg::of(a, w, s);
                 int pid16 = g.tiles > 0 ? g.page_of(a, w, g.t0, lane) : -2;
+                if (n_tile == 0) first_rows = g.rows;
                 for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k, ++n_tile) {
                     ok = *gave_up == 0;
                     const int pid16n = k + 1 < g.t0 + g.tiles ? g.page_of(a, w, k + 1, lane) : -2;
@@ -634,6 +636,12 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     const int from = mine ? (lane << (a.pc.page_shift - 4)) + __ffs(mine) - 1 : 0;
                     const int pid = __shfl_sync(0xffffffffu, pid16, from);
                     const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine != 0));
+                    // the first item's Q goes before all but one tile: 64 KB behind 128 KB per SM came 5 us late
+                    if (n_tile == 1) {
+                        bar_wait_far(smem_u32(&bars.q_ready[0]), 0, gave_up);
+                        if (first_rows > 128) bar_wait_far(smem_u32(&bars.q_ready[1]), 0, gave_up);
+                        __syncwarp();
+                    }
                     for (int kv = 0; kv < 2; ++kv, ++n_stage) {
                         const size_t slot = pg_slot(a.pc, mine ? pid : 0, kv, w.h, 0);
                         if (FMT == PF_16) {
@@ -704,68 +712,90 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     }
 }
 
-// Joins split items: a thread per row, grid.y over CH_JOIN dimensions each.
+// Joins split items: a thread per row, CH_JOIN dimensions at a time.  The blocks, one wave of them, share out the
+// (item, dimensions) pairs; a block per pair that might be would mostly find nothing to do, in several waves.
 constexpr int CH_JOIN = 8;
 template <typename T, int D>
-__global__ void __launch_bounds__(CH_ROWS)
+__global__ void __launch_bounds__(CH_ROWS, 4)
 k_paged_join_chunk(PtArgs a, int blocks) {
-    __shared__ int list[PT_MAX_BLOCKS + 1];
+    constexpr int N = CH_JOIN / 4, PARTS = D / CH_JOIN;
+    __shared__ int list[PT_MAX_BLOCKS + 1], tails[PT_MAX_BLOCKS], kind[PT_MAX_BLOCKS], in_warp[CH_ROWS / 32];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     grid_wait();
-    constexpr int N = CH_JOIN / 4;
-    const int4 hd = a.head[blockIdx.x];
-    if (hd.y == 0) return;
-    const int row = threadIdx.x, b = hd.z, h = hd.y - 1, rt = hd.w;
-    const PgSeq s = pg_seq(a.sq, a.pc, b);
-    const int n = pt_records(a, blockIdx.x, blocks, list);
-    const int rr = rt * CH_ROWS + row;
-    if (rr >= s.n * a.G) return;
-    // the maximum moves along with the records: one pass over them, eight under way at a time
-    constexpr int AHEAD = 8;
-    float M = PT_NONE, l = 0.0f;
-    float4 o[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i0 = 0; i0 < n; i0 += AHEAD) {
-        float2 st[AHEAD];
-        float4 v[AHEAD][N];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const size_t t = (size_t)list[min(i0 + u, n - 1)];
-            const float4* src = reinterpret_cast<const float4*>(a.part) + (t * (D / 4) + blockIdx.y * N) * CH_ROWS + row;
-            st[u] = a.stat[t * CH_ROWS + row];
-#pragma unroll
-            for (int x = 0; x < N; ++x) v[u][x] = __ldcs(src + x * CH_ROWS);
+    int n_tails = 0;                         // the blocks that left a tail, in their order
+    for (int c0 = 0; c0 < blocks; c0 += CH_ROWS) {
+        const int c = c0 + threadIdx.x;
+        const int4 hd = c < blocks ? a.head[c] : make_int4(0, 0, 0, 0);
+        const uint32_t has = __ballot_sync(0xffffffffu, hd.y != 0);
+        if (c < blocks) kind[c] = hd.x;
+        if (lane == 0) in_warp[wid] = __popc(has);
+        __syncthreads();
+        int at = n_tails + __popc(has & ((1u << lane) - 1u));
+        for (int i = 0; i < CH_ROWS / 32; ++i) {
+            if (i < wid) at += in_warp[i];
+            n_tails += in_warp[i];
         }
-        float nm = M;
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) nm = fmaxf(nm, st[u].x);
-        const float f = ex2(M - nm);
-        M = nm;
-        l *= f;
-#pragma unroll
-        for (int x = 0; x < N; ++x) o[x] = make_float4(o[x].x * f, o[x].y * f, o[x].z * f, o[x].w * f);
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const float e = i0 + u < n ? ex2(st[u].x - M) : 0.0f;
-            l += e * st[u].y;
-#pragma unroll
-            for (int x = 0; x < N; ++x) {
-                o[x].x += e * v[u][x].x;
-                o[x].y += e * v[u][x].y;
-                o[x].z += e * v[u][x].z;
-                o[x].w += e * v[u][x].w;
-            }
-        }
+        if (hd.y != 0) tails[at] = c;
+        __syncthreads();
     }
-    const int hq = h * a.G + rr % a.G;
-    const long long tok = s.row0 + rr / a.G;
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    uint4* dst = reinterpret_cast<uint4*>(a.out + tok * a.out_stride + (long long)hq * D + blockIdx.y * CH_JOIN);
+    for (int unit = blockIdx.x; unit < n_tails * PARTS; unit += gridDim.x) {
+        const int blk = tails[unit / PARTS], part = unit % PARTS;
+        const int4 hd = a.head[blk];
+        const int row = threadIdx.x, b = hd.z, h = hd.y - 1, rt = hd.w;
+        const PgSeq s = pg_seq(a.sq, a.pc, b);
+        const int n = pt_records([&](int c) { return kind[c]; }, blk, blocks, list);
+        const int rr = rt * CH_ROWS + row;
+        if (rr < s.n * a.G) {
+            // the maximum moves along with the records: one pass over them, eight under way at a time
+            constexpr int AHEAD = 8;
+            float M = PT_NONE, l = 0.0f;
+            float4 o[N];
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i)
-        dst[i] = make_uint4(T::pack(o[2 * i].x * inv, o[2 * i].y * inv), T::pack(o[2 * i].z * inv, o[2 * i].w * inv),
-                            T::pack(o[2 * i + 1].x * inv, o[2 * i + 1].y * inv), T::pack(o[2 * i + 1].z * inv, o[2 * i + 1].w * inv));
-    if (a.lse && blockIdx.y == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (M + log2f(l)) * PT_LN2 : -INFINITY;
+            for (int i = 0; i < N; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int i0 = 0; i0 < n; i0 += AHEAD) {
+                float2 st[AHEAD];
+                float4 v[AHEAD][N];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const size_t t = (size_t)list[min(i0 + u, n - 1)];
+                    const float4* src = reinterpret_cast<const float4*>(a.part) + (t * (D / 4) + part * N) * CH_ROWS + row;
+                    st[u] = a.stat[t * CH_ROWS + row];
+#pragma unroll
+                    for (int x = 0; x < N; ++x) v[u][x] = __ldcs(src + x * CH_ROWS);
+                }
+                float nm = M;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) nm = fmaxf(nm, st[u].x);
+                const float f = ex2(M - nm);
+                M = nm;
+                l *= f;
+#pragma unroll
+                for (int x = 0; x < N; ++x) o[x] = make_float4(o[x].x * f, o[x].y * f, o[x].z * f, o[x].w * f);
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const float e = i0 + u < n ? ex2(st[u].x - M) : 0.0f;
+                    l += e * st[u].y;
+#pragma unroll
+                    for (int x = 0; x < N; ++x) {
+                        o[x].x += e * v[u][x].x;
+                        o[x].y += e * v[u][x].y;
+                        o[x].z += e * v[u][x].z;
+                        o[x].w += e * v[u][x].w;
+                    }
+                }
+            }
+            const int hq = h * a.G + rr % a.G;
+            const long long tok = s.row0 + rr / a.G;
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            uint4* dst = reinterpret_cast<uint4*>(a.out + tok * a.out_stride + (long long)hq * D + part * CH_JOIN);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i)
+                dst[i] = make_uint4(T::pack(o[2 * i].x * inv, o[2 * i].y * inv), T::pack(o[2 * i].z * inv, o[2 * i].w * inv),
+                                    T::pack(o[2 * i + 1].x * inv, o[2 * i + 1].y * inv), T::pack(o[2 * i + 1].z * inv, o[2 * i + 1].w * inv));
+            if (a.lse && part == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (M + log2f(l)) * PT_LN2 : -INFINITY;
+        }
+        __syncthreads();                     // the list is used up
+    }
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -803,7 +833,7 @@ int launch_chunk(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * CH_ROWS * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * CH_ROWS);
     SC_CHECK(pt_launch(k_paged_chunk<T, FMT, D>, dim3(blocks), CH_THREADS, BYTES, st, a, map, blocks));
-    SC_CHECK(pt_launch(k_paged_join_chunk<T, D>, dim3(blocks, D / CH_JOIN), CH_ROWS, 0, st, a, blocks));
+    SC_CHECK(pt_launch(k_paged_join_chunk<T, D>, dim3(4 * blocks), CH_ROWS, 0, st, a, blocks));
     c->launches += 2;
     return SALICACHE_OK;
 }

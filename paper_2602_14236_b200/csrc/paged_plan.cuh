@@ -305,15 +305,16 @@ __device__ __forceinline__ void pt_next_far(PtWalk& w, PgSeq& s, const PtArgs& a
 }
 
 // The record slots of the item that block c left as its tail: its tail, then later blocks' heads until one ends.  All
-// threads of the block get the count.
-__device__ __forceinline__ int pt_records(const PtArgs& a, int c, int blocks, int* list) {
+// threads of the block get the count.  flag(c): the kind of block c's head record.
+template <typename F>
+__device__ __forceinline__ int pt_records(F flag, int c, int blocks, int* list) {
     __shared__ int count;
     if (threadIdx.x < 32) {
         const int lane = threadIdx.x;
         int n = 1;
         if (lane == 0) list[0] = 2 * c + 1;
         for (int c0 = c + 1; c0 < blocks; c0 += 32) {
-            const int f = c0 + lane < blocks ? a.head[c0 + lane].x : 0;
+            const int f = c0 + lane < blocks ? flag(c0 + lane) : 0;
             const uint32_t ends = __ballot_sync(0xffffffffu, f == 2);
             const uint32_t upto = ends ? (2u << (__ffs(ends) - 1)) - 1u : 0xffffffffu;       // lanes up to the first that ends
             const uint32_t has = __ballot_sync(0xffffffffu, f != 0) & upto;
@@ -337,7 +338,7 @@ k_paged_join(PtArgs a, int blocks) {
     constexpr int N = D / 32;
     const int4 hd = a.head[blockIdx.x];
     if (hd.y == 0) return;
-    const int n = pt_records(a, blockIdx.x, blocks, list);
+    const int n = pt_records([&](int c) { return a.head[c].x; }, blockIdx.x, blocks, list);
     const int lane = threadIdx.x & 31, row = blockIdx.y * 8 + (threadIdx.x >> 5);
     const int b = hd.z, h = hd.y - 1, rt = hd.w;
     const PgSeq s = pg_seq(a.sq, a.pc, b);
