@@ -180,7 +180,7 @@ k_paged_step(PtArgs a, int blocks) {
     __shared__ float2 sh_stat[ST_WARPS][ST_ROUND];
     __shared__ PtShared sh_plan;
     __shared__ int sh_gave_up;
-    using Seg = PtSeg<RT, SM::ITEM>;
+    using Seg = PtSeg<SM::ITEM>;
     const uint32_t q_ring = smem_u32(ring) + STAGES * SM::STAGE + SM::ACC;
     float (*sh_acc)[ST_ROUND][D + 4] = reinterpret_cast<float (*)[ST_ROUND][D + 4]>(ring + STAGES * SM::STAGE);
     volatile int* gave_up = &sh_gave_up;
@@ -200,7 +200,7 @@ k_paged_step(PtArgs a, int blocks) {
     }
     grid_wait();
     grid_release();
-    const PtPlace start = pt_start<RT, ST_THREADS, SM::ITEM>(a, c, blocks, sh_plan);
+    const PtPlace start = pt_start<ST_THREADS, SM::ITEM>(a, c, blocks, sh_plan);
     PtWalk w = start.w;
     PgSeq s = start.s;
     __syncthreads();
@@ -257,7 +257,7 @@ k_paged_step(PtArgs a, int blocks) {
                 }
             }
             w.left -= g.k1 - g.k0;
-            if (w.left > 0) pt_next<RT>(w, s, a);
+            if (w.left > 0) pt_next(w, s, a);
         }
         if (!ok) {                           // given up: copies in flight end before the block does
             for (uint32_t i = n_stage > STAGES ? n_stage - STAGES : 0; i < n_stage; ++i)
@@ -471,7 +471,7 @@ k_paged_step(PtArgs a, int blocks) {
             } else hd.x = g.last ? 2 : 1;
         }
         w.left -= g.k1 - g.k0;
-        if (w.left > 0) pt_next<RT>(w, s, a);
+        if (w.left > 0) pt_next(w, s, a);
     }
     if (threadIdx.x == 0) {
         a.head[c] = hd;
@@ -487,6 +487,7 @@ int launch_step(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     // no more blocks than there can be tiles of work: rows of q times heads times the table's tiles
     const long long most = (long long)a.sq.n_rows * a.pc.heads * ((((long long)a.sq.width << a.pc.page_shift) + PT_KEYS - 1) / PT_KEYS);
     const int blocks = (int)max(1ll, min(min(most, (long long)PT_MAX_BLOCKS), (long long)c->sm_count * SM::BLOCKS));
+    a.tile_rows = RT;
     a.part = reinterpret_cast<float*>(work);
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * RT * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * RT);

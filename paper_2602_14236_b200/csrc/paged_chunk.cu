@@ -5,12 +5,14 @@
 // halves of 128 = the lanes of tensor memory; scores S = Q K^T and sums O += P V of both halves stand in all 512 columns.
 // Roles by warp group:
 //   0, 1   one thread per row of half 0 / 1: maximum over the row's 128 scores, weights, row sum; P overwrites S as the
-//          16-bit operand of the second product, handed on in two parts; also the output, and the next item's Q, which
-//          is under way while the present item ends
+//          16-bit operand of the second product, handed on in two parts; also the output
 //   2      codes from a ring of raw stages to 16-bit operands; of 16-bit pages only the V tiles that hold positions no
-//          row sees, which are stored as zeros whatever the page holds there
+//          row sees, which become zeros whatever the page holds there
 //   3      one thread issues the matrix instructions; one warp feeds the rings with bulk copies, a lane per page: tensor
-//          copies straight into the operand stages (16-bit pages), plain ones of codes and scales into the raw stages
+//          copies straight into the operand stages (16-bit pages), plain ones of codes and scales into the raw stages; and
+//          Q, of the next item as soon as the last scores of the present one are done
+// A half holds the query heads of 128 / G whole tokens, so that Q is one box of (64 dimensions, G heads, tokens) per copy.
+// (Asynchronous 16-byte copies by the threads instead took 4.8 us for an item's 64 KB.)
 // While one half's weights are formed, the tensor core works for the other: the products of a half are issued as
 // P(t) V(t), then Q K(t+1).  Instructions of one thread run in order there, so S may be overwritten right behind the
 // product that read P from the same columns, and whoever sees the scores of tile t knows the sums of tile t-1 complete.
@@ -39,6 +41,11 @@ __device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tensor_copy3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+                 "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -133,10 +140,6 @@ __device__ __forceinline__ uint32_t swz(int r, int c) { return (uint32_t)((c >> 
 __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-// 16 bytes into shared memory behind the thread's back, or zeros.
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool get) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(get ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 constexpr int CH_RAW = 4;                    // raw stages at most
@@ -161,7 +164,8 @@ __device__ __forceinline__ uint64_t add2f(uint64_t a, uint64_t b) {
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
 struct ChBars {
-    uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_ready[2], s_full[2], p_ready[2][2], o_done[2];
+    uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_land[2], q_ready[2], q_empty[2], v_land[2], s_full[2], p_ready[2][2],
+        o_done[2];
     uint32_t tmem;
     int gave_up;
     uint32_t pages[8];                       // per tile (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
@@ -179,36 +183,18 @@ struct ChSmem {
 
 // An item's fixed cost (Q, output) in tiles' time, as measured.
 constexpr int CH_ITEM = 3;
-using ChSeg = PtSeg<CH_ROWS, CH_ITEM>;
+using ChSeg = PtSeg<CH_ITEM>;
 
-// Q of a half's rows x0 .. of an item: a row by D / 8 lanes, asynchronously; each thread works out its own row's address.
+// INT4: a half's Q, which a copy has brought, into the order in which codes leave their words; a thread per row.
 template <int D>
-__device__ __noinline__ void fetch_rows(const PtArgs& a, uint32_t q_tile, int x0, int rows, int head, int row0) {
-    const int row = threadIdx.x & 127, lane = row & 31, r0 = row & ~31;
-    const int x = x0 + min(row, rows - 1);
-    const long long at = (long long)(row0 + x / a.G) * a.q_stride + (long long)(head * a.G + x % a.G) * D;
-    constexpr int LPR = D / 8, RPP = 32 / LPR;
-#pragma unroll 4
-    for (int p = 0; p < 32 / RPP; ++p) {
-        const int lr = p * RPP + lane / LPR, c = lane % LPR;
-        const long long src = __shfl_sync(0xffffffffu, at, lr);
-        cp16(q_tile + swz(r0 + lr, c), a.q + src + c * 8, r0 + lr < rows);
-    }
-}
-// ... and when they have arrived
-template <int FMT, int D>
-__device__ __noinline__ void hand_rows(uint32_t q_tile, uint32_t q_ready) {
+__device__ __noinline__ void permute_rows(uint32_t q_tile, uint32_t q_ready) {
     const int row = threadIdx.x & 127;
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncwarp();
-    if (FMT == PF_I4) {                          // the order in which codes leave their words
-#pragma unroll 2
-        for (int c = 0; c < D / 8; ++c) {
-            uint32_t v[4];
-            lds16(v, q_tile + swz(row, c));
-            sts16(q_tile + swz(row, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632), __byte_perm(v[1], v[3], 0x5410),
-                  __byte_perm(v[1], v[3], 0x7632));
-        }
+#pragma unroll 4
+    for (int c = 0; c < D / 8; ++c) {
+        uint32_t v[4];
+        lds16(v, q_tile + swz(row, c));
+        sts16(q_tile + swz(row, c), __byte_perm(v[0], v[2], 0x5410), __byte_perm(v[0], v[2], 0x7632), __byte_perm(v[1], v[3], 0x5410),
+              __byte_perm(v[1], v[3], 0x7632));
     }
     fence_async();
     __syncwarp();
@@ -217,7 +203,7 @@ __device__ __noinline__ void hand_rows(uint32_t q_tile, uint32_t q_ready) {
 
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(CH_THREADS, 1)
-k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
+k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map, int blocks) {
     using SM = ChSmem<FMT, D>;
     extern __shared__ uint8_t raw[];
     __shared__ PtShared plan;
@@ -236,7 +222,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             bar_init(smem_u32(&bars.raw_empty[i]), 4);
         }
         for (int i = 0; i < 2; ++i) {
+            bar_init(smem_u32(&bars.q_land[i]), 1);
             bar_init(smem_u32(&bars.q_ready[i]), 4);      // a lane of each of the half's warps
+            bar_init(smem_u32(&bars.q_empty[i]), 1);
+            bar_init(smem_u32(&bars.v_land[i]), 1);
             bar_init(smem_u32(&bars.s_full[i]), 1);
             bar_init(smem_u32(&bars.p_ready[i][0]), 4);
             bar_init(smem_u32(&bars.p_ready[i][1]), 4);
@@ -252,13 +241,14 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
     grid_wait();
     grid_release();
     tc_before();
-    const PtPlace start = pt_start<CH_ROWS, CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks, plan);
+    const PtPlace start = pt_start<CH_THREADS, CH_ITEM>(a, blockIdx.x, blocks, plan);
     PtWalk w = start.w;
     PgSeq s = start.s;
     __syncthreads();
     tc_after();
     const uint32_t tmem = bars.tmem;
     ChSeg g;
+    const int HR = a.tile_rows >> 1;         // rows of a half
 
     if (wid < 8) {
         // ---------------- rows: softmax, Q, output
@@ -271,39 +261,38 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
         uint32_t n_s = 0, n_o = 0, n_tile = 0;               // scores, outputs of this half and tiles seen so far
         int4 hd = make_int4(0, 0, 0, 0);
         bool ok = true;
-        auto fetch_q = [&](const ChSeg& gg, const PtWalk& ww, const PgSeq& ss) {
-            const int rows = min(128, gg.rows - half * 128);
-            if (rows > 0 && gg.tiles > 0) fetch_rows<D>(a, q_tile, ww.rt * CH_ROWS + half * 128, rows, ww.h, ss.row0);
-        };
+        uint32_t n_q = 0;
         auto hand_q = [&](const ChSeg& gg) {
-            if (gg.rows > half * 128 && gg.tiles > 0) hand_rows<FMT, D>(q_tile, q_ready);
+            if (FMT != PF_I4 || gg.rows <= half * HR || gg.tiles == 0) return;
+            bar_wait_far(smem_u32(&bars.q_land[half]), n_q++ & 1, gave_up);
+            __syncwarp();
+            permute_rows<D>(q_tile, q_ready);
         };
         if (w.left > 0) {
             g = ChSeg::of(a, w, s);
-            fetch_q(g, w, s);
             hand_q(g);
         }
         while (w.left > 0 && ok) {
             const bool first = g.t0 == 0, lastp = g.last, done = first && lastp;
-            const int rows = min(128, g.rows - half * 128);  // of this half
+            const int rows = min(HR, g.rows - half * HR);    // of this half
             if (tid == 0 && s.cut && s.pos0 + s.n > s.len) atomicMin(a.status, SALICACHE_E_CAPACITY);
             // the item after this one
             PtWalk wn = w;
             PgSeq sn = s;
             wn.left -= g.k1 - g.k0;
-            if (wn.left > 0) pt_next_far<CH_ROWS>(wn, sn, a);
+            if (wn.left > 0) pt_next_far(wn, sn, a);
             ChSeg gn;
             gn.rows = gn.tiles = 0;
             if (wn.left > 0) gn = ChSeg::of(a, wn, sn);
             bool handed = false;
             if (rows > 0) {
-                const int rr = w.rt * CH_ROWS + half * 128 + row;                 // this thread's row of the item
+                const int rr = w.rt * a.tile_rows + half * HR + row;                 // this thread's row of the item
                 const bool live = row < rows;
                 const int pos = s.pos0 + (live ? rr : 0) / a.G;
                 float m = PT_NONE, l = 0.0f;
                 if (g.tiles > 0) {
                     // positions that every row of this half sees in full tiles need no mask
-                    const PtSpan hs = pt_span(s, a.G, w.rt * CH_ROWS + half * 128, w.rt * CH_ROWS + half * 128 + rows, a.window, a.sinks);
+                    const PtSpan hs = pt_span(s, a.G, w.rt * a.tile_rows + half * HR, w.rt * a.tile_rows + half * HR + rows, a.window, a.sinks);
                     const int vis_hi = live ? max(0, min(pos + 1, s.len)) : 0;
                     const int vis_lo = a.window ? pos - a.window + 1 : 0;
                     for (int k = 0; k < g.tiles && ok; ++k, ++n_tile) {
@@ -341,7 +330,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                             if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
                         }
                         tc_ld32(x[0], S);
-                        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
+                        const float top = live ? fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale : PT_NONE;
                         if (k == 0) m = fmaxf(m, top);
                         else if (__any_sync(0xffffffffu, top > m + 8.0f)) {
                             const float nm = fmaxf(m, top), f = ex2(m - nm);
@@ -387,7 +376,6 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         float s0, s1;
                         unpack2(add2f(sum[0], sum[1]), s0, s1);
                         l += s0 + s1;
-                        if (k == g.tiles - 1) fetch_q(gn, wn, sn);           // the scores are done with this item's Q
                     }
                     if (ok) {
                         hand_q(gn);
@@ -436,10 +424,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     if (live && !done) a.stat[slot * CH_ROWS + half * 128 + row] = make_float2(m, l);
                 }
             } else n_tile += g.tiles;
-            if (!handed) {
-                fetch_q(gn, wn, sn);
-                hand_q(gn);
-            }
+            if (!handed) hand_q(gn);
             if (!done && g.real) {
                 if (first) {
                     hd.y = w.h + 1;
@@ -451,13 +436,12 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             s = sn;
             g = gn;
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
         if (tid == 0) a.head[blockIdx.x] = hd;
     } else if (wid < 12) {
         // ---------------- operands
         const Codes<T> cd;
         const int lw = wid - 8;                              // this warp's rows: 32 lw .. 32 lw + 31 of a tile
-        uint32_t n_stage = 0;
+        uint32_t n_stage = 0, n_land = 0;
         bool ok = true;
         while (w.left > 0 && ok) {
             g = ChSeg::of(a, w, s);
@@ -472,23 +456,23 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     const int j = j0 + lw * 32 + r;
                     return j < g.sp.hi && (j >= g.sp.lo || j < a.sinks) && !(bad >> (lw * 2 + (r >> 4)) & 1u);
                 };
-                const int pg0 = __shfl_sync(0xffffffffu, pid, lw * 2), pg1 = __shfl_sync(0xffffffffu, pid, lw * 2 + 1);
                 for (int kv = 0; kv < 2; ++kv, ++n_stage) {
                     const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE;
                     if (n_stage >= CH_STAGES)
                         bar_wait_far(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
                     __syncwarp();
                     if (FMT == PF_16) {
-                        if (kv == 1 && !clean) {
+                        if (kv == 1 && !clean) {         // the pages have been copied: zeros where no row sees them
+                            bar_wait_far(smem_u32(&bars.v_land[n_land & 1]), n_land >> 1 & 1, gave_up);
+                            ++n_land;
+                            __syncwarp();
                             constexpr int LPR = D / 8, RPP = 32 / LPR;
                             const int c = lane % LPR;
+#pragma unroll 1
                             for (int p = 0; p < 32 / RPP; ++p) {
-                                const int r = p * RPP + lane / LPR, page = r < 16 ? pg0 : pg1;
-                                const bool get = seen(r) && page >= 0;
-                                const size_t slot = pg_slot(a.pc, get ? page : 0, 1, w.h, (j0 + lw * 32 + r) & ((1 << a.pc.page_shift) - 1));
-                                cp16(dst + swz(lw * 32 + r, c), a.pc.data + slot * (2 * D) + c * 16, get);
+                                const int r = p * RPP + lane / LPR;
+                                if (!seen(r)) sts16(dst + swz(lw * 32 + r, c), 0u, 0u, 0u, 0u);
                             }
-                            asm volatile("cp.async.wait_all;" ::: "memory");
                             fence_async();
                             __syncwarp();
                         }
@@ -543,7 +527,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 }
             }
             w.left -= g.k1 - g.k0;
-            if (w.left > 0) pt_next_far<CH_ROWS>(w, s, a);
+            if (w.left > 0) pt_next_far(w, s, a);
         }
     } else {
         if (wid == 12) {
@@ -556,7 +540,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                 bar_wait_far(smem_u32(&bar), parity, gave_up);
                 __syncwarp();
             };
-            auto scores = [&](int h, uint32_t st) {
+            auto scores = [&](int h, uint32_t st, bool last) {
                 const uint32_t qa = q_lo + h * (SM::TILE >> 4), kb = k_lo + st * (SM::TILE >> 4);
                 if (elect_one()) {
 #pragma unroll
@@ -565,6 +549,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         mma_ss(tmem + 128 * h, desc(qa + off), desc(kb + off), ID_S, i > 0);
                     }
                     tc_commit(smem_u32(&bars.s_full[h]));
+                    if (last) tc_commit(smem_u32(&bars.q_empty[h]));
                 }
                 __syncwarp();
             };
@@ -579,8 +564,8 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
             };
             while (w.left > 0 && ok) {
                 g = ChSeg::of(a, w, s);
-                const int halves = g.rows > 128 ? 2 : 1;
-                for (int h = 0; h < halves && g.tiles > 0; ++h) wait(bars.q_ready[h], n_q[h]++ & 1);
+                const int halves = g.rows > HR ? 2 : 1;
+                for (int h = 0; h < halves && g.tiles > 0; ++h) wait(FMT == PF_I4 ? bars.q_ready[h] : bars.q_land[h], n_q[h]++ & 1);
                 for (int t = 0; t <= g.tiles && ok && g.tiles > 0; ++t) {
                     ok = *gave_up == 0;
                     // stages in order: K(0), V(0), K(1), ...: V(t - 1) then K(t)
@@ -600,7 +585,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         }
                         if (t < g.tiles) {
                             tc_after();
-                            scores(h, ks % CH_STAGES);
+                            scores(h, ks % CH_STAGES, t == g.tiles - 1);
                         }
                     }
                     if (elect_one()) {
@@ -611,20 +596,19 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     n_stage += (t > 0) + (t < g.tiles);
                 }
                 w.left -= g.k1 - g.k0;
-                if (w.left > 0) pt_next_far<CH_ROWS>(w, s, a);
+                if (w.left > 0) pt_next_far(w, s, a);
             }
         }
         if (wid == 13) {
             // ---------------- feeder: lane i < 128 / page copies page i of a tile
             uint32_t n_stage = 0, n_tile = 0;
-            int first_rows = 0;
+            uint32_t n_q[2] = {0, 0}, n_land = 0;
             bool ok = true;
             const int per_page = 1 << a.pc.page_shift, n_pages = PT_KEYS >> a.pc.page_shift;
             if (FMT == PF_16 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
             while (w.left > 0 && ok) {
                 g = ChSeg::of(a, w, s);
                 int pid16 = g.tiles > 0 ? g.page_of(a, w, g.t0, lane) : -2;
-                if (n_tile == 0) first_rows = g.rows;
                 for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k, ++n_tile) {
                     ok = *gave_up == 0;
                     const int pid16n = k + 1 < g.t0 + g.tiles ? g.page_of(a, w, k + 1, lane) : -2;
@@ -636,12 +620,6 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     const int from = mine ? (lane << (a.pc.page_shift - 4)) + __ffs(mine) - 1 : 0;
                     const int pid = __shfl_sync(0xffffffffu, pid16, from);
                     const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine != 0));
-                    // the first item's Q goes before all but one tile: 64 KB behind 128 KB per SM came 5 us late
-                    if (n_tile == 1) {
-                        bar_wait_far(smem_u32(&bars.q_ready[0]), 0, gave_up);
-                        if (first_rows > 128) bar_wait_far(smem_u32(&bars.q_ready[1]), 0, gave_up);
-                        __syncwarp();
-                    }
                     for (int kv = 0; kv < 2; ++kv, ++n_stage) {
                         const size_t slot = pg_slot(a.pc, mine ? pid : 0, kv, w.h, 0);
                         if (FMT == PF_16) {
@@ -649,16 +627,20 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                             if (n_stage >= CH_STAGES)
                                 bar_wait_far(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
                             __syncwarp();
-                            const bool copy = kv == 0 || clean;          // group 2 stores the others
+                            // V with keys that no row sees goes through group 2, which waits for it by barriers of their own (two: as
+                            // many V stages as the ring has)
+                            const bool direct = kv == 0 || clean;
+                            const uint32_t land = direct ? bar : smem_u32(&bars.v_land[n_land & 1]);
                             if (lane == 0) {
                                 if (kv == 0) *(volatile uint32_t*)&bars.pages[n_tile & 7] = ~bad & 0xffu;
-                                if (copy) bar_expect(bar, copies * (uint32_t)(per_page * D * 2));
-                                else bar_arrive(bar);
+                                bar_expect(land, copies * (uint32_t)(per_page * D * 2));
+                                if (!direct) bar_arrive(bar);
                             }
+                            n_land += !direct;
                             __syncwarp();
-                            if (copy && mine) {
+                            if (mine) {
 #pragma unroll
-                                for (int x = 0; x < D; x += 64) tensor_copy(dst + x * 256 + lane * per_page * 128, &map, x, (int)slot, bar);
+                                for (int x = 0; x < D; x += 64) tensor_copy(dst + x * 256 + lane * per_page * 128, &map, x, (int)slot, land);
                             }
                         } else {
                             constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
@@ -679,9 +661,24 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                         }
                     }
                     pid16 = pid16n;
+                    if (k == g.t0) {                     // Q behind the first tile: a lane per half
+                        for (int h = 0; h < 2; ++h) {
+                            if (h > 0 && g.rows <= HR) break;
+                            if (n_q[h] > 0) bar_wait_far(smem_u32(&bars.q_empty[h]), (n_q[h] - 1) & 1, gave_up);
+                            __syncwarp();
+                            ++n_q[h];
+                            if (lane == 0) {
+                                const uint32_t bar = smem_u32(&bars.q_land[h]);
+                                bar_expect(bar, (uint32_t)(HR * D * 2));
+                                for (int x = 0; x < D; x += 64)
+                                    tensor_copy3(base + SM::Q + h * SM::TILE + x * 256, &q_map, x, w.h * a.G, s.row0 + (w.rt * 2 + h) * (HR / a.G), bar);
+                            }
+                        }
+                        __syncwarp();
+                    }
                 }
                 w.left -= g.k1 - g.k0;
-                if (w.left > 0) pt_next_far<CH_ROWS>(w, s, a);
+                if (w.left > 0) pt_next_far(w, s, a);
             }
             // copies in flight end before the block does: their stages have been waited for by those who used them; after
             // an early leave, wait here
@@ -691,6 +688,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, int blocks) {
                     const uint32_t bar = FMT == PF_16 ? smem_u32(&bars.kv_full[i % n]) : smem_u32(&bars.raw_full[i % n]);
                     for (int t = 0; t < (1 << 16) && !bar_try(bar, (i / n) & 1); ++t) {}
                 }
+                for (int h = 0; h < 2; ++h)
+                    for (int t = 0; t < (1 << 16) && n_q[h] > 0 && !bar_try(smem_u32(&bars.q_land[h]), (n_q[h] - 1) & 1); ++t) {}
+                for (uint32_t i = n_land > 2 ? n_land - 2 : 0; i < n_land; ++i)
+                    for (int t = 0; t < (1 << 16) && !bar_try(smem_u32(&bars.v_land[i & 1]), i >> 1 & 1); ++t) {}
             }
         }
         __syncwarp();
@@ -744,8 +745,8 @@ k_paged_join_chunk(PtArgs a, int blocks) {
         const int row = threadIdx.x, b = hd.z, h = hd.y - 1, rt = hd.w;
         const PgSeq s = pg_seq(a.sq, a.pc, b);
         const int n = pt_records([&](int c) { return kind[c]; }, blk, blocks, list);
-        const int rr = rt * CH_ROWS + row;
-        if (rr < s.n * a.G) {
+        const int HR = a.tile_rows >> 1, rr = rt * a.tile_rows + (row >> 7) * HR + (row & 127);
+        if ((row & 127) < HR && rr < s.n * a.G) {
             // the maximum moves along with the records: one pass over them, eight under way at a time
             constexpr int AHEAD = 8;
             float M = PT_NONE, l = 0.0f;
@@ -822,17 +823,31 @@ bool page_map(CUtensorMap* map, const PgCache& pc, int D, bool bf16) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The rows of q as (dimension, query head, row); a copy takes 64 dimensions of G heads of 128 / G rows.
+bool rows_map(CUtensorMap* map, const PtArgs& a, int D, bool bf16) {
+    const EncodeTiled fn = tensor_encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.pc.heads * a.G, (cuuint64_t)a.sq.n_rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)(128 / a.G)}, step[3] = {1, 1, 1};
+    return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<uint16_t*>(a.q), dims, strides, box,
+              step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int FMT, int D>
 int launch_chunk(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     constexpr int BYTES = ChSmem<FMT, D>::BYTES;
-    CUtensorMap map{};
+    a.tile_rows = 2 * (128 / a.G) * a.G;
+    CUtensorMap map{}, q_map{};
+    if (!rows_map(&q_map, a, D, T::ONE == TypeBF16::ONE)) return SALICACHE_E_CUDA;
     if (FMT == PF_16 && !page_map(&map, a.pc, D, T::ONE == TypeBF16::ONE)) return SALICACHE_E_CUDA;
     SC_CHECK(cudaFuncSetAttribute(k_paged_chunk<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
     const int blocks = min(c->sm_count, PT_MAX_BLOCKS);
     a.part = reinterpret_cast<float*>(work);
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * CH_ROWS * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * CH_ROWS);
-    SC_CHECK(pt_launch(k_paged_chunk<T, FMT, D>, dim3(blocks), CH_THREADS, BYTES, st, a, map, blocks));
+    SC_CHECK(pt_launch(k_paged_chunk<T, FMT, D>, dim3(blocks), CH_THREADS, BYTES, st, a, map, q_map, blocks));
     SC_CHECK(pt_launch(k_paged_join_chunk<T, D>, dim3(4 * blocks), CH_ROWS, 0, st, a, blocks));
     c->launches += 2;
     return SALICACHE_OK;

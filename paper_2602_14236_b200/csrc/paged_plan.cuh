@@ -26,6 +26,7 @@ struct PtArgs {
     float* lse;
     long long q_stride, out_stride;
     int G, window, sinks;
+    int tile_rows;                           // rows of an item at most
     float scale;                             // softmax scale * log2(e): the kernels work in powers of two
     float* part;                             // [2 * blocks][rows of a tile][D], tail records after head records of a block
     float2* stat;                            // [2 * blocks][rows of a tile]: running maximum (powers of two), denominator
@@ -61,11 +62,9 @@ __device__ __forceinline__ bool pt_sees(int pos, int j, int window, int sinks) {
     return j <= pos && (window == 0 || j > pos - window || j < sinks);
 }
 
-template <int RT>
-__device__ __forceinline__ int pt_row_tiles(const PgSeq& s, int G) { return (int)(((long long)s.n * G + RT - 1) / RT); }
-template <int RT>
+__device__ __forceinline__ int pt_row_tiles(const PgSeq& s, const PtArgs& a) { return (s.n * a.G + a.tile_rows - 1) / a.tile_rows; }
 __device__ __forceinline__ PtSpan pt_item(const PgSeq& s, const PtArgs& a, int rt) {
-    const int r0 = rt * RT, r1 = (int)min((long long)r0 + RT, (long long)s.n * a.G);
+    const int r0 = rt * a.tile_rows, r1 = min(r0 + a.tile_rows, s.n * a.G);
     return pt_span(s, a.G, r0, r1, a.window, a.sinks);
 }
 
@@ -82,7 +81,7 @@ struct PtPlace {
 
 // A block's share of one item, which every role of a block works out for itself.  An item counts ITEM units before its
 // tiles' for its fixed cost, so that a stretch of many short items is not longer than one long item's.
-template <int RT, int ITEM>
+template <int ITEM>
 struct PtSeg {
     PtSpan sp;
     int k0, k1, t0, tiles, rows;             // units [k0, k1), first tile, tiles with keys, rows in the item
@@ -93,11 +92,11 @@ struct PtSeg {
         return g;
     }
     __device__ __forceinline__ void set(const PtArgs& a, const PtWalk& w, const PgSeq& s) {
-        sp = pt_item<RT>(s, a, w.rt);
+        sp = pt_item(s, a, w.rt);
         const int units = ITEM + max(sp.n, 1);
         k0 = w.k;
         k1 = (int)min((long long)units, k0 + w.left);
-        rows = min(RT, s.n * a.G - w.rt * RT);
+        rows = min(a.tile_rows, s.n * a.G - w.rt * a.tile_rows);
         t0 = max(0, k0 - ITEM);
         const int t1 = max(0, k1 - ITEM);
         last = k1 == units;
@@ -120,24 +119,24 @@ struct PtSeg {
 
 // Tiles (and fixed costs) of one head of the sequence that each lane of a warp has; a lane sums a few row tiles by itself,
 // the warp sums them together where there are many.
-template <int RT, int ITEM>
+template <int ITEM>
 __device__ __forceinline__ long long pt_per_head(const PtArgs& a, PgSeq s) {
     constexpr int ALONE = 2;
-    const int lane = threadIdx.x & 31, R = pt_row_tiles<RT>(s, a.G);
+    const int lane = threadIdx.x & 31, R = pt_row_tiles(s, a);
     long long w = 0;
     if (R <= ALONE)
 #pragma unroll 1
-        for (int rt = 0; rt < R; ++rt) w += ITEM + max(1, pt_item<RT>(s, a, rt).n);
+        for (int rt = 0; rt < R; ++rt) w += ITEM + max(1, pt_item(s, a, rt).n);
     for (uint32_t many = __ballot_sync(0xffffffffu, R > ALONE); many; many &= many - 1) {
         const int from = __ffs(many) - 1;
         PgSeq o{};
         o.n = __shfl_sync(0xffffffffu, s.n, from);
         o.pos0 = __shfl_sync(0xffffffffu, s.pos0, from);
         o.len = __shfl_sync(0xffffffffu, s.len, from);
-        const int Ro = pt_row_tiles<RT>(o, a.G);
+        const int Ro = pt_row_tiles(o, a);
         long long x = 0;
 #pragma unroll 1
-        for (int rt = lane; rt < Ro; rt += 32) x += ITEM + max(1, pt_item<RT>(o, a, rt).n);
+        for (int rt = lane; rt < Ro; rt += 32) x += ITEM + max(1, pt_item(o, a, rt).n);
 #pragma unroll
         for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
         if (lane == from) w = x;
@@ -170,9 +169,9 @@ __device__ __forceinline__ void pt_share(long long total, int block, int blocks,
     end = each * (block + 1) + over * (uint32_t)(block + 1) / (uint32_t)blocks;
 }
 // `at` units into sequence `s` (w units): head, row tile and unit within it.  Called by whole warps.
-template <int RT, int ITEM>
+template <int ITEM>
 __device__ __forceinline__ PtWalk pt_find(const PtArgs& a, PgSeq s, long long w, long long at, PtWalk walk) {
-    const int lane = threadIdx.x & 31, R = pt_row_tiles<RT>(s, a.G);
+    const int lane = threadIdx.x & 31, R = pt_row_tiles(s, a);
     long long rem;
     if (w >> 32) {
         const long long ph = w / a.pc.heads;
@@ -185,7 +184,7 @@ __device__ __forceinline__ PtWalk pt_find(const PtArgs& a, PgSeq s, long long w,
     }
 #pragma unroll 1
     for (int r0 = 0;; r0 += 32) {
-        const int n = r0 + lane < R ? ITEM + max(1, pt_item<RT>(s, a, r0 + lane).n) : 0;
+        const int n = r0 + lane < R ? ITEM + max(1, pt_item(s, a, r0 + lane).n) : 0;
         const long long incl = pt_scan(n);
         const uint32_t hit = __ballot_sync(0xffffffffu, rem >= incl - n && rem < incl);
         if (hit || r0 + 32 >= R) {
@@ -207,7 +206,7 @@ struct PtShared {
     int b;
     PgSeq s;
 };
-template <int RT, int THREADS, int ITEM>
+template <int THREADS, int ITEM>
 __device__ __forceinline__ PtPlace pt_start(const PtArgs& a, int block, int blocks, PtShared& sh) {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     PtPlace place{};
@@ -217,7 +216,7 @@ __device__ __forceinline__ PtPlace pt_start(const PtArgs& a, int block, int bloc
     if (a.sq.n_seqs <= 32) {
         PgSeq s{};
         if (lane < a.sq.n_seqs) s = pg_seq(a.sq, a.pc, lane);
-        const long long w = pt_per_head<RT, ITEM>(a, s) * a.pc.heads, incl = pt_scan(w);
+        const long long w = pt_per_head<ITEM>(a, s) * a.pc.heads, incl = pt_scan(w);
         pt_share(__shfl_sync(0xffffffffu, incl, 31), block, blocks, beg, end);
         if (beg == end) return place;
         const uint32_t hit = __ballot_sync(0xffffffffu, beg >= incl - w && beg < incl);
@@ -225,13 +224,13 @@ __device__ __forceinline__ PtPlace pt_start(const PtArgs& a, int block, int bloc
         seq = pt_seq_of(s, from);
         walk.b = from;
         walk.left = end - beg;
-        walk = pt_find<RT, ITEM>(a, seq, __shfl_sync(0xffffffffu, w, from), __shfl_sync(0xffffffffu, beg - (incl - w), from), walk);
+        walk = pt_find<ITEM>(a, seq, __shfl_sync(0xffffffffu, w, from), __shfl_sync(0xffffffffu, beg - (incl - w), from), walk);
         return place;
     }
     auto units = [&](int b, PgSeq& s) -> long long {
         s = PgSeq{};
         if (b < a.sq.n_seqs) s = pg_seq(a.sq, a.pc, b);
-        return pt_per_head<RT, ITEM>(a, s) * a.pc.heads;
+        return pt_per_head<ITEM>(a, s) * a.pc.heads;
     };
     PgSeq s0, s;
     const long long w0 = units(threadIdx.x, s0);
@@ -271,15 +270,14 @@ __device__ __forceinline__ PtPlace pt_start(const PtArgs& a, int block, int bloc
     seq = sh.s;
     walk.b = sh.b;
     walk.left = end - beg;
-    walk = pt_find<RT, ITEM>(a, seq, sh.w, sh.at, walk);
+    walk = pt_find<ITEM>(a, seq, sh.w, sh.at, walk);
     return place;
 }
 
 // On to the next item: row tiles, then heads, then sequences with rows.
-template <int RT>
 __device__ __forceinline__ void pt_next(PtWalk& w, PgSeq& s, const PtArgs& a) {
     w.k = 0;
-    if (++w.rt < pt_row_tiles<RT>(s, a.G)) return;
+    if (++w.rt < pt_row_tiles(s, a)) return;
     w.rt = 0;
     if (++w.h < a.pc.heads) return;
     w.h = 0;
@@ -292,14 +290,12 @@ __device__ __forceinline__ void pt_next(PtWalk& w, PgSeq& s, const PtArgs& a) {
 }
 // The same in a function, for a kernel of many roles: with a copy of all this at each call it had grown past the
 // instruction cache (170 KB).
-template <int RT>
-__device__ __noinline__ PtPlace pt_after(const PtArgs& a, PtPlace p) {
-    pt_next<RT>(p.w, p.s, a);
+static __device__ __noinline__ PtPlace pt_after(const PtArgs& a, PtPlace p) {
+    pt_next(p.w, p.s, a);
     return p;
 }
-template <int RT>
 __device__ __forceinline__ void pt_next_far(PtWalk& w, PgSeq& s, const PtArgs& a) {
-    const PtPlace p = pt_after<RT>(a, PtPlace{w, s});
+    const PtPlace p = pt_after(a, PtPlace{w, s});
     w = p.w;
     s = p.s;
 }
