@@ -204,7 +204,7 @@ k_paged_step(PtArgs a, int blocks) {
     PtWalk w = start.w;
     PgSeq s = start.s;
     __syncthreads();
-    int4 hd = make_int4(0, 0, 0, 0);
+    int4 hd[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
     uint32_t n_stage = 0, n_q = 0;
     bool ok = true;
     Seg g;
@@ -465,16 +465,15 @@ k_paged_step(PtArgs a, int blocks) {
         }
         if (!done && g.real) {
             if (first) {
-                hd.y = w.h + 1;
-                hd.z = w.b;
-                hd.w = w.rt;
-            } else hd.x = g.last ? 2 : 1;
+                pt_tail(hd, w, s);
+            } else hd[0].x = g.last ? 2 : 1;
         }
         w.left -= g.k1 - g.k0;
         if (w.left > 0) pt_next(w, s, a);
     }
     if (threadIdx.x == 0) {
-        a.head[c] = hd;
+        a.head[2 * c] = hd[0];
+        a.head[2 * c + 1] = hd[1];
         if (sh_gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
     }
 }
@@ -506,7 +505,7 @@ int launch_attend(salicache_ctx* c, const PtArgs& a, char* work, cudaStream_t st
 
 }  // namespace
 
-int64_t sc_paged_work_bytes(const salicache_ctx* c, int head_dim) { return 2ll * c->sm_count * (256 * (head_dim + 2) * 4 + 16); }
+int64_t sc_paged_work_bytes(const salicache_ctx* c, int head_dim) { return 2ll * c->sm_count * (256 * (head_dim + 2) * 4 + 32); }
 
 int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* q, const void* d_q, int64_t q_stride,
                     int q_per_kv, float softmax_scale, int window, int sinks, void* d_out, int64_t out_stride, float* d_lse,

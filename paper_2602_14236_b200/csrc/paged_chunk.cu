@@ -25,6 +25,7 @@
 // staged and the output back when it is written.
 #include <cuda.h>
 #include <math.h>
+#include <type_traits>
 
 #include "paged_async.cuh"
 #include "paged_plan.cuh"
@@ -259,7 +260,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
         const uint32_t p_ready = smem_u32(&bars.p_ready[half][0]), o_done = smem_u32(&bars.o_done[half]);
         const uint32_t q_tile = base + SM::Q + half * SM::TILE;
         uint32_t n_s = 0, n_o = 0, n_tile = 0;               // scores, outputs of this half and tiles seen so far
-        int4 hd = make_int4(0, 0, 0, 0);
+        int4 hd[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
         bool ok = true;
         uint32_t n_q = 0;
         auto hand_q = [&](const ChSeg& gg) {
@@ -426,17 +427,17 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
             } else n_tile += g.tiles;
             if (!handed) hand_q(gn);
             if (!done && g.real) {
-                if (first) {
-                    hd.y = w.h + 1;
-                    hd.z = w.b;
-                    hd.w = w.rt;
-                } else hd.x = lastp ? 2 : 1;
+                if (first) pt_tail(hd, w, s);
+                else hd[0].x = lastp ? 2 : 1;
             }
             w = wn;
             s = sn;
             g = gn;
         }
-        if (tid == 0) a.head[blockIdx.x] = hd;
+        if (tid == 0) {
+            a.head[2 * blockIdx.x] = hd[0];
+            a.head[2 * blockIdx.x + 1] = hd[1];
+        }
     } else if (wid < 12) {
         // ---------------- operands
         const Codes<T> cd;
@@ -713,22 +714,27 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
     }
 }
 
-// Joins split items: a thread per row, CH_JOIN dimensions at a time.  The blocks, one wave of them, share out the
-// (item, dimensions) pairs; a block per pair that might be would mostly find nothing to do, in several waves.
-constexpr int CH_JOIN = 8;
+// Joins split items: a thread per row, four dimensions at a time.  The blocks, one wave of them, share out the (item,
+// dimensions) pairs; a block per pair that might be would mostly find nothing to do, in several waves.  What the blocks
+// said of their records is read at once, so that nothing but the records themselves has to be waited for after it.
 template <typename T, int D>
-__global__ void __launch_bounds__(CH_ROWS, 4)
+__global__ void __launch_bounds__(CH_ROWS, 2)
 k_paged_join_chunk(PtArgs a, int blocks) {
-    constexpr int N = CH_JOIN / 4, PARTS = D / CH_JOIN;
+    constexpr int PARTS = D / 4;
     __shared__ int list[PT_MAX_BLOCKS + 1], tails[PT_MAX_BLOCKS], kind[PT_MAX_BLOCKS], in_warp[CH_ROWS / 32];
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    __shared__ int4 item[PT_MAX_BLOCKS];     // head, row tile, first row, rows
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, row = threadIdx.x;
     grid_wait();
     int n_tails = 0;                         // the blocks that left a tail, in their order
     for (int c0 = 0; c0 < blocks; c0 += CH_ROWS) {
         const int c = c0 + threadIdx.x;
-        const int4 hd = c < blocks ? a.head[c] : make_int4(0, 0, 0, 0);
+        int4 hd = make_int4(0, 0, 0, 0), sq = hd;
+        if (c < blocks) {
+            hd = a.head[2 * c];
+            sq = a.head[2 * c + 1];
+            kind[c] = hd.x;
+        }
         const uint32_t has = __ballot_sync(0xffffffffu, hd.y != 0);
-        if (c < blocks) kind[c] = hd.x;
         if (lane == 0) in_warp[wid] = __popc(has);
         __syncthreads();
         int at = n_tails + __popc(has & ((1u << lane) - 1u));
@@ -736,63 +742,58 @@ k_paged_join_chunk(PtArgs a, int blocks) {
             if (i < wid) at += in_warp[i];
             n_tails += in_warp[i];
         }
-        if (hd.y != 0) tails[at] = c;
+        if (hd.y != 0) {
+            tails[at] = c;
+            item[at] = make_int4(hd.y - 1, hd.z, sq.x, sq.y);
+        }
         __syncthreads();
     }
     for (int unit = blockIdx.x; unit < n_tails * PARTS; unit += gridDim.x) {
         const int blk = tails[unit / PARTS], part = unit % PARTS;
-        const int4 hd = a.head[blk];
-        const int row = threadIdx.x, b = hd.z, h = hd.y - 1, rt = hd.w;
-        const PgSeq s = pg_seq(a.sq, a.pc, b);
+        const int4 it = item[unit / PARTS];
         const int n = pt_records([&](int c) { return kind[c]; }, blk, blocks, list);
-        const int HR = a.tile_rows >> 1, rr = rt * a.tile_rows + (row >> 7) * HR + (row & 127);
-        if ((row & 127) < HR && rr < s.n * a.G) {
-            // the maximum moves along with the records: one pass over them, eight under way at a time
-            constexpr int AHEAD = 8;
+        const int HR = a.tile_rows >> 1, rr = it.y * a.tile_rows + (row >> 7) * HR + (row & 127);
+        if ((row & 127) < HR && rr < it.w * a.G) {
+            // the maximum moves along with the records: one pass over them, 3 or 12 under way at a time (most items
+            // that a stretch cuts have two records; a few rows over a long cache have many)
             float M = PT_NONE, l = 0.0f;
-            float4 o[N];
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            auto pass = [&](auto ahead) {
+                constexpr int AHEAD = decltype(ahead)::value;
+                for (int i0 = 0; i0 < n; i0 += AHEAD) {
+                    float2 st[AHEAD];
+                    float4 v[AHEAD];
 #pragma unroll
-            for (int i = 0; i < N; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int i0 = 0; i0 < n; i0 += AHEAD) {
-                float2 st[AHEAD];
-                float4 v[AHEAD][N];
+                    for (int u = 0; u < AHEAD; ++u) {
+                        const size_t t = (size_t)list[min(i0 + u, n - 1)];
+                        st[u] = a.stat[t * CH_ROWS + row];
+                        v[u] = __ldcs(reinterpret_cast<const float4*>(a.part) + (t * PARTS + part) * CH_ROWS + row);
+                    }
+                    float nm = M;
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const size_t t = (size_t)list[min(i0 + u, n - 1)];
-                    const float4* src = reinterpret_cast<const float4*>(a.part) + (t * (D / 4) + part * N) * CH_ROWS + row;
-                    st[u] = a.stat[t * CH_ROWS + row];
+                    for (int u = 0; u < AHEAD; ++u) nm = fmaxf(nm, st[u].x);
+                    const float f = ex2(M - nm);
+                    M = nm;
+                    l *= f;
+                    o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
 #pragma unroll
-                    for (int x = 0; x < N; ++x) v[u][x] = __ldcs(src + x * CH_ROWS);
-                }
-                float nm = M;
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) nm = fmaxf(nm, st[u].x);
-                const float f = ex2(M - nm);
-                M = nm;
-                l *= f;
-#pragma unroll
-                for (int x = 0; x < N; ++x) o[x] = make_float4(o[x].x * f, o[x].y * f, o[x].z * f, o[x].w * f);
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const float e = i0 + u < n ? ex2(st[u].x - M) : 0.0f;
-                    l += e * st[u].y;
-#pragma unroll
-                    for (int x = 0; x < N; ++x) {
-                        o[x].x += e * v[u][x].x;
-                        o[x].y += e * v[u][x].y;
-                        o[x].z += e * v[u][x].z;
-                        o[x].w += e * v[u][x].w;
+                    for (int u = 0; u < AHEAD; ++u) {
+                        const float e = i0 + u < n ? ex2(st[u].x - M) : 0.0f;
+                        l += e * st[u].y;
+                        o.x += e * v[u].x;
+                        o.y += e * v[u].y;
+                        o.z += e * v[u].z;
+                        o.w += e * v[u].w;
                     }
                 }
-            }
-            const int hq = h * a.G + rr % a.G;
-            const long long tok = s.row0 + rr / a.G;
+            };
+            if (n <= 3) pass(std::integral_constant<int, 3>{});
+            else pass(std::integral_constant<int, 12>{});
+            const int hq = it.x * a.G + rr % a.G;
+            const long long tok = it.z + rr / a.G;
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            uint4* dst = reinterpret_cast<uint4*>(a.out + tok * a.out_stride + (long long)hq * D + part * CH_JOIN);
-#pragma unroll
-            for (int i = 0; i < N / 2; ++i)
-                dst[i] = make_uint4(T::pack(o[2 * i].x * inv, o[2 * i].y * inv), T::pack(o[2 * i].z * inv, o[2 * i].w * inv),
-                                    T::pack(o[2 * i + 1].x * inv, o[2 * i + 1].y * inv), T::pack(o[2 * i + 1].z * inv, o[2 * i + 1].w * inv));
+            *reinterpret_cast<uint2*>(a.out + tok * a.out_stride + (long long)hq * D + part * 4) =
+                make_uint2(T::pack(o.x * inv, o.y * inv), T::pack(o.z * inv, o.w * inv));
             if (a.lse && part == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (M + log2f(l)) * PT_LN2 : -INFINITY;
         }
         __syncthreads();                     // the list is used up
@@ -848,7 +849,7 @@ int launch_chunk(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * CH_ROWS * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * CH_ROWS);
     SC_CHECK(pt_launch(k_paged_chunk<T, FMT, D>, dim3(blocks), CH_THREADS, BYTES, st, a, map, q_map, blocks));
-    SC_CHECK(pt_launch(k_paged_join_chunk<T, D>, dim3(4 * blocks), CH_ROWS, 0, st, a, blocks));
+    SC_CHECK(pt_launch(k_paged_join_chunk<T, D>, dim3(2 * blocks), CH_ROWS, 0, st, a, blocks));
     c->launches += 2;
     return SALICACHE_OK;
 }

@@ -30,7 +30,8 @@ struct PtArgs {
     float scale;                             // softmax scale * log2(e): the kernels work in powers of two
     float* part;                             // [2 * blocks][rows of a tile][D], tail records after head records of a block
     float2* stat;                            // [2 * blocks][rows of a tile]: running maximum (powers of two), denominator
-    int4* head;                              // [blocks]: head record (0 none, 1 the item goes on, 2 it ends); tail record: 1 + head or 0, b, rt
+    int4* head;                              // [2 * blocks]: per block: head record (0 none, 1 the item goes on, 2 it ends); tail record:
+                                             // 1 + head or 0, row tile, -; then its sequence's first row, rows, -, -
     int* status;
 };
 
@@ -325,6 +326,14 @@ __device__ __forceinline__ int pt_records(F flag, int c, int blocks, int* list) 
 }
 constexpr int PT_MAX_BLOCKS = 1024;          // of the attention kernels
 
+// What a block says of its records (see PtArgs::head).
+__device__ __forceinline__ void pt_tail(int4 (&hd)[2], const PtWalk& w, const PgSeq& s) {
+    hd[0].y = w.h + 1;
+    hd[0].z = w.rt;
+    hd[1].x = s.row0;
+    hd[1].y = s.n;
+}
+
 // Joins split items.  grid.x: blocks of the first kernel, grid.y: groups of 8 rows, one warp per row.
 template <typename T, int RT, int D>
 __global__ void __launch_bounds__(256)
@@ -332,32 +341,45 @@ k_paged_join(PtArgs a, int blocks) {
     __shared__ int list[PT_MAX_BLOCKS + 1];
     grid_wait();
     constexpr int N = D / 32;
-    const int4 hd = a.head[blockIdx.x];
+    const int4 hd = a.head[2 * blockIdx.x], sq = a.head[2 * blockIdx.x + 1];
     if (hd.y == 0) return;
-    const int n = pt_records([&](int c) { return a.head[c].x; }, blockIdx.x, blocks, list);
+    const int n = pt_records([&](int c) { return a.head[2 * c].x; }, blockIdx.x, blocks, list);
     const int lane = threadIdx.x & 31, row = blockIdx.y * 8 + (threadIdx.x >> 5);
-    const int b = hd.z, h = hd.y - 1, rt = hd.w;
-    const PgSeq s = pg_seq(a.sq, a.pc, b);
-    const int r = rt * RT + row;
-    if (r >= s.n * a.G) return;
-    float M = PT_NONE;
-    for (int i = lane; i < n; i += 32) M = fmaxf(M, a.stat[(size_t)list[i] * RT + row].x);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    float o[N], l = 0.0f;
+    const int h = hd.y - 1, r = hd.z * RT + row;
+    if (r >= sq.y * a.G) return;
+    // the maximum moves along with the records, eight under way at a time
+    constexpr int AHEAD = 8;
+    float M = PT_NONE, o[N], l = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-        const size_t t = (size_t)list[i] * RT + row;
-        const float2 st = a.stat[t];
-        const float e = ex2(st.x - M);
-        l += e * st.y;
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        float2 st[AHEAD];
+        float v[AHEAD][N];
 #pragma unroll
-        for (int x = 0; x < N; ++x) o[x] += e * a.part[t * D + lane * N + x];
+        for (int u = 0; u < AHEAD; ++u) {
+            const size_t t = (size_t)list[min(i0 + u, n - 1)] * RT + row;
+            st[u] = a.stat[t];
+#pragma unroll
+            for (int x = 0; x < N; ++x) v[u][x] = a.part[t * D + lane * N + x];
+        }
+        float nm = M;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) nm = fmaxf(nm, st[u].x);
+        const float f = ex2(M - nm);
+        M = nm;
+        l *= f;
+#pragma unroll
+        for (int x = 0; x < N; ++x) o[x] *= f;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const float e = i0 + u < n ? ex2(st[u].x - M) : 0.0f;
+            l += e * st[u].y;
+#pragma unroll
+            for (int x = 0; x < N; ++x) o[x] += e * v[u][x];
+        }
     }
     const int hq = h * a.G + r % a.G;
-    const long long tok = s.row0 + r / a.G;
+    const long long tok = sq.x + r / a.G;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     uint16_t* dst = a.out + tok * a.out_stride + (long long)hq * D + lane * N;
 #pragma unroll
