@@ -417,7 +417,7 @@ typedef struct salicache_pages {
  * d_row_start[b] on are its LAST n positions: row i is position d_len[b] - n + i (write first, attend to the same batch
  * after).  n may be 0; rows with a negative position (n > d_len[b]) exist in no page.  Rows from d_row_start[n_seqs] on
  * belong to nobody and are left as they are.  d_row_start is non-decreasing, within [0, n_rows].
- * Positions at or past table_width * page, and positions whose table entry lies outside [0, n_pages), are in no page: a
+ * Positions at or past table_width * page (or 2^30), and positions whose table entry lies outside [0, n_pages), are in no page: a
  * call that has to touch one records E_CAPACITY in the status word and treats it as stated with the call.  Table entries
  * of positions that no row has to touch are never used: they may be stale.
  * The offsets are read on the device: calls can be captured and replayed with other lengths of the same n_rows. */
@@ -464,7 +464,7 @@ SALICACHE_API int salicache_paged_read(salicache_ctx* ctx, const salicache_pages
  * sees nothing: out = 0, lse = -infinity.  What pages hold at positions that no row of the sequence sees has no effect,
  * NaN included; at positions that some rows see, V is finite.
  *   d_q, d_out  DEVICE [n_rows] rows of [heads * q_per_kv][head_dim], q_stride / out_stride elements from row to row
- *               (>= heads * q_per_kv * head_dim, multiples of 8)
+ *               (>= heads * q_per_kv * head_dim, multiples of 8); d_out does not overlap d_q
  *   d_lse       DEVICE f32 [n_rows][heads * q_per_kv], or NULL
  *   d_work      DEVICE, 16-byte aligned, salicache_paged_work_bytes() of it: partial results of rows whose keys are
  *               split.  Its content matters only while a call runs; calls that may overlap (other streams, captured
@@ -481,7 +481,7 @@ SALICACHE_API int salicache_paged_attend(salicache_ctx* ctx, const salicache_pag
 SALICACHE_API int64_t salicache_paged_work_bytes(const salicache_ctx* ctx, const salicache_pages* pages, int q_per_kv);
 
 /* Synchronises `cuda_stream`, returns the deferred device status (0, E_CAPACITY, E_NOCONVERGE or
- * E_EVICTED; E_CUDA if the stream reports an error) and clears it. */
+ * E_EVICTED; E_CUDA if the stream reports an error, or a wait inside salicache_paged_attend ran out) and clears it. */
 SALICACHE_API int salicache_poll_status(salicache_ctx* ctx, void* cuda_stream);
 
 #ifdef __cplusplus

@@ -77,7 +77,7 @@ __device__ __forceinline__ PgSeq pg_seq(const PgSeqs& s, const PgCache& c, int b
     PgSeq r;
     const int a = min(max(s.start[b], 0), s.n_rows), e = min(max(s.start[b + 1], a), s.n_rows);
     const int len = max(s.len[b], 0);
-    const long long cap = (long long)s.width << c.page_shift;
+    const long long cap = min((long long)s.width << c.page_shift, 1ll << 30);        // sums of positions stay within 32 bits
     r.row0 = a;
     r.n = e - a;
     r.pos0 = len - r.n;

@@ -190,6 +190,35 @@ def test_chunks_under_a_window(ctx, fmt, dt, window, sinks):
         _attend(ctx, w, 2, window, sinks)
 
 
+@pytest.mark.parametrize("G", [5, 7, 20, 33, 48])
+def test_groups_that_do_not_divide_a_tile(ctx, G):
+    """Rows of a tile are whole tokens: 125, 126, 120, 99 and 96 of 128."""
+    for fmt, dt in (("fp16", "f16"), ("int4", "bf16")):
+        w = pu.World(45 + G, fmt, _t(dt), 1, 64, 32, [333, 90], [29, 11])
+        _attend(ctx, w, G)
+        _attend(ctx, w, G, 100, 5)
+
+
+@pytest.mark.parametrize("fmt,dt,D", [("fp16", "f16", 128), ("int8", "bf16", 64)])
+def test_chunks_of_many_sequences(ctx, fmt, dt, D):
+    """More sequences than a warp has lanes, some without rows, some without positions."""
+    rng = np.random.default_rng(46)
+    lens = rng.integers(0, 200, 75).tolist()
+    news = [int(rng.integers(0, n + 1)) if i % 3 else 0 for i, n in enumerate(lens)]
+    news[4] = lens[4] + 3
+    w = pu.World(47, fmt, _t(dt), 1, D, 16, lens, news)
+    _attend(ctx, w, 2, extra=7)
+    _attend(ctx, w, 2, 50, 60)
+
+
+def test_a_prompt_of_many_tiles(ctx):
+    """Enough tiles that every block of the grid has some, with items cut in two and more."""
+    w = pu.World(48, "fp16", _t("bf16"), 2, 64, 64, [1500], [1500])
+    _attend(ctx, w, 2)
+    w = pu.World(49, "int8", _t("f16"), 1, 128, 128, [9000], [40])
+    _attend(ctx, w, 4)
+
+
 def test_largest_group_of_query_heads(ctx):
     _attend(ctx, pu.World(50, "fp16", _t("f16"), 1, 128, 16, [200, 33], [3, 1]), 64)
 
@@ -386,6 +415,46 @@ def test_captured_and_replayed_with_other_lengths(ctx, news):
         for ln in lanes:
             ln.verify()
     assert sc.salicache_poll_status(ctx) == 0
+
+
+_FIRST = """
+import sys
+sys.path.insert(0, {root!r})
+sys.path.insert(0, {tests!r})
+import numpy as np, torch
+import paged_util as pu
+from paper_2602_14236_b200 import binding as sc
+ctx = sc.Context(sc.salicache_default_params(max_batch=1, chunk_frames=1, L=1))
+for news in ([1, 1], [60, 3]):
+    w = pu.World(61, "int8", torch.float16, 2, 128, 16, [200, 90], news)
+    pages, seqs = w.device()
+    qh = torch.from_numpy(np.random.default_rng(1).standard_normal((w.rows, 4 * 128))).half()
+    q, x = qh.cuda(), torch.empty((2, w.rows, 256), dtype=torch.float16, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros((w.rows, 4), device="cuda")
+    work = torch.empty(sc.salicache_paged_work_bytes(ctx, pages.c, 2), dtype=torch.uint8, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sc.salicache_paged_read(ctx, pages.c, seqs.c, x[0], x[1], 256, 256)
+        sc.salicache_paged_write(ctx, pages.c, seqs.c, x[0], x[1], 256, 256)
+        sc.salicache_paged_attend(ctx, pages.c, seqs.c, q, 512, 2, 0.09, 0, 0, out, 512, lse, work, work.numel())
+    g.replay()
+    torch.cuda.synchronize()
+    assert sc.salicache_poll_status(ctx) == 0
+    assert torch.isfinite(out).all() and (out != 0).any(1).all()
+    held = np.stack([np.concatenate([w.kv(b, h, 0)[w.lens[b] - n:] for b, n in enumerate(news)]) for h in range(2)], 1)
+    assert np.array_equal(x[0].double().cpu().numpy().reshape(held.shape), held)
+print("captured")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_captured(ctx):
+    import os
+    import subprocess
+    import sys
+    tests = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-c", _FIRST.format(root=os.path.dirname(tests), tests=tests)], capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
 
 
 def test_repeated_calls_give_the_same_bits(ctx):
