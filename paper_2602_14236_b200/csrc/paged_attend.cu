@@ -37,7 +37,7 @@ struct StSmem {
     static constexpr int STAGES = ROOM / STAGE < 8 ? ROOM / STAGE : 8;
     static constexpr int BYTES = STAGES * STAGE + ACC + 2 * Q;
     // an item's fixed cost (its rows of q, joining the warps, the output) in tiles' time, as measured
-    static constexpr int ITEM = FMT == PF_I4 ? 2 : 1;
+    static constexpr int ITEM = FMT == PF_I4 ? 3 : 2;
 };
 
 template <typename T>

@@ -144,23 +144,6 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uin
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 constexpr int CH_RAW = 4;                    // raw stages at most
-// Two binary32 numbers at a time.
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2f(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add2f(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
@@ -349,20 +332,17 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                         }
                         tc_wait_ld(x[0]);
                         // P takes half the columns of S: what it overwrites has been read
-                        const uint64_t scale2 = pack2(a.scale, a.scale), m2 = pack2(-m, -m);
-                        uint64_t sum[2] = {0ull, 0ull};
+                        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             if (c < 3) tc_ld32(x[(c + 1) & 1], S + 32 * (c + 1));
                             uint32_t pk[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
-                                const uint64_t y = fma2f(pack2(__uint_as_float(x[c & 1][2 * i]), __uint_as_float(x[c & 1][2 * i + 1])), scale2, m2);
-                                float p0, p1;
-                                unpack2(y, p0, p1);
-                                p0 = ex2(p0);
-                                p1 = ex2(p1);
-                                sum[i & 1] = add2f(sum[i & 1], pack2(p0, p1));
+                                const float p0 = ex2(fmaf(__uint_as_float(x[c & 1][2 * i]), a.scale, -m));
+                                const float p1 = ex2(fmaf(__uint_as_float(x[c & 1][2 * i + 1]), a.scale, -m));
+                                sum[2 * (i & 1)] += p0;
+                                sum[2 * (i & 1) + 1] += p1;
                                 pk[i] = T::pack(p0, p1);
                             }
                             if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
@@ -374,9 +354,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                                 if (lane == 0) bar_arrive(p_ready + 8 * (c >> 1));
                             }
                         }
-                        float s0, s1;
-                        unpack2(add2f(sum[0], sum[1]), s0, s1);
-                        l += s0 + s1;
+                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     }
                     if (ok) {
                         hand_q(gn);
