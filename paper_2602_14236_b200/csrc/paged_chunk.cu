@@ -726,26 +726,30 @@ k_paged_join_chunk(PtArgs a, int blocks) {
         }
         __syncthreads();
     }
-    for (int unit = blockIdx.x; unit < n_tails * PARTS; unit += gridDim.x) {
-        const int blk = tails[unit / PARTS], part = unit % PARTS;
-        const int4 it = item[unit / PARTS];
-        const int n = pt_records([&](int c) { return kind[c]; }, blk, blocks, list);
-        const int HR = a.tile_rows >> 1, rr = it.y * a.tile_rows + (row >> 7) * HR + (row & 127);
-        if ((row & 127) < HR && rr < it.w * a.G) {
-            // the maximum moves along with the records: one pass over them, 3 or 12 under way at a time (most items
-            // that a stretch cuts have two records; a few rows over a long cache have many)
-            float M = PT_NONE, l = 0.0f;
-            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            auto pass = [&](auto ahead) {
-                constexpr int AHEAD = decltype(ahead)::value;
+    // A unit is one item's sums of P x 4 dimensions, AHEAD records under way at a time.
+    auto units = [&](auto p_, auto ahead_) {
+        constexpr int P = decltype(p_)::value, AHEAD = decltype(ahead_)::value, UNITS = PARTS / P;
+        for (int unit = blockIdx.x; unit < n_tails * UNITS; unit += gridDim.x) {
+            const int blk = tails[unit / UNITS], part = unit % UNITS * P;
+            const int4 it = item[unit / UNITS];
+            const int n = pt_records([&](int c) { return kind[c]; }, blk, blocks, list);
+            const int HR = a.tile_rows >> 1, rr = it.y * a.tile_rows + (row >> 7) * HR + (row & 127);
+            if ((row & 127) < HR && rr < it.w * a.G) {
+                // the maximum moves along with the records: one pass over them
+                float M = PT_NONE, l = 0.0f;
+                float4 o[P];
+#pragma unroll
+                for (int x = 0; x < P; ++x) o[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 for (int i0 = 0; i0 < n; i0 += AHEAD) {
                     float2 st[AHEAD];
-                    float4 v[AHEAD];
+                    float4 v[AHEAD][P];
 #pragma unroll
                     for (int u = 0; u < AHEAD; ++u) {
                         const size_t t = (size_t)list[min(i0 + u, n - 1)];
                         st[u] = a.stat[t * CH_ROWS + row];
-                        v[u] = __ldcs(reinterpret_cast<const float4*>(a.part) + (t * PARTS + part) * CH_ROWS + row);
+#pragma unroll
+                        for (int x = 0; x < P; ++x)
+                            v[u][x] = __ldcs(reinterpret_cast<const float4*>(a.part) + (t * PARTS + part + x) * CH_ROWS + row);
                     }
                     float nm = M;
 #pragma unroll
@@ -753,29 +757,36 @@ k_paged_join_chunk(PtArgs a, int blocks) {
                     const float f = ex2(M - nm);
                     M = nm;
                     l *= f;
-                    o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+#pragma unroll
+                    for (int x = 0; x < P; ++x) o[x] = make_float4(o[x].x * f, o[x].y * f, o[x].z * f, o[x].w * f);
 #pragma unroll
                     for (int u = 0; u < AHEAD; ++u) {
                         const float e = i0 + u < n ? ex2(st[u].x - M) : 0.0f;
                         l += e * st[u].y;
-                        o.x += e * v[u].x;
-                        o.y += e * v[u].y;
-                        o.z += e * v[u].z;
-                        o.w += e * v[u].w;
+#pragma unroll
+                        for (int x = 0; x < P; ++x) {
+                            o[x].x += e * v[u][x].x;
+                            o[x].y += e * v[u][x].y;
+                            o[x].z += e * v[u][x].z;
+                            o[x].w += e * v[u][x].w;
+                        }
                     }
                 }
-            };
-            if (n <= 3) pass(std::integral_constant<int, 3>{});
-            else pass(std::integral_constant<int, 12>{});
-            const int hq = it.x * a.G + rr % a.G;
-            const long long tok = it.z + rr / a.G;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            *reinterpret_cast<uint2*>(a.out + tok * a.out_stride + (long long)hq * D + part * 4) =
-                make_uint2(T::pack(o.x * inv, o.y * inv), T::pack(o.z * inv, o.w * inv));
-            if (a.lse && part == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (M + log2f(l)) * PT_LN2 : -INFINITY;
+                const int hq = it.x * a.G + rr % a.G;
+                const long long tok = it.z + rr / a.G;
+                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                uint2* dst = reinterpret_cast<uint2*>(a.out + tok * a.out_stride + (long long)hq * D + part * 4);
+#pragma unroll
+                for (int x = 0; x < P; ++x) dst[x] = make_uint2(T::pack(o[x].x * inv, o[x].y * inv), T::pack(o[x].z * inv, o[x].w * inv));
+                if (a.lse && part == 0) a.lse[tok * ((long long)a.pc.heads * a.G) + hq] = l > 0.0f ? (M + log2f(l)) * PT_LN2 : -INFINITY;
+            }
+            __syncthreads();                 // the list is used up
         }
-        __syncthreads();                     // the list is used up
-    }
+    };
+    // A few rows over a long cache leave few items of many records each, a long prompt one item of two or three records at
+    // every block's edge.
+    if (n_tails * PARTS <= 2 * (int)gridDim.x) units(std::integral_constant<int, 1>{}, std::integral_constant<int, 12>{});
+    else units(std::integral_constant<int, 4>{}, std::integral_constant<int, 3>{});
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
