@@ -12,7 +12,11 @@
 // 16-bit type there.
 // One more warp feeds a ring of tiles in shared memory by bulk copies of whole pages, so that some 130 to 200 KB per SM are
 // under way whatever the registers hold.  (Loading each lane's next operands into registers instead: 32 ragged streams
-// over INT4 pages took 149 us, 0.27 of the copy bandwidth.)
+// over INT4 pages took 149 us.)
+// Measured: 16-bit pages, 16 sequences of 8000 positions: 100 us = 5.2 TB/s, 0.81 of the copy bandwidth, bound by memory;
+// INT8: 64 us = 4.2 TB/s; INT4, 32 ragged streams, 270 MB: 92 us = 2.9 TB/s = 0.45.  Codes are bound by issue slots: 433
+// instructions per 16 INT4 keys of a head, of which 192 turn codes into numbers (and, subtract, multiply-add per pair of
+// them: the values are rounded as salicache_paged_read rounds them, so the scales cannot be taken out of the sums).
 // The weights' reference maximum moves only when a score exceeds it by 2^8 (in powers of two): until then no lane needs
 // another's, weights stay below 2^8, and the sums are joined across lanes once at the end of an item.
 #include <math.h>
@@ -499,8 +503,10 @@ int launch_step(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
 
 template <typename T, int FMT, int D>
 int launch_attend(salicache_ctx* c, const PtArgs& a, char* work, cudaStream_t st) {
-    if ((long long)a.sq.n_rows * a.G <= 8ll * a.sq.n_seqs) return launch_step<T, FMT, D, 1>(c, a, work, st);
-    return launch_step<T, FMT, D, 2>(c, a, work, st);
+    // one column tile of 8 rows, or two of them: codes are expanded once for both, at half the blocks per SM
+    if constexpr (FMT != PF_16)
+        if ((long long)a.sq.n_rows * a.G > 8ll * a.sq.n_seqs) return launch_step<T, FMT, D, 2>(c, a, work, st);
+    return launch_step<T, FMT, D, 1>(c, a, work, st);
 }
 
 }  // namespace
@@ -524,7 +530,12 @@ int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache
     a.scale = softmax_scale * PT_LOG2E;
     a.status = c->d_status;
     char* work = (char*)d_work;
-    if ((long long)a.sq.n_rows * a.G > 16ll * a.sq.n_seqs) return sc_paged_chunk(c, a, pg, work, st);
+    // Rows (of q, times the query heads of a group) per sequence up to which reading the pages is the work: 8 of 16-bit
+    // pages, 16 of codes.  Measured with 16 sequences of 8000 positions, 8 key/value heads, this kernel against
+    // paged_chunk.cu's: 16-bit 8 rows 103 / 116 us, 16 rows 122 / 116; INT8 16 rows 93 / 131, 32 rows 164 / 131; INT4 16 rows
+    // 87 / 123, 32 rows 154 / 123.
+    const long long few = pg->format == SALICACHE_FP16 ? 8 : 16;
+    if ((long long)a.sq.n_rows * a.G > few * a.sq.n_seqs) return sc_paged_chunk(c, a, pg, work, st);
 #define GO(T, F, D) return launch_attend<T, F, D>(c, a, work, st)
 #define GO_FORMAT(T, D)                                      \
     do {                                                     \

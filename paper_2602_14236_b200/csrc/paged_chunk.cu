@@ -19,6 +19,12 @@
 // The reference maximum moves only when a row exceeds it by 2^8; then, and only then, O is rescaled, by the thread that
 // found it and before it hands its weights on.
 //
+// Measured (bf16, 8192 new rows, 32 query and 8 key/value heads x 128): 563 us = 976 TFLOP/s, 0.58 of the cuBLAS burst rate;
+// two streams' 2304 rows over 20736 and 6912 INT4 positions: 1135 us = 996 TFLOP/s.  A (256 x 128) tile takes some 3500
+// clocks, of which the tensor core works 2050 (counted: 54 % of the kernel): the round of a half, S, weights, P V, is as
+// long as that.  Without the weights (products and copies alone) a tile takes 2800, shared memory being read at its full
+// rate for them.
+//
 // Both operands use the 128-byte swizzle: rows of 64 elements, eight rows to a 1024-byte atom.  K has the contracted
 // dimension contiguous; V has it across rows, which the instruction descriptor's transpose bit covers, so neither is
 // transposed in memory.  INT4 codes come out of their words in the order 0 4 1 5 2 6 3 7; Q is permuted alike when it is

@@ -199,8 +199,8 @@ __device__ __forceinline__ PtWalk pt_find(const PtArgs& a, PgSeq s, long long w,
 }
 
 // Where the block starts, and the sequence it starts in; the same for every thread.  Up to 32 sequences every warp works
-// it out for itself, a lane per sequence, without a barrier (1.4 us less of the 3.0 us that the first tile waited); more
-// of them are shared out over the block's threads, with scans through shared memory.
+// it out for itself, a lane per sequence, without a barrier (2.2 us after the start instead of 3.0); more of them are
+// shared out over the block's threads, with scans through shared memory.
 struct PtShared {
     long long wsum[32];
     long long left, at, w;
