@@ -79,18 +79,19 @@ struct KTile {
     static constexpr int W = pg_row_bytes<FMT, D>() / 16;       // words of a key row per lane
     uint32_t k[2][W];
     uint32_t s[2];                                              // scale, or (scale, zero)
-    __device__ __forceinline__ void load(uint32_t rows, uint32_t meta, int g8, int c4) {
-        constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
+    static constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
+    // this lane's first bytes of 16 keys' rows, and of their scales
+    static __device__ __forceinline__ uint32_t at(int g8, int c4) { return key_of(g8) * RB + (RB >= 64 ? 16 : 8) * c4; }
+    static __device__ __forceinline__ uint32_t meta_at(int g8) { return key_of(g8) * MB; }
+    __device__ __forceinline__ void load(uint32_t rows, uint32_t meta) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int key = key_of(g8) + 8 * r;
-            const uint32_t p = rows + key * RB;
             if (RB >= 64) {
 #pragma unroll
-                for (int i = 0; i < RB / 64; ++i) lds16(&k[r][4 * i], p + 64 * i + 16 * c4);
-            } else lds_words<2>(&k[r][0], p + 8 * c4);
-            if (FMT == PF_I8) s[r] = lds_u16(meta + key * MB);
-            if (FMT == PF_I4) lds_words<1>(&s[r], meta + key * MB);
+                for (int i = 0; i < RB / 64; ++i) lds16(&k[r][4 * i], rows + 8 * r * RB + 64 * i);
+            } else lds_words<2>(&k[r][0], rows + 8 * r * RB);
+            if (FMT == PF_I8) s[r] = lds_u16(meta + 8 * r * MB);
+            if (FMT == PF_I4) lds_words<1>(&s[r], meta + 8 * r * MB);
         }
     }
 };
@@ -99,16 +100,18 @@ struct VTile {
     static constexpr int W = pg_row_bytes<FMT, D>() / 32;       // words of a value row per lane
     uint32_t v[4][W];
     uint32_t s[2][FMT == PF_I4 ? 2 : 1];                        // per pair of keys: their scales in one word, or (scale, zero) each
-    __device__ __forceinline__ void load(uint32_t rows, uint32_t meta, int g8, int c4) {
-        constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
+    static constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
+    static __device__ __forceinline__ uint32_t at(int g8, int c4) { return c4 * RB + (W == 8 ? 16 : 4 * W) * g8; }
+    static __device__ __forceinline__ uint32_t meta_at(int c4) { return c4 * MB; }
+    __device__ __forceinline__ void load(uint32_t rows, uint32_t meta) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int key = c4 + 4 * (j & 1) + 8 * (j >> 1);
+            const int key = 4 * (j & 1) + 8 * (j >> 1);          // from this lane's first
             const uint32_t p = rows + key * RB;
             if (W == 8) {
-                lds16(&v[j][0], p + 16 * g8);
-                lds16(&v[j][W == 8 ? 4 : 0], p + 128 + 16 * g8);
-            } else lds_words<W == 8 ? 4 : W>(&v[j][0], p + 4 * W * g8);
+                lds16(&v[j][0], p);
+                lds16(&v[j][W == 8 ? 4 : 0], p + 128);
+            } else lds_words<W == 8 ? 4 : W>(&v[j][0], p);
             if (FMT == PF_I4) lds_words<1>(&s[j >> 1][FMT == PF_I4 ? j & 1 : 0], meta + key * MB);
             if (FMT == PF_I8) {
                 const uint32_t x = lds_u16(meta + key * MB);
@@ -273,6 +276,11 @@ k_paged_step(PtArgs a, int blocks) {
     }
 
     const Codes<T> cd;
+    uint32_t stage = 0, phase = 0;
+    // this lane's places in a stage
+    constexpr uint32_t RB16 = 16 * pg_row_bytes<FMT, D>(), MB16 = 16 * pg_meta_bytes<FMT>();
+    const uint32_t k_at = SM::K + wid * RB16 + KTile<FMT, D>::at(g8, c4), km_at = SM::KM + wid * MB16 + KTile<FMT, D>::meta_at(g8);
+    const uint32_t v_at = SM::V + wid * RB16 + VTile<FMT, D>::at(g8, c4), vm_at = SM::VM + wid * MB16 + VTile<FMT, D>::meta_at(c4);
     while (w.left > 0 && ok) {
         g.set(a, w, s);
         const PtSpan& sp = g.sp;
@@ -315,22 +323,25 @@ k_paged_step(PtArgs a, int blocks) {
             for (int t = 0; t < VS; ++t) acc[n][t][0] = acc[n][t][1] = acc[n][t][2] = acc[n][t][3] = 0.0f;
         }
 
-        for (int k = g.t0; k < g.t0 + g.tiles; ++k, ++n_stage) {
-            const uint32_t st = n_stage % STAGES, src = smem_u32(ring) + st * SM::STAGE;
-            bar_wait(smem_u32(&full[st]), (n_stage / STAGES) & 1, gave_up);
+        for (int k = g.t0; k < g.t0 + g.tiles; ++k) {
+            const uint32_t st = stage, src = smem_u32(ring) + st * SM::STAGE;
+            bar_wait(smem_u32(&full[st]), phase, gave_up);
             __syncwarp();
+            if (++stage == STAGES) {
+                stage = 0;
+                phase ^= 1;
+            }
             const int j0 = sp.tile(k) * PT_KEYS + wid * 16;
             if (!(*(volatile uint32_t*)&kinds[st] >> wid & 1u)) {
                 if (lane == 0) bar_arrive(smem_u32(&empty[st]));
                 continue;
             }
-            constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
             float sc[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
             {
                 KTile<FMT, D> kt;
-                kt.load(src + SM::K + wid * 16 * RB, src + SM::KM + wid * 16 * MB, g8, c4);
+                kt.load(src + k_at, src + km_at);
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
                     uint32_t a0, a1, a2, a3;
@@ -341,7 +352,7 @@ k_paged_step(PtArgs a, int blocks) {
                 }
             }
             VTile<FMT, D> vt;
-            vt.load(src + SM::V + wid * 16 * RB, src + SM::VM + wid * 16 * MB, g8, c4);
+            vt.load(src + v_at, src + vm_at);
             __syncwarp();
             if (lane == 0) bar_arrive(smem_u32(&empty[st]));
             {
