@@ -201,9 +201,10 @@ __device__ __forceinline__ void fetch_group(Fetched<FMT>& f, const RowPlace& rp,
         f.meta = *reinterpret_cast<const uint32_t*>(meta);
     }
 }
-// Codes to numbers by putting them into the mantissa of 2^23.  A nibble i places up stands for 16^i times its value, which
-// the scale, divided by the same power of two, makes good exactly; the offset is taken off in the same fused step, whose
-// exact result q * s fits binary32, so that nothing is rounded before the zero is added.
+// Codes to numbers by putting them into the mantissa of 2^23, which is then taken off: exact, and before the scale, whose
+// product with 2^23 need not be finite.  A nibble i places up stands for 16^i times its value, which the scale, divided by
+// the same power of two, makes good exactly (its last place, 2^-133 or more, leaves room for 12 bits); q * s fits binary32,
+// so that the fused step that adds the zero rounds as a multiplication and an addition do.
 template <typename T, int FMT>
 __device__ __forceinline__ uint4 expand_group(const Fetched<FMT>& f) {
     if (FMT == PF_16) return f.c;
@@ -225,7 +226,7 @@ __device__ __forceinline__ uint4 expand_group(const Fetched<FMT>& f) {
             const float si = s * (1.0f / (float)(1 << (4 * (i & 3))));
             const uint32_t w = i < 4 ? f.c.x : w1;
             const uint32_t b = (i & 3) == 0 ? and_or<0xfu>(w, big) : (i & 3) == 1 ? and_or<0xf0u>(w, big) : (i & 3) == 2 ? and_or<0xf00u>(w, big) : and_or<0xf000u>(w, big);
-            x[i] = __fadd_rn(__fmaf_rn(__uint_as_float(b), si, -8388608.0f * si), z);
+            x[i] = __fmaf_rn(__fsub_rn(__uint_as_float(b), 8388608.0f), si, z);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = T::pack(x[2 * i], x[2 * i + 1]);

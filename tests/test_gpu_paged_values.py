@@ -1,0 +1,56 @@
+"""GPU tests of what the paged cache does with extreme values: both ends of the types' ranges."""
+import numpy as np
+import pytest
+
+import paged_util as pu
+from paper_2602_14236_b200 import binding as sc
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return sc.Context(sc.salicache_default_params(max_batch=1, chunk_frames=1, L=1))
+
+
+def _t(name):
+    import torch
+    return {"f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def _i32(a):
+    import torch
+    return torch.tensor(a, dtype=torch.int32, device="cuda")
+
+
+def _stored(ctx, x, fmt, t, page=16):
+    """Writes x float64 [2][R][heads][D] as one sequence of R positions and reads it back: float64, same shape."""
+    import torch
+    _, R, heads, D = x.shape
+    n = -(-R // page)
+    pages = sc.PageSet(n, page, heads, D, pu.FMT[fmt], t)
+    seqs = sc.Seqs(_i32([0, R]), _i32([R]), _i32([list(range(n))]), R)
+    d = torch.from_numpy(x.reshape(2, R, heads * D)).to(t).cuda()
+    out = torch.full_like(d, 7.0)
+    sc.salicache_paged_write(ctx, pages.c, seqs.c, d[0], d[1], heads * D, heads * D)
+    sc.salicache_paged_read(ctx, pages.c, seqs.c, out[0], out[1], heads * D, heads * D)
+    assert sc.salicache_poll_status(ctx) == 0
+    return out.double().cpu().numpy().reshape(x.shape)
+
+
+# Largest magnitudes (INT4 groups span twice that, which has to stay below binary32's 3.4e38), and smallest ones: their
+# scales are the type's smallest normal numbers, whose reciprocals are still below binary32's largest.
+@pytest.mark.parametrize("fmt,dt,largest", [
+    ("int8", "bf16", 3.0e38), ("int8", "bf16", 1.0e33), ("int8", "bf16", 3.0e-36), ("int8", "f16", 6.0e4), ("int8", "f16", 9.0e-3),
+    ("int4", "bf16", 1.6e38), ("int4", "bf16", 4.0e36), ("int4", "bf16", 3.0e35), ("int4", "bf16", 2.0e34), ("int4", "bf16", 1.0e33),
+    ("int4", "bf16", 2.0e32), ("int4", "bf16", 3.0e-37), ("int4", "f16", 6.4e4), ("int4", "f16", 1.0e-3),
+])
+@pytest.mark.parametrize("D", [64, 128])
+def test_written_and_read_at_the_ends_of_the_range(ctx, fmt, dt, largest, D):
+    t = _t(dt)
+    rng = np.random.default_rng(80)
+    x = pu.to_t(rng.uniform(-largest, largest, (2, 21, 3, D)), t)
+    x[..., 5], x[..., D - 3] = pu.to_t(np.array(largest), t), pu.to_t(np.array(-largest), t)
+    want = pu.decode(*pu.encode(x, fmt, t), fmt, t)
+    assert np.isfinite(want).all()
+    assert np.array_equal(_stored(ctx, x, fmt, t), want)
