@@ -436,7 +436,8 @@ typedef struct salicache_seqs {
  * operations, to nearest even:
  *   INT8: s = T(max|x| / 127), 0 -> 1;           q = rint(x * (1/s)) clamped to +-127
  *   INT4: zero = min x, s = T((max - zero) / 15), 0 -> 1;  q = rint((x - zero) * (1/s)) clamped to 0 .. 15
- * (an s whose reciprocal overflows binary32 counts as 0).  Rows in no page are dropped (deferred E_CAPACITY for the
+ * (an s whose reciprocal overflows binary32 counts as 0).  A group with a NaN or an infinity in it, or whose max - zero
+ * overflows binary32 (bf16 only), gets the scale NaN: all of it is read as NaN.  Rows in no page are dropped (deferred E_CAPACITY for the
  * reasons above; silently for a negative position).  Two rows of one call must not land in the same slot.
  * Errors: E_NULL, E_SHAPE, E_ALIGN (16 bytes), E_PARAM (unsupported value; the current device is not the context's),
  * E_CUDA.

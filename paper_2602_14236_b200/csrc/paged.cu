@@ -74,10 +74,11 @@ __device__ __forceinline__ void map_rows(RowMap<ROWS>& m, const PgSeqs& sq, cons
 __device__ __forceinline__ uint32_t rint_bits(float d, float inv) {
     return __float_as_uint(__fadd_rn(__fmul_rn(d, inv), 12582912.0f));
 }
+// A NaN among the two is the result.
 template <typename T>
-__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) { return as_word(__hmax2(as_pair<T>(a), as_pair<T>(b))); }
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) { return as_word(__hmax2_nan(as_pair<T>(a), as_pair<T>(b))); }
 template <typename T>
-__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) { return as_word(__hmin2(as_pair<T>(a), as_pair<T>(b))); }
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) { return as_word(__hmin2_nan(as_pair<T>(a), as_pair<T>(b))); }
 
 // Four words per lane, each the two halves' maximum to be taken over a group of LPG lanes: quarter u of the group's lanes
 // (lane / (LPG / 4)) gets word u's.
@@ -129,16 +130,18 @@ __device__ __forceinline__ void store_groups(const uint4 (&v)[PM_AHEAD], const R
             e[u] = max2<T>(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
         }
     }
-    const uint32_t x = quarter_max<T, LPG>(e, gl);
+    uint32_t x = quarter_max<T, LPG>(e, gl);
+    if (FMT == PF_I8) x = max2<T>(x, __byte_perm(x, 0u, 0x1032));
     const int mine = gl / Q;                 // the group whose scale this lane forms
     const float zero = FMT == PF_I4 ? -T::hi(x) : 0.0f;
-    const float span = FMT == PF_I4 ? __fsub_rn(T::lo(x), zero) : fmaxf(T::lo(x), T::hi(x));
+    const float span = FMT == PF_I4 ? __fsub_rn(T::lo(x), zero) : T::lo(x);
     uint16_t s16 = T::round(__fdiv_rn(span, FMT == PF_I4 ? 15.0f : 127.0f));
     float inv = __frcp_rn(T::lo(s16));
     if (!(inv < INFINITY)) {                 // zero, and what has no reciprocal in binary32
         s16 = (uint16_t)T::ONE;
         inv = 1.0f;
     }
+    if (!(span < INFINITY)) s16 = (uint16_t)T::NOT_A_NUMBER;         // whatever the codes: every value of the group is read as NaN
     if (live && gl % Q == 0 && p0 + mine < p1) {
         uint8_t* at = rp.scale + (p0 + mine) * rp.scale_step;
         if (FMT == PF_I8) *reinterpret_cast<uint16_t*>(at) = s16;

@@ -15,7 +15,7 @@ struct TypeF16 {
         return *reinterpret_cast<uint32_t*>(&h);
     }
     static __device__ __forceinline__ uint16_t round(float a) { return __half_as_ushort(__float2half_rn(a)); }
-    static constexpr uint32_t ONE = 0x3c00u, NORMAL = 0x0400u;     // 1, the smallest normal number
+    static constexpr uint32_t ONE = 0x3c00u, NORMAL = 0x0400u, NOT_A_NUMBER = 0x7e00u;      // 1, the smallest normal number
 };
 struct TypeBF16 {
     using pair = __nv_bfloat162;
@@ -26,7 +26,7 @@ struct TypeBF16 {
         return *reinterpret_cast<uint32_t*>(&h);
     }
     static __device__ __forceinline__ uint16_t round(float a) { return __bfloat16_as_ushort(__float2bfloat16_rn(a)); }
-    static constexpr uint32_t ONE = 0x3f80u, NORMAL = 0x0080u;
+    static constexpr uint32_t ONE = 0x3f80u, NORMAL = 0x0080u, NOT_A_NUMBER = 0x7fc0u;
 };
 template <typename T>
 __device__ __forceinline__ typename T::pair as_pair(uint32_t w) { return *reinterpret_cast<typename T::pair*>(&w); }

@@ -54,3 +54,34 @@ def test_written_and_read_at_the_ends_of_the_range(ctx, fmt, dt, largest, D):
     want = pu.decode(*pu.encode(x, fmt, t), fmt, t)
     assert np.isfinite(want).all()
     assert np.array_equal(_stored(ctx, x, fmt, t), want)
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "int8", "int4"])
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_group_that_is_not_finite_is_read_as_nan(ctx, fmt, dt, D):
+    """All of it, wherever in it the NaN or the infinity stands, and none of its neighbours; 16-bit pages hold a copy."""
+    t = _t(dt)
+    rng = np.random.default_rng(81)
+    x = pu.to_t(rng.standard_normal((2, 40, 5, D)), t)
+    want = pu.decode(*pu.encode(x, fmt, t), fmt, t)
+    at = 0
+    for r, v in enumerate([[np.nan], [np.inf], [-np.inf], [np.inf, -np.inf], [np.nan, np.inf], [np.nan, np.nan]] * 6):
+        for kv, h in ((0, 1), (1, 4)) if r % 2 else ((0, 3), (1, 0)):
+            for a in v:
+                at = (at * 5 + 3) % D
+                x[kv, r, h, at] = a
+            want[kv, r, h] = x[kv, r, h] if fmt == "fp16" else np.nan
+    assert np.array_equal(_stored(ctx, x, fmt, t), want, equal_nan=True)
+
+
+def test_a_span_past_binary32_is_read_as_nan(ctx):
+    t = _t("bf16")
+    x = pu.to_t(np.random.default_rng(82).standard_normal((2, 3, 2, 128)), t)
+    x[0, 1, 0, 3], x[0, 1, 0, 90] = 3.0e38, -3.0e38
+    x = pu.to_t(x, t)
+    ordinary = x.copy()
+    ordinary[0, 1, 0] = 0.0
+    want = pu.decode(*pu.encode(ordinary, "int4", t), "int4", t)
+    want[0, 1, 0] = np.nan
+    assert np.array_equal(_stored(ctx, x, "int4", t), want, equal_nan=True)
