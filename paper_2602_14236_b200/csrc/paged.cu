@@ -54,8 +54,7 @@ __device__ __forceinline__ void map_rows(RowMap<ROWS>& m, const PgSeqs& sq, cons
                 if (r >= s.row0 && r < s.row0 + s.n) {
                     slot = -1;
                     if (pos >= 0) {
-                        const int pg = pos >> pc.page_shift;
-                        if (pg < sq.width) pid = sq.table[(size_t)b * sq.width + pg];
+                        if (pos < s.len) pid = sq.table[(size_t)b * sq.width + (pos >> pc.page_shift)];
                         if (pid >= 0 && pid < pc.n_pages) slot = pos & ((1 << pc.page_shift) - 1);
                         else {
                             pid = -1;

@@ -85,3 +85,37 @@ def test_a_span_past_binary32_is_read_as_nan(ctx):
     want = pu.decode(*pu.encode(ordinary, "int4", t), "int4", t)
     want[0, 1, 0] = np.nan
     assert np.array_equal(_stored(ctx, x, "int4", t), want, equal_nan=True)
+
+
+def test_positions_from_two_to_the_thirtieth_on_are_in_no_page(ctx):
+    """A table that reaches past them: they are dropped, come back as zeros and are left out, with E_CAPACITY each time."""
+    import torch
+    t, D, page, n = torch.float16, 64, 128, 10
+    width = 2 ** 30 // page + 1
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, -2:] = torch.tensor([1, 0], dtype=torch.int32)
+    pages = sc.PageSet(2, page, 1, D, sc.FP16, t)
+    seqs = sc.Seqs(_i32([0, n]), _i32([2 ** 30 + 4]), table, n)         # rows 0 .. 5 below 2^30
+    x = torch.randn((3, n, D), device="cuda").to(t)
+    sc.salicache_paged_write(ctx, pages.c, seqs.c, x[0], x[1], D, D)
+    assert sc.salicache_poll_status(ctx) == sc.E_CAPACITY
+    assert (pages.data[0] == 0).all()
+    assert torch.equal(pages.data[1, :, 0, page - 6:], x[:2, :6])
+    out = torch.full((2, n, D), 7.0, dtype=t, device="cuda")
+    sc.salicache_paged_read(ctx, pages.c, seqs.c, out[0], out[1], D, D)
+    assert sc.salicache_poll_status(ctx) == sc.E_CAPACITY
+    assert torch.equal(out[:, :6], x[:2, :6]) and (out[:, 6:] == 0).all()
+    # window 3: the row at position p sees p - 2 .. p, below 2^30
+    work = torch.empty(sc.salicache_paged_work_bytes(ctx, pages.c, 1), dtype=torch.uint8, device="cuda")
+    o, lse = torch.empty((n, D), dtype=t, device="cuda"), torch.empty((n, 1), device="cuda")
+    sc.salicache_paged_attend(ctx, pages.c, seqs.c, x[2], D, 1, 0.125, 3, 0, o, D, lse, work, work.numel())
+    assert sc.salicache_poll_status(ctx) == sc.E_CAPACITY
+    q, k, v = (y.double().cpu().numpy() for y in (x[2], x[0], x[1]))
+    for i in range(n):
+        j = np.arange(max(0, i - 2), min(i + 1, 6))
+        # positions before row 0 hold zeros: rows 0 and 1 see two and one of them
+        z = np.zeros((max(0, 2 - i), D))
+        kk, vv = (np.concatenate([z, y[j]]) for y in (k, v))
+        want, wl, tol, ltol = pu.attend(q[i], kk, vv, 0.125, t, "fp16")
+        pu.check(o[i].double().cpu().numpy(), want, tol, f"row {i}")
+        pu.check(lse[i, 0].item(), wl, ltol, f"lse {i}")
