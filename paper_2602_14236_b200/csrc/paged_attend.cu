@@ -333,6 +333,7 @@ k_paged_step(PtArgs a, int blocks) {
             }
             const int j0 = sp.tile(k) * PT_KEYS + wid * 16;
             if (!(*(volatile uint32_t*)&kinds[st] >> wid & 1u)) {
+                __syncwarp();                // every lane has read it: the feeder may write the next one
                 if (lane == 0) bar_arrive(smem_u32(&empty[st]));
                 continue;
             }
