@@ -481,6 +481,15 @@ SALICACHE_API int salicache_paged_attend(salicache_ctx* ctx, const salicache_pag
 /* Bytes of d_work for salicache_paged_attend over such pages (any batch), or a negative error. */
 SALICACHE_API int64_t salicache_paged_work_bytes(const salicache_ctx* ctx, const salicache_pages* pages, int q_per_kv);
 
+/*
+ * How often a part of a block inside salicache_paged_attend looks for what another part has to bring before it gives up:
+ * `tries` times in calls made (or captured) from now on, 2^24 at first, which takes a second or more.  A call in which a
+ * wait is given up ends what it has under way, returns, and records E_CUDA in the status word; its rows of d_out and
+ * d_lse are undefined.  0 gives up every wait, so that a caller can test what it does then.  Errors: E_NULL, E_PARAM
+ * (negative).
+ */
+SALICACHE_API int salicache_paged_wait_limit(salicache_ctx* ctx, int tries);
+
 /* Synchronises `cuda_stream`, returns the deferred device status (0, E_CAPACITY, E_NOCONVERGE or
  * E_EVICTED; E_CUDA if the stream reports an error, or a wait inside salicache_paged_attend ran out) and clears it. */
 SALICACHE_API int salicache_poll_status(salicache_ctx* ctx, void* cuda_stream);

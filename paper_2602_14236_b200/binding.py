@@ -71,7 +71,7 @@ EXPORTS = [
     "salicache_frame_redundancy", "salicache_source_frames", "salicache_diff_score", "salicache_attend",
     "salicache_select_anchored", "salicache_select_ranked", "salicache_attend_gqa", "salicache_select_anchored_batch",
     "salicache_frames_resident", "salicache_tokens_live", "salicache_paged_write", "salicache_paged_read",
-    "salicache_paged_attend", "salicache_paged_work_bytes",
+    "salicache_paged_attend", "salicache_paged_work_bytes", "salicache_paged_wait_limit",
 ]
 
 _lib = None
@@ -117,6 +117,7 @@ def lib():
         _lib.salicache_paged_read.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, vp, i64, i64, vp]
         _lib.salicache_paged_attend.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, i64, i32, C.c_float, i32, i32, vp, i64,
                                                 vp, vp, i64, vp]
+        _lib.salicache_paged_wait_limit.argtypes = [vp, i32]
         _lib.salicache_paged_work_bytes.argtypes = [vp, C.POINTER(Pages), i32]
         _lib.salicache_paged_work_bytes.restype = i64
         _lib.salicache_tokens_live.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp]
@@ -331,6 +332,10 @@ def salicache_paged_attend(ctx: Context, pages: Pages, seqs: SeqsC, d_q, q_strid
                                       st if stream is None else stream.cuda_stream)
     if rc:
         raise SalicacheError(rc, "salicache_paged_attend")
+
+
+def salicache_paged_wait_limit(ctx: Context, tries: int):
+    _check(lib().salicache_paged_wait_limit(ctx.handle, tries), "salicache_paged_wait_limit")
 
 
 def salicache_poll_status(ctx: Context, stream=None) -> int:

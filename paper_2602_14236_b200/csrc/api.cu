@@ -114,6 +114,7 @@ int salicache_create(salicache_ctx** out, const salicache_params* p) {
     }
     c->sm_count = prop.multiProcessorCount;
     c->device = dev;
+    c->paged_wait = 1 << 24;
     const size_t P0 = (size_t)p->H * p->W;
     const size_t slots = (size_t)2 * c->chunk;   // independent pairs need prev and cur; a video needs chunk+1
     const int words = (p->W + 31) / 32;
@@ -475,6 +476,13 @@ int64_t salicache_paged_work_bytes(const salicache_ctx* c, const salicache_pages
     if (q_per_kv < 1 || q_per_kv > 64) return SALICACHE_E_PARAM;
     if (!c) return SALICACHE_E_NULL;
     return sc_paged_work_bytes(c, pages->head_dim);
+}
+
+int salicache_paged_wait_limit(salicache_ctx* c, int tries) {
+    if (!c) return SALICACHE_E_NULL;
+    if (tries < 0) return SALICACHE_E_PARAM;
+    c->paged_wait = tries;
+    return SALICACHE_OK;
 }
 
 int salicache_paged_attend(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, const void* d_q,

@@ -53,6 +53,7 @@ struct salicache_ctx {
     int* d_status;             // deferred status word
     int sm_count;
     int device;                // the CUDA device the context was created on
+    int paged_wait;            // tries before a wait inside the paged attention is given up
     long long launches;        // kernels launched through this context so far
 };
 

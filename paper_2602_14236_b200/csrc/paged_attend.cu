@@ -226,7 +226,7 @@ k_paged_step(PtArgs a, int blocks) {
             g.set(a, w, s);
             if (g.tiles > 0) {               // the item's rows of q, a lane per row
                 const uint32_t qb = n_q & 1, bar = smem_u32(&q_full[qb]);
-                if (n_q >= 2) bar_wait(smem_u32(&q_empty[qb]), (n_q / 2 - 1) & 1, gave_up);
+                if (n_q >= 2 && !warp_wait(smem_u32(&q_empty[qb]), (n_q / 2 - 1) & 1, a.wait_limit, gave_up)) break;
                 __syncwarp();
                 if (lane == 0) bar_expect(bar, (uint32_t)g.rows * (D * 2));
                 __syncwarp();
@@ -238,8 +238,7 @@ k_paged_step(PtArgs a, int blocks) {
                 ++n_q;
             }
             int next = g.tiles > 0 ? g.page_of(a, w, g.t0, lane) : -2;
-            for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k, ++n_stage) {
-                ok = *gave_up == 0;
+            for (int k = g.t0; k < g.t0 + g.tiles; ++k, ++n_stage) {
                 const int pid16 = next;
                 next = k + 1 < g.t0 + g.tiles ? g.page_of(a, w, k + 1, lane) : -2;
                 const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), need = __ballot_sync(0xffffffffu, pid16 >= 0);
@@ -249,7 +248,10 @@ k_paged_step(PtArgs a, int blocks) {
                 const int pid = __shfl_sync(0xffffffffu, pid16, from);
                 const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine != 0 && piece == 0));
                 const uint32_t st = n_stage % STAGES, bar = smem_u32(&full[st]), dst = smem_u32(ring) + st * SM::STAGE;
-                if (n_stage >= STAGES) bar_wait(smem_u32(&empty[st]), (n_stage / STAGES - 1) & 1, gave_up);
+                if (n_stage >= STAGES && !warp_wait(smem_u32(&empty[st]), (n_stage / STAGES - 1) & 1, a.wait_limit, gave_up)) {
+                    ok = false;
+                    break;
+                }
                 __syncwarp();
                 if (lane == 0) {
                     *(volatile uint32_t*)&kinds[st] = need;
@@ -266,11 +268,10 @@ k_paged_step(PtArgs a, int blocks) {
             w.left -= g.k1 - g.k0;
             if (w.left > 0) pt_next(w, s, a);
         }
-        if (!ok) {                           // given up: copies in flight end before the block does
-            for (uint32_t i = n_stage > STAGES ? n_stage - STAGES : 0; i < n_stage; ++i)
-                for (int t = 0; t < (1 << 16) && !bar_try(smem_u32(&full[i % STAGES]), (i / STAGES) & 1); ++t) {}
-            for (uint32_t i = n_q > 2 ? n_q - 2 : 0; i < n_q; ++i)
-                for (int t = 0; t < (1 << 16) && !bar_try(smem_u32(&q_full[i & 1]), (i / 2) & 1); ++t) {}
+        join_roles();
+        if (*gave_up) {                      // copies in flight end before the block does
+            for (uint32_t i = n_stage > STAGES ? n_stage - STAGES : 0; i < n_stage; ++i) bar_drain(smem_u32(&full[i % STAGES]), (i / STAGES) & 1);
+            for (uint32_t i = n_q > 2 ? n_q - 2 : 0; i < n_q; ++i) bar_drain(smem_u32(&q_full[i & 1]), (i / 2) & 1);
         }
         return;
     }
@@ -289,14 +290,14 @@ k_paged_step(PtArgs a, int blocks) {
 
         // q as B fragments: column g8 of column tile n is row 8 n + g8
         uint32_t qf[NT][KS][2];
+        bool on = true;                      // no wait of this warp has been given up in this item
         if (g.tiles > 0) {
             const uint32_t qb = n_q & 1;
-            bar_wait(smem_u32(&q_full[qb]), (n_q / 2) & 1, gave_up);
-            __syncwarp();
+            on = warp_wait(smem_u32(&q_full[qb]), (n_q / 2) & 1, a.wait_limit, gave_up);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const uint32_t src = q_ring + qb * SM::Q + (8 * n + g8) * (D * 2);
-                const bool in = 8 * n + g8 < rows;
+                const bool in = on && 8 * n + g8 < rows;
 #pragma unroll
                 for (int st = 0; st < KS; ++st) {
                     int d[4];
@@ -311,7 +312,7 @@ k_paged_step(PtArgs a, int blocks) {
                 }
             }
             __syncwarp();
-            if (lane == 0) bar_arrive(smem_u32(&q_empty[qb]));
+            if (lane == 0 && on) bar_arrive(smem_u32(&q_empty[qb]));
             ++n_q;
         }
         float acc[NT][VS][4], m[NT][2], l[NT][2];
@@ -323,10 +324,10 @@ k_paged_step(PtArgs a, int blocks) {
             for (int t = 0; t < VS; ++t) acc[n][t][0] = acc[n][t][1] = acc[n][t][2] = acc[n][t][3] = 0.0f;
         }
 
-        for (int k = g.t0; k < g.t0 + g.tiles; ++k) {
+        for (int k = g.t0; on && k < g.t0 + g.tiles; ++k) {
             const uint32_t st = stage, src = smem_u32(ring) + st * SM::STAGE;
-            bar_wait(smem_u32(&full[st]), phase, gave_up);
-            __syncwarp();
+            on = warp_wait(smem_u32(&full[st]), phase, a.wait_limit, gave_up);
+            if (!on) break;
             if (++stage == STAGES) {
                 stage = 0;
                 phase ^= 1;
@@ -445,7 +446,7 @@ k_paged_step(PtArgs a, int blocks) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sh_acc[wid][lr + (i & 1)][value_dim<FMT, D>(t, i >> 1, g8)] = acc[n][t][i];
             }
-            ok = !any_of(*gave_up != 0);
+            ok = !any_of(!on);
             const int r = r0 + (wid >> 1), d0 = (wid & 1) * (D / 2) + lane * (D / 64);        // two warps per row
             if (r < rows && ok) {
                 float M = PT_NONE, L = 0.0f, o[D / 64];
@@ -479,7 +480,7 @@ k_paged_step(PtArgs a, int blocks) {
             }
             any_of(false);
         }
-        if (!done && g.real) {
+        if (!done && g.real && ok) {
             if (first) {
                 pt_tail(hd, w, s);
             } else hd[0].x = g.last ? 2 : 1;
@@ -487,10 +488,11 @@ k_paged_step(PtArgs a, int blocks) {
         w.left -= g.k1 - g.k0;
         if (w.left > 0) pt_next(w, s, a);
     }
+    join_roles();
     if (threadIdx.x == 0) {
         a.head[2 * c] = hd[0];
         a.head[2 * c + 1] = hd[1];
-        if (sh_gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
+        if (*gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
     }
 }
 
@@ -541,6 +543,7 @@ int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache
     a.sinks = window ? sinks : 0;
     a.scale = softmax_scale * PT_LOG2E;
     a.status = c->d_status;
+    a.wait_limit = c->paged_wait;
     char* work = (char*)d_work;
     // Rows (of q, times the query heads of a group) per sequence up to which reading the pages is the work: 8 of 16-bit
     // pages, 16 of codes.  Measured with 16 sequences of 8000 positions, 8 key/value heads, this kernel against

@@ -155,7 +155,7 @@ __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 
 
 struct ChBars {
     uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_land[2], q_ready[2], q_empty[2], v_land[2], s_full[2], p_ready[2][2],
-        o_done[2];
+        o_done[2], left;
     uint32_t tmem;
     int gave_up;
     uint32_t pages[8];                       // per tile (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
@@ -204,7 +204,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
 
     if (tid == 0) {
         for (int i = 0; i < CH_STAGES; ++i) {
-            bar_init(smem_u32(&bars.kv_full[i]), FMT == PF_16 ? 5 : 4);      // the four warps of group 2, and the feeder
+            bar_init(smem_u32(&bars.kv_full[i]), 4);       // the four warps of group 2, or four lanes of the feeder
             bar_init(smem_u32(&bars.kv_empty[i]), 1);
         }
         for (int i = 0; i < CH_RAW; ++i) {
@@ -221,6 +221,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
             bar_init(smem_u32(&bars.p_ready[i][1]), 4);
             bar_init(smem_u32(&bars.o_done[i]), 1);
         }
+        bar_init(smem_u32(&bars.left), 1);
         bars.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -239,28 +240,28 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
     const uint32_t tmem = bars.tmem;
     ChSeg g;
     const int HR = a.tile_rows >> 1;         // rows of a half
+    auto wait = [&](uint64_t& bar, uint32_t parity) -> bool { return warp_wait_far(smem_u32(&bar), parity, a.wait_limit, gave_up); };
 
     if (wid < 8) {
         // ---------------- rows: softmax, Q, output
         const int half = wid >> 2, row = tid & 127;
         const uint32_t lane_base = (uint32_t)((wid & 3) * 32) << 16;
         const uint32_t S = tmem + 128 * half + lane_base, O = tmem + 256 + 128 * half + lane_base;
-        const uint32_t q_ready = smem_u32(&bars.q_ready[half]), s_full = smem_u32(&bars.s_full[half]);
-        const uint32_t p_ready = smem_u32(&bars.p_ready[half][0]), o_done = smem_u32(&bars.o_done[half]);
+        const uint32_t q_ready = smem_u32(&bars.q_ready[half]), p_ready = smem_u32(&bars.p_ready[half][0]);
         const uint32_t q_tile = base + SM::Q + half * SM::TILE;
         uint32_t n_s = 0, n_o = 0, n_tile = 0;               // scores, outputs of this half and tiles seen so far
         int4 hd[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
         bool ok = true;
         uint32_t n_q = 0;
-        auto hand_q = [&](const ChSeg& gg) {
-            if (FMT != PF_I4 || gg.rows <= half * HR || gg.tiles == 0) return;
-            bar_wait_far(smem_u32(&bars.q_land[half]), n_q++ & 1, gave_up);
-            __syncwarp();
+        auto hand_q = [&](const ChSeg& gg) -> bool {
+            if (FMT != PF_I4 || gg.rows <= half * HR || gg.tiles == 0) return true;
+            if (!wait(bars.q_land[half], n_q++ & 1)) return false;
             permute_rows<D>(q_tile, q_ready);
+            return true;
         };
         if (w.left > 0) {
             g = ChSeg::of(a, w, s);
-            hand_q(g);
+            ok = hand_q(g);
         }
         while (w.left > 0 && ok) {
             const bool first = g.t0 == 0, lastp = g.last, done = first && lastp;
@@ -285,11 +286,12 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                     const PtSpan hs = pt_span(s, a.G, w.rt * a.tile_rows + half * HR, w.rt * a.tile_rows + half * HR + rows, a.window, a.sinks);
                     const int vis_hi = live ? max(0, min(pos + 1, s.len)) : 0;
                     const int vis_lo = a.window ? pos - a.window + 1 : 0;
-                    for (int k = 0; k < g.tiles && ok; ++k, ++n_tile) {
-                        bar_wait_far(s_full, n_s++ & 1, gave_up);
-                        __syncwarp();
+                    for (int k = 0; k < g.tiles; ++k, ++n_tile) {
+                        if (!wait(bars.s_full[half], n_s++ & 1)) {
+                            ok = false;
+                            break;
+                        }
                         tc_after();
-                        ok = *gave_up == 0;
                         const int j0 = g.sp.tile(g.t0 + k) * PT_KEYS;
                         const uint32_t pages = *(volatile uint32_t*)&bars.pages[n_tile & 7];
                         uint32_t x[2][32];
@@ -363,10 +365,9 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     }
                     if (ok) {
-                        hand_q(gn);
+                        ok = hand_q(gn);
                         handed = true;
-                        bar_wait_far(o_done, n_o++ & 1, gave_up);
-                        __syncwarp();
+                        ok = ok && wait(bars.o_done[half], n_o++ & 1);
                         tc_after();
                     }
                 }
@@ -409,8 +410,8 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                     if (live && !done) a.stat[slot * CH_ROWS + half * 128 + row] = make_float2(m, l);
                 }
             } else n_tile += g.tiles;
-            if (!handed) hand_q(gn);
-            if (!done && g.real) {
+            if (ok && !handed) ok = hand_q(gn);
+            if (!done && g.real && ok) {
                 if (first) pt_tail(hd, w, s);
                 else hd[0].x = lastp ? 2 : 1;
             }
@@ -431,7 +432,6 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
         while (w.left > 0 && ok) {
             g = ChSeg::of(a, w, s);
             for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k) {
-                ok = *gave_up == 0;
                 const int j0 = g.sp.tile(k) * PT_KEYS;
                 const int pid = g.page_of(a, w, k, lane);
                 const uint32_t bad = __ballot_sync(0xffffffffu, pid == -1);
@@ -443,30 +443,32 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                 };
                 for (int kv = 0; kv < 2; ++kv, ++n_stage) {
                     const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE;
-                    if (n_stage >= CH_STAGES)
-                        bar_wait_far(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
-                    __syncwarp();
                     if (FMT == PF_16) {
-                        if (kv == 1 && !clean) {         // the pages have been copied: zeros where no row sees them
-                            bar_wait_far(smem_u32(&bars.v_land[n_land & 1]), n_land >> 1 & 1, gave_up);
-                            ++n_land;
-                            __syncwarp();
-                            constexpr int LPR = D / 8, RPP = 32 / LPR;
-                            const int c = lane % LPR;
-#pragma unroll 1
-                            for (int p = 0; p < 32 / RPP; ++p) {
-                                const int r = p * RPP + lane / LPR;
-                                if (!seen(r)) sts16(dst + swz(lw * 32 + r, c), 0u, 0u, 0u, 0u);
-                            }
-                            fence_async();
-                            __syncwarp();
+                        if (kv == 0 || clean) continue;  // the feeder's copies are all there is to it
+                        // the pages have been copied: zeros where no row sees them
+                        if (!wait(bars.v_land[n_land & 1], n_land >> 1 & 1)) {
+                            ok = false;
+                            break;
                         }
+                        ++n_land;
+                        constexpr int LPR = D / 8, RPP = 32 / LPR;
+                        const int c = lane % LPR;
+#pragma unroll 1
+                        for (int p = 0; p < 32 / RPP; ++p) {
+                            const int r = p * RPP + lane / LPR;
+                            if (!seen(r)) sts16(dst + swz(lw * 32 + r, c), 0u, 0u, 0u, 0u);
+                        }
+                        fence_async();
+                        __syncwarp();
                     } else {
                         constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
                         constexpr int LPR = pg_row_bytes<FMT, D>() >= 16 ? pg_row_bytes<FMT, D>() / 16 : 1, RPP = 32 / LPR;
                         const uint32_t rs = n_stage % N_RAW, raw0 = base + SM::RAWS + rs * SM::RAW;
-                        bar_wait_far(smem_u32(&bars.raw_full[rs]), (n_stage / N_RAW) & 1, gave_up);
-                        __syncwarp();
+                        if ((n_stage >= CH_STAGES && !wait(bars.kv_empty[stage], (n_stage / CH_STAGES - 1) & 1)) ||
+                            !wait(bars.raw_full[rs], (n_stage / N_RAW) & 1)) {
+                            ok = false;
+                            break;
+                        }
                         const int c = lane % LPR;
                         constexpr int BATCH = LPR < 4 ? LPR : 4;             // rows in flight
 #pragma unroll
@@ -521,10 +523,6 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
             uint32_t n_stage = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
             bool ok = true;
             const uint32_t q_lo = desc_lo(base + SM::Q, 16), k_lo = desc_lo(base + SM::KV, 16), v_lo = desc_lo(base + SM::KV, 16384);
-            auto wait = [&](uint64_t& bar, uint32_t parity) {
-                bar_wait_far(smem_u32(&bar), parity, gave_up);
-                __syncwarp();
-            };
             auto scores = [&](int h, uint32_t st, bool last) {
                 const uint32_t qa = q_lo + h * (SM::TILE >> 4), kb = k_lo + st * (SM::TILE >> 4);
                 if (elect_one()) {
@@ -550,21 +548,22 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
             while (w.left > 0 && ok) {
                 g = ChSeg::of(a, w, s);
                 const int halves = g.rows > HR ? 2 : 1;
-                for (int h = 0; h < halves && g.tiles > 0; ++h) wait(FMT == PF_I4 ? bars.q_ready[h] : bars.q_land[h], n_q[h]++ & 1);
+                for (int h = 0; h < halves && g.tiles > 0 && ok; ++h) ok = wait(FMT == PF_I4 ? bars.q_ready[h] : bars.q_land[h], n_q[h]++ & 1);
                 for (int t = 0; t <= g.tiles && ok && g.tiles > 0; ++t) {
-                    ok = *gave_up == 0;
                     // stages in order: K(0), V(0), K(1), ...: V(t - 1) then K(t)
                     const uint32_t vs = n_stage, ks = t > 0 ? n_stage + 1 : n_stage;
-                    if (t > 0) wait(bars.kv_full[vs % CH_STAGES], (vs / CH_STAGES) & 1);
-                    if (t < g.tiles) wait(bars.kv_full[ks % CH_STAGES], (ks / CH_STAGES) & 1);
+                    if (t > 0) ok = wait(bars.kv_full[vs % CH_STAGES], (vs / CH_STAGES) & 1);
+                    if (t < g.tiles && ok) ok = wait(bars.kv_full[ks % CH_STAGES], (ks / CH_STAGES) & 1);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        if (h >= halves) break;
+                        if (h >= halves || !ok) break;
                         if (t > 0) {
-                            wait(bars.p_ready[h][0], n_p[h] & 1);
+                            ok = wait(bars.p_ready[h][0], n_p[h] & 1);
+                            if (!ok) break;
                             tc_after();
                             sums(h, vs % CH_STAGES, 0, t > 1, false);
-                            wait(bars.p_ready[h][1], n_p[h]++ & 1);
+                            ok = wait(bars.p_ready[h][1], n_p[h]++ & 1);
+                            if (!ok) break;
                             tc_after();
                             sums(h, vs % CH_STAGES, 1, true, t == g.tiles);
                         }
@@ -573,6 +572,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                             scores(h, ks % CH_STAGES, t == g.tiles - 1);
                         }
                     }
+                    if (!ok) break;
                     if (elect_one()) {
                         if (t > 0) tc_commit(smem_u32(&bars.kv_empty[vs % CH_STAGES]));
                         if (t < g.tiles) tc_commit(smem_u32(&bars.kv_empty[ks % CH_STAGES]));
@@ -583,11 +583,22 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                 w.left -= g.k1 - g.k0;
                 if (w.left > 0) pt_next_far(w, s, a);
             }
+            // what the instructions' ends arrive at is there until they have: the last uses of the stages and of Q, which
+            // nobody else waits for; after an early leave, all that is under way
+            for (uint32_t i = n_stage > CH_STAGES ? n_stage - CH_STAGES : 0; i < n_stage && ok; ++i) ok = wait(bars.kv_empty[i % CH_STAGES], (i / CH_STAGES) & 1);
+            for (int h = 0; h < 2 && ok; ++h)
+                if (n_q[h] > 0) ok = wait(bars.q_empty[h], (n_q[h] - 1) & 1);
+            if (!ok) {
+                if (elect_one()) tc_commit(smem_u32(&bars.left));
+                __syncwarp();
+                bar_drain(smem_u32(&bars.left), 0);
+            }
         }
         if (wid == 13) {
             // ---------------- feeder: lane i < 128 / page copies page i of a tile
             uint32_t n_stage = 0, n_tile = 0;
             uint32_t n_q[2] = {0, 0}, n_land = 0;
+            uint32_t landed = 0;                     // bit i: the copies of the last stage but i arrive on kv_full
             bool ok = true;
             const int per_page = 1 << a.pc.page_shift, n_pages = PT_KEYS >> a.pc.page_shift;
             if (FMT == PF_16 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
@@ -595,7 +606,6 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                 g = ChSeg::of(a, w, s);
                 int pid16 = g.tiles > 0 ? g.page_of(a, w, g.t0, lane) : -2;
                 for (int k = g.t0; k < g.t0 + g.tiles && ok; ++k, ++n_tile) {
-                    ok = *gave_up == 0;
                     const int pid16n = k + 1 < g.t0 + g.tiles ? g.page_of(a, w, k + 1, lane) : -2;
                     const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), need = __ballot_sync(0xffffffffu, pid16 >= 0);
                     const bool clean = g.clean(a, k) && bad == 0;
@@ -609,9 +619,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                         const size_t slot = pg_slot(a.pc, mine ? pid : 0, kv, w.h, 0);
                         if (FMT == PF_16) {
                             const uint32_t stage = n_stage % CH_STAGES, dst = base + SM::KV + stage * SM::TILE, bar = smem_u32(&bars.kv_full[stage]);
-                            if (n_stage >= CH_STAGES)
-                                bar_wait_far(smem_u32(&bars.kv_empty[stage]), (n_stage / CH_STAGES - 1) & 1, gave_up);
-                            __syncwarp();
+                            if (n_stage >= CH_STAGES && !wait(bars.kv_empty[stage], (n_stage / CH_STAGES - 1) & 1)) {
+                                ok = false;
+                                break;
+                            }
                             // V with keys that no row sees goes through group 2, which waits for it by barriers of their own (two: as
                             // many V stages as the ring has)
                             const bool direct = kv == 0 || clean;
@@ -619,9 +630,9 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                             if (lane == 0) {
                                 if (kv == 0) *(volatile uint32_t*)&bars.pages[n_tile & 7] = ~bad & 0xffu;
                                 bar_expect(land, copies * (uint32_t)(per_page * D * 2));
-                                if (!direct) bar_arrive(bar);
-                            }
+                            } else if (direct && lane < 4) bar_arrive(bar);
                             n_land += !direct;
+                            landed = landed << 1 | (uint32_t)direct;
                             __syncwarp();
                             if (mine) {
 #pragma unroll
@@ -630,9 +641,10 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                         } else {
                             constexpr int N_RAW = SM::N_RAW > 0 ? SM::N_RAW : 1;
                             const uint32_t rs = n_stage % N_RAW, dst = base + SM::RAWS + rs * SM::RAW, bar = smem_u32(&bars.raw_full[rs]);
-                            if (n_stage >= N_RAW)
-                                bar_wait_far(smem_u32(&bars.raw_empty[rs]), (n_stage / N_RAW - 1) & 1, gave_up);
-                            __syncwarp();
+                            if (n_stage >= N_RAW && !wait(bars.raw_empty[rs], (n_stage / N_RAW - 1) & 1)) {
+                                ok = false;
+                                break;
+                            }
                             constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
                             if (lane == 0) {
                                 if (kv == 0) *(volatile uint32_t*)&bars.pages[n_tile & 7] = ~bad & 0xffu;
@@ -646,11 +658,13 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                         }
                     }
                     pid16 = pid16n;
-                    if (k == g.t0) {                     // Q behind the first tile: a lane per half
+                    if (k == g.t0 && ok) {               // Q behind the first tile: a lane per half
                         for (int h = 0; h < 2; ++h) {
                             if (h > 0 && g.rows <= HR) break;
-                            if (n_q[h] > 0) bar_wait_far(smem_u32(&bars.q_empty[h]), (n_q[h] - 1) & 1, gave_up);
-                            __syncwarp();
+                            if (n_q[h] > 0 && !wait(bars.q_empty[h], (n_q[h] - 1) & 1)) {
+                                ok = false;
+                                break;
+                            }
                             ++n_q[h];
                             if (lane == 0) {
                                 const uint32_t bar = smem_u32(&bars.q_land[h]);
@@ -665,34 +679,27 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
                 w.left -= g.k1 - g.k0;
                 if (w.left > 0) pt_next_far(w, s, a);
             }
-            // copies in flight end before the block does: their stages have been waited for by those who used them; after
-            // an early leave, wait here
-            if (!ok) {
-                const uint32_t n = FMT == PF_16 ? CH_STAGES : (SM::N_RAW > 0 ? SM::N_RAW : 1);
-                for (uint32_t i = n_stage > n ? n_stage - n : 0; i < n_stage; ++i) {
-                    const uint32_t bar = FMT == PF_16 ? smem_u32(&bars.kv_full[i % n]) : smem_u32(&bars.raw_full[i % n]);
-                    for (int t = 0; t < (1 << 16) && !bar_try(bar, (i / n) & 1); ++t) {}
+            join_roles();
+            // copies in flight end before the block does: who uses a stage waits for them, unless a role has left early
+            if (*gave_up) {
+                constexpr uint32_t N = FMT == PF_16 ? CH_STAGES : SM::N_RAW > 0 ? SM::N_RAW : 1;
+                for (uint32_t x = 0; x < N && x < n_stage; ++x) {
+                    const uint32_t i = n_stage - 1 - x;
+                    if (FMT != PF_16) bar_drain(smem_u32(&bars.raw_full[i % N]), (i / N) & 1);
+                    else if (landed >> x & 1u) bar_drain(smem_u32(&bars.kv_full[i % N]), (i / N) & 1);
                 }
                 for (int h = 0; h < 2; ++h)
-                    for (int t = 0; t < (1 << 16) && n_q[h] > 0 && !bar_try(smem_u32(&bars.q_land[h]), (n_q[h] - 1) & 1); ++t) {}
-                for (uint32_t i = n_land > 2 ? n_land - 2 : 0; i < n_land; ++i)
-                    for (int t = 0; t < (1 << 16) && !bar_try(smem_u32(&bars.v_land[i & 1]), i >> 1 & 1); ++t) {}
+                    if (n_q[h] > 0) bar_drain(smem_u32(&bars.q_land[h]), (n_q[h] - 1) & 1);
+                for (uint32_t i = n_land > 2 ? n_land - 2 : 0; i < n_land; ++i) bar_drain(smem_u32(&bars.v_land[i & 1]), i >> 1 & 1);
             }
+            return;
         }
         __syncwarp();
     }
     tc_before();
-    __syncthreads();
-    if (tid == 0 && bars.gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
+    join_roles();
+    if (tid == 0 && *gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
     if (wid == 12) {
-        if (bars.gave_up) {                  // a role left early: matrix instructions may be under way
-            if (lane == 0) {
-                bar_init(smem_u32(&bars.o_done[0]), 1);
-                tc_commit(smem_u32(&bars.o_done[0]));
-                for (int i = 0; i < WAIT_LIMIT && !bar_try(smem_u32(&bars.o_done[0]), 0); ++i) {}
-            }
-            __syncwarp();
-        }
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     }

@@ -33,6 +33,7 @@ struct PtArgs {
     int4* head;                              // [2 * blocks]: per block: head record (0 none, 1 the item goes on, 2 it ends); tail record:
                                              // 1 + head or 0, row tile, -; then its sequence's first row, rows, -, -
     int* status;
+    int wait_limit;                          // tries before a wait between a block's roles is given up
 };
 
 // paged_chunk.cu
