@@ -484,8 +484,8 @@ SALICACHE_API int64_t salicache_paged_work_bytes(const salicache_ctx* ctx, const
 /*
  * How often a part of a block inside salicache_paged_attend looks for what another part has to bring before it gives up:
  * `tries` times in calls made (or captured) from now on, 2^24 at first, which takes a second or more.  A call in which a
- * wait is given up ends what it has under way, returns, and records E_CUDA in the status word; its rows of d_out and
- * d_lse are undefined.  0 gives up every wait, so that a caller can test what it does then.  Errors: E_NULL, E_PARAM
+ * wait is given up ends what it has under way, returns, and records E_CUDA in the status word, which hides any other
+ * status there; its rows of d_out and d_lse are undefined.  0 gives up every wait, so that a caller can test what it does then.  Errors: E_NULL, E_PARAM
  * (negative).
  */
 SALICACHE_API int salicache_paged_wait_limit(salicache_ctx* ctx, int tries);

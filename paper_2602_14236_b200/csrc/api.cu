@@ -515,7 +515,7 @@ int salicache_poll_status(salicache_ctx* c, void* cuda_stream) {
     if (cudaMemcpyAsync(&h, c->d_status, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess) return SALICACHE_E_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return SALICACHE_E_CUDA;
     if (h != 0 && cudaMemsetAsync(c->d_status, 0, sizeof(int), st) != cudaSuccess) return SALICACHE_E_CUDA;
-    return h;
+    return h == SC_GAVE_UP ? SALICACHE_E_CUDA : h;
 }
 
 }  // extern "C"

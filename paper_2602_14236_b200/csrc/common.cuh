@@ -11,6 +11,10 @@
         if (e__ != cudaSuccess) return SALICACHE_E_CUDA; \
     } while (0)
 
+// Status word: the reasons recorded there are negative numbers and the least one stays.  A kernel that gave up a wait records
+// this one, below all others: what it left out is not in any other's meaning.  The caller gets E_CUDA for it.
+constexpr int SC_GAVE_UP = -1000;
+
 // One image plane the pixel stages run on: the frame itself, or the anyres base image.
 struct PlaneGeom {
     int H, W;        // pixels

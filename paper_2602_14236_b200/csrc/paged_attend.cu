@@ -492,7 +492,7 @@ k_paged_step(PtArgs a, int blocks) {
     if (threadIdx.x == 0) {
         a.head[2 * c] = hd[0];
         a.head[2 * c + 1] = hd[1];
-        if (*gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
+        if (*gave_up) atomicMin(a.status, SC_GAVE_UP);
     }
 }
 

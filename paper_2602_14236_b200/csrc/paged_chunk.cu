@@ -698,7 +698,7 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
     }
     tc_before();
     join_roles();
-    if (tid == 0 && *gave_up) atomicMin(a.status, SALICACHE_E_CUDA);
+    if (tid == 0 && *gave_up) atomicMin(a.status, SC_GAVE_UP);
     if (wid == 12) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");

@@ -96,3 +96,27 @@ def test_calls_after_one_that_gave_up_are_not_held_up(ctx):
     pu.check(out[:c.w.rows].double().cpu().numpy().reshape(c.w.rows, c.Hq, 128), c.want[0], c.want[2], "out")
     c.ctx = sc.Context(sc.salicache_default_params(max_batch=1, chunk_frames=1, L=1))
     assert c.run(ORDINARY) == 0
+
+
+@pytest.mark.parametrize("news", [[1, 1], [150, 60]])
+def test_a_missing_page_does_not_hide_that_a_wait_was_given_up(ctx, news):
+    """Before or after it, in the same call or another one."""
+    c = Call(ctx, "int4", "f16", 2, 4, 128, 32, [2500, 300], news)
+    whole = c.seqs
+    table = whole.table.clone()
+    table[0, 3], table[1, 0] = -1, c.w.n_pages
+    holes = sc.Seqs(whole.row_start, whole.length, table, c.w.rows + 4)
+
+    def call(seqs, limit):
+        import torch
+        sc.salicache_paged_wait_limit(ctx, limit)
+        sc.salicache_paged_attend(ctx, c.pages.c, seqs.c, c.q, c.Hq * 128, 4, 0.1, 0, 0, torch.empty_like(c.q), c.Hq * 128, None, c.work,
+                                  c.work.numel())
+
+    call(holes, ORDINARY)
+    assert sc.salicache_poll_status(ctx) == sc.E_CAPACITY
+    for run in ([(holes, 0)], [(holes, ORDINARY), (whole, 0)], [(whole, 0), (holes, ORDINARY)], [(holes, 0), (holes, ORDINARY)]):
+        for seqs, limit in run:
+            call(seqs, limit)
+        assert sc.salicache_poll_status(ctx) == sc.E_CUDA
+        assert sc.salicache_poll_status(ctx) == 0
