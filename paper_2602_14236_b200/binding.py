@@ -50,6 +50,7 @@ class Pools(C.Structure):
 
 
 class Pages(C.Structure):
+    device = None        # CUDA device of the pages, where known
     _fields_ = [
         ("d_data", C.c_void_p), ("d_scale", C.c_void_p),
         ("n_pages", C.c_int32), ("page", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
@@ -58,6 +59,7 @@ class Pages(C.Structure):
 
 
 class SeqsC(C.Structure):
+    device = None
     _fields_ = [
         ("n_seqs", C.c_int32), ("table_width", C.c_int32), ("n_rows", C.c_int32),
         ("d_row_start", C.c_void_p), ("d_len", C.c_void_p), ("d_table", C.c_void_p),
@@ -142,13 +144,40 @@ def _here():
 _torch_c = None
 
 
-def _dptr(t, dev):
-    """The address of a tensor on device `dev`: the C entry points cannot tell host memory or another device's from their own."""
+def _dptr(t, dev, dtype, n):
+    """The address of `n` elements of type `dtype` (None: bytes, of any type) from a tensor's first on, on device `dev`.  The C
+    entry points see an address only: not whose memory it is, what it holds or where it ends."""
     if t is None:
         return None
     if t.get_device() != dev:
         raise ValueError(f"a tensor on cuda:{dev}, the current device, expected, got one on {t.device}")
+    if dtype is None:
+        n = -(-n // t.element_size())
+    elif t.dtype is not dtype:
+        raise ValueError(f"a tensor of type {dtype} expected, got {t.dtype}")
+    # a tensor without gaps, or a part of a wider one: rows may go on behind the view's end, not behind its memory's
+    if t.numel() < n or not t.is_contiguous():
+        held = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if held < n:
+            raise ValueError(f"memory for {n} elements expected from the tensor's first on, got {held}")
     return t.data_ptr()
+
+
+def _types():
+    global _torch_types
+    import torch
+    _torch_types = {F16: torch.float16, BF16: torch.bfloat16, "lse": torch.float32}
+    return _torch_types
+
+
+_torch_types = None
+
+
+def _batch(pages: Pages, seqs: SeqsC, dev: int, stream):
+    """Refuses pages, offsets or a stream of another device than the current one (structs filled by hand name none)."""
+    for what, at in (("pages", pages.device), ("offsets", seqs.device), ("stream", None if stream is None else stream.device_index)):
+        if at is not None and at != dev:
+            raise ValueError(f"{what} of cuda:{dev}, the current device, expected, got cuda:{at}")
 
 
 def _stream(stream=None):
@@ -303,8 +332,12 @@ def salicache_tokens_live(ctx: Context, d_src, B: int, first_frame: int, d_resid
 
 def _paged_move(name: str, ctx: Context, pages: Pages, seqs: SeqsC, d_K, d_V, k_stride: int, v_stride: int, stream):
     dev, st = _here()
-    rc = getattr(lib(), name)(ctx.handle, pages, seqs, _dptr(d_K, dev), _dptr(d_V, dev), k_stride, v_stride,
-                              st if stream is None else stream.cuda_stream)
+    if not pages.device == seqs.device == dev or stream is not None:
+        _batch(pages, seqs, dev, stream)
+    t, gaps, width = (_torch_types or _types()).get(pages.dtype), seqs.n_rows - 1, pages.heads * pages.head_dim
+    rc = getattr(_lib or lib(), name)(ctx.handle, pages, seqs, _dptr(d_K, dev, t, gaps * k_stride + width if gaps >= 0 else 0),
+                                      _dptr(d_V, dev, t, gaps * v_stride + width if gaps >= 0 else 0), k_stride, v_stride,
+                                      st if stream is None else stream.cuda_stream)
     if rc:
         raise SalicacheError(rc, name)
 
@@ -327,9 +360,15 @@ def salicache_paged_work_bytes(ctx: Context, pages: Pages, q_per_kv: int) -> int
 def salicache_paged_attend(ctx: Context, pages: Pages, seqs: SeqsC, d_q, q_stride: int, q_per_kv: int, softmax_scale: float,
                            window: int, sinks: int, d_out, out_stride: int, d_lse, d_work, work_bytes: int, stream=None):
     dev, st = _here()
-    rc = lib().salicache_paged_attend(ctx.handle, pages, seqs, _dptr(d_q, dev), q_stride, q_per_kv, softmax_scale, window, sinks,
-                                      _dptr(d_out, dev), out_stride, _dptr(d_lse, dev), _dptr(d_work, dev), work_bytes,
-                                      st if stream is None else stream.cuda_stream)
+    if not pages.device == seqs.device == dev or stream is not None:
+        _batch(pages, seqs, dev, stream)
+    types, rows, heads = _torch_types or _types(), seqs.n_rows, pages.heads * q_per_kv
+    t, gaps, width = types.get(pages.dtype), rows - 1, heads * pages.head_dim
+    rc = (_lib or lib()).salicache_paged_attend(
+        ctx.handle, pages, seqs, _dptr(d_q, dev, t, gaps * q_stride + width if rows > 0 else 0), q_stride, q_per_kv, softmax_scale,
+        window, sinks, _dptr(d_out, dev, t, gaps * out_stride + width if rows > 0 else 0), out_stride,
+        _dptr(d_lse, dev, types["lse"], rows * heads), _dptr(d_work, dev, None, work_bytes), work_bytes,
+        st if stream is None else stream.cuda_stream)
     if rc:
         raise SalicacheError(rc, "salicache_paged_attend")
 
@@ -379,13 +418,14 @@ class PageSet:
         self.data = torch.zeros(shape, dtype=el, device=device) if data is None else data
         self.scale = (None if sshape is None else torch.zeros(sshape, dtype=dtype, device=device)) if scale is None else scale
         for t, want, ty in ((self.data, shape, el), (self.scale, sshape, dtype)):
-            if t is not None and not t.is_cuda:
-                raise ValueError(f"pages on a CUDA device expected, got {t.device}")
+            if t is not None and (not t.is_cuda or t.device != self.data.device):
+                raise ValueError(f"pages on one CUDA device expected, got {t.device}")
             if t is not None and (tuple(t.shape) != want or t.dtype != ty or not t.is_contiguous()):
                 raise ValueError(f"pages of shape {want} and type {ty} expected, got {tuple(t.shape)}, {t.dtype}")
         self.dtype = dtype
         self.c = Pages(self.data.data_ptr(), None if self.scale is None else self.scale.data_ptr(), n_pages, page, heads, head_dim,
                        format, {torch.float16: F16, torch.bfloat16: BF16}[dtype])
+        self.c.device, self.c.memory = self.data.get_device(), (self.data, self.scale)
 
     def nbytes(self) -> int:
         return sum(t.numel() * t.element_size() for t in (self.data, self.scale) if t is not None)
@@ -404,3 +444,4 @@ class Seqs:
                 raise ValueError(f"int32 tensor of shape {want} expected, got {tuple(t.shape)}, {t.dtype}")
         self.row_start, self.length, self.table = row_start, length, table
         self.c = SeqsC(n, table.shape[1], n_rows, row_start.data_ptr(), length.data_ptr(), table.data_ptr())
+        self.c.device, self.c.memory = table.get_device(), (row_start, length, table)
