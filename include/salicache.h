@@ -470,8 +470,9 @@ SALICACHE_API int salicache_paged_read(salicache_ctx* ctx, const salicache_pages
  *   d_work      DEVICE, 16-byte aligned, salicache_paged_work_bytes() of it: partial results of rows whose keys are
  *               split.  Its content matters only while a call runs; calls that may overlap (other streams, captured
  *               graphs replayed side by side) need one each.
- * q_per_kv 1 .. 64, n_rows * q_per_kv below 2^30; window, sinks >= 0; softmax_scale > 0 and finite.  Errors as for salicache_paged_write; E_SHAPE
- * also when work_bytes is too small.
+ * q_per_kv 1 .. 64, n_rows * q_per_kv below 2^30; window, sinks >= 0; softmax_scale above 0 and at most 2^127.  Scores
+ * beyond 2e38 in magnitude count as infinite.  Errors as for salicache_paged_write; E_SHAPE also when work_bytes is too
+ * small.
  */
 SALICACHE_API int salicache_paged_attend(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
                                          const void* d_q, int64_t q_stride, int q_per_kv, float softmax_scale, int window,

@@ -492,7 +492,8 @@ int salicache_paged_attend(salicache_ctx* c, const salicache_pages* pages, const
     int rc = check_pages(pages);
     if (rc == SALICACHE_OK) rc = check_seqs(seqs);
     if (rc != SALICACHE_OK) return rc;
-    if (q_per_kv < 1 || q_per_kv > 64 || window < 0 || sinks < 0 || !(softmax_scale > 0.0f) || !(softmax_scale < INFINITY))
+    // the kernels work in powers of two: scale * log2(e) has to be finite
+    if (q_per_kv < 1 || q_per_kv > 64 || window < 0 || sinks < 0 || !(softmax_scale > 0.0f) || !(softmax_scale <= 0x1p127f))
         return SALICACHE_E_PARAM;
     if ((int64_t)seqs->n_rows * q_per_kv >= (1ll << 30)) return SALICACHE_E_SHAPE;
     const int64_t width = (int64_t)pages->heads * q_per_kv * pages->head_dim;
