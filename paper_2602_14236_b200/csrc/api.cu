@@ -418,7 +418,7 @@ static int check_pages(const salicache_pages* p) {
     if (p->head_dim != 64 && p->head_dim != 128) return SALICACHE_E_PARAM;
     if (p->heads < 1 || p->heads > 256) return SALICACHE_E_PARAM;
     if (p->n_pages < 1 || (int64_t)p->n_pages * 2 * p->heads * p->page >= (1ll << 31)) return SALICACHE_E_SHAPE;
-    if (!aligned16(p->d_data) || !aligned16(p->d_scale)) return SALICACHE_E_ALIGN;
+    if (!aligned16(p->d_data) || (p->format != SALICACHE_FP16 && !aligned16(p->d_scale))) return SALICACHE_E_ALIGN;
     return SALICACHE_OK;
 }
 
