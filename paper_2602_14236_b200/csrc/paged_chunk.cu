@@ -831,7 +831,8 @@ bool rows_map(CUtensorMap* map, const PtArgs& a, int D, bool bf16) {
     const EncodeTiled fn = tensor_encoder();
     if (!fn) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.pc.heads * a.G, (cuuint64_t)a.sq.n_rows};
-    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
+    // one row has no next one: its stride may be anything, which the encoder would refuse
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, a.sq.n_rows > 1 ? (cuuint64_t)a.q_stride * 2 : dims[1] * D * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)(128 / a.G)}, step[3] = {1, 1, 1};
     return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<uint16_t*>(a.q), dims, strides, box,
               step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
