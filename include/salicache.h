@@ -448,8 +448,9 @@ SALICACHE_API int salicache_paged_write(salicache_ctx* ctx, const salicache_page
 
 /*
  * The inverse: the batch's rows as their pages hold them, T(q * s) and T(q * s + zero) (multiply, then add) or the
- * copy.  Rows in no page come back as zeros.  To read whole sequences, let d_row_start be the running sum of d_len.
- * Arguments and errors as for salicache_paged_write; d_K_out, d_V_out are written.
+ * copy.  Where a group reaches the 16-bit type's largest numbers the rounded scale can carry its extremes past them: they
+ * are read as infinities (under INT8 65504, f16's largest).  Rows in no page come back as zeros.  To read whole
+ * sequences, let d_row_start be the running sum of d_len.  Arguments and errors as for salicache_paged_write; d_K_out, d_V_out are written.
  */
 SALICACHE_API int salicache_paged_read(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
                                        void* d_K_out, void* d_V_out, int64_t k_stride, int64_t v_stride, void* cuda_stream);
@@ -460,7 +461,9 @@ SALICACHE_API int salicache_paged_read(salicache_ctx* ctx, const salicache_pages
  * sees position j when j <= p, j < d_len and (window == 0 or j > p - window or j < sinks): causal, optionally under a
  * sliding window of `window` positions (its own among them) with the first `sinks` positions visible throughout.
  *   score_j = softmax_scale * q . K^_j,  out = T(sum_j softmax(score)_j V^_j),  lse = ln sum_j e^score_j
- * K^, V^ are the values salicache_paged_read returns.  Products are accumulated in binary32; the softmax weights go
+ * K^, V^ are what the pages stand for: the copy, T(q * s), or T(q * s + zero) with one rounding.  (salicache_paged_read rounds
+ * the INT4 sum to binary32 first, so that the two differ, rarely, by one unit in the last place; the others are equal bit for
+ * bit.)  Products are accumulated in binary32; the softmax weights go
  * through the second product in the 16-bit type.  Positions in no page are left out (deferred E_CAPACITY).  A row that
  * sees nothing: out = 0, lse = -infinity.  What pages hold at positions that no row of the sequence sees has no effect,
  * NaN included; at positions that some rows see, V is finite.

@@ -16,7 +16,7 @@
 // Measured: 16-bit pages, 16 sequences of 8000 positions: 100 us = 5.2 TB/s, 0.81 of the copy bandwidth, bound by memory;
 // INT8: 64 us = 4.2 TB/s; INT4, 32 ragged streams, 270 MB: 92 us = 2.9 TB/s = 0.45.  Codes are bound by issue slots: 433
 // instructions per 16 INT4 keys of a head, of which 192 turn codes into numbers (and, subtract, multiply-add per pair of
-// them: the values are rounded as salicache_paged_read rounds them, so the scales cannot be taken out of the sums).
+// them: the values attended to are of the 16-bit type, so the scales cannot be taken out of the sums).
 // The weights' reference maximum moves only when a score exceeds it by 2^8 (in powers of two): until then no lane needs
 // another's, weights stay below 2^8, and the sums are joined across lanes once at the end of an item.
 #include <math.h>

@@ -119,3 +119,14 @@ def test_positions_from_two_to_the_thirtieth_on_are_in_no_page(ctx):
         want, wl, tol, ltol = pu.attend(q[i], kk, vv, 0.125, t, "fp16")
         pu.check(o[i].double().cpu().numpy(), want, tol, f"row {i}")
         pu.check(lse[i, 0].item(), wl, ltol, f"lse {i}")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "int4"])
+def test_the_largest_f16_numbers_are_read_as_the_rounded_scale_makes_them(ctx, fmt):
+    t = _t("f16")
+    x = pu.to_t(np.random.default_rng(83).uniform(-6.0e4, 6.0e4, (2, 5, 2, 128)), t)
+    x[:, 1:3, :, 9], x[:, 1:3, :, 70] = 65504.0, -65504.0
+    with np.errstate(over="ignore"):
+        want = pu.decode(*pu.encode(x, fmt, t), fmt, t)
+    assert np.isinf(want[:, 1:3]).any(-1).all() and np.isfinite(want[:, [0, 3, 4]]).all()
+    assert np.array_equal(_stored(ctx, x, fmt, t), want)
