@@ -9,8 +9,8 @@
 // through one transposing butterfly (5 exchanges instead of 16), after which a quarter of the lanes each divides for one of
 // the four, integers are found in the mantissa bits of 1.5 * 2^23 + x instead of by the conversion unit, and a row's place
 // is one pointer and a step per pair.
-// Measured: 11520 rows of 32 x 128 into INT4 pages and back, 478 MB: 86 us = 5.5 TB/s, 0.86 of the copy bandwidth (116 us
-// before the above); 49279 INT4 rows of 8 x 128 read back, 255 MB: 47 us = 5.5 TB/s; a token each of eight streams into
+// Measured: 11520 rows of 32 x 128 into INT4 pages and back, 478 MB: 85 us = 5.6 TB/s, 0.87 of the copy bandwidth (116 us
+// before the above); 49279 INT4 rows of 8 x 128 read back, 255 MB: 45 us = 5.7 TB/s; a token each of eight streams into
 // INT8 pages and back: 6.2 us in a graph, two launches.
 #include "paged_async.cuh"
 #include "paged.cuh"

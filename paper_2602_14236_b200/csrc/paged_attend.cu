@@ -13,10 +13,13 @@
 // One more warp feeds a ring of tiles in shared memory by bulk copies of whole pages, so that some 130 to 200 KB per SM are
 // under way whatever the registers hold.  (Loading each lane's next operands into registers instead: 32 ragged streams
 // over INT4 pages took 149 us.)
-// Measured: 16-bit pages, 16 sequences of 8000 positions: 100 us = 5.2 TB/s, 0.81 of the copy bandwidth, bound by memory;
-// INT8: 64 us = 4.2 TB/s; INT4, 32 ragged streams, 270 MB: 92 us = 2.9 TB/s = 0.45.  Codes are bound by issue slots: 433
-// instructions per 16 INT4 keys of a head, of which 192 turn codes into numbers (and, subtract, multiply-add per pair of
-// them: the values attended to are of the 16-bit type, so the scales cannot be taken out of the sums).
+// Measured: 16-bit pages, 16 sequences of 8000 positions: 99 us = 5.3 TB/s, 0.83 of the copy bandwidth, bound by memory;
+// INT8: 65 us = 4.1 TB/s; INT4, 32 ragged streams, 270 MB: 94 us = 2.9 TB/s = 0.45.  Over codes neither memory nor the issue
+// slots are full (60 % of them for INT4, 51 % for INT8): a warp's load, expansion, products, maximum, expansion and products
+// follow one another, with nothing of the next keys under way, and 4.2 warps a scheduler do not cover that.  The ninth
+// warp leaves two blocks 96 registers a thread, of which codes at head_dim 128 spill some (184 bytes for f16 INT4, 268 for
+// INT8).  446 instructions go into 16 INT4 keys of a head; 192 of them turn codes into numbers (and, subtract,
+// multiply-add per pair of them: the values attended to are of the 16-bit type, so the scales stay inside the sums).
 // The weights' reference maximum moves only when a score exceeds it by 2^8 (in powers of two): until then no lane needs
 // another's, weights stay below 2^8, and the sums are joined across lanes once at the end of an item.
 #include <math.h>
@@ -547,8 +550,11 @@ int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache
     char* work = (char*)d_work;
     // Rows (of q, times the query heads of a group) per sequence up to which reading the pages is the work: 8 of 16-bit
     // pages, 16 of codes.  Measured with 16 sequences of 8000 positions, 8 key/value heads, this kernel against
-    // paged_chunk.cu's: 16-bit 8 rows 103 / 116 us, 16 rows 122 / 116; INT8 16 rows 93 / 131, 32 rows 164 / 131; INT4 16 rows
-    // 87 / 123, 32 rows 154 / 123.
+    // paged_chunk.cu's: 16-bit 8 rows 101 / 115 us, 16 rows 176 / 116; INT8 16 rows 94 / 124, 32 rows 164 / 125; INT4 16 rows
+    // 89 / 125, 32 rows 158 / 126.  The mean over all sequences decides, as the host knows no other number, and a batch whose
+    // sequences differ much pays for it: 64 single tokens over 4000 positions beside 900 rows over 16000 (INT8, one query
+    // head a group) take 620 us here, 326 there; 63 single tokens and 193 rows (four) 542 / 320.  A caller that knows its
+    // batch is better off with a call for each kind.
     const long long few = pg->format == SALICACHE_FP16 ? 8 : 16;
     if ((long long)a.sq.n_rows * a.G > few * a.sq.n_seqs) return sc_paged_chunk(c, a, pg, work, st);
 #define GO(T, F, D) return launch_attend<T, F, D>(c, a, work, st)

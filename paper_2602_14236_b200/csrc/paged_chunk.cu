@@ -19,8 +19,8 @@
 // The reference maximum moves only when a row exceeds it by 2^8; then, and only then, O is rescaled, by the thread that
 // found it and before it hands its weights on.
 //
-// Measured (bf16, 8192 new rows, 32 query and 8 key/value heads x 128): 563 us = 976 TFLOP/s, 0.58 of the cuBLAS burst rate;
-// two streams' 2304 rows over 20736 and 6912 INT4 positions: 1135 us = 996 TFLOP/s.  A (256 x 128) tile takes some 3500
+// Measured (bf16, 8192 new rows, 32 query and 8 key/value heads x 128): 560 us = 980 TFLOP/s, 0.58 of the cuBLAS burst rate;
+// two streams' 2304 rows over 20736 and 6912 INT4 positions: 1150 us = 983 TFLOP/s.  A (256 x 128) tile takes some 3500
 // clocks, of which the tensor core works 2050 (counted: 54 % of the kernel): the round of a half, S, weights, P V, is as
 // long as that.  Without the weights (products and copies alone) a tile takes 2800, shared memory being read at its full
 // rate for them.
