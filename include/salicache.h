@@ -437,8 +437,8 @@ typedef struct salicache_seqs {
  *   INT8: s = T(max|x| / 127), 0 -> 1;           q = rint(x * (1/s)) clamped to +-127
  *   INT4: zero = min x, s = T((max - zero) / 15), 0 -> 1;  q = rint((x - zero) * (1/s)) clamped to 0 .. 15
  * (an s whose reciprocal overflows binary32 counts as 0).  A group with a NaN or an infinity in it, or whose max - zero
- * overflows binary32 (bf16 only), gets the scale NaN: all of it is read as NaN.  Rows in no page are dropped (deferred E_CAPACITY for the
- * reasons above; silently for a negative position).  Two rows of one call must not land in the same slot.
+ * overflows binary32 (bf16 only), gets the scale NaN: all of it is read as NaN.  Rows in no page are dropped (deferred
+ * E_CAPACITY for the reasons above; silently for a negative position).  Two rows of one call must not land in the same slot.
  * Errors: E_NULL, E_SHAPE, E_ALIGN (16 bytes), E_PARAM (unsupported value; the current device is not the context's),
  * E_CUDA.
  */
@@ -450,7 +450,8 @@ SALICACHE_API int salicache_paged_write(salicache_ctx* ctx, const salicache_page
  * The inverse: the batch's rows as their pages hold them, T(q * s) and T(q * s + zero) (multiply, then add) or the
  * copy.  Where a group reaches the 16-bit type's largest numbers the rounded scale can carry its extremes past them: they
  * are read as infinities (under INT8 65504, f16's largest).  Rows in no page come back as zeros.  To read whole
- * sequences, let d_row_start be the running sum of d_len.  Arguments and errors as for salicache_paged_write; d_K_out, d_V_out are written.
+ * sequences, let d_row_start be the running sum of d_len.  Arguments and errors as for salicache_paged_write; d_K_out,
+ * d_V_out are written.
  */
 SALICACHE_API int salicache_paged_read(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
                                        void* d_K_out, void* d_V_out, int64_t k_stride, int64_t v_stride, void* cuda_stream);
@@ -487,10 +488,10 @@ SALICACHE_API int64_t salicache_paged_work_bytes(const salicache_ctx* ctx, const
 
 /*
  * How often a part of a block inside salicache_paged_attend looks for what another part has to bring before it gives up:
- * `tries` times in calls made (or captured) from now on, 2^24 at first, which takes a second or more.  A call in which a
+ * `tries` times in calls made (or captured) from now on, 2^19 at first, which takes about two seconds.  A call in which a
  * wait is given up ends what it has under way, returns, and records E_CUDA in the status word, which hides any other
- * status there; its rows of d_out and d_lse are undefined.  0 gives up every wait, so that a caller can test what it does then.  Errors: E_NULL, E_PARAM
- * (negative).
+ * status there; its rows of d_out and d_lse are undefined.  0 gives up every wait, so that a caller can test what it does
+ * then.  Errors: E_NULL, E_PARAM (negative).
  */
 SALICACHE_API int salicache_paged_wait_limit(salicache_ctx* ctx, int tries);
 

@@ -114,7 +114,7 @@ int salicache_create(salicache_ctx** out, const salicache_params* p) {
     }
     c->sm_count = prop.multiProcessorCount;
     c->device = dev;
-    c->paged_wait = 1 << 24;
+    c->paged_wait = SC_WAIT_LIMIT;
     const size_t P0 = (size_t)p->H * p->W;
     const size_t slots = (size_t)2 * c->chunk;   // independent pairs need prev and cur; a video needs chunk+1
     const int words = (p->W + 31) / 32;

@@ -14,6 +14,9 @@
 // Status word: the reasons recorded there are negative numbers and the least one stays.  A kernel that gave up a wait records
 // this one, below all others: what it left out is not in any other's meaning.  The caller gets E_CUDA for it.
 constexpr int SC_GAVE_UP = -1000;
+// Tries before a wait inside a kernel is given up, unless the caller sets another limit: a try that has to wait takes 4 us
+// (measured), all of them about two seconds.
+constexpr int SC_WAIT_LIMIT = 1 << 19;
 
 // One image plane the pixel stages run on: the frame itself, or the anyres base image.
 struct PlaneGeom {
