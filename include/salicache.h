@@ -483,11 +483,13 @@ SALICACHE_API int salicache_paged_attend(salicache_ctx* ctx, const salicache_pag
                                          int sinks, void* d_out, int64_t out_stride, float* d_lse, void* d_work,
                                          int64_t work_bytes, void* cuda_stream);
 
-/* Bytes of d_work for salicache_paged_attend over such pages (any batch), or a negative error. */
+/* Bytes of d_work for salicache_paged_attend, salicache_paged_attend_tree or salicache_paged_weigh over such pages (any
+ * batch), or a negative error. */
 SALICACHE_API int64_t salicache_paged_work_bytes(const salicache_ctx* ctx, const salicache_pages* pages, int q_per_kv);
 
 /*
- * How often a part of a block inside salicache_paged_attend looks for what another part has to bring before it gives up:
+ * How often a part of a block inside salicache_paged_attend, salicache_paged_attend_tree or salicache_paged_weigh looks for
+ * what another part has to bring before it gives up:
  * `tries` times in calls made (or captured) from now on, 2^19 at first, which takes about two seconds.  A call in which a
  * wait is given up ends what it has under way, returns, and records E_CUDA in the status word, which hides any other
  * status there; its rows of d_out and d_lse are undefined.  0 gives up every wait, so that a caller can test what it does
@@ -495,8 +497,131 @@ SALICACHE_API int64_t salicache_paged_work_bytes(const salicache_ctx* ctx, const
  */
 SALICACHE_API int salicache_paged_wait_limit(salicache_ctx* ctx, int tries);
 
+/*
+ * Rotary positions.  A head's first 2 * pairs dimensions are taken in pairs, (i, i + pairs) with SALICACHE_HALVES or
+ * (2 i, 2 i + 1) with SALICACHE_NEIGHBOURS, and pair i is turned by position[axis[i]] * freq[i] radians:
+ *   first' = first cos - second sin,  second' = second cos + first sin
+ * The other dimensions stay.  A position has 1 .. 4 axes (one: plain rotary positions; time, height and width: the visual
+ * tokens of images and video), and freq may be any finite numbers, scaled for long contexts or not; negated ones turn back.
+ * The angle is reduced exactly, whatever the position: the kernel multiplies it with freq / 2 pi as a 64-bit fraction of a
+ * turn, modulo one.  Cosine, sine and products are binary32, the result is rounded to the 16-bit type.
+ * HOST memory, read during the call. */
+#define SALICACHE_HALVES     0
+#define SALICACHE_NEIGHBOURS 1
+typedef struct salicache_rotary {
+    double freq[64];         /* radians per position, pairs of them                                    */
+    uint8_t axis[64];        /* which of the position's axes turns pair i, below n_axes                */
+    int32_t pairs;           /* a multiple of 8, at most head_dim / 2                                  */
+    int32_t n_axes;          /* 1 .. 4                                                                 */
+    int32_t pairing;         /* SALICACHE_HALVES or SALICACHE_NEIGHBOURS                               */
+} salicache_rotary;
+
+/*
+ * salicache_paged_write with K turned by its rows' positions before it is quantised, and the rows of q turned beside it.
+ * What the pages hold is what salicache_paged_write makes of the turned K, rounded to the 16-bit type; V is not turned.
+ *   d_pos    DEVICE i32 [n_rows][n_axes]: positions of the rows on each axis, any values, also negative; they need not be
+ *            the positions that the sequences' tables go by (the visual tokens of a frame share their position in time)
+ *   d_q      DEVICE [n_rows] rows of [heads * q_per_kv][head_dim], q_stride elements from row to row (>= the row's width, a
+ *            multiple of 8), or NULL: no q, and q_per_kv, q_stride, d_q_out and q_out_stride are not looked at
+ *   d_q_out  the turned rows, q_out_stride elements apart; may be d_q with the same stride, else the two do not overlap.
+ *            Rows of no sequence are left as they are; rows in no page are turned all the same.
+ * pages, seqs, d_K, d_V, strides and errors as for salicache_paged_write; q_per_kv 1 .. 64.  E_NULL also for d_pos and
+ * rotary, E_PARAM for what the struct does not allow, E_ALIGN for d_pos off a 4-byte boundary.
+ */
+SALICACHE_API int salicache_paged_write_rotary(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
+                                               const salicache_rotary* rotary, const int32_t* d_pos, const void* d_q,
+                                               int64_t q_stride, int q_per_kv, void* d_q_out, int64_t q_out_stride,
+                                               const void* d_K, const void* d_V, int64_t k_stride, int64_t v_stride,
+                                               void* cuda_stream);
+
+/*
+ * Attention of drafted tokens that form a tree.  A sequence's n rows of this call (its LAST n positions, written before) are
+ * the tree's nodes in any order, and every row says which of them it sees: bit c % 64 of word c / 64 of its tree_words words
+ * names the sequence's row c of this call.  Usually those are its ancestors and itself; a row whose own bit is not set does
+ * not see itself.  Of the positions before the call's rows a row sees all, or with a window those that a row at position
+ *   d_len - n + (number of its bits) - 1   (d_len - n, when none is set)
+ * sees under salicache_paged_attend's rule: the number of its bits is its depth in the tree.  The window does not bound
+ * what the bits name.  Bits past the sequence's rows mean nothing; rows past 64 * tree_words are named by none.
+ *   d_tree   DEVICE u64 [n_rows][tree_words], 8-byte aligned; tree_words 1 .. 16
+ * A chain of at most 64 * tree_words rows (row i has bits 0 .. i) without a window gives what salicache_paged_attend gives,
+ * bit for bit.  V is finite at all of the call's own positions, and from d_len - n - window + 1 on under a window, whether
+ * or not a bit names them; those positions' pages count as touched.  All other arguments, the workspace, the waits and the
+ * errors are those of salicache_paged_attend; E_PARAM also for tree_words, E_NULL and E_ALIGN for d_tree.
+ */
+SALICACHE_API int salicache_paged_attend_tree(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
+                                              const uint64_t* d_tree, int tree_words, const void* d_q, int64_t q_stride,
+                                              int q_per_kv, float softmax_scale, int window, int sinks, void* d_out,
+                                              int64_t out_stride, float* d_lse, void* d_work, int64_t work_bytes,
+                                              void* cuda_stream);
+
+/*
+ * What attention gave each cached position: the weight that eviction goes by.  For every sequence b with rows in the call,
+ * every key/value head h and every position j below d_len[b],
+ *   out[b][h][j] = (j < d_len - n ? decay * in[b][h][j] : 0) + sum over the call's rows i at positions >= j and the query
+ *                  heads hq of h of e^(softmax_scale * q_i,hq . K^_j - lse_i,hq)
+ * with the K^ of salicache_paged_attend and its logarithms of the softmax sums, of the same rows without a window.  A
+ * position that is new in this call starts at 0, whatever the array holds there.  A sequence without rows keeps what it
+ * had.  The sums are binary32, in an order that depends on the batch's lengths only.
+ *   d_lse         DEVICE f32 [n_rows][heads * q_per_kv]
+ *   d_weight_in   DEVICE f32 [n_seqs][heads][weight_stride], or NULL: zeros
+ *   d_weight_out  the same shape, written below d_len[b]; may be d_weight_in, else the two do not overlap
+ *   decay         0 .. 1: 1 adds up over all calls, less forgets older ones
+ * Positions in no page gain nothing (deferred E_CAPACITY); positions at or past weight_stride are left out (deferred
+ * E_CAPACITY).  To weigh by the last m rows of a prompt only, let d_row_start name those m: the positions before them then
+ * have to hold their weights, or zeros.  A row's -infinity in d_lse (it sees nothing) counts as no row.
+ * q, pages, seqs, d_work and errors as for salicache_paged_attend; E_PARAM also for a decay outside [0, 1], E_SHAPE for
+ * weight_stride < 1.
+ */
+SALICACHE_API int salicache_paged_weigh(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
+                                        const void* d_q, int64_t q_stride, int q_per_kv, float softmax_scale,
+                                        const float* d_lse, float decay, const float* d_weight_in, float* d_weight_out,
+                                        int64_t weight_stride, void* d_work, int64_t work_bytes, void* cuda_stream);
+
+/*
+ * The positions that a budget keeps, for every sequence b and key/value head h: all of them while d_len[b] <= budget; else
+ * the first `sinks`, the last `recent`, and of the rest the budget - sinks - recent heaviest, equal weights by the lower
+ * position.  A weight that is not a number counts as less than all others.
+ *   d_weight  DEVICE f32 [n_seqs][heads][weight_stride], weight_stride >= d_len[b] (positions past it count as not held:
+ *             d_len is taken as weight_stride, deferred E_CAPACITY)
+ *   d_len     DEVICE i32 [n_seqs]
+ *   d_keep    DEVICE i32 [n_seqs][heads][budget], written: ascending positions, -1 behind the last
+ *   d_kept    DEVICE i32 [n_seqs], written: min(d_len[b], budget), which is the sequence's length after
+ *             salicache_paged_keep
+ * sinks + recent <= budget, all of them >= 0, budget >= 1 (E_PARAM); heads 1 .. 256, n_seqs >= 0, n_seqs * heads below 2^16 (E_SHAPE).
+ * Errors: E_NULL, E_ALIGN (4 bytes), E_PARAM, E_SHAPE, E_CUDA.
+ */
+SALICACHE_API int salicache_select_heavy(salicache_ctx* ctx, const float* d_weight, int64_t weight_stride, int heads, int n_seqs,
+                                         const int32_t* d_len, int budget, int sinks, int recent, int32_t* d_keep,
+                                         int32_t* d_kept, void* cuda_stream);
+
+/*
+ * Moves the kept positions together: position first + k of sequence b gets what position d_keep[b][h][k] holds, K, V and
+ * scales bit for bit, for k < d_kept[b], per key/value head.  After an eviction the lists are salicache_select_heavy's; after
+ * a draft has been verified, the positions of the accepted path, the same for all heads.
+ *   seqs       where the rows are: n_seqs, d_len, d_table, table_width (the row offsets are not used)
+ *   d_keep     DEVICE i32 [n_seqs][keep_heads][keep_width]; keep_heads is the pages' heads, or 1: one list for all heads
+ *   d_first    DEVICE i32 [n_seqs] (not negative), or NULL: 0
+ *   d_kept     DEVICE i32 [n_seqs]; more than keep_width counts as keep_width, less than 0 as 0
+ *   to_or_null where they go: n_seqs, d_table and table_width of other pages of the same array (its d_len and row offsets
+ *              are not used).  No page may be among both the sources and the destinations, nor twice among the destinations.
+ *              NULL: in place.  The lists are then strictly ascending with d_keep[b][h][k] >= first + k, and no page that
+ *              is written belongs to two sequences: rows of shared prefixes are not to be moved in place.
+ *   d_weight_in, d_weight_out  DEVICE f32 [n_seqs][heads][weight_stride], both or neither: the weights move along; the two
+ *              may be one array where the lists are as for in place, else they do not overlap
+ * Entries outside [0, d_len[b]), and rows whose source or destination is in no page (past the table, an entry outside
+ * [0, n_pages)), are not moved (deferred E_CAPACITY); the destination, and the weight there, stays as it is.  A weight at or
+ * past weight_stride is not moved.
+ * Errors: as for salicache_paged_write; E_SHAPE also for keep_heads, keep_width < 0, another n_seqs in to_or_null, n_seqs *
+ * heads at or past 2^16, weight_stride < 1 with weights; E_PARAM when the two tables are one; E_NULL for one of the weights.
+ */
+SALICACHE_API int salicache_paged_keep(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
+                                       const int32_t* d_keep, int keep_heads, int keep_width, const int32_t* d_first,
+                                       const int32_t* d_kept, const salicache_seqs* to_or_null, const float* d_weight_in,
+                                       float* d_weight_out, int64_t weight_stride, void* cuda_stream);
+
 /* Synchronises `cuda_stream`, returns the deferred device status (0, E_CAPACITY, E_NOCONVERGE or
- * E_EVICTED; E_CUDA if the stream reports an error, or a wait inside salicache_paged_attend ran out) and clears it. */
+ * E_EVICTED; E_CUDA if the stream reports an error, or a wait inside one of the attention calls over pages ran out) and
+ * clears it. */
 SALICACHE_API int salicache_poll_status(salicache_ctx* ctx, void* cuda_stream);
 
 #ifdef __cplusplus

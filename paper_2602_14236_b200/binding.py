@@ -14,6 +14,7 @@ from . import build as _build
 REUSE, PRUNE, INT4, INT8, FP16 = 0, 1, 2, 3, 4
 
 F16, BF16 = 0, 1
+HALVES, NEIGHBOURS = 0, 1
 
 E_NULL, E_SHAPE, E_ALIGN, E_PARAM, E_CUDA, E_CAPACITY, E_NOCONVERGE, E_NOMEM, E_EVICTED = -1, -2, -3, -4, -5, -6, -7, -8, -9
 
@@ -66,6 +67,21 @@ class SeqsC(C.Structure):
     ]
 
 
+class Rotary(C.Structure):
+    """Radians per position of every pair, the axis of the position that turns it (none: all on the one there is), and how the
+    pairs lie (HALVES or NEIGHBOURS)."""
+    _fields_ = [
+        ("freq", C.c_double * 64), ("axis", C.c_uint8 * 64), ("pairs", C.c_int32), ("n_axes", C.c_int32), ("pairing", C.c_int32),
+    ]
+
+    def __init__(self, freq, axis=None, n_axes: int = 1, pairing: int = HALVES):
+        freq = [float(x) for x in freq]
+        axis = [0] * len(freq) if axis is None else [int(x) for x in axis]
+        if len(freq) > 64 or len(axis) != len(freq) or any(not 0 <= x < 256 for x in axis):
+            raise ValueError("at most 64 frequencies, and an axis for each, expected")
+        super().__init__((C.c_double * 64)(*freq), (C.c_uint8 * 64)(*axis), len(freq), n_axes, pairing)
+
+
 EXPORTS = [
     "salicache_default_params", "salicache_create", "salicache_destroy", "salicache_strerror",
     "salicache_tokens_per_frame", "salicache_launch_count", "salicache_flow_score", "salicache_saliency", "salicache_select",
@@ -73,7 +89,8 @@ EXPORTS = [
     "salicache_frame_redundancy", "salicache_source_frames", "salicache_diff_score", "salicache_attend",
     "salicache_select_anchored", "salicache_select_ranked", "salicache_attend_gqa", "salicache_select_anchored_batch",
     "salicache_frames_resident", "salicache_tokens_live", "salicache_paged_write", "salicache_paged_read",
-    "salicache_paged_attend", "salicache_paged_work_bytes", "salicache_paged_wait_limit",
+    "salicache_paged_attend", "salicache_paged_work_bytes", "salicache_paged_wait_limit", "salicache_paged_write_rotary",
+    "salicache_paged_attend_tree", "salicache_paged_weigh", "salicache_select_heavy", "salicache_paged_keep",
 ]
 
 _lib = None
@@ -119,6 +136,15 @@ def lib():
         _lib.salicache_paged_read.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, vp, i64, i64, vp]
         _lib.salicache_paged_attend.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, i64, i32, C.c_float, i32, i32, vp, i64,
                                                 vp, vp, i64, vp]
+        _lib.salicache_paged_write_rotary.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), C.POINTER(Rotary), vp, vp, i64, i32, vp,
+                                                      i64, vp, vp, i64, i64, vp]
+        _lib.salicache_paged_attend_tree.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, i32, vp, i64, i32, C.c_float, i32, i32,
+                                                     vp, i64, vp, vp, i64, vp]
+        _lib.salicache_paged_weigh.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, i64, i32, C.c_float, vp, C.c_float, vp, vp,
+                                               i64, vp, i64, vp]
+        _lib.salicache_select_heavy.argtypes = [vp, vp, i64, i32, i32, vp, i32, i32, i32, vp, vp, vp]
+        _lib.salicache_paged_keep.argtypes = [vp, C.POINTER(Pages), C.POINTER(SeqsC), vp, i32, i32, vp, vp, C.POINTER(SeqsC), vp, vp,
+                                              i64, vp]
         _lib.salicache_paged_wait_limit.argtypes = [vp, i32]
         _lib.salicache_paged_work_bytes.argtypes = [vp, C.POINTER(Pages), i32]
         _lib.salicache_paged_work_bytes.restype = i64
@@ -166,7 +192,7 @@ def _dptr(t, dev, dtype, n):
 def _types():
     global _torch_types
     import torch
-    _torch_types = {F16: torch.float16, BF16: torch.bfloat16, "lse": torch.float32}
+    _torch_types = {F16: torch.float16, BF16: torch.bfloat16, "lse": torch.float32, "i32": torch.int32, "i64": torch.int64}
     return _torch_types
 
 
@@ -350,6 +376,29 @@ def salicache_paged_read(ctx: Context, pages: Pages, seqs: SeqsC, d_K_out, d_V_o
     _paged_move("salicache_paged_read", ctx, pages, seqs, d_K_out, d_V_out, k_stride, v_stride, stream)
 
 
+def _span(rows: int, stride: int, width: int) -> int:
+    """Elements from the first of `rows` rows to the end of the last one."""
+    return (rows - 1) * stride + width if rows > 0 else 0
+
+
+def salicache_paged_write_rotary(ctx: Context, pages: Pages, seqs: SeqsC, rotary: Rotary, d_pos, d_q, q_stride: int, q_per_kv: int,
+                                 d_q_out, q_out_stride: int, d_K, d_V, k_stride: int, v_stride: int, stream=None):
+    """d_q None: no rows of q."""
+    dev, st = _here()
+    if not pages.device == seqs.device == dev or stream is not None:
+        _batch(pages, seqs, dev, stream)
+    types, rows, width = _torch_types or _types(), seqs.n_rows, pages.heads * pages.head_dim
+    t = types.get(pages.dtype)
+    q, q_out = (None, None) if d_q is None else (_dptr(d_q, dev, t, _span(rows, q_stride, width * q_per_kv)),
+                                                 _dptr(d_q_out, dev, t, _span(rows, q_out_stride, width * q_per_kv)))
+    rc = (_lib or lib()).salicache_paged_write_rotary(
+        ctx.handle, pages, seqs, rotary, _dptr(d_pos, dev, types["i32"], rows * rotary.n_axes), q, q_stride, q_per_kv, q_out, q_out_stride,
+        _dptr(d_K, dev, t, _span(rows, k_stride, width)), _dptr(d_V, dev, t, _span(rows, v_stride, width)), k_stride, v_stride,
+        st if stream is None else stream.cuda_stream)
+    if rc:
+        raise SalicacheError(rc, "salicache_paged_write_rotary")
+
+
 def salicache_paged_work_bytes(ctx: Context, pages: Pages, q_per_kv: int) -> int:
     n = int(lib().salicache_paged_work_bytes(ctx.handle, C.byref(pages), q_per_kv))
     if n < 0:
@@ -371,6 +420,73 @@ def salicache_paged_attend(ctx: Context, pages: Pages, seqs: SeqsC, d_q, q_strid
         st if stream is None else stream.cuda_stream)
     if rc:
         raise SalicacheError(rc, "salicache_paged_attend")
+
+
+def salicache_paged_attend_tree(ctx: Context, pages: Pages, seqs: SeqsC, d_tree, tree_words: int, d_q, q_stride: int, q_per_kv: int,
+                                softmax_scale: float, window: int, sinks: int, d_out, out_stride: int, d_lse, d_work, work_bytes: int,
+                                stream=None):
+    """d_tree: int64, whose bits are taken as they are."""
+    dev, st = _here()
+    if not pages.device == seqs.device == dev or stream is not None:
+        _batch(pages, seqs, dev, stream)
+    types, rows, heads = _torch_types or _types(), seqs.n_rows, pages.heads * q_per_kv
+    t, width = types.get(pages.dtype), heads * pages.head_dim
+    rc = (_lib or lib()).salicache_paged_attend_tree(
+        ctx.handle, pages, seqs, _dptr(d_tree, dev, types["i64"], rows * tree_words), tree_words,
+        _dptr(d_q, dev, t, _span(rows, q_stride, width)), q_stride, q_per_kv, softmax_scale, window, sinks,
+        _dptr(d_out, dev, t, _span(rows, out_stride, width)), out_stride, _dptr(d_lse, dev, types["lse"], rows * heads),
+        _dptr(d_work, dev, None, work_bytes), work_bytes, st if stream is None else stream.cuda_stream)
+    if rc:
+        raise SalicacheError(rc, "salicache_paged_attend_tree")
+
+
+def salicache_paged_weigh(ctx: Context, pages: Pages, seqs: SeqsC, d_q, q_stride: int, q_per_kv: int, softmax_scale: float, d_lse,
+                          decay: float, d_weight_in, d_weight_out, weight_stride: int, d_work, work_bytes: int, stream=None):
+    """d_weight_in None: zeros."""
+    dev, st = _here()
+    if not pages.device == seqs.device == dev or stream is not None:
+        _batch(pages, seqs, dev, stream)
+    types, rows, heads = _torch_types or _types(), seqs.n_rows, pages.heads * q_per_kv
+    f32, held = types["lse"], seqs.n_seqs * pages.heads * weight_stride
+    rc = (_lib or lib()).salicache_paged_weigh(
+        ctx.handle, pages, seqs, _dptr(d_q, dev, types.get(pages.dtype), _span(rows, q_stride, heads * pages.head_dim)), q_stride, q_per_kv,
+        softmax_scale, _dptr(d_lse, dev, f32, rows * heads), decay, _dptr(d_weight_in, dev, f32, held), _dptr(d_weight_out, dev, f32, held),
+        weight_stride, _dptr(d_work, dev, None, work_bytes), work_bytes, st if stream is None else stream.cuda_stream)
+    if rc:
+        raise SalicacheError(rc, "salicache_paged_weigh")
+
+
+def salicache_select_heavy(ctx: Context, d_weight, weight_stride: int, heads: int, n_seqs: int, d_len, budget: int, sinks: int,
+                           recent: int, d_keep, d_kept, stream=None):
+    dev, st = _here()
+    if stream is not None:
+        _batch(Pages(), SeqsC(), dev, stream)
+    types = _torch_types or _types()
+    i32 = types["i32"]
+    rc = (_lib or lib()).salicache_select_heavy(
+        ctx.handle, _dptr(d_weight, dev, types["lse"], n_seqs * heads * weight_stride), weight_stride, heads, n_seqs,
+        _dptr(d_len, dev, i32, n_seqs), budget, sinks, recent, _dptr(d_keep, dev, i32, n_seqs * heads * budget),
+        _dptr(d_kept, dev, i32, n_seqs), st if stream is None else stream.cuda_stream)
+    if rc:
+        raise SalicacheError(rc, "salicache_select_heavy")
+
+
+def salicache_paged_keep(ctx: Context, pages: Pages, seqs: SeqsC, d_keep, keep_heads: int, keep_width: int, d_first, d_kept, to,
+                         d_weight_in=None, d_weight_out=None, weight_stride: int = 0, stream=None):
+    """to: the SeqsC of the pages they go into, or None: in place.  d_first None: from position 0 on."""
+    dev, st = _here()
+    if not pages.device == seqs.device == dev or stream is not None:
+        _batch(pages, seqs, dev, stream)
+    if to is not None and to.device != dev:
+        _batch(pages, to, dev, stream)
+    types, n = _torch_types or _types(), seqs.n_seqs
+    i32, f32, held = types["i32"], types["lse"], n * pages.heads * weight_stride
+    rc = (_lib or lib()).salicache_paged_keep(
+        ctx.handle, pages, seqs, _dptr(d_keep, dev, i32, n * keep_heads * keep_width), keep_heads, keep_width, _dptr(d_first, dev, i32, n),
+        _dptr(d_kept, dev, i32, n), to, _dptr(d_weight_in, dev, f32, held), _dptr(d_weight_out, dev, f32, held), weight_stride,
+        st if stream is None else stream.cuda_stream)
+    if rc:
+        raise SalicacheError(rc, "salicache_paged_keep")
 
 
 def salicache_paged_wait_limit(ctx: Context, tries: int):

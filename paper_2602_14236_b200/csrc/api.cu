@@ -470,6 +470,40 @@ int salicache_paged_read(salicache_ctx* c, const salicache_pages* pages, const s
     return paged_move(c, pages, seqs, d_K_out, d_V_out, k_stride, v_stride, false, cuda_stream);
 }
 
+static int check_rotary(const salicache_rotary* r, const int32_t* d_pos, int head_dim) {
+    if (!r || !d_pos) return SALICACHE_E_NULL;
+    if (r->pairs < 8 || r->pairs % 8 != 0 || 2 * r->pairs > head_dim || r->n_axes < 1 || r->n_axes > 4) return SALICACHE_E_PARAM;
+    if (r->pairing != SALICACHE_HALVES && r->pairing != SALICACHE_NEIGHBOURS) return SALICACHE_E_PARAM;
+    for (int i = 0; i < r->pairs; ++i)
+        if (!isfinite(r->freq[i]) || r->axis[i] >= r->n_axes) return SALICACHE_E_PARAM;
+    return reinterpret_cast<uintptr_t>(d_pos) & 3u ? SALICACHE_E_ALIGN : SALICACHE_OK;
+}
+
+int salicache_paged_write_rotary(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs,
+                                 const salicache_rotary* rotary, const int32_t* d_pos, const void* d_q, int64_t q_stride, int q_per_kv,
+                                 void* d_q_out, int64_t q_out_stride, const void* d_K, const void* d_V, int64_t k_stride,
+                                 int64_t v_stride, void* cuda_stream) {
+    Range range__("salicache_paged_write_rotary");
+    int rc = check_pages(pages);
+    if (rc == SALICACHE_OK) rc = check_seqs(seqs);
+    if (rc == SALICACHE_OK) rc = check_rotary(rotary, d_pos, pages->head_dim);
+    if (rc != SALICACHE_OK) return rc;
+    const int64_t width = (int64_t)pages->heads * pages->head_dim;
+    if (d_q) {
+        if (q_per_kv < 1 || q_per_kv > 64) return SALICACHE_E_PARAM;
+        rc = check_rows(d_q, q_stride, width * q_per_kv);
+        if (rc == SALICACHE_OK) rc = check_rows(d_q_out, q_out_stride, width * q_per_kv);
+        if (rc == SALICACHE_OK && d_q == d_q_out && q_stride != q_out_stride) rc = SALICACHE_E_SHAPE;
+    }
+    if (rc == SALICACHE_OK) rc = check_rows(d_K, k_stride, width);
+    if (rc == SALICACHE_OK) rc = check_rows(d_V, v_stride, width);
+    if (rc == SALICACHE_OK) rc = check_device(c);
+    if (rc != SALICACHE_OK) return rc;
+    if (seqs->n_seqs == 0 || seqs->n_rows == 0) return SALICACHE_OK;
+    return sc_paged_write_rotary(c, pages, seqs, rotary, d_pos, d_q, q_stride, d_q ? q_per_kv : 0, d_q_out, q_out_stride, d_K, d_V,
+                                 k_stride, v_stride, (cudaStream_t)cuda_stream);
+}
+
 int64_t salicache_paged_work_bytes(const salicache_ctx* c, const salicache_pages* pages, int q_per_kv) {
     int rc = check_pages(pages);
     if (rc != SALICACHE_OK) return rc;
@@ -485,10 +519,9 @@ int salicache_paged_wait_limit(salicache_ctx* c, int tries) {
     return SALICACHE_OK;
 }
 
-int salicache_paged_attend(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, const void* d_q,
-                           int64_t q_stride, int q_per_kv, float softmax_scale, int window, int sinks, void* d_out,
-                           int64_t out_stride, float* d_lse, void* d_work, int64_t work_bytes, void* cuda_stream) {
-    Range range__("salicache_paged_attend");
+// What the attention calls share: rows of q, the scale, the workspace.
+static int check_attend(const salicache_pages* pages, const salicache_seqs* seqs, const void* d_q, int64_t q_stride, int q_per_kv,
+                        float softmax_scale, int window, int sinks, void* d_out, int64_t out_stride, const float* d_lse, void* d_work) {
     int rc = check_pages(pages);
     if (rc == SALICACHE_OK) rc = check_seqs(seqs);
     if (rc != SALICACHE_OK) return rc;
@@ -501,12 +534,95 @@ int salicache_paged_attend(salicache_ctx* c, const salicache_pages* pages, const
     if (rc == SALICACHE_OK) rc = check_rows(d_out, out_stride, width);
     if (rc == SALICACHE_OK && !d_work) rc = SALICACHE_E_NULL;
     if (rc == SALICACHE_OK && (!aligned16(d_work) || (reinterpret_cast<uintptr_t>(d_lse) & 3u))) rc = SALICACHE_E_ALIGN;
+    return rc;
+}
+
+int salicache_paged_attend(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, const void* d_q,
+                           int64_t q_stride, int q_per_kv, float softmax_scale, int window, int sinks, void* d_out,
+                           int64_t out_stride, float* d_lse, void* d_work, int64_t work_bytes, void* cuda_stream) {
+    Range range__("salicache_paged_attend");
+    int rc = check_attend(pages, seqs, d_q, q_stride, q_per_kv, softmax_scale, window, sinks, d_out, out_stride, d_lse, d_work);
     if (rc == SALICACHE_OK) rc = check_device(c);
     if (rc != SALICACHE_OK) return rc;
     if (work_bytes < sc_paged_work_bytes(c, pages->head_dim)) return SALICACHE_E_SHAPE;
     if (seqs->n_seqs == 0 || seqs->n_rows == 0) return SALICACHE_OK;
-    return sc_paged_attend(c, pages, seqs, d_q, q_stride, q_per_kv, softmax_scale, window, sinks, d_out, out_stride, d_lse,
+    return sc_paged_attend(c, pages, seqs, nullptr, 0, d_q, q_stride, q_per_kv, softmax_scale, window, sinks, d_out, out_stride, d_lse,
                            d_work, (cudaStream_t)cuda_stream);
+}
+
+int salicache_paged_attend_tree(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, const uint64_t* d_tree,
+                                int tree_words, const void* d_q, int64_t q_stride, int q_per_kv, float softmax_scale, int window,
+                                int sinks, void* d_out, int64_t out_stride, float* d_lse, void* d_work, int64_t work_bytes,
+                                void* cuda_stream) {
+    Range range__("salicache_paged_attend_tree");
+    int rc = check_attend(pages, seqs, d_q, q_stride, q_per_kv, softmax_scale, window, sinks, d_out, out_stride, d_lse, d_work);
+    if (rc == SALICACHE_OK && !d_tree) rc = SALICACHE_E_NULL;
+    if (rc == SALICACHE_OK && (tree_words < 1 || tree_words > 16)) rc = SALICACHE_E_PARAM;
+    if (rc == SALICACHE_OK && (reinterpret_cast<uintptr_t>(d_tree) & 7u)) rc = SALICACHE_E_ALIGN;
+    if (rc == SALICACHE_OK) rc = check_device(c);
+    if (rc != SALICACHE_OK) return rc;
+    if (work_bytes < sc_paged_work_bytes(c, pages->head_dim)) return SALICACHE_E_SHAPE;
+    if (seqs->n_seqs == 0 || seqs->n_rows == 0) return SALICACHE_OK;
+    return sc_paged_attend(c, pages, seqs, d_tree, tree_words, d_q, q_stride, q_per_kv, softmax_scale, window, sinks, d_out, out_stride,
+                           d_lse, d_work, (cudaStream_t)cuda_stream);
+}
+
+int salicache_paged_weigh(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, const void* d_q, int64_t q_stride,
+                          int q_per_kv, float softmax_scale, const float* d_lse, float decay, const float* d_weight_in,
+                          float* d_weight_out, int64_t weight_stride, void* d_work, int64_t work_bytes, void* cuda_stream) {
+    Range range__("salicache_paged_weigh");
+    // no output rows here: the rows of q stand in for them
+    int rc = check_attend(pages, seqs, d_q, q_stride, q_per_kv, softmax_scale, 0, 0, const_cast<void*>(d_q), q_stride, d_lse, d_work);
+    if (rc == SALICACHE_OK && (!d_lse || !d_weight_out)) rc = SALICACHE_E_NULL;
+    if (rc == SALICACHE_OK && !(decay >= 0.0f && decay <= 1.0f)) rc = SALICACHE_E_PARAM;
+    if (rc == SALICACHE_OK && weight_stride < 1) rc = SALICACHE_E_SHAPE;
+    if (rc == SALICACHE_OK && ((reinterpret_cast<uintptr_t>(d_weight_in) | reinterpret_cast<uintptr_t>(d_weight_out)) & 3u))
+        rc = SALICACHE_E_ALIGN;
+    if (rc == SALICACHE_OK) rc = check_device(c);
+    if (rc != SALICACHE_OK) return rc;
+    if (work_bytes < sc_paged_work_bytes(c, pages->head_dim)) return SALICACHE_E_SHAPE;
+    if (seqs->n_seqs == 0) return SALICACHE_OK;
+    return sc_paged_weigh(c, pages, seqs, d_q, q_stride, q_per_kv, softmax_scale, d_lse, decay, d_weight_in, d_weight_out, weight_stride,
+                          d_work, (cudaStream_t)cuda_stream);
+}
+
+int salicache_select_heavy(salicache_ctx* c, const float* d_weight, int64_t weight_stride, int heads, int n_seqs, const int32_t* d_len,
+                           int budget, int sinks, int recent, int32_t* d_keep, int32_t* d_kept, void* cuda_stream) {
+    Range range__("salicache_select_heavy");
+    if (!d_weight || !d_len || !d_keep || !d_kept) return SALICACHE_E_NULL;
+    if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return SALICACHE_E_PARAM;
+    if (heads < 1 || heads > 256 || n_seqs < 0 || (int64_t)n_seqs * heads >= (1 << 16) || weight_stride < 1) return SALICACHE_E_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(d_weight) | reinterpret_cast<uintptr_t>(d_len) | reinterpret_cast<uintptr_t>(d_keep) |
+         reinterpret_cast<uintptr_t>(d_kept)) & 3u)
+        return SALICACHE_E_ALIGN;
+    const int rc = check_device(c);
+    if (rc != SALICACHE_OK) return rc;
+    if (n_seqs == 0) return SALICACHE_OK;
+    return sc_select_heavy(c, d_weight, weight_stride, heads, n_seqs, d_len, budget, sinks, recent, d_keep, d_kept,
+                           (cudaStream_t)cuda_stream);
+}
+
+int salicache_paged_keep(salicache_ctx* c, const salicache_pages* pages, const salicache_seqs* seqs, const int32_t* d_keep,
+                         int keep_heads, int keep_width, const int32_t* d_first, const int32_t* d_kept, const salicache_seqs* to,
+                         const float* d_weight_in, float* d_weight_out, int64_t weight_stride, void* cuda_stream) {
+    Range range__("salicache_paged_keep");
+    int rc = check_pages(pages);
+    if (rc == SALICACHE_OK) rc = check_seqs(seqs);
+    if (rc == SALICACHE_OK && to) rc = check_seqs(to);
+    if (rc != SALICACHE_OK) return rc;
+    if (!d_keep || !d_kept || !d_weight_in != !d_weight_out) return SALICACHE_E_NULL;
+    if ((keep_heads != 1 && keep_heads != pages->heads) || keep_width < 0 || (to && to->n_seqs != seqs->n_seqs) ||
+        (int64_t)seqs->n_seqs * pages->heads >= (1 << 16) || (d_weight_in && weight_stride < 1))
+        return SALICACHE_E_SHAPE;
+    if (to && to->n_seqs > 0 && to->d_table == seqs->d_table) return SALICACHE_E_PARAM;
+    if ((reinterpret_cast<uintptr_t>(d_keep) | reinterpret_cast<uintptr_t>(d_first) | reinterpret_cast<uintptr_t>(d_kept) |
+         reinterpret_cast<uintptr_t>(d_weight_in) | reinterpret_cast<uintptr_t>(d_weight_out)) & 3u)
+        return SALICACHE_E_ALIGN;
+    rc = check_device(c);
+    if (rc != SALICACHE_OK) return rc;
+    if (seqs->n_seqs == 0 || keep_width == 0) return SALICACHE_OK;
+    return sc_paged_keep(c, pages, seqs, d_keep, keep_heads, keep_width, d_first, d_kept, to, d_weight_in, d_weight_out, weight_stride,
+                         (cudaStream_t)cuda_stream);
 }
 
 int salicache_poll_status(salicache_ctx* c, void* cuda_stream) {

@@ -101,9 +101,21 @@ int sc_attend(salicache_ctx* c, const void* d_q, int q_per_kv, const salicache_p
 int sc_paged_move(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, void* d_K, void* d_V, int64_t k_stride,
                   int64_t v_stride, bool write, cudaStream_t st);
 int64_t sc_paged_work_bytes(const salicache_ctx* c, int head_dim);
-int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, const void* d_q, int64_t q_stride,
-                    int q_per_kv, float softmax_scale, int window, int sinks, void* d_out, int64_t out_stride, float* d_lse,
-                    void* d_work, cudaStream_t st);
+int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, const uint64_t* d_tree, int tree_words,
+                    const void* d_q, int64_t q_stride, int q_per_kv, float softmax_scale, int window, int sinks, void* d_out,
+                    int64_t out_stride, float* d_lse, void* d_work, cudaStream_t st);
+// paged_rotary.cu, paged_weigh.cu, paged_evict.cu: likewise
+int sc_paged_write_rotary(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, const salicache_rotary* rotary,
+                          const int32_t* d_pos, const void* d_q, int64_t q_stride, int q_per_kv, void* d_q_out, int64_t q_out_stride,
+                          const void* d_K, const void* d_V, int64_t k_stride, int64_t v_stride, cudaStream_t st);
+int sc_paged_weigh(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, const void* d_q, int64_t q_stride,
+                   int q_per_kv, float softmax_scale, const float* d_lse, float decay, const float* d_weight_in, float* d_weight_out,
+                   int64_t weight_stride, void* d_work, cudaStream_t st);
+int sc_select_heavy(salicache_ctx* c, const float* d_weight, int64_t weight_stride, int heads, int n_seqs, const int32_t* d_len,
+                    int budget, int sinks, int recent, int32_t* d_keep, int32_t* d_kept, cudaStream_t st);
+int sc_paged_keep(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* sq, const int32_t* d_keep, int keep_heads,
+                  int keep_width, const int32_t* d_first, const int32_t* d_kept, const salicache_seqs* to, const float* d_weight_in,
+                  float* d_weight_out, int64_t weight_stride, cudaStream_t st);
 // kv.cu
 int sc_pack(salicache_ctx* c, const void* d_K, const void* d_V, int64_t frame_stride, const int32_t* d_idx,
             const int32_t* d_counts, const int64_t* d_row_offset, int B, const salicache_pools* pools, cudaStream_t st);

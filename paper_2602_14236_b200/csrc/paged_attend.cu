@@ -24,6 +24,7 @@
 // another's, weights stay below 2^8, and the sums are joined across lanes once at the end of an item.
 #include <math.h>
 
+#include "paged_frags.cuh"
 #include "paged_plan.cuh"
 
 namespace {
@@ -47,18 +48,6 @@ struct StSmem {
     static constexpr int ITEM = FMT == PF_I4 ? 3 : 2;
 };
 
-template <typename T>
-__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
-template <>
-__device__ __forceinline__ void mma16816<TypeF16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-template <>
-__device__ __forceinline__ void mma16816<TypeBF16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 // Joins the computing warps; whether any of their threads says so.
 __device__ __forceinline__ bool any_of(bool x) {
     uint32_t r;
@@ -71,33 +60,7 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
     return d;
 }
-// Key of row slot r of the fragments: the keys 2 c, 2 c + 1 that a lane multiplies are c and c + 4, which lie in
-// different banks.
-__device__ __forceinline__ int key_of(int g8) { return (g8 >> 1) + 4 * (g8 & 1); }
-
-// What a lane (g8 = lane / 4, c4 = lane % 4) takes of 16 keys: the shares of the keys of slots g8 and g8 + 8 of K that make
-// its A fragments, and its share of slots 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9 of V.
-template <int FMT, int D>
-struct KTile {
-    static constexpr int W = pg_row_bytes<FMT, D>() / 16;       // words of a key row per lane
-    uint32_t k[2][W];
-    uint32_t s[2];                                              // scale, or (scale, zero)
-    static constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
-    // this lane's first bytes of 16 keys' rows, and of their scales
-    static __device__ __forceinline__ uint32_t at(int g8, int c4) { return key_of(g8) * RB + (RB >= 64 ? 16 : 8) * c4; }
-    static __device__ __forceinline__ uint32_t meta_at(int g8) { return key_of(g8) * MB; }
-    __device__ __forceinline__ void load(uint32_t rows, uint32_t meta) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            if (RB >= 64) {
-#pragma unroll
-                for (int i = 0; i < RB / 64; ++i) lds16(&k[r][4 * i], rows + 8 * r * RB + 64 * i);
-            } else lds_words<2>(&k[r][0], rows + 8 * r * RB);
-            if (FMT == PF_I8) s[r] = lds_u16(meta + 8 * r * MB);
-            if (FMT == PF_I4) lds_words<1>(&s[r], meta + 8 * r * MB);
-        }
-    }
-};
+// What a lane takes of 16 values: its share of slots 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9 of V.
 template <int FMT, int D>
 struct VTile {
     static constexpr int W = pg_row_bytes<FMT, D>() / 32;       // words of a value row per lane
@@ -124,36 +87,6 @@ struct VTile {
     }
 };
 
-// K fragments of matrix instruction st: registers (a0, a2) of one key row.
-template <typename T, int FMT, int D>
-__device__ __forceinline__ void key_frag(const Codes<T>& cd, const uint32_t (&k)[KTile<FMT, D>::W], uint32_t s, int st, uint32_t& x, uint32_t& y) {
-    if (FMT == PF_16) {
-        x = k[2 * st];
-        y = k[2 * st + 1];
-    } else if (FMT == PF_I8) {
-        const uint32_t s2 = dup_lo(s);
-        x = mul2<T>(cd.bytes(k[st], 0x5140), s2);
-        y = mul2<T>(cd.bytes(k[st], 0x5342), s2);
-    } else {
-        const uint32_t s2 = dup_lo(s), z2 = dup_hi(s), w = k[st >> 1] >> (8 * (st & 1));
-        x = fma2<T>(cd.nib_lo(w), s2, z2);
-        y = fma2<T>(cd.nib_hi(w), s2, z2);
-    }
-}
-// The dimension pairs that instruction st multiplies in a lane's registers b0 and b1.
-template <int FMT>
-__device__ __forceinline__ void q_dims(int st, int c4, int D, int (&d)[4]) {
-    if (FMT == PF_16) {
-        const int base = (st >> 1) * 32 + c4 * 8 + (st & 1) * 4;
-        d[0] = base; d[1] = base + 1; d[2] = base + 2; d[3] = base + 3;
-    } else if (FMT == PF_I8) {
-        const int base = (st >> 2) * 64 + c4 * 16 + (st & 3) * 4;
-        d[0] = base; d[1] = base + 1; d[2] = base + 2; d[3] = base + 3;
-    } else {
-        const int base = c4 * (D / 4) + (st >> 1) * 8 + (st & 1) * 2;      // nibbles 2 (st & 1) and + 4; then + 1 and + 5
-        d[0] = base; d[1] = base + 4; d[2] = base + 1; d[3] = base + 5;
-    }
-}
 // V fragments of dimension tile t: rows g8 (half 0) and g8 + 8 (half 1) of V transposed, key pairs 0 and 1.
 template <typename T, int FMT, int D>
 __device__ __forceinline__ uint32_t value_frag(const Codes<T>& cd, const VTile<FMT, D>& v, int t, int half, int pair) {
@@ -177,8 +110,8 @@ __device__ __forceinline__ int value_dim(int t, int half, int g8) {
     return g8 * (D / 8) + half * (D / 16) + t;
 }
 
-// NT: 8-row column tiles per item.
-template <typename T, int FMT, int D, int NT>
+// NT: 8-row column tiles per item.  TREE: the rows are a tree's.
+template <typename T, int FMT, int D, int NT, bool TREE>
 __global__ void __launch_bounds__(ST_THREADS, StSmem<FMT, D, NT>::BLOCKS)
 k_paged_step(PtArgs a, int blocks) {
     using SM = StSmem<FMT, D, NT>;
@@ -369,7 +302,12 @@ k_paged_step(PtArgs a, int blocks) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int j = j0 + key_of(g8) + 8 * (i >> 1), rr = w.rt * RT + 8 * n + 2 * c4 + (i & 1);
-                            if (j >= s.len || !pt_sees(s.pos0 + rr / a.G, j, a.window, a.sinks)) sc[n][i] = -INFINITY;
+                            bool sees = j < s.len;
+                            if (!TREE) sees = sees && pt_sees(s.pos0 + rr / a.G, j, a.window, a.sinks);
+                            else if (rr >= s.n * a.G) sees = false;
+                            else if (j >= s.pos0) sees = sees && (pt_bits(a, s.row0 + rr / a.G, j - s.pos0, s.n) & 1u);
+                            else if (a.window) sees = sees && pt_sees(s.pos0 + pt_depth(a, s.row0 + rr / a.G, s.n), j, a.window, a.sinks);
+                            if (!sees) sc[n][i] = -INFINITY;
                         }
                     // values that no row sees may be anything: keep them out of the product
 #pragma unroll
@@ -499,11 +437,11 @@ k_paged_step(PtArgs a, int blocks) {
     }
 }
 
-template <typename T, int FMT, int D, int NT>
+template <typename T, int FMT, int D, int NT, bool TREE>
 int launch_step(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     using SM = StSmem<FMT, D, NT>;
     constexpr int RT = 8 * NT;
-    SC_CHECK(cudaFuncSetAttribute(k_paged_step<T, FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::BYTES));
+    SC_CHECK(cudaFuncSetAttribute(k_paged_step<T, FMT, D, NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::BYTES));
     // no more blocks than there can be tiles of work: rows of q times heads times the table's tiles
     const long long most = (long long)a.sq.n_rows * a.pc.heads * ((((long long)a.sq.width << a.pc.page_shift) + PT_KEYS - 1) / PT_KEYS);
     const int blocks = (int)max(1ll, min(min(most, (long long)PT_MAX_BLOCKS), (long long)c->sm_count * SM::BLOCKS));
@@ -511,29 +449,31 @@ int launch_step(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     a.part = reinterpret_cast<float*>(work);
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * RT * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * RT);
-    SC_CHECK(pt_launch(k_paged_step<T, FMT, D, NT>, dim3(blocks), ST_THREADS, SM::BYTES, st, a, blocks));
+    SC_CHECK(pt_launch(k_paged_step<T, FMT, D, NT, TREE>, dim3(blocks), ST_THREADS, SM::BYTES, st, a, blocks));
     SC_CHECK(pt_launch(k_paged_join<T, RT, D>, dim3(blocks, NT), 256, 0, st, a, blocks));
     c->launches += 2;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;
 }
 
-template <typename T, int FMT, int D>
+template <typename T, int FMT, int D, bool TREE>
 int launch_attend(salicache_ctx* c, const PtArgs& a, char* work, cudaStream_t st) {
     // one column tile of 8 rows, or two of them: codes are expanded once for both, at half the blocks per SM
     if constexpr (FMT != PF_16)
-        if ((long long)a.sq.n_rows * a.G > 8ll * a.sq.n_seqs) return launch_step<T, FMT, D, 2>(c, a, work, st);
-    return launch_step<T, FMT, D, 1>(c, a, work, st);
+        if ((long long)a.sq.n_rows * a.G > 8ll * a.sq.n_seqs) return launch_step<T, FMT, D, 2, TREE>(c, a, work, st);
+    return launch_step<T, FMT, D, 1, TREE>(c, a, work, st);
 }
 
 }  // namespace
 
 int64_t sc_paged_work_bytes(const salicache_ctx* c, int head_dim) { return 2ll * c->sm_count * (256 * (head_dim + 2) * 4 + 32); }
 
-int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* q, const void* d_q, int64_t q_stride,
-                    int q_per_kv, float softmax_scale, int window, int sinks, void* d_out, int64_t out_stride, float* d_lse,
-                    void* d_work, cudaStream_t st) {
+int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache_seqs* q, const uint64_t* d_tree, int tree_words,
+                    const void* d_q, int64_t q_stride, int q_per_kv, float softmax_scale, int window, int sinks, void* d_out,
+                    int64_t out_stride, float* d_lse, void* d_work, cudaStream_t st) {
     PtArgs a{};
+    a.tree = d_tree;
+    a.tree_words = tree_words;
     a.pc = pg_cache(pg);
     a.sq = pg_seqs(q);
     a.q = (const uint16_t*)d_q;
@@ -557,7 +497,7 @@ int sc_paged_attend(salicache_ctx* c, const salicache_pages* pg, const salicache
     // batch is better off with a call for each kind.
     const long long few = pg->format == SALICACHE_FP16 ? 8 : 16;
     if ((long long)a.sq.n_rows * a.G > few * a.sq.n_seqs) return sc_paged_chunk(c, a, pg, work, st);
-#define GO(T, F, D) return launch_attend<T, F, D>(c, a, work, st)
+#define GO(T, F, D) return a.tree ? launch_attend<T, F, D, true>(c, a, work, st) : launch_attend<T, F, D, false>(c, a, work, st)
 #define GO_FORMAT(T, D)                                      \
     do {                                                     \
         if (pg->format == SALICACHE_FP16) GO(T, PF_16, D);   \

@@ -150,8 +150,6 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uin
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 constexpr int CH_RAW = 4;                    // raw stages at most
-// Bits 0 .. n - 1.
-__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
 struct ChBars {
     uint64_t kv_full[CH_STAGES], kv_empty[CH_STAGES], raw_full[CH_RAW], raw_empty[CH_RAW], q_land[2], q_ready[2], q_empty[2], v_land[2], s_full[2], p_ready[2][2],
@@ -191,7 +189,8 @@ __device__ __noinline__ void permute_rows(uint32_t q_tile, uint32_t q_ready) {
     if ((threadIdx.x & 31) == 0) bar_arrive(q_ready);
 }
 
-template <typename T, int FMT, int D>
+// TREE: the rows are a tree's, and see what their bits name of the call's own positions.
+template <typename T, int FMT, int D, bool TREE>
 __global__ void __launch_bounds__(CH_THREADS, 1)
 k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map, int blocks) {
     using SM = ChSmem<FMT, D>;
@@ -279,12 +278,12 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
             if (rows > 0) {
                 const int rr = w.rt * a.tile_rows + half * HR + row;                 // this thread's row of the item
                 const bool live = row < rows;
-                const int pos = s.pos0 + (live ? rr : 0) / a.G;
+                const int own = (live ? rr : 0) / a.G, pos = s.pos0 + (TREE ? a.window ? pt_depth(a, s.row0 + own, s.n) : 0 : own);
                 float m = PT_NONE, l = 0.0f;
                 if (g.tiles > 0) {
                     // positions that every row of this half sees in full tiles need no mask
-                    const PtSpan hs = pt_span(s, a.G, w.rt * a.tile_rows + half * HR, w.rt * a.tile_rows + half * HR + rows, a.window, a.sinks);
-                    const int vis_hi = live ? max(0, min(pos + 1, s.len)) : 0;
+                    const PtSpan hs = pt_span(s, a.G, w.rt * a.tile_rows + half * HR, w.rt * a.tile_rows + half * HR + rows, a.window, a.sinks, TREE);
+                    const int vis_hi = live ? max(0, min(TREE ? s.pos0 : pos + 1, s.len)) : 0;
                     const int vis_lo = a.window ? pos - a.window + 1 : 0;
                     for (int k = 0; k < g.tiles; ++k, ++n_tile) {
                         if (!wait(bars.s_full[half], n_s++ & 1)) {
@@ -300,7 +299,12 @@ k_paged_chunk(PtArgs a, const __grid_constant__ CUtensorMap map, const __grid_co
 #pragma unroll 1
                             for (int c = 0; c < 4; ++c) {        // 32 keys at a time as a word of visible ones
                                 const uint32_t there = ((pages >> (2 * c) & 1u) ? 0xffffu : 0u) | ((pages >> (2 * c + 1) & 1u) ? 0xffff0000u : 0u);
-                                const uint32_t vis = below(hi - 32 * c) & (~below(lo - 32 * c) | below(sk - 32 * c)) & there;
+                                uint32_t vis = below(hi - 32 * c) & (~below(lo - 32 * c) | below(sk - 32 * c));
+                                if (TREE) {
+                                    const int j = j0 + 32 * c;
+                                    if (live && j + 32 > s.pos0) vis |= pt_bits(a, s.row0 + own, j - s.pos0, s.n) & below(s.len - j);
+                                }
+                                vis &= there;
                                 tc_ld32(x[0], S + 32 * c);
                                 tc_wait_ld(x[0]);
 #pragma unroll
@@ -839,29 +843,33 @@ bool rows_map(CUtensorMap* map, const PtArgs& a, int D, bool bf16) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int FMT, int D>
+template <typename T, int FMT, int D, bool TREE>
 int launch_chunk(salicache_ctx* c, PtArgs a, char* work, cudaStream_t st) {
     constexpr int BYTES = ChSmem<FMT, D>::BYTES;
     a.tile_rows = 2 * (128 / a.G) * a.G;
     CUtensorMap map{}, q_map{};
     if (!rows_map(&q_map, a, D, T::ONE == TypeBF16::ONE)) return SALICACHE_E_CUDA;
     if (FMT == PF_16 && !page_map(&map, a.pc, D, T::ONE == TypeBF16::ONE)) return SALICACHE_E_CUDA;
-    SC_CHECK(cudaFuncSetAttribute(k_paged_chunk<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
+    SC_CHECK(cudaFuncSetAttribute(k_paged_chunk<T, FMT, D, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
     const int blocks = min(c->sm_count, PT_MAX_BLOCKS);
     a.part = reinterpret_cast<float*>(work);
     a.stat = reinterpret_cast<float2*>(a.part + (size_t)2 * blocks * CH_ROWS * D);
     a.head = reinterpret_cast<int4*>(a.stat + (size_t)2 * blocks * CH_ROWS);
-    SC_CHECK(pt_launch(k_paged_chunk<T, FMT, D>, dim3(blocks), CH_THREADS, BYTES, st, a, map, q_map, blocks));
+    SC_CHECK(pt_launch(k_paged_chunk<T, FMT, D, TREE>, dim3(blocks), CH_THREADS, BYTES, st, a, map, q_map, blocks));
     SC_CHECK(pt_launch(k_paged_join_chunk<T, D>, dim3(2 * blocks), CH_ROWS, 0, st, a, blocks));
     c->launches += 2;
     return SALICACHE_OK;
 }
 
+template <typename T, int FMT, int D>
+int chunk_tree(salicache_ctx* c, const PtArgs& a, char* work, cudaStream_t st) {
+    return a.tree ? launch_chunk<T, FMT, D, true>(c, a, work, st) : launch_chunk<T, FMT, D, false>(c, a, work, st);
+}
 template <typename T, int D>
 int chunk_format(salicache_ctx* c, const PtArgs& a, int format, char* work, cudaStream_t st) {
-    if (format == SALICACHE_FP16) return launch_chunk<T, PF_16, D>(c, a, work, st);
-    if (format == SALICACHE_INT8) return launch_chunk<T, PF_I8, D>(c, a, work, st);
-    return launch_chunk<T, PF_I4, D>(c, a, work, st);
+    if (format == SALICACHE_FP16) return chunk_tree<T, PF_16, D>(c, a, work, st);
+    if (format == SALICACHE_INT8) return chunk_tree<T, PF_I8, D>(c, a, work, st);
+    return chunk_tree<T, PF_I4, D>(c, a, work, st);
 }
 
 }  // namespace

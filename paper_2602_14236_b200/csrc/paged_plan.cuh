@@ -34,6 +34,8 @@ struct PtArgs {
                                              // 1 + head or 0, row tile, -; then its sequence's first row, rows, -, -
     int* status;
     int wait_limit;                          // tries before a wait between a block's roles is given up
+    const uint64_t* tree;                    // rows that form a tree: [rows][tree_words] bits, which of the call's rows each sees; or NULL
+    int tree_words;
 };
 
 // paged_chunk.cu
@@ -47,11 +49,12 @@ struct PtSpan {
     int all_lo, all_hi;                      // positions in [all_lo, all_hi) or below min(sinks, all_hi) are seen by every row
     __device__ __forceinline__ int tile(int k) const { return k < sink_tiles ? k : first + (k - sink_tiles); }
 };
-__device__ __forceinline__ PtSpan pt_span(const PgSeq& s, int G, int r0, int r1, int window, int sinks) {
+// Rows of a tree are at positions from the first row's to the last one's, and see what their bits name of the call's rows.
+__device__ __forceinline__ PtSpan pt_span(const PgSeq& s, int G, int r0, int r1, int window, int sinks, bool tree) {
     PtSpan p;
-    const int p0 = s.pos0 + r0 / G, p1 = s.pos0 + (r1 - 1) / G;      // first and last row's position
+    const int p0 = tree ? s.pos0 : s.pos0 + r0 / G, p1 = tree ? s.pos0 + s.n - 1 : s.pos0 + (r1 - 1) / G;    // lowest and highest row's position
     p.hi = max(0, min(p1 + 1, s.len));
-    p.all_hi = max(0, min(p0 + 1, s.len));
+    p.all_hi = max(0, min(p0 + (tree ? 0 : 1), s.len));
     p.lo = window ? max(0, p0 - window + 1) : 0;
     p.all_lo = window ? max(0, p1 - window + 1) : 0;
     p.first = p.lo / PT_KEYS;
@@ -64,10 +67,26 @@ __device__ __forceinline__ bool pt_sees(int pos, int j, int window, int sinks) {
     return j <= pos && (window == 0 || j > pos - window || j < sinks);
 }
 
+// Bits 0 .. n - 1.
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+// Which of the call's rows t .. t + 31 of a sequence of n row `row` of the caller's arrays sees (t > -32).
+__device__ __forceinline__ uint32_t pt_bits(const PtArgs& a, int row, int t, int n) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(a.tree + (size_t)row * a.tree_words);
+    auto word = [&](int i) -> uint32_t { return i >= 0 && i < 2 * a.tree_words ? w[i] : 0u; };
+    return __funnelshift_r(word(t >> 5), word((t >> 5) + 1), t & 31) & below(n - t);
+}
+// How far behind the call's first position the window takes the row to be: its depth in the tree.
+__device__ __forceinline__ int pt_depth(const PtArgs& a, int row, int n) {
+    int bits = 0;
+#pragma unroll 1
+    for (int t = 0; t < min(n, 64 * a.tree_words); t += 32) bits += __popc(pt_bits(a, row, t, n));
+    return max(bits, 1) - 1;
+}
+
 __device__ __forceinline__ int pt_row_tiles(const PgSeq& s, const PtArgs& a) { return (s.n * a.G + a.tile_rows - 1) / a.tile_rows; }
 __device__ __forceinline__ PtSpan pt_item(const PgSeq& s, const PtArgs& a, int rt) {
     const int r0 = rt * a.tile_rows, r1 = min(r0 + a.tile_rows, s.n * a.G);
-    return pt_span(s, a.G, r0, r1, a.window, a.sinks);
+    return pt_span(s, a.G, r0, r1, a.window, a.sinks, a.tree != nullptr);
 }
 
 // A block's place in the line of tiles.
