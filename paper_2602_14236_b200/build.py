@@ -10,7 +10,7 @@ _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB = os.path.join(_PKG, "libsalicache.so")
 SOURCES = ["api.cu", "flow.cu", "saliency.cu", "select.cu", "anchor.cu", "ranked.cu", "kv.cu", "attend.cu", "noalloc.cu",
-           "paged.cu", "paged_attend.cu", "paged_chunk.cu", "paged_rotary.cu", "paged_weigh.cu", "paged_evict.cu"]
+           "paged.cu", "paged_attend.cu", "paged_chunk.cu", "paged_rotary.cu", "paged_weigh.cu", "paged_weigh_many.cu", "paged_evict.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--fmad=true",
          "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-I", os.path.join(_ROOT, "include"), "-I", CSRC]
 

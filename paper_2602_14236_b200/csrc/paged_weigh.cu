@@ -12,21 +12,9 @@
 #include <math.h>
 
 #include "paged_frags.cuh"
-#include "paged_plan.cuh"
+#include "paged_weigh.cuh"
 
 namespace {
-
-struct WgArgs {
-    PgCache pc;
-    PgSeqs sq;
-    const uint16_t* q;
-    const float *lse, *in;
-    float* out;
-    long long q_stride, w_stride;
-    int G;
-    float scale, decay;                      // scale * log2(e)
-    int* status;
-};
 
 constexpr int WG_THREADS = 256, WG_WARPS = WG_THREADS / 32;
 
@@ -36,7 +24,6 @@ struct WgPlace {
     PgSeq s;
     int held;                                // positions that have a weight
 };
-__device__ __forceinline__ int wg_held(const PgSeq& s, const WgArgs& a) { return (int)min((long long)s.len, a.w_stride); }
 __device__ __forceinline__ void wg_enter(WgPlace& p, const WgArgs& a) {
     p.s = pg_seq(a.sq, a.pc, p.b);
     p.held = wg_held(p.s, a);
@@ -178,11 +165,10 @@ k_weigh_few(WgArgs a) {
         const PgSeq& s = p.s;
         const int j0 = p.k << 4, rows = s.n * a.G;
         float had[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};
-        const size_t at = ((size_t)p.b * a.pc.heads + p.h) * a.w_stride + j0 + key_of(g8);
-        if (c4 == 0 && a.in) {
+        if (c4 == 0) {
 #pragma unroll
             for (int r = 0; r < 2; ++r)
-                if (j0 + key_of(g8) + 8 * r < min(s.n > 0 ? s.pos0 : p.held, p.held)) had[r] = a.in[at + 8 * r];
+                if (j0 + key_of(g8) + 8 * r < p.held) had[r] = wg_had(a, s, p.b, p.h, j0 + key_of(g8) + 8 * r);
         }
         if (lane == 0 && (pid == -1 || (p.k == 0 && (p.s.cut || p.s.len > a.w_stride)))) atomicMin(a.status, SALICACHE_E_CAPACITY);
         if (pid >= 0) {
@@ -219,7 +205,7 @@ k_weigh_few(WgArgs a) {
         for (int r = 0; r < 2; ++r) {
             sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 1);
             sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 2);
-            if (c4 == 0 && j0 + key_of(g8) + 8 * r < p.held) a.out[at + 8 * r] = fmaf(s.n > 0 ? a.decay : 1.0f, had[r], sum[r]);
+            if (c4 == 0 && j0 + key_of(g8) + 8 * r < p.held) wg_put(a, s, p.b, p.h, j0 + key_of(g8) + 8 * r, had[r], sum[r]);
         }
         if (--left == 0) break;
         t = next;
@@ -236,7 +222,7 @@ int launch_few(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
     return SALICACHE_OK;
 }
 template <typename T, int D>
-int weigh_format(salicache_ctx* c, const WgArgs& a, int format, cudaStream_t st) {
+int few_format(salicache_ctx* c, const WgArgs& a, int format, cudaStream_t st) {
     if (format == SALICACHE_FP16) return launch_few<T, PF_16, D>(c, a, st);
     if (format == SALICACHE_INT8) return launch_few<T, PF_I8, D>(c, a, st);
     return launch_few<T, PF_I4, D>(c, a, st);
@@ -260,7 +246,9 @@ int sc_paged_weigh(salicache_ctx* c, const salicache_pages* pg, const salicache_
     a.scale = softmax_scale * PT_LOG2E;
     a.decay = decay;
     a.status = c->d_status;
+    a.wait_limit = c->paged_wait;
+    if ((long long)sq->n_rows * q_per_kv > 16ll * sq->n_seqs) return sc_weigh_many(c, a, pg, (char*)d_work, st);
     if (pg->dtype == SALICACHE_F16)
-        return pg->head_dim == 128 ? weigh_format<TypeF16, 128>(c, a, pg->format, st) : weigh_format<TypeF16, 64>(c, a, pg->format, st);
-    return pg->head_dim == 128 ? weigh_format<TypeBF16, 128>(c, a, pg->format, st) : weigh_format<TypeBF16, 64>(c, a, pg->format, st);
+        return pg->head_dim == 128 ? few_format<TypeF16, 128>(c, a, pg->format, st) : few_format<TypeF16, 64>(c, a, pg->format, st);
+    return pg->head_dim == 128 ? few_format<TypeBF16, 128>(c, a, pg->format, st) : few_format<TypeBF16, 64>(c, a, pg->format, st);
 }

@@ -1,0 +1,34 @@
+// What the two kernels of salicache_paged_weigh share.
+#pragma once
+#include "paged_plan.cuh"
+
+struct WgArgs {
+    PgCache pc;
+    PgSeqs sq;
+    const uint16_t* q;
+    const float *lse, *in;
+    float* out;
+    long long q_stride, w_stride;
+    int G;
+    float scale, decay;                      // scale * log2(e)
+    int* status;
+    int wait_limit;                          // tries before a wait between a block's roles is given up
+    float* part;                             // [2 * blocks][keys of a tile]: sums of a tile's rows so far, tail after head records of a block
+    int4* head;                              // [2 * blocks]: per block: head record (0 none, 1 the tile goes on, 2 it ends), tail record
+                                             // (0, 1), its sequence, its head; then its tile of keys, -, -, -
+};
+
+// Positions of a sequence that have a weight.
+__device__ __forceinline__ int wg_held(const PgSeq& s, const WgArgs& a) { return (int)min((long long)s.len, a.w_stride); }
+
+// What position j of (sequence b, head h) had before, of which decay is left.
+__device__ __forceinline__ float wg_had(const WgArgs& a, const PgSeq& s, int b, int h, int j) {
+    if (!a.in || (s.n > 0 && j >= s.pos0)) return 0.0f;
+    return a.in[((size_t)b * a.pc.heads + h) * a.w_stride + j];
+}
+__device__ __forceinline__ void wg_put(const WgArgs& a, const PgSeq& s, int b, int h, int j, float had, float sum) {
+    a.out[((size_t)b * a.pc.heads + h) * a.w_stride + j] = fmaf(s.n > 0 ? a.decay : 1.0f, had, sum);
+}
+
+// paged_weigh_many.cu
+int sc_weigh_many(salicache_ctx* c, const WgArgs& a, const salicache_pages* pg, char* work, cudaStream_t st);

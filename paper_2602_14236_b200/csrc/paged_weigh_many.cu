@@ -1,0 +1,563 @@
+// What attention gave each cached position, many rows per sequence: the scores' product is the work, and runs on the
+// fifth-generation tensor cores; then every score costs one exponential.
+//
+// One block per SM walks its stretch of the line of (256 keys x 128 rows) tiles.  An item is 256 keys of one head, and its
+// tiles those of rows (new tokens times query heads of a group) that see some of the keys.  The scores stand transposed in
+// tensor memory, S^T = K Q^T: a lane is a key, a column a row of q, so that a thread sums its own key's weights over all rows in
+// a register and nothing is exchanged.  Two tiles' scores (2 x 2 x 128 columns) fill tensor memory: one is summed while the
+// other is multiplied.
+// Roles by warp group:
+//   0, 1   one thread per key of the first / last 128: e^(s - lse) over the columns, and at the item's end the weight
+//   2      codes from the pages to 16-bit operands, an item's keys at a time
+//   3      one thread issues the matrix instructions; one warp feeds K of 16-bit pages and the rows of q by tensor copies
+// K is double-buffered, and read once per item; the rows of q come once per tile, from the L2.
+// An item that the ends of blocks' stretches cut leaves partial sums, which a second kernel adds in the order of the blocks.
+#include <math.h>
+
+#include "paged_tc.cuh"
+#include "paged_weigh.cuh"
+
+namespace {
+
+constexpr int WM_THREADS = 512, WM_KEYS = 256, WM_K = 2, WM_Q = 2;
+// An item's fixed cost (its keys) in tiles' time.
+constexpr int WM_ITEM = 2;
+
+// A block's place in the line.
+struct WmWalk {
+    long long left;                          // units still to do
+    int b, h, kt, k;                         // sequence, head, tile of keys, unit within the item
+    PgSeq s;
+};
+// The tiles of rows of an item.
+struct WmRows {
+    int R, HR;                               // tiles of the sequence, rows of one (whole tokens)
+    __device__ __forceinline__ WmRows(const PgSeq& s, int G) : R((s.n + 128 / G - 1) / (128 / G)), HR(128 / G * G) {}
+};
+// First tile of rows that sees some key from j0 on.
+__device__ __forceinline__ int wm_first(const PgSeq& s, int G, int j0) { return max(0, j0 - s.pos0) / (128 / G); }
+__device__ __forceinline__ int wm_items(const PgSeq& s, const WgArgs& a) { return (wg_held(s, a) + WM_KEYS - 1) / WM_KEYS; }
+// Units of an item: its fixed cost and its tiles, one at least (a sequence without rows has its weights copied).
+__device__ __forceinline__ int wm_units(const PgSeq& s, int G, int kt) {
+    return WM_ITEM + max(1, WmRows(s, G).R - wm_first(s, G, kt * WM_KEYS));
+}
+// Items at the front that all rows see.
+__device__ __forceinline__ int wm_whole(const PgSeq& s, const WgArgs& a) {
+    return s.n == 0 ? wm_items(s, a) : min(wm_items(s, a), s.pos0 >= 0 ? s.pos0 / WM_KEYS + 1 : 0);
+}
+// Units of one head of the sequence that each lane of a warp has; the warp sums the items of long ones together.
+__device__ __forceinline__ long long wm_per_head(const WgArgs& a, const PgSeq& s) {
+    constexpr int ALONE = 2;
+    const int lane = threadIdx.x & 31, n = wm_items(s, a), whole = wm_whole(s, a);
+    long long w = whole > 0 ? (long long)whole * wm_units(s, a.G, 0) : 0;
+    if (n - whole <= ALONE)
+#pragma unroll 1
+        for (int kt = whole; kt < n; ++kt) w += wm_units(s, a.G, kt);
+    for (uint32_t many = __ballot_sync(0xffffffffu, n - whole > ALONE); many; many &= many - 1) {
+        const int from = __ffs(many) - 1;
+        const PgSeq o = pt_seq_of(s, from);
+        long long x = 0;
+#pragma unroll 1
+        for (int kt = __shfl_sync(0xffffffffu, whole, from) + lane; kt < __shfl_sync(0xffffffffu, n, from) + lane; kt += 32)
+            if (kt < wm_items(o, a)) x += wm_units(o, a.G, kt);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        if (lane == from) w += x;
+    }
+    return w;
+}
+// Where the block starts; the same for every thread, each warp for itself.
+__device__ __noinline__ WmWalk wm_start(const WgArgs& a, int block, int blocks) {
+    const int lane = threadIdx.x & 31;
+    auto seq = [&](int b) -> PgSeq {
+        PgSeq s{};
+        if (b < a.sq.n_seqs) s = pg_seq(a.sq, a.pc, b);
+        return s;
+    };
+    const PgSeq s0 = seq(lane);
+    const long long mine = wm_per_head(a, s0) * a.pc.heads;
+    long long total = 0;
+    for (int b0 = 0; b0 < a.sq.n_seqs; b0 += 32)
+        total += __shfl_sync(0xffffffffu, pt_scan(b0 == 0 ? mine : wm_per_head(a, seq(b0 + lane)) * a.pc.heads), 31);
+    WmWalk w{};
+    long long beg, end, before = 0;
+    pt_share(total, block, blocks, beg, end);
+    if (beg == end) return w;
+    for (int b0 = 0; b0 < a.sq.n_seqs; b0 += 32) {
+        const PgSeq s = b0 == 0 ? s0 : seq(b0 + lane);
+        const long long n = b0 == 0 ? mine : wm_per_head(a, s) * a.pc.heads, incl = before + pt_scan(n);
+        const uint32_t hit = __ballot_sync(0xffffffffu, beg >= incl - n && beg < incl);
+        before = __shfl_sync(0xffffffffu, incl, 31);
+        if (!hit) continue;
+        const int from = __ffs(hit) - 1;
+        w.s = pt_seq_of(s, from);
+        w.b = b0 + from;
+        w.left = end - beg;
+        const long long at = __shfl_sync(0xffffffffu, beg - (incl - n), from), per = __shfl_sync(0xffffffffu, n, from) / a.pc.heads;
+        w.h = (int)(at / per);
+        long long rem = at - w.h * per;
+        const int items = wm_items(w.s, a), whole = wm_whole(w.s, a), each = wm_units(w.s, a.G, 0);
+        if (rem < (long long)whole * each) {
+            w.kt = (int)(rem / each);
+            w.k = (int)(rem - (long long)w.kt * each);
+            return w;
+        }
+        rem -= (long long)whole * each;
+#pragma unroll 1
+        for (int k0 = whole;; k0 += 32) {
+            const int u = k0 + lane < items ? wm_units(w.s, a.G, k0 + lane) : 0;
+            const long long upto = pt_scan(u);
+            const uint32_t in = __ballot_sync(0xffffffffu, rem >= upto - u && rem < upto);
+            if (in || k0 + 32 >= items) {
+                const int f = in ? __ffs(in) - 1 : 0;
+                w.kt = k0 + f;
+                w.k = __shfl_sync(0xffffffffu, (int)(rem - (upto - u)), f);
+                return w;
+            }
+            rem -= __shfl_sync(0xffffffffu, upto, 31);
+        }
+    }
+    w.left = 0;
+    return w;
+}
+__device__ __noinline__ WmWalk wm_after(const WgArgs& a, WmWalk w) {
+    w.k = 0;
+    if (++w.kt < wm_items(w.s, a)) return w;
+    w.kt = 0;
+    if (++w.h < a.pc.heads) return w;
+    w.h = 0;
+#pragma unroll 1
+    do {
+        if (++w.b >= a.sq.n_seqs) return w;  // cannot happen while units are left
+        w.s = pg_seq(a.sq, a.pc, w.b);
+    } while (wm_items(w.s, a) == 0);
+    return w;
+}
+
+// A block's share of one item.
+struct WmSeg {
+    int k0, k1, tiles, rt, j0, held;         // units [k0, k1); tiles of rows from rt on; first key; positions with a weight
+    bool first, last, real;                  // the item begins, ends here; some of its tiles are here
+    __device__ __forceinline__ WmSeg(const WgArgs& a, const WmWalk& w) {
+        j0 = w.kt * WM_KEYS;
+        held = wg_held(w.s, a);
+        const int f = wm_first(w.s, a.G, j0), n = WmRows(w.s, a.G).R - f, units = WM_ITEM + max(1, n);
+        k0 = w.k;
+        k1 = (int)min((long long)units, k0 + w.left);
+        const int t0 = max(0, k0 - WM_ITEM), t1 = max(0, k1 - WM_ITEM);
+        first = t0 == 0;
+        last = k1 == units;
+        real = t1 > t0;
+        tiles = w.s.n == 0 ? 0 : t1 - t0;
+        rt = f + t0;
+    }
+    // Page of keys 16 grp .. of the item: -2 there are none (or grp > 15), -1 there is no such page.
+    __device__ __forceinline__ int page_of(const WgArgs& a, const WmWalk& w, int grp) const {
+        const int j = j0 + grp * 16;
+        if (grp > 15 || j >= held) return -2;
+        const int p = a.sq.table[(size_t)w.b * a.sq.width + (j >> a.pc.page_shift)];
+        return p >= 0 && p < a.pc.n_pages ? p : -1;
+    }
+};
+
+struct WmBars {
+    uint64_t k_full[WM_K], k_empty[WM_K], q_full[WM_Q], q_empty[WM_Q], s_full[2], s_free[2], left;
+    uint32_t tmem;
+    int gave_up;
+    uint32_t pages[8];                       // per item with tiles (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
+};
+template <int D>
+struct WmSmem {
+    static constexpr int TILE = 128 * D * 2;         // bytes of an operand tile
+    static constexpr int K = 0, Q = K + WM_K * 2 * TILE, LSE = Q + WM_Q * TILE, BARS = LSE + 8 * 128 * 4;
+    static constexpr int BYTES = BARS + (int)sizeof(WmBars) + 1024;
+    static_assert(BYTES <= 227 * 1024, "shared memory");
+};
+
+template <typename T, int FMT, int D>
+__global__ void __launch_bounds__(WM_THREADS, 1)
+k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map, int blocks) {
+    using SM = WmSmem<D>;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    uint8_t* const mem = raw + (base - smem_u32(raw));
+    WmBars& bars = *reinterpret_cast<WmBars*>(mem + SM::BARS);
+    const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
+    volatile int* gave_up = &bars.gave_up;
+    if (tid == 0) {
+        for (int i = 0; i < WM_K; ++i) {
+            bar_init(smem_u32(&bars.k_full[i]), FMT == PF_16 ? 1 : 4);       // the feeder, or the warps of group 2
+            bar_init(smem_u32(&bars.k_empty[i]), 1);
+        }
+        for (int i = 0; i < WM_Q; ++i) {
+            bar_init(smem_u32(&bars.q_full[i]), 1);
+            bar_init(smem_u32(&bars.q_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_u32(&bars.s_full[i]), 1);
+            bar_init(smem_u32(&bars.s_free[i]), 8);          // a lane of each warp that reads them
+        }
+        bar_init(smem_u32(&bars.left), 1);
+        bars.gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (wid == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // rows of a tile that no copy fills (128 is no multiple of G) are zeros
+    const int HR = 128 / a.G * a.G;
+    for (int i = tid; i < WM_Q * (128 - HR) * (D / 8); i += WM_THREADS) {
+        const int c = i % (D / 8), r = i / (D / 8) % (128 - HR), q = i / (D / 8) / (128 - HR);
+        sts16(base + SM::Q + q * SM::TILE + swz(HR + r, c), 0u, 0u, 0u, 0u);
+    }
+    fence_async();
+    grid_wait();
+    grid_release();
+    tc_before();
+    WmWalk w = wm_start(a, blockIdx.x, blocks);
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = bars.tmem;
+    auto wait = [&](uint64_t& bar, uint32_t parity) -> bool { return warp_wait_far(smem_u32(&bar), parity, a.wait_limit, gave_up); };
+    auto next = [&](const WmSeg& g) {
+        w.left -= g.k1 - g.k0;
+        if (w.left > 0) w = wm_after(a, w);
+    };
+
+    if (wid < 8) {
+        // ---------------- weights
+        const int half = wid >> 2;
+        const uint32_t S = tmem + 128 * half + ((uint32_t)((wid & 3) * 32) << 16);
+        float4* const lses = reinterpret_cast<float4*>(mem + SM::LSE) + wid * 32;        // a warp's own copy: no barrier between warps
+        int4 hd[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+        uint32_t n = 0, n_item = 0;              // tiles, items with tiles so far
+        bool ok = true;
+        // minus the sums of columns 4 lane .. 4 lane + 3 of tile rt, in powers of two; -inf for what is no row
+        int off[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) off[i] = (4 * lane + i) / a.G * (a.pc.heads * a.G) + (4 * lane + i) % a.G;
+        auto lse_of = [&](const WmWalk& x, int rt, float (&l)[4]) {
+            const float* p = a.lse + (long long)(x.s.row0 + rt * (128 / a.G)) * (a.pc.heads * a.G) + x.h * a.G;
+            const int cols = min(HR, x.s.n * a.G - rt * HR);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                l[i] = -INFINITY;
+                if (4 * lane + i < cols) {
+                    const float y = __ldg(p + off[i]);
+                    l[i] = y == -INFINITY ? y : -y * PT_LOG2E;
+                }
+            }
+        };
+        while (w.left > 0 && ok) {
+            const WmSeg g(a, w);
+            if (tid == 0 && (w.s.cut || w.s.len > a.w_stride)) atomicMin(a.status, SALICACHE_E_CAPACITY);
+            const int j = g.j0 + tid;            // this thread's key
+            float sum = 0.0f, l[4];
+            if (g.tiles > 0) lse_of(w, g.rt, l);
+            const bool mine = j < g.held;
+            const float had = mine && g.first && g.last ? wg_had(a, w.s, w.b, w.h, j) : 0.0f;
+            for (int t = 0; t < g.tiles; ++t, ++n) {
+                const uint32_t buf = n & 1;
+                __syncwarp();                    // the tile before has been read
+                lses[lane] = make_float4(l[0], l[1], l[2], l[3]);
+                __syncwarp();
+                if (t + 1 < g.tiles) lse_of(w, g.rt + t + 1, l);
+                if (!wait(bars.s_full[buf], n >> 1 & 1)) {
+                    ok = false;
+                    break;
+                }
+                tc_after();
+                // columns that see this key: rows from its own on, up to the last one
+                const int r0 = (g.rt + t) * HR, c_hi = min(HR, w.s.n * a.G - r0);
+                const bool whole = c_hi == HR && (long long)(g.j0 + half * 128 + 127 - w.s.pos0) * a.G <= r0;
+                const int c_lo = max(0, min(128, max(0, j - w.s.pos0) * a.G - r0));
+                float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                uint32_t x[2][32];
+                tc_ld32(x[0], S + 256 * buf);
+                tc_wait_ld(x[0]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (c < 3) tc_ld32(x[(c + 1) & 1], S + 256 * buf + 32 * (c + 1));
+                    const float4* ls = lses + 8 * c;
+                    if (whole) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 lv = ls[i];
+                            acc[0] += ex2(fmaf(__uint_as_float(x[c & 1][4 * i]), a.scale, lv.x));
+                            acc[1] += ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 1]), a.scale, lv.y));
+                            acc[2] += ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 2]), a.scale, lv.z));
+                            acc[3] += ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 3]), a.scale, lv.w));
+                        }
+                    } else {
+                        const uint32_t sees = below(c_hi - 32 * c) & ~below(c_lo - 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 lv = ls[i];
+                            const float p0 = ex2(fmaf(__uint_as_float(x[c & 1][4 * i]), a.scale, lv.x)), p1 = ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 1]), a.scale, lv.y));
+                            const float p2 = ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 2]), a.scale, lv.z)), p3 = ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 3]), a.scale, lv.w));
+                            acc[0] += sees & 1u << (4 * i) ? p0 : 0.0f;
+                            acc[1] += sees & 2u << (4 * i) ? p1 : 0.0f;
+                            acc[2] += sees & 4u << (4 * i) ? p2 : 0.0f;
+                            acc[3] += sees & 8u << (4 * i) ? p3 : 0.0f;
+                        }
+                    }
+                    if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
+                    if (c == 2) {                // all columns are in registers
+                        tc_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_u32(&bars.s_free[buf]));
+                    }
+                }
+                sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+            }
+            if (!ok) break;
+            if (g.tiles > 0) {
+                if (!(*(volatile uint32_t*)&bars.pages[n_item & 7] >> (tid >> 4) & 1u)) sum = 0.0f;
+                ++n_item;
+            }
+            if (g.real) {
+                if (g.first && g.last) {
+                    if (mine) wg_put(a, w.s, w.b, w.h, j, had, sum);
+                } else {
+                    a.part[(2 * (size_t)blockIdx.x + (g.first ? 1 : 0)) * WM_KEYS + tid] = sum;
+                    if (g.first) {
+                        hd[0].y = 1;
+                        hd[0].z = w.b;
+                        hd[0].w = w.h;
+                        hd[1].x = w.kt;
+                    } else hd[0].x = g.last ? 2 : 1;
+                }
+            }
+            next(g);
+        }
+        if (tid == 0) {
+            a.head[2 * blockIdx.x] = hd[0];
+            a.head[2 * blockIdx.x + 1] = hd[1];
+        }
+    } else if (wid < 12) {
+        // ---------------- codes to operands: 64 keys a warp
+        if (FMT != PF_16) {
+            constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>(), LPR = RB / 16, RPP = 32 / LPR, P = 16 / RPP;
+            static_assert(P >= 1, "16 keys at a time");
+            const Codes<T> cd;
+            const int lw = wid - 8, c = lane % LPR;
+            uint32_t n_item = 0;
+            while (w.left > 0) {
+                const WmSeg g(a, w);
+                if (g.tiles > 0) {
+                    const uint32_t kb = n_item % WM_K;
+                    const int pid16 = g.page_of(a, w, lane);
+                    if (n_item >= WM_K && !wait(bars.k_empty[kb], (n_item / WM_K - 1) & 1)) break;
+                    if (lw == 0) {
+                        const uint32_t there = __ballot_sync(0xffffffffu, pid16 >= 0), bad = __ballot_sync(0xffffffffu, pid16 == -1);
+                        if (lane == 0) {
+                            *(volatile uint32_t*)&bars.pages[n_item & 7] = there;
+                            if (bad) atomicMin(a.status, SALICACHE_E_CAPACITY);
+                        }
+                    }
+                    const uint32_t dst = base + SM::K + kb * 2 * SM::TILE + (lw >> 1) * SM::TILE;
+#pragma unroll
+                    for (int grp = 0; grp < 4; ++grp) {
+                        const int pid = __shfl_sync(0xffffffffu, pid16, lw * 4 + grp);
+                        if (pid < 0) continue;                   // what lies there is not looked at
+                        const size_t slot = pg_slot(a.pc, pid, 0, w.h, (g.j0 + lw * 64 + grp * 16) & ((1 << a.pc.page_shift) - 1));
+                        uint4 words[P];
+                        uint32_t meta[P];
+#pragma unroll
+                        for (int p = 0; p < P; ++p) {
+                            const int r = p * RPP + lane / LPR;
+                            words[p] = __ldcs(reinterpret_cast<const uint4*>(a.pc.data + (slot + r) * RB) + c);
+                            const uint8_t* m = a.pc.scale + (slot + r) * MB;
+                            meta[p] = FMT == PF_I8 ? *reinterpret_cast<const uint16_t*>(m) : *reinterpret_cast<const uint32_t*>(m);
+                        }
+#pragma unroll
+                        for (int p = 0; p < P; ++p) {
+                            const int row = (lw & 1) * 64 + grp * 16 + p * RPP + lane / LPR;
+                            const uint32_t s2 = dup_lo(meta[p]), z2 = dup_hi(meta[p]), w4[4] = {words[p].x, words[p].y, words[p].z, words[p].w};
+                            if (FMT == PF_I8) {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i)
+                                    sts16(dst + swz(row, 2 * c + i), mul2<T>(cd.bytes(w4[2 * i], 0x5140), s2), mul2<T>(cd.bytes(w4[2 * i], 0x5342), s2),
+                                          mul2<T>(cd.bytes(w4[2 * i + 1], 0x5140), s2), mul2<T>(cd.bytes(w4[2 * i + 1], 0x5342), s2));
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {                    // elements 0 4, 1 5, 2 6, 3 7 in their words: put in order
+                                    const uint32_t y = w4[i] >> 8, e04 = fma2<T>(cd.nib_lo(w4[i]), s2, z2), e15 = fma2<T>(cd.nib_hi(w4[i]), s2, z2);
+                                    const uint32_t e26 = fma2<T>(cd.nib_lo(y), s2, z2), e37 = fma2<T>(cd.nib_hi(y), s2, z2);
+                                    sts16(dst + swz(row, 4 * c + i), __byte_perm(e04, e15, 0x5410), __byte_perm(e26, e37, 0x5410),
+                                          __byte_perm(e04, e15, 0x7632), __byte_perm(e26, e37, 0x7632));
+                                }
+                            }
+                        }
+                    }
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(&bars.k_full[kb]));
+                    ++n_item;
+                }
+                next(g);
+            }
+        }
+    } else {
+        if (wid == 12) {
+            // ---------------- matrix instructions: the warp stays together, one lane issues
+            constexpr uint32_t ID = instr_desc<T>(128, false);
+            const uint32_t k_lo = desc_lo(base + SM::K, 16), q_lo = desc_lo(base + SM::Q, 16);
+            uint32_t n = 0, n_item = 0;
+            bool ok = true;
+            while (w.left > 0 && ok) {
+                const WmSeg g(a, w);
+                const uint32_t kb = n_item % WM_K;
+                const int halves = g.held - g.j0 > 128 ? 2 : 1;
+                if (g.tiles > 0) ok = wait(bars.k_full[kb], n_item / WM_K & 1);
+                for (int t = 0; t < g.tiles && ok; ++t, ++n) {
+                    const uint32_t buf = n & 1, st = n % WM_Q;
+                    ok = wait(bars.q_full[st], n / WM_Q & 1);
+                    if (ok && n >= 2) ok = wait(bars.s_free[buf], (n / 2 - 1) & 1);
+                    if (!ok) break;
+                    tc_after();
+                    if (elect_one()) {
+                        for (int h = 0; h < halves; ++h) {
+                            const uint32_t ka = k_lo + (kb * 2 + h) * (SM::TILE >> 4), qb = q_lo + st * (SM::TILE >> 4);
+#pragma unroll
+                            for (int i = 0; i < D / 16; ++i) {
+                                const uint32_t off = (i >> 2) * 1024 + (i & 3) * 2;
+                                mma_ss(tmem + 256 * buf + 128 * h, desc(ka + off), desc(qb + off), ID, i > 0);
+                            }
+                        }
+                        tc_commit(smem_u32(&bars.s_full[buf]));
+                        tc_commit(smem_u32(&bars.q_empty[st]));
+                        if (t == g.tiles - 1) tc_commit(smem_u32(&bars.k_empty[kb]));
+                    }
+                    __syncwarp();
+                }
+                n_item += g.tiles > 0;
+                next(g);
+            }
+            // what the instructions' ends arrive at is there until they have
+            for (uint32_t i = n > WM_Q ? n - WM_Q : 0; i < n && ok; ++i) ok = wait(bars.q_empty[i % WM_Q], i / WM_Q & 1);
+            for (uint32_t i = n_item > WM_K ? n_item - WM_K : 0; i < n_item && ok; ++i) ok = wait(bars.k_empty[i % WM_K], i / WM_K & 1);
+            if (!ok) {
+                if (elect_one()) tc_commit(smem_u32(&bars.left));
+                __syncwarp();
+                bar_drain(smem_u32(&bars.left), 0);
+            }
+        }
+        if (wid == 13) {
+            // ---------------- feeder
+            uint32_t n = 0, n_item = 0;
+            bool ok = true;
+            const int per_page = 1 << a.pc.page_shift;
+            if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+            while (w.left > 0 && ok) {
+                const WmSeg g(a, w);
+                if (FMT == PF_16 && g.tiles > 0) {
+                    const uint32_t kb = n_item % WM_K, bar = smem_u32(&bars.k_full[kb]);
+                    const int pid16 = g.page_of(a, w, lane);
+                    const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), there = __ballot_sync(0xffffffffu, pid16 >= 0);
+                    // the first group of 16 keys of this lane's page names the page
+                    const int pid = __shfl_sync(0xffffffffu, pid16, (lane << (a.pc.page_shift - 4)) & 31);
+                    const bool mine = lane < WM_KEYS >> a.pc.page_shift && pid >= 0;
+                    const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine));
+                    if (n_item >= WM_K && !wait(bars.k_empty[kb], (n_item / WM_K - 1) & 1)) {
+                        ok = false;
+                        break;
+                    }
+                    if (lane == 0) {
+                        *(volatile uint32_t*)&bars.pages[n_item & 7] = there;
+                        if (bad) atomicMin(a.status, SALICACHE_E_CAPACITY);
+                        bar_expect(bar, copies * (uint32_t)(per_page * D * 2));
+                    }
+                    __syncwarp();
+                    if (mine) {
+                        const size_t slot = pg_slot(a.pc, pid, 0, w.h, 0);
+                        const int key = lane << a.pc.page_shift;
+                        const uint32_t dst = base + SM::K + (kb * 2 + (key >> 7)) * SM::TILE + (key & 127) * 128;
+#pragma unroll
+                        for (int x = 0; x < D; x += 64) tensor_copy(dst + x * 256, &map, x, (int)slot, bar);
+                    }
+                    __syncwarp();
+                }
+                n_item += g.tiles > 0;
+                for (int t = 0; t < g.tiles; ++t, ++n) {
+                    const uint32_t st = n % WM_Q, bar = smem_u32(&bars.q_full[st]);
+                    if (n >= WM_Q && !wait(bars.q_empty[st], (n / WM_Q - 1) & 1)) {
+                        ok = false;
+                        break;
+                    }
+                    if (lane == 0) {
+                        bar_expect(bar, (uint32_t)(HR * D * 2));
+                        for (int x = 0; x < D; x += 64)
+                            tensor_copy3(base + SM::Q + st * SM::TILE + x * 256, &q_map, x, w.h * a.G, w.s.row0 + (g.rt + t) * (128 / a.G), bar);
+                    }
+                    __syncwarp();
+                }
+                if (ok) next(g);
+            }
+            join_roles();
+            // copies in flight end before the block does: who uses a stage waits for them, unless a role has left early
+            if (*gave_up) {
+                for (uint32_t i = n > WM_Q ? n - WM_Q : 0; i < n; ++i) bar_drain(smem_u32(&bars.q_full[i % WM_Q]), i / WM_Q & 1);
+                if (FMT == PF_16)
+                    for (uint32_t i = n_item > WM_K ? n_item - WM_K : 0; i < n_item; ++i) bar_drain(smem_u32(&bars.k_full[i % WM_K]), i / WM_K & 1);
+            }
+            return;
+        }
+        __syncwarp();
+    }
+    tc_before();
+    join_roles();
+    if (tid == 0 && *gave_up) atomicMin(a.status, SC_GAVE_UP);
+    if (wid == 12) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+// Joins split items: block c that item whose tail block c of the first kernel left; a thread per key.
+__global__ void __launch_bounds__(WM_KEYS)
+k_weigh_join(WgArgs a, int blocks) {
+    __shared__ int list[PT_MAX_BLOCKS + 1];
+    grid_wait();
+    const int4 hd = a.head[2 * blockIdx.x];
+    if (hd.y == 0) return;
+    const int b = hd.z, h = hd.w, j = a.head[2 * blockIdx.x + 1].x * WM_KEYS + threadIdx.x;
+    const int n = pt_records([&](int c) { return a.head[2 * c].x; }, blockIdx.x, blocks, list);
+    const PgSeq s = pg_seq(a.sq, a.pc, b);
+    float sum = 0.0f;
+    for (int i = 0; i < n; ++i) sum += a.part[(size_t)list[i] * WM_KEYS + threadIdx.x];
+    if (j < wg_held(s, a)) wg_put(a, s, b, h, j, wg_had(a, s, b, h, j), sum);
+}
+
+template <typename T, int FMT, int D>
+int launch_many(salicache_ctx* c, WgArgs a, char* work, cudaStream_t st) {
+    constexpr int BYTES = WmSmem<D>::BYTES;
+    CUtensorMap map{}, q_map{};
+    const bool bf16 = T::ONE == TypeBF16::ONE;
+    if (!rows_map(&q_map, a.q, a.q_stride, a.pc.heads, a.G, a.sq.n_rows, D, bf16)) return SALICACHE_E_CUDA;
+    if (FMT == PF_16 && !page_map(&map, a.pc, D, bf16)) return SALICACHE_E_CUDA;
+    SC_CHECK(cudaFuncSetAttribute(k_weigh_many<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
+    const int blocks = min(c->sm_count, PT_MAX_BLOCKS);
+    a.part = reinterpret_cast<float*>(work);
+    a.head = reinterpret_cast<int4*>(a.part + (size_t)2 * blocks * WM_KEYS);
+    SC_CHECK(pt_launch(k_weigh_many<T, FMT, D>, dim3(blocks), WM_THREADS, BYTES, st, a, map, q_map, blocks));
+    SC_CHECK(pt_launch(k_weigh_join, dim3(blocks), WM_KEYS, 0, st, a, blocks));
+    c->launches += 2;
+    SC_CHECK(cudaGetLastError());
+    return SALICACHE_OK;
+}
+template <typename T, int D>
+int many_format(salicache_ctx* c, const WgArgs& a, int format, char* work, cudaStream_t st) {
+    if (format == SALICACHE_FP16) return launch_many<T, PF_16, D>(c, a, work, st);
+    if (format == SALICACHE_INT8) return launch_many<T, PF_I8, D>(c, a, work, st);
+    return launch_many<T, PF_I4, D>(c, a, work, st);
+}
+
+}  // namespace
+
+int sc_weigh_many(salicache_ctx* c, const WgArgs& a, const salicache_pages* pg, char* work, cudaStream_t st) {
+    if (pg->dtype == SALICACHE_F16)
+        return pg->head_dim == 128 ? many_format<TypeF16, 128>(c, a, pg->format, work, st) : many_format<TypeF16, 64>(c, a, pg->format, work, st);
+    return pg->head_dim == 128 ? many_format<TypeBF16, 128>(c, a, pg->format, work, st) : many_format<TypeBF16, 64>(c, a, pg->format, work, st);
+}
