@@ -7,19 +7,27 @@
 // a register and nothing is exchanged.  Two tiles' scores (2 x 2 x 128 columns) fill tensor memory: one is summed while the
 // other is multiplied.
 // Roles by warp group:
-//   0, 1   one thread per key of the first / last 128: e^(s - lse) over the columns, and at the item's end the weight
-//   2      codes from the pages to 16-bit operands, an item's keys at a time
-//   3      one thread issues the matrix instructions; one warp feeds K of 16-bit pages and the rows of q by tensor copies
+//   0 .. 3 two threads per key, one for odd tiles and one for even ones: e^(s - lse) over the columns, and at the item's end the
+//          weight.  The two groups of a half never wait for one another within an item, so that one has exponentials to do while
+//          the other waits for its scores
+//   4      codes from the pages to 16-bit operands, an item's keys at a time
+//   5      one thread issues the matrix instructions; one warp feeds K of 16-bit pages and the rows of q by tensor copies, another
+//          one the rows' sums
 // K is double-buffered, and read once per item; the rows of q come once per tile, from the L2.
 // An item that the ends of blocks' stretches cut leaves partial sums, which a second kernel adds in the order of the blocks.
 #include <math.h>
+#include <type_traits>
 
 #include "paged_tc.cuh"
 #include "paged_weigh.cuh"
 
 namespace {
 
-constexpr int WM_THREADS = 512, WM_KEYS = 256, WM_K = 2, WM_Q = 2;
+constexpr int WM_KEYS = 256, WM_K = 2, WM_Q = 3;
+// Which of eight columns take their exponentials on the FMA pipe instead of the special-function unit.
+#ifndef WM_POLY
+#define WM_POLY 0x11
+#endif
 // An item's fixed cost (its keys) in tiles' time.
 constexpr int WM_ITEM = 2;
 
@@ -160,8 +168,38 @@ struct WmSeg {
     }
 };
 
+// 2^x without the special-function unit, to 2.2e-7: x = n + f, n the nearest integer, which 1.5 * 2^23 + x holds in its low bits;
+// a polynomial of degree 5 for 2^f on [-1/2, 1/2] (least largest relative error, by the Remez exchange); n goes into the
+// exponent.  Below -126 the result is some number below 2^-126; above 127 it is not right.
+__device__ __forceinline__ float ex2_fma(float x) {
+    const float y = fmaxf(x, -127.0f), t = y + 12582912.0f, f = y - (t - 12582912.0f);
+    float p = fmaf(0x1.5c08e6p-10f, f, 0x1.3d0c52p-7f);
+    p = fmaf(p, f, 0x1.c6b6e4p-5f);
+    p = fmaf(p, f, 0x1.ebf918p-3f);
+    p = fmaf(p, f, 0x1.62e428p-1f);
+    p = fmaf(p, f, 0x1.000002p+0f);
+    return __uint_as_float((__float_as_uint(t) << 23) + __float_as_uint(p));
+}
+
+__device__ __forceinline__ uint64_t pair2(float lo, float hi) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ void split2(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2x(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2x(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 struct WmBars {
-    uint64_t k_full[WM_K], k_empty[WM_K], q_full[WM_Q], q_empty[WM_Q], s_full[2], s_free[2], left;
+    uint64_t k_full[WM_K], k_empty[WM_K], q_full[WM_Q], q_empty[WM_Q], l_full[2], s_full[2][2], s_free[2][2], o_full, o_empty, left;
+    int4 hd[2];                              // what the block says of its records
     uint32_t tmem;
     int gave_up;
     uint32_t pages[8];                       // per item with tiles (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
@@ -169,18 +207,21 @@ struct WmBars {
 template <int D>
 struct WmSmem {
     static constexpr int TILE = 128 * D * 2;         // bytes of an operand tile
-    static constexpr int K = 0, Q = K + WM_K * 2 * TILE, LSE = Q + WM_Q * TILE, BARS = LSE + 8 * 128 * 4;
-    static constexpr int BYTES = BARS + (int)sizeof(WmBars) + 1024;
+    static constexpr int K = 0, Q = K + WM_K * 2 * TILE, LSE = Q + WM_Q * TILE, OTHER = LSE + 2 * 128 * 4, BARS = OTHER + WM_KEYS * 4;
+    static constexpr int BYTES = BARS + (int)sizeof(WmBars);
     static_assert(BYTES <= 227 * 1024, "shared memory");
 };
 
+// Warps: 16 for the weights, 4 for codes where there are any, 4 more.
+template <int FMT> __host__ __device__ constexpr int wm_threads() { return FMT == PF_16 ? 640 : 768; }
+
 template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(WM_THREADS, 1)
+__global__ void __launch_bounds__(wm_threads<FMT>(), 1)
 k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map, int blocks) {
     using SM = WmSmem<D>;
-    extern __shared__ uint8_t raw[];
-    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    uint8_t* const mem = raw + (base - smem_u32(raw));
+    constexpr int WM_THREADS = wm_threads<FMT>(), LAST = WM_THREADS / 32 - 4;           // first warp of the last group
+    extern __shared__ __align__(1024) uint8_t mem[];         // the swizzle's atoms; there is no room to align by hand
+    const uint32_t base = smem_u32(mem);
     WmBars& bars = *reinterpret_cast<WmBars*>(mem + SM::BARS);
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
     volatile int* gave_up = &bars.gave_up;
@@ -194,14 +235,20 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
             bar_init(smem_u32(&bars.q_empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            bar_init(smem_u32(&bars.s_full[i]), 1);
-            bar_init(smem_u32(&bars.s_free[i]), 8);          // a lane of each warp that reads them
+            bar_init(smem_u32(&bars.l_full[i]), 1);
+            for (int h = 0; h < 2; ++h) {
+                bar_init(smem_u32(&bars.s_full[i][h]), 1);
+                bar_init(smem_u32(&bars.s_free[i][h]), 4);   // a lane of each warp that reads them
+            }
         }
+        bar_init(smem_u32(&bars.o_full), 8);
+        bar_init(smem_u32(&bars.o_empty), 8);
         bar_init(smem_u32(&bars.left), 1);
         bars.gave_up = 0;
+        bars.hd[0] = bars.hd[1] = make_int4(0, 0, 0, 0);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (wid == 12) {
+    if (wid == LAST) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -225,45 +272,24 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
         if (w.left > 0) w = wm_after(a, w);
     };
 
-    if (wid < 8) {
+    if (wid < 16) {
         // ---------------- weights
-        const int half = wid >> 2;
-        const uint32_t S = tmem + 128 * half + ((uint32_t)((wid & 3) * 32) << 16);
-        float4* const lses = reinterpret_cast<float4*>(mem + SM::LSE) + wid * 32;        // a warp's own copy: no barrier between warps
-        int4 hd[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+        const int half = wid >> 2 & 1, part = wid >> 3, key = tid & 255;         // keys; tiles with odd numbers, or even ones
+        const uint32_t S = tmem + 256 * part + 128 * half + ((uint32_t)((wid & 3) * 32) << 16);
+        const ulonglong2* const ls = reinterpret_cast<const ulonglong2*>(mem + SM::LSE) + 32 * part;
+        float* const other = reinterpret_cast<float*>(mem + SM::OTHER) + key;
         uint32_t n = 0, n_item = 0;              // tiles, items with tiles so far
         bool ok = true;
-        // minus the sums of columns 4 lane .. 4 lane + 3 of tile rt, in powers of two; -inf for what is no row
-        int off[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) off[i] = (4 * lane + i) / a.G * (a.pc.heads * a.G) + (4 * lane + i) % a.G;
-        auto lse_of = [&](const WmWalk& x, int rt, float (&l)[4]) {
-            const float* p = a.lse + (long long)(x.s.row0 + rt * (128 / a.G)) * (a.pc.heads * a.G) + x.h * a.G;
-            const int cols = min(HR, x.s.n * a.G - rt * HR);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                l[i] = -INFINITY;
-                if (4 * lane + i < cols) {
-                    const float y = __ldg(p + off[i]);
-                    l[i] = y == -INFINITY ? y : -y * PT_LOG2E;
-                }
-            }
-        };
         while (w.left > 0 && ok) {
             const WmSeg g(a, w);
             if (tid == 0 && (w.s.cut || w.s.len > a.w_stride)) atomicMin(a.status, SALICACHE_E_CAPACITY);
-            const int j = g.j0 + tid;            // this thread's key
-            float sum = 0.0f, l[4];
-            if (g.tiles > 0) lse_of(w, g.rt, l);
+            const int j = g.j0 + key;
+            float sum = 0.0f;
             const bool mine = j < g.held;
-            const float had = mine && g.first && g.last ? wg_had(a, w.s, w.b, w.h, j) : 0.0f;
+            const float had = part == 0 && mine && g.first && g.last ? wg_had(a, w.s, w.b, w.h, j) : 0.0f;
             for (int t = 0; t < g.tiles; ++t, ++n) {
-                const uint32_t buf = n & 1;
-                __syncwarp();                    // the tile before has been read
-                lses[lane] = make_float4(l[0], l[1], l[2], l[3]);
-                __syncwarp();
-                if (t + 1 < g.tiles) lse_of(w, g.rt + t + 1, l);
-                if (!wait(bars.s_full[buf], n >> 1 & 1)) {
+                if ((int)(n & 1) != part) continue;
+                if (!(wait(bars.l_full[part], n >> 1 & 1) && wait(bars.s_full[part][half], n >> 1 & 1))) {
                     ok = false;
                     break;
                 }
@@ -272,76 +298,93 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                 const int r0 = (g.rt + t) * HR, c_hi = min(HR, w.s.n * a.G - r0);
                 const bool whole = c_hi == HR && (long long)(g.j0 + half * 128 + 127 - w.s.pos0) * a.G <= r0;
                 const int c_lo = max(0, min(128, max(0, j - w.s.pos0) * a.G - r0));
-                float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                uint32_t x[2][32];
-                tc_ld32(x[0], S + 256 * buf);
-                tc_wait_ld(x[0]);
+                uint64_t acc[2] = {0ull, 0ull};
+                const uint64_t scale2 = pair2(a.scale, a.scale);
+                auto columns = [&](auto masked_) {
+                    constexpr bool MASKED = decltype(masked_)::value;
+                    uint32_t x[2][16];
+                    tc_ld16(x[0], S);
+                    tc_wait_ld16(x[0]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if (c < 3) tc_ld32(x[(c + 1) & 1], S + 256 * buf + 32 * (c + 1));
-                    const float4* ls = lses + 8 * c;
-                    if (whole) {
+                    for (int c = 0; c < 8; ++c) {
+                        if (c < 7) tc_ld16(x[(c + 1) & 1], S + 16 * (c + 1));
+                        const uint32_t(&y)[16] = x[c & 1];
+                        const uint32_t sees = MASKED ? below(c_hi - 16 * c) & ~below(c_lo - 16 * c) : 0u;
+                        ulonglong2 l[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) l[i] = ls[4 * c + i];
+                        if (c == 7) {            // the scores and their rows' sums are in registers
+                            tc_before();
+                            __syncwarp();
+                            if (lane == 0) bar_arrive(smem_u32(&bars.s_free[part][half]));
+                        }
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const float4 lv = ls[i];
-                            acc[0] += ex2(fmaf(__uint_as_float(x[c & 1][4 * i]), a.scale, lv.x));
-                            acc[1] += ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 1]), a.scale, lv.y));
-                            acc[2] += ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 2]), a.scale, lv.z));
-                            acc[3] += ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 3]), a.scale, lv.w));
+                            float lo, hi;
+                            split2(fma2x(pair2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), scale2, i & 1 ? l[i >> 1].y : l[i >> 1].x), lo, hi);
+                            lo = WM_POLY >> (2 * (i & 3)) & 1 ? ex2_fma(lo) : ex2(lo);
+                            hi = WM_POLY >> (2 * (i & 3) + 1) & 1 ? ex2_fma(hi) : ex2(hi);
+                            if (MASKED) {
+                                lo = sees & 1u << (2 * i) ? lo : 0.0f;
+                                hi = sees & 2u << (2 * i) ? hi : 0.0f;
+                            }
+                            acc[i & 1] = add2x(acc[i & 1], pair2(lo, hi));
                         }
-                    } else {
-                        const uint32_t sees = below(c_hi - 32 * c) & ~below(c_lo - 32 * c);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 lv = ls[i];
-                            const float p0 = ex2(fmaf(__uint_as_float(x[c & 1][4 * i]), a.scale, lv.x)), p1 = ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 1]), a.scale, lv.y));
-                            const float p2 = ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 2]), a.scale, lv.z)), p3 = ex2(fmaf(__uint_as_float(x[c & 1][4 * i + 3]), a.scale, lv.w));
-                            acc[0] += sees & 1u << (4 * i) ? p0 : 0.0f;
-                            acc[1] += sees & 2u << (4 * i) ? p1 : 0.0f;
-                            acc[2] += sees & 4u << (4 * i) ? p2 : 0.0f;
-                            acc[3] += sees & 8u << (4 * i) ? p3 : 0.0f;
-                        }
+                        if (c < 7) tc_wait_ld16(x[(c + 1) & 1]);
                     }
-                    if (c < 3) tc_wait_ld(x[(c + 1) & 1]);
-                    if (c == 2) {                // all columns are in registers
-                        tc_before();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(smem_u32(&bars.s_free[buf]));
-                    }
-                }
-                sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+                };
+                if (whole) columns(std::false_type{});
+                else columns(std::true_type{});
+                float s_lo, s_hi;
+                split2(add2x(acc[0], acc[1]), s_lo, s_hi);
+                sum += s_lo + s_hi;
             }
             if (!ok) break;
             if (g.tiles > 0) {
-                if (!(*(volatile uint32_t*)&bars.pages[n_item & 7] >> (tid >> 4) & 1u)) sum = 0.0f;
+                // the odd and the even tiles come together
+                if (part == 1) {
+                    if (n_item > 0 && !wait(bars.o_empty, (n_item - 1) & 1)) break;
+                    *other = sum;
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(&bars.o_full));
+                } else {
+                    if (!wait(bars.o_full, n_item & 1)) break;
+                    sum += *other;
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(&bars.o_empty));
+                    // what lies in no page is not a weight, nor is what is left of exponentials of minus infinity
+                    if (!(*(volatile uint32_t*)&bars.pages[n_item & 7] >> (key >> 4) & 1u) || sum < 1e-33f) sum = 0.0f;
+                }
                 ++n_item;
             }
-            if (g.real) {
+            if (g.real && part == 0) {
                 if (g.first && g.last) {
                     if (mine) wg_put(a, w.s, w.b, w.h, j, had, sum);
                 } else {
-                    a.part[(2 * (size_t)blockIdx.x + (g.first ? 1 : 0)) * WM_KEYS + tid] = sum;
-                    if (g.first) {
-                        hd[0].y = 1;
-                        hd[0].z = w.b;
-                        hd[0].w = w.h;
-                        hd[1].x = w.kt;
-                    } else hd[0].x = g.last ? 2 : 1;
+                    a.part[(2 * (size_t)blockIdx.x + (g.first ? 1 : 0)) * WM_KEYS + key] = sum;
+                    if (tid == 0) {
+                        if (g.first) {
+                            bars.hd[0].y = 1;
+                            bars.hd[0].z = w.b;
+                            bars.hd[0].w = w.h;
+                            bars.hd[1].x = w.kt;
+                        } else bars.hd[0].x = g.last ? 2 : 1;
+                    }
                 }
             }
             next(g);
         }
         if (tid == 0) {
-            a.head[2 * blockIdx.x] = hd[0];
-            a.head[2 * blockIdx.x + 1] = hd[1];
+            a.head[2 * blockIdx.x] = bars.hd[0];
+            a.head[2 * blockIdx.x + 1] = bars.hd[1];
         }
-    } else if (wid < 12) {
+    } else if (wid < LAST) {
         // ---------------- codes to operands: 64 keys a warp
         if (FMT != PF_16) {
             constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>(), LPR = RB / 16, RPP = 32 / LPR, P = 16 / RPP;
             static_assert(P >= 1, "16 keys at a time");
             const Codes<T> cd;
-            const int lw = wid - 8, c = lane % LPR;
+            const int lw = wid - 16, c = lane % LPR;
             uint32_t n_item = 0;
             while (w.left > 0) {
                 const WmSeg g(a, w);
@@ -400,7 +443,7 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
             }
         }
     } else {
-        if (wid == 12) {
+        if (wid == LAST) {
             // ---------------- matrix instructions: the warp stays together, one lane issues
             constexpr uint32_t ID = instr_desc<T>(128, false);
             const uint32_t k_lo = desc_lo(base + SM::K, 16), q_lo = desc_lo(base + SM::Q, 16);
@@ -414,23 +457,27 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                 for (int t = 0; t < g.tiles && ok; ++t, ++n) {
                     const uint32_t buf = n & 1, st = n % WM_Q;
                     ok = wait(bars.q_full[st], n / WM_Q & 1);
-                    if (ok && n >= 2) ok = wait(bars.s_free[buf], (n / 2 - 1) & 1);
-                    if (!ok) break;
-                    tc_after();
-                    if (elect_one()) {
-                        for (int h = 0; h < halves; ++h) {
+                    for (int h = 0; h < 2; ++h) {
+                        if (ok && n >= 2) ok = wait(bars.s_free[buf][h], (n / 2 - 1) & 1);
+                        if (!ok) break;
+                        tc_after();
+                        if (elect_one()) {
                             const uint32_t ka = k_lo + (kb * 2 + h) * (SM::TILE >> 4), qb = q_lo + st * (SM::TILE >> 4);
+                            if (h < halves)
 #pragma unroll
-                            for (int i = 0; i < D / 16; ++i) {
-                                const uint32_t off = (i >> 2) * 1024 + (i & 3) * 2;
-                                mma_ss(tmem + 256 * buf + 128 * h, desc(ka + off), desc(qb + off), ID, i > 0);
+                                for (int i = 0; i < D / 16; ++i) {
+                                    const uint32_t off = (i >> 2) * 1024 + (i & 3) * 2;
+                                    mma_ss(tmem + 256 * buf + 128 * h, desc(ka + off), desc(qb + off), ID, i > 0);
+                                }
+                            tc_commit(smem_u32(&bars.s_full[buf][h]));
+                            if (h == 1) {
+                                tc_commit(smem_u32(&bars.q_empty[st]));
+                                if (t == g.tiles - 1) tc_commit(smem_u32(&bars.k_empty[kb]));
                             }
                         }
-                        tc_commit(smem_u32(&bars.s_full[buf]));
-                        tc_commit(smem_u32(&bars.q_empty[st]));
-                        if (t == g.tiles - 1) tc_commit(smem_u32(&bars.k_empty[kb]));
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    if (!ok) break;
                 }
                 n_item += g.tiles > 0;
                 next(g);
@@ -444,42 +491,48 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                 bar_drain(smem_u32(&bars.left), 0);
             }
         }
-        if (wid == 13) {
+        if (wid == LAST + 1) {
             // ---------------- feeder
             uint32_t n = 0, n_item = 0;
             bool ok = true;
             const int per_page = 1 << a.pc.page_shift;
             if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+            // the keys of an item, those of 16-bit pages: group 2 brings the others
+            auto feed_keys = [&](const WmWalk& x, const WmSeg& g) -> bool {
+                const uint32_t kb = n_item % WM_K, bar = smem_u32(&bars.k_full[kb]);
+                const int pid16 = g.page_of(a, x, lane);
+                const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), there = __ballot_sync(0xffffffffu, pid16 >= 0);
+                // the first group of 16 keys of this lane's page names the page
+                const int pid = __shfl_sync(0xffffffffu, pid16, (lane << (a.pc.page_shift - 4)) & 31);
+                const bool mine = lane < WM_KEYS >> a.pc.page_shift && pid >= 0;
+                const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine));
+                if (n_item >= WM_K && !wait(bars.k_empty[kb], (n_item / WM_K - 1) & 1)) return false;
+                if (lane == 0) {
+                    *(volatile uint32_t*)&bars.pages[n_item & 7] = there;
+                    if (bad) atomicMin(a.status, SALICACHE_E_CAPACITY);
+                    bar_expect(bar, copies * (uint32_t)(per_page * D * 2));
+                }
+                __syncwarp();
+                if (mine) {
+                    const size_t slot = pg_slot(a.pc, pid, 0, x.h, 0);
+                    const int key = lane << a.pc.page_shift;
+                    const uint32_t dst = base + SM::K + (kb * 2 + (key >> 7)) * SM::TILE + (key & 127) * 128;
+#pragma unroll
+                    for (int y = 0; y < D; y += 64) tensor_copy(dst + y * 256, &map, y, (int)slot, bar);
+                }
+                __syncwarp();
+                ++n_item;
+                return true;
+            };
+            if (FMT == PF_16 && w.left > 0) {
+                const WmSeg g(a, w);
+                if (g.tiles > 0) ok = feed_keys(w, g);
+            }
             while (w.left > 0 && ok) {
                 const WmSeg g(a, w);
-                if (FMT == PF_16 && g.tiles > 0) {
-                    const uint32_t kb = n_item % WM_K, bar = smem_u32(&bars.k_full[kb]);
-                    const int pid16 = g.page_of(a, w, lane);
-                    const uint32_t bad = __ballot_sync(0xffffffffu, pid16 == -1), there = __ballot_sync(0xffffffffu, pid16 >= 0);
-                    // the first group of 16 keys of this lane's page names the page
-                    const int pid = __shfl_sync(0xffffffffu, pid16, (lane << (a.pc.page_shift - 4)) & 31);
-                    const bool mine = lane < WM_KEYS >> a.pc.page_shift && pid >= 0;
-                    const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine));
-                    if (n_item >= WM_K && !wait(bars.k_empty[kb], (n_item / WM_K - 1) & 1)) {
-                        ok = false;
-                        break;
-                    }
-                    if (lane == 0) {
-                        *(volatile uint32_t*)&bars.pages[n_item & 7] = there;
-                        if (bad) atomicMin(a.status, SALICACHE_E_CAPACITY);
-                        bar_expect(bar, copies * (uint32_t)(per_page * D * 2));
-                    }
-                    __syncwarp();
-                    if (mine) {
-                        const size_t slot = pg_slot(a.pc, pid, 0, w.h, 0);
-                        const int key = lane << a.pc.page_shift;
-                        const uint32_t dst = base + SM::K + (kb * 2 + (key >> 7)) * SM::TILE + (key & 127) * 128;
-#pragma unroll
-                        for (int x = 0; x < D; x += 64) tensor_copy(dst + x * 256, &map, x, (int)slot, bar);
-                    }
-                    __syncwarp();
-                }
-                n_item += g.tiles > 0;
+                WmWalk wn = w;
+                wn.left -= g.k1 - g.k0;
+                if (wn.left > 0) wn = wm_after(a, wn);
                 for (int t = 0; t < g.tiles; ++t, ++n) {
                     const uint32_t st = n % WM_Q, bar = smem_u32(&bars.q_full[st]);
                     if (n >= WM_Q && !wait(bars.q_empty[st], (n / WM_Q - 1) & 1)) {
@@ -492,8 +545,21 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                             tensor_copy3(base + SM::Q + st * SM::TILE + x * 256, &q_map, x, w.h * a.G, w.s.row0 + (g.rt + t) * (128 / a.G), bar);
                     }
                     __syncwarp();
+                    // the next item's keys, once the rows' ring has gone past the item before, whose keys they replace
+                    if (FMT == PF_16 && t == min(WM_Q, g.tiles) - 1 && wn.left > 0) {
+                        const WmSeg gn(a, wn);
+                        if (gn.tiles > 0 && !feed_keys(wn, gn)) {
+                            ok = false;
+                            ++n;
+                            break;
+                        }
+                    }
                 }
-                if (ok) next(g);
+                if (FMT == PF_16 && g.tiles == 0 && wn.left > 0 && ok) {
+                    const WmSeg gn(a, wn);
+                    if (gn.tiles > 0) ok = feed_keys(wn, gn);
+                }
+                w = wn;
             }
             join_roles();
             // copies in flight end before the block does: who uses a stage waits for them, unless a role has left early
@@ -504,12 +570,43 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
             }
             return;
         }
+        if (wid == LAST + 2) {
+            // ---------------- the rows' sums: minus their logarithms, in powers of two; -inf for what is no row.  A lane has four columns
+            const int Hq = a.pc.heads * a.G;
+            int off[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) off[i] = (4 * lane + i) / a.G * Hq + (4 * lane + i) % a.G;
+            uint32_t n = 0;
+            bool ok = true;
+            while (w.left > 0 && ok) {
+                const WmSeg g(a, w);
+                for (int t = 0; t < g.tiles; ++t, ++n) {
+                    const float* p = a.lse + (long long)(w.s.row0 + (g.rt + t) * (128 / a.G)) * Hq + w.h * a.G;
+                    const int cols = min(HR, w.s.n * a.G - (g.rt + t) * HR);
+                    float l[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float y = 4 * lane + i < cols ? __ldg(p + off[i]) : -INFINITY;
+                        l[i] = y == -INFINITY ? y : -y * PT_LOG2E;
+                    }
+                    // who frees tile n - 2 has read its sums
+                    if (n >= 2 && !(wait(bars.s_free[n & 1][0], (n / 2 - 1) & 1) && wait(bars.s_free[n & 1][1], (n / 2 - 1) & 1))) {
+                        ok = false;
+                        break;
+                    }
+                    reinterpret_cast<float4*>(mem + SM::LSE)[(n & 1) * 32 + lane] = make_float4(l[0], l[1], l[2], l[3]);
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(&bars.l_full[n & 1]));
+                }
+                next(g);
+            }
+        }
         __syncwarp();
     }
     tc_before();
     join_roles();
     if (tid == 0 && *gave_up) atomicMin(a.status, SC_GAVE_UP);
-    if (wid == 12) {
+    if (wid == LAST) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     }
@@ -541,7 +638,7 @@ int launch_many(salicache_ctx* c, WgArgs a, char* work, cudaStream_t st) {
     const int blocks = min(c->sm_count, PT_MAX_BLOCKS);
     a.part = reinterpret_cast<float*>(work);
     a.head = reinterpret_cast<int4*>(a.part + (size_t)2 * blocks * WM_KEYS);
-    SC_CHECK(pt_launch(k_weigh_many<T, FMT, D>, dim3(blocks), WM_THREADS, BYTES, st, a, map, q_map, blocks));
+    SC_CHECK(pt_launch(k_weigh_many<T, FMT, D>, dim3(blocks), wm_threads<FMT>(), BYTES, st, a, map, q_map, blocks));
     SC_CHECK(pt_launch(k_weigh_join, dim3(blocks), WM_KEYS, 0, st, a, blocks));
     c->launches += 2;
     SC_CHECK(cudaGetLastError());
