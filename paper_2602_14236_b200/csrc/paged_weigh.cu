@@ -5,10 +5,11 @@
 // The logarithms of the softmax sums come from the attention, so every position stands for itself: no maximum, no division,
 // and nothing to be joined.  Only K is read.
 //
-// This file's kernel: a warp has 16 keys of one head as the long side of m16n8k16 matrix instructions, straight from the pages
-// into the registers of its operands, the next 16 under way meanwhile; rows of q are the columns, 8 at a time.  A lane sums its
-// columns' weights, four lanes join at the end.  All groups of 16 keys stand in one line, of which every warp takes an equal
-// stretch, so that lengths on the device decide the split and warps never wait for one another.
+// This file's kernel, for few rows per sequence: a warp has 16 keys of one head as the long side of m16n8k16 matrix
+// instructions, rows of q are the columns, 8 at a time.  A lane sums its columns' weights, four lanes join at the end.  Every
+// warp has a ring of its own in shared memory, which its first lane fills by bulk copies of 16 keys' rows and scales.  All
+// groups of 16 keys stand in one line, of which every warp takes an equal stretch, so that the lengths on the device decide the
+// split, and warps never wait for one another.
 #include <math.h>
 
 #include "paged_frags.cuh"
@@ -16,7 +17,15 @@
 
 namespace {
 
-constexpr int WG_THREADS = 256, WG_WARPS = WG_THREADS / 32;
+constexpr int WG_THREADS = 256, WG_WARPS = WG_THREADS / 32, WG_BLOCKS = 2;      // per SM: 128 registers a thread
+
+// A warp's ring: stages of 16 keys' rows and their scales.
+template <int FMT, int D>
+struct WgRing {
+    static constexpr int ROWS = 16 * pg_row_bytes<FMT, D>(), META = 16 * pg_meta_bytes<FMT>(), STAGE = ROWS + META;
+    static constexpr int ROOM = 108 * 1024 / WG_WARPS, STAGES = ROOM / STAGE < 6 ? ROOM / STAGE : 6;
+    static constexpr int BYTES = WG_WARPS * STAGES * STAGE;
+};
 
 // A group of 16 keys: its sequence, head and first position.
 struct WgPlace {
@@ -71,33 +80,6 @@ __device__ __forceinline__ WgPlace wg_start(const WgArgs& a, int warp, int warps
     return p;
 }
 
-// 16 keys' rows and scales from their page.
-template <int FMT, int D>
-__device__ __forceinline__ void fetch_keys(KTile<FMT, D>& t, const PgCache& pc, size_t slot, int g8, int c4) {
-    using KT = KTile<FMT, D>;
-    const uint8_t* p = pc.data + slot * KT::RB + KT::at(g8, c4);
-    const uint8_t* m = pc.scale + slot * KT::MB + KT::meta_at(g8);
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        if constexpr (KT::RB >= 64) {
-#pragma unroll
-            for (int i = 0; i < KT::RB / 64; ++i) {
-                const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p + 8 * r * KT::RB + 64 * i));
-                t.k[r][4 * i] = v.x;
-                t.k[r][4 * i + 1] = v.y;
-                t.k[r][4 * i + 2] = v.z;
-                t.k[r][4 * i + 3] = v.w;
-            }
-        } else {
-            const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p + 8 * r * KT::RB));
-            t.k[r][0] = v.x;
-            t.k[r][1] = v.y;
-        }
-        if (FMT == PF_I8) t.s[r] = *reinterpret_cast<const uint16_t*>(m + 8 * r * KT::MB);
-        if (FMT == PF_I4) t.s[r] = *reinterpret_cast<const uint32_t*>(m + 8 * r * KT::MB);
-    }
-}
-
 // Column tile n of a sequence's rows for one head: B fragments, and the columns' sums (as powers of two).
 template <int FMT, int D>
 struct Columns {
@@ -131,92 +113,170 @@ struct Columns {
 };
 
 template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(WG_THREADS)
+__global__ void __launch_bounds__(WG_THREADS, WG_BLOCKS)
 k_weigh_few(WgArgs a) {
-    const int lane = threadIdx.x & 31, g8 = lane >> 2, c4 = lane & 3;
+    using R = WgRing<FMT, D>;
+    constexpr int STAGES = R::STAGES;
+    constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
+    static_assert(STAGES >= 2, "ring");
+    extern __shared__ __align__(128) uint8_t rings[];
+    __shared__ uint64_t full[WG_WARPS][STAGES];
+    __shared__ int sh_gave_up;
+    volatile int* gave_up = &sh_gave_up;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g8 = lane >> 2, c4 = lane & 3;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < WG_WARPS * STAGES; ++i) bar_init(smem_u32(&full[0][0]) + 8 * i, 1);
+        sh_gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     grid_wait();
     grid_release();
     long long left;
-    WgPlace p = wg_start(a, blockIdx.x * WG_WARPS + (threadIdx.x >> 5), gridDim.x * WG_WARPS, left);
-    if (left == 0) return;
-    const Codes<T> cd;
-    // the page of a group: -1 there is none, -2 no row needs it
-    auto page_of = [&](const WgPlace& x) -> int {
-        if (x.s.n == 0) return -2;
-        const int pid = __ldg(a.sq.table + (size_t)x.b * a.sq.width + ((x.k << 4) >> a.pc.page_shift));
-        return pid >= 0 && pid < a.pc.n_pages ? pid : -1;
-    };
-    auto fetch = [&](KTile<FMT, D>& t, const WgPlace& x, int pid) {
-        if (pid >= 0) fetch_keys<FMT, D>(t, a.pc, pg_slot(a.pc, pid, 0, x.h, (x.k << 4) & ((1 << a.pc.page_shift) - 1)), g8, c4);
-    };
-    KTile<FMT, D> t{}, next{};
-    int pid = page_of(p);
-    fetch(t, p, pid);
-    Columns<FMT, D> col;
-    int have_b = -1, have_h = -1;            // what `col` holds column tile 0 of
-    while (true) {
-        WgPlace pn = p;
-        int pid_n = -2;
-        if (left > 1) {
-            wg_next(pn, a);
-            pid_n = page_of(pn);
-            fetch(next, pn, pid_n);
-        }
-        const PgSeq& s = p.s;
-        const int j0 = p.k << 4, rows = s.n * a.G;
-        float had[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};
-        if (c4 == 0) {
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-                if (j0 + key_of(g8) + 8 * r < p.held) had[r] = wg_had(a, s, p.b, p.h, j0 + key_of(g8) + 8 * r);
-        }
-        if (lane == 0 && (pid == -1 || (p.k == 0 && (p.s.cut || p.s.len > a.w_stride)))) atomicMin(a.status, SALICACHE_E_CAPACITY);
-        if (pid >= 0) {
-            // the first row that sees the first key, and its column tile
-            for (int n = max(0, j0 - s.pos0) * a.G / 8; 8 * n < rows; ++n) {
-                if (n != 0 || have_b != p.b || have_h != p.h) {
-                    col.load(a, s, p.h, n, rows, g8, c4);
-                    have_b = n == 0 ? p.b : -1;
-                    have_h = p.h;
+    WgPlace p = wg_start(a, blockIdx.x * WG_WARPS + wid, gridDim.x * WG_WARPS, left);
+    __syncthreads();
+    const uint32_t ring = smem_u32(rings) + wid * STAGES * R::STAGE, bars = smem_u32(&full[wid][0]);
+
+    // What is fetched goes STAGES groups ahead of what is summed.  A lane looks up the page of one of 32 groups; `pages` has a bit
+    // for each group under way, the newest lowest: its page exists.
+    WgPlace f = p;
+    long long to_fetch = left;
+    int ids = 0, ids_at = -1;                // pages of groups ids_at .. ids_at + 31 of sequence f.b
+    uint32_t put = 0, pages = 0;             // next stage to fill
+    int under_way = 0;                       // stages filled or about to be
+    auto fetch = [&]() {
+        pages <<= 1;
+        if (to_fetch == 0) return;
+        if (f.s.n > 0) {
+            if (ids_at < 0 || f.k >= ids_at + 32 || f.k < ids_at) {
+                ids_at = f.k;
+                ids = f.k + lane < f.groups ? __ldg(a.sq.table + (size_t)f.b * a.sq.width + ((f.k + lane) << 4 >> a.pc.page_shift)) : -1;
+                if (ids >= a.pc.n_pages) ids = -1;
+            }
+            const int pid = __shfl_sync(0xffffffffu, ids, f.k - ids_at);
+            if (pid >= 0) {
+                pages |= 1u;
+                if (lane == 0) {
+                    const size_t slot = pg_slot(a.pc, pid, 0, f.h, (f.k << 4) & ((1 << a.pc.page_shift) - 1));
+                    const uint32_t bar = bars + 8 * put, dst = ring + put * R::STAGE;
+                    bar_expect(bar, 16 * (RB + MB));
+                    bulk_copy(dst, a.pc.data + slot * RB, 16 * RB, bar);
+                    if (MB > 0) bulk_copy(dst + R::ROWS, a.pc.scale + slot * MB, 16 * MB, bar);
                 }
+            } else if (lane == 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
+        }
+        if (!(pages & 1u) && lane == 0) bar_arrive(bars + 8 * put);          // nothing to come
+        put = put + 1 == STAGES ? 0 : put + 1;
+        ++under_way;
+        if (--to_fetch > 0) {
+            const int b = f.b;
+            wg_next(f, a);
+            if (f.b != b) ids_at = -1;
+        }
+    };
+#pragma unroll 1
+    for (int i = 0; i < STAGES; ++i) fetch();
+
+    const Codes<T> cd;
+    uint32_t stage = 0, phase = 0;
+    bool ok = true;
+    while (left > 0 && ok) {                 // the groups of one head
+        const PgSeq& s = p.s;
+        const int rows = s.n * a.G, run = (int)min(left, (long long)(p.groups - p.k));
+        const int jl = key_of(g8) + 8 * (c4 & 1);                        // the key that this lane writes, if c4 < 2
+        const size_t row = ((size_t)p.b * a.pc.heads + p.h) * a.w_stride + jl;
+        float* const out = a.out + row;
+        const float* const in = a.in + row;
+        const float decay = s.n > 0 ? a.decay : 1.0f;
+        // positions below had_to had a weight before, which is looked at some groups ahead
+        const int had_to = c4 > 1 || !a.in ? 0 : s.n > 0 ? min(s.pos0, p.held) : p.held, put_to = c4 < 2 ? p.held : 0;
+        auto load_had = [&](int k) { return 16 * k + jl < had_to && k < p.k + run ? in[16 * k] : 0.0f; };
+        if (lane == 0 && p.k == 0 && (s.cut || s.len > a.w_stride)) atomicMin(a.status, SALICACHE_E_CAPACITY);
+        float had[4] = {0.0f, load_had(p.k), load_had(p.k + 1), load_had(p.k + 2)};
+        Columns<FMT, D> col;
+        if (rows > 0) col.load(a, s, p.h, 0, rows, g8, c4);
+        bool first_columns = true;           // `col` holds column tile 0
+        const bool live[2] = {2 * c4 < rows, 2 * c4 + 1 < rows};
+#pragma unroll 1
+        for (int t = 0; t < run; ++t) {
+            const int j0 = (p.k + t) << 4;
+            had[0] = had[1];
+            had[1] = had[2];
+            had[2] = had[3];
+            had[3] = load_had(p.k + t + 3);
+            ok = warp_wait(bars + 8 * stage, phase, a.wait_limit, gave_up);
+            if (!ok) break;
+            --under_way;
+            KTile<FMT, D> kt;
+            kt.load(ring + stage * R::STAGE + KTile<FMT, D>::at(g8, c4), ring + stage * R::STAGE + R::ROWS + KTile<FMT, D>::meta_at(g8));
+            const bool there = pages >> (STAGES - 1) & 1u;
+            __syncwarp();                    // the stage has been read
+            fetch();
+            if (++stage == STAGES) {
+                stage = 0;
+                phase ^= 1;
+            }
+            float sum[2] = {0.0f, 0.0f};
+            auto columns = [&](int n) {
                 float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
                     uint32_t a0, a1, a2, a3;
-                    key_frag<T, FMT, D>(cd, t.k[0], t.s[0], i, a0, a2);
-                    key_frag<T, FMT, D>(cd, t.k[1], t.s[1], i, a1, a3);
+                    key_frag<T, FMT, D>(cd, kt.k[0], kt.s[0], i, a0, a2);
+                    key_frag<T, FMT, D>(cd, kt.k[1], kt.s[1], i, a1, a3);
                     mma16816<T>(sc, a0, a1, a2, a3, col.q[i][0], col.q[i][1]);
                 }
                 float w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] = ex2(fmaf(sc[i], a.scale, -col.lse[i & 1]));
-                if (s.pos0 + 8 * n / a.G < j0 + 15 || 8 * n + 8 > rows) {
+                if (j0 + 15 > s.pos0) {      // some row may be before some key
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = 8 * n + 2 * c4 + (i & 1);
-                        if (r >= rows || s.pos0 + r / a.G < j0 + key_of(g8) + 8 * (i >> 1)) w[i] = 0.0f;
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        if (s.pos0 + (8 * n + 2 * c4 + (i & 1)) / a.G < j0 + key_of(g8) + 8 * (i >> 1)) w[i] = 0.0f;
                 }
-                sum[0] += w[0] + w[1];
-                sum[1] += w[2] + w[3];
+                // a column that is no row has q = 0, which a key that is not finite would turn into no number
+                const bool l0 = n == 0 ? live[0] : 8 * n + 2 * c4 < rows, l1 = n == 0 ? live[1] : 8 * n + 2 * c4 + 1 < rows;
+                sum[0] += (l0 ? w[0] : 0.0f) + (l1 ? w[1] : 0.0f);
+                sum[1] += (l0 ? w[2] : 0.0f) + (l1 ? w[3] : 0.0f);
+            };
+            if (there) {
+                if (rows <= 8) columns(0);
+                else
+#pragma unroll 1
+                    for (int n = j0 > s.pos0 ? (j0 - s.pos0) * a.G / 8 : 0; 8 * n < rows; ++n) {     // from the first row that sees the first key on
+                        if (n != 0 || !first_columns) col.load(a, s, p.h, n, rows, g8, c4);
+                        first_columns = n == 0;
+                        columns(n);
+                    }
             }
+            // four lanes' sums of two keys: a lane pair exchanges one for the other
+            float x = c4 & 1 ? sum[1] : sum[0];
+            x += __shfl_xor_sync(0xffffffffu, c4 & 1 ? sum[0] : sum[1], 1);
+            x += __shfl_xor_sync(0xffffffffu, x, 2);
+            if (j0 + jl < put_to) out[j0] = fmaf(decay, had[0], x);
         }
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 1);
-            sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 2);
-            if (c4 == 0 && j0 + key_of(g8) + 8 * r < p.held) wg_put(a, s, p.b, p.h, j0 + key_of(g8) + 8 * r, had[r], sum[r]);
-        }
-        if (--left == 0) break;
-        t = next;
-        p = pn;
-        pid = pid_n;
+        left -= run;
+        p.k += run - 1;
+        if (left > 0) wg_next(p, a);
     }
+    for (; !ok && under_way > 0; --under_way) {              // copies in flight end before the block does
+        bar_drain(bars + 8 * stage, phase);
+        if (++stage == STAGES) {
+            stage = 0;
+            phase ^= 1;
+        }
+    }
+    join_roles();
+    if (threadIdx.x == 0 && *gave_up) atomicMin(a.status, SC_GAVE_UP);
 }
 
 template <typename T, int FMT, int D>
 int launch_few(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
-    SC_CHECK(pt_launch(k_weigh_few<T, FMT, D>, dim3((unsigned)(2 * c->sm_count)), WG_THREADS, 0, st, a));
+    using R = WgRing<FMT, D>;
+    SC_CHECK(cudaFuncSetAttribute(k_weigh_few<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::BYTES));
+    // no more blocks than there can be groups of keys for: sequences times heads times the table's groups
+    const long long most = (long long)a.sq.n_seqs * a.pc.heads * (((long long)a.sq.width << a.pc.page_shift) >> 4);
+    const int blocks = (int)max(1ll, min((most + WG_WARPS - 1) / WG_WARPS, (long long)c->sm_count * WG_BLOCKS));
+    SC_CHECK(pt_launch(k_weigh_few<T, FMT, D>, dim3((unsigned)blocks), WG_THREADS, R::BYTES, st, a));
     c->launches++;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;
