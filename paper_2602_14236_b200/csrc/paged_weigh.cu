@@ -7,8 +7,8 @@
 //
 // This file's kernel, for few rows per sequence: a warp has 16 keys of one head as the long side of m16n8k16 matrix
 // instructions, rows of q are the columns, 8 at a time.  A lane sums its columns' weights, four lanes join at the end.  Every
-// warp has a ring of its own in shared memory, which its first lane fills by bulk copies of 16 keys' rows and scales.  All
-// groups of 16 keys stand in one line, of which every warp takes an equal stretch, so that the lengths on the device decide the
+// warp has a ring of its own in shared memory, which its first lanes fill by bulk copies of 16 keys' rows and scales.  All
+// groups of keys stand in one line, of which every warp takes an equal stretch, so that the lengths on the device decide the
 // split, and warps never wait for one another.
 #include <math.h>
 
@@ -19,25 +19,31 @@ namespace {
 
 constexpr int WG_THREADS = 256, WG_WARPS = WG_THREADS / 32, WG_BLOCKS = 2;      // per SM: 128 registers a thread
 
-// A warp's ring: stages of 16 keys' rows and their scales.
+// Keys of a group: 32, so that what a group costs beside its products is shared by two of them, unless the rings hold too few
+// such groups (72 us with 16 keys for 32 single tokens over INT4 pages).
+template <int FMT, int D> __host__ __device__ constexpr int wg_keys() { return FMT == PF_16 && D == 128 ? 16 : 32; }
+
+// A warp's ring: stages of a group's rows and their scales.
 template <int FMT, int D>
 struct WgRing {
-    static constexpr int ROWS = 16 * pg_row_bytes<FMT, D>(), META = 16 * pg_meta_bytes<FMT>(), STAGE = ROWS + META;
+    static constexpr int ROWS = wg_keys<FMT, D>() * pg_row_bytes<FMT, D>(), META = wg_keys<FMT, D>() * pg_meta_bytes<FMT>(), STAGE = ROWS + META;
     static constexpr int ROOM = 108 * 1024 / WG_WARPS, STAGES = ROOM / STAGE < 6 ? ROOM / STAGE : 6;
     static constexpr int BYTES = WG_WARPS * STAGES * STAGE;
 };
 
-// A group of 16 keys: its sequence, head and first position.
+// A group of KEYS keys: its sequence, head and first position.
 struct WgPlace {
     int b, h, k, groups;                     // the k-th of `groups`
     PgSeq s;
     int held;                                // positions that have a weight
 };
+template <int KEYS>
 __device__ __forceinline__ void wg_enter(WgPlace& p, const WgArgs& a) {
     p.s = pg_seq(a.sq, a.pc, p.b);
     p.held = wg_held(p.s, a);
-    p.groups = (p.held + 15) >> 4;
+    p.groups = (p.held + KEYS - 1) / KEYS;
 }
+template <int KEYS>
 __device__ __forceinline__ void wg_next(WgPlace& p, const WgArgs& a) {
     if (++p.k < p.groups) return;
     p.k = 0;
@@ -45,14 +51,15 @@ __device__ __forceinline__ void wg_next(WgPlace& p, const WgArgs& a) {
     p.h = 0;
     do {
         if (++p.b >= a.sq.n_seqs) return;
-        wg_enter(p, a);
+        wg_enter<KEYS>(p, a);
     } while (p.groups == 0);
 }
 // Where the warp's stretch of the line starts; `left` groups, none if that is 0.
+template <int KEYS>
 __device__ __forceinline__ WgPlace wg_start(const WgArgs& a, int warp, int warps, long long& left) {
     const int lane = threadIdx.x & 31;
     auto units = [&](int b) -> long long {
-        return b < a.sq.n_seqs ? (long long)((wg_held(pg_seq(a.sq, a.pc, b), a) + 15) >> 4) * a.pc.heads : 0ll;
+        return b < a.sq.n_seqs ? (long long)((wg_held(pg_seq(a.sq, a.pc, b), a) + KEYS - 1) / KEYS) * a.pc.heads : 0ll;
     };
     long long total = 0;
     const long long mine = units(lane);
@@ -69,7 +76,7 @@ __device__ __forceinline__ WgPlace wg_start(const WgArgs& a, int warp, int warps
             const int from = __ffs(hit) - 1;
             const long long at = __shfl_sync(0xffffffffu, beg - (incl - n), from);
             p.b = b0 + from;
-            wg_enter(p, a);
+            wg_enter<KEYS>(p, a);
             p.h = (int)(at / p.groups);
             p.k = (int)(at - (long long)p.h * p.groups);
             return p;
@@ -116,7 +123,7 @@ template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(WG_THREADS, WG_BLOCKS)
 k_weigh_few(WgArgs a) {
     using R = WgRing<FMT, D>;
-    constexpr int STAGES = R::STAGES;
+    constexpr int STAGES = R::STAGES, KEYS = wg_keys<FMT, D>(), U = KEYS / 16;
     constexpr uint32_t RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>();
     static_assert(STAGES >= 2, "ring");
     extern __shared__ __align__(128) uint8_t rings[];
@@ -132,44 +139,46 @@ k_weigh_few(WgArgs a) {
     grid_wait();
     grid_release();
     long long left;
-    WgPlace p = wg_start(a, blockIdx.x * WG_WARPS + wid, gridDim.x * WG_WARPS, left);
+    WgPlace p = wg_start<KEYS>(a, blockIdx.x * WG_WARPS + wid, gridDim.x * WG_WARPS, left);
     __syncthreads();
     const uint32_t ring = smem_u32(rings) + wid * STAGES * R::STAGE, bars = smem_u32(&full[wid][0]);
 
-    // What is fetched goes STAGES groups ahead of what is summed.  A lane looks up the page of one of 32 groups; `pages` has a bit
-    // for each group under way, the newest lowest: its page exists.
+    // What is fetched goes STAGES groups ahead of what is summed.  The first U lanes bring 16 keys each; a lane looks up the
+    // page of one of the next 32 times 16 keys.  `pages` has U bits for each group under way, the newest lowest: its pages exist.
     WgPlace f = p;
     long long to_fetch = left;
-    int ids = 0, ids_at = -1;                // pages of groups ids_at .. ids_at + 31 of sequence f.b
+    int ids = 0, ids_at = -1;                // pages of 16 keys each from group ids_at of sequence f.b on
     uint32_t put = 0, pages = 0;             // next stage to fill
     int under_way = 0;                       // stages filled or about to be
     auto fetch = [&]() {
-        pages <<= 1;
+        pages <<= U;
         if (to_fetch == 0) return;
+        const uint32_t bar = bars + 8 * put, dst = ring + put * R::STAGE + lane * 16 * RB;
         if (f.s.n > 0) {
-            if (ids_at < 0 || f.k >= ids_at + 32 || f.k < ids_at) {
+            if (ids_at < 0 || f.k >= ids_at + 32 / U || f.k < ids_at) {
                 ids_at = f.k;
-                ids = f.k + lane < f.groups ? __ldg(a.sq.table + (size_t)f.b * a.sq.width + ((f.k + lane) << 4 >> a.pc.page_shift)) : -1;
-                if (ids >= a.pc.n_pages) ids = -1;
+                const int j = f.k * KEYS + lane * 16;
+                ids = j < f.held ? __ldg(a.sq.table + (size_t)f.b * a.sq.width + (j >> a.pc.page_shift)) : -2;
+                if (j < f.held && (ids < 0 || ids >= a.pc.n_pages)) ids = -1;
             }
-            const int pid = __shfl_sync(0xffffffffu, ids, f.k - ids_at);
-            if (pid >= 0) {
-                pages |= 1u;
-                if (lane == 0) {
-                    const size_t slot = pg_slot(a.pc, pid, 0, f.h, (f.k << 4) & ((1 << a.pc.page_shift) - 1));
-                    const uint32_t bar = bars + 8 * put, dst = ring + put * R::STAGE;
-                    bar_expect(bar, 16 * (RB + MB));
+            const int pid = __shfl_sync(0xffffffffu, ids, U * (f.k - ids_at) + lane % U);
+            const uint32_t there = __ballot_sync(0xffffffffu, pid >= 0) & ((1u << U) - 1u);
+            pages |= there;
+            if (lane == 0) bar_expect(bar, __popc(there) * 16 * (RB + MB));
+            __syncwarp();
+            if (lane < U) {
+                if (pid >= 0) {
+                    const size_t slot = pg_slot(a.pc, pid, 0, f.h, (f.k * KEYS + lane * 16) & ((1 << a.pc.page_shift) - 1));
                     bulk_copy(dst, a.pc.data + slot * RB, 16 * RB, bar);
-                    if (MB > 0) bulk_copy(dst + R::ROWS, a.pc.scale + slot * MB, 16 * MB, bar);
-                }
-            } else if (lane == 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
-        }
-        if (!(pages & 1u) && lane == 0) bar_arrive(bars + 8 * put);          // nothing to come
+                    if (MB > 0) bulk_copy(ring + put * R::STAGE + R::ROWS + lane * 16 * MB, a.pc.scale + slot * MB, 16 * MB, bar);
+                } else if (pid == -1) atomicMin(a.status, SALICACHE_E_CAPACITY);
+            }
+        } else if (lane == 0) bar_arrive(bar);           // nothing to come
         put = put + 1 == STAGES ? 0 : put + 1;
         ++under_way;
         if (--to_fetch > 0) {
             const int b = f.b;
-            wg_next(f, a);
+            wg_next<KEYS>(f, a);
             if (f.b != b) ids_at = -1;
         }
     };
@@ -182,81 +191,92 @@ k_weigh_few(WgArgs a) {
     while (left > 0 && ok) {                 // the groups of one head
         const PgSeq& s = p.s;
         const int rows = s.n * a.G, run = (int)min(left, (long long)(p.groups - p.k));
-        const int jl = key_of(g8) + 8 * (c4 & 1);                        // the key that this lane writes, if c4 < 2
+        const int jl = key_of(g8) + 8 * (c4 & 1) + 16 * (c4 >> 1);       // the key that this lane writes, if the group has it
         const size_t row = ((size_t)p.b * a.pc.heads + p.h) * a.w_stride + jl;
         float* const out = a.out + row;
         const float* const in = a.in + row;
         const float decay = s.n > 0 ? a.decay : 1.0f;
         // positions below had_to had a weight before, which is looked at some groups ahead
-        const int had_to = c4 > 1 || !a.in ? 0 : s.n > 0 ? min(s.pos0, p.held) : p.held, put_to = c4 < 2 ? p.held : 0;
-        auto load_had = [&](int k) { return 16 * k + jl < had_to && k < p.k + run ? in[16 * k] : 0.0f; };
+        const bool writes = jl < KEYS;
+        const int had_to = !a.in || !writes ? 0 : s.n > 0 ? min(s.pos0, p.held) : p.held, put_to = writes ? p.held : 0;
+        auto load_had = [&](int k) { return KEYS * k + jl < had_to && k < p.k + run ? in[KEYS * k] : 0.0f; };
         if (lane == 0 && p.k == 0 && (s.cut || s.len > a.w_stride)) atomicMin(a.status, SALICACHE_E_CAPACITY);
-        float had[4] = {0.0f, load_had(p.k), load_had(p.k + 1), load_had(p.k + 2)};
+        float had[3] = {0.0f, load_had(p.k), load_had(p.k + 1)};
         Columns<FMT, D> col;
         if (rows > 0) col.load(a, s, p.h, 0, rows, g8, c4);
         bool first_columns = true;           // `col` holds column tile 0
         const bool live[2] = {2 * c4 < rows, 2 * c4 + 1 < rows};
 #pragma unroll 1
         for (int t = 0; t < run; ++t) {
-            const int j0 = (p.k + t) << 4;
+            const int j0 = (p.k + t) * KEYS;
             had[0] = had[1];
             had[1] = had[2];
-            had[2] = had[3];
-            had[3] = load_had(p.k + t + 3);
+            had[2] = load_had(p.k + t + 2);
             ok = warp_wait(bars + 8 * stage, phase, a.wait_limit, gave_up);
             if (!ok) break;
             --under_way;
-            KTile<FMT, D> kt;
-            kt.load(ring + stage * R::STAGE + KTile<FMT, D>::at(g8, c4), ring + stage * R::STAGE + R::ROWS + KTile<FMT, D>::meta_at(g8));
-            const bool there = pages >> (STAGES - 1) & 1u;
-            __syncwarp();                    // the stage has been read
-            fetch();
+            const uint32_t there = pages >> (U * (STAGES - 1));
+            // 16 keys at a time: four lanes' sums of slots g8 and g8 + 8, of which a lane pair exchanges one for the other
+            const bool odd = c4 & 1, high = c4 & 2;
+            float y[U];
+#pragma unroll 1
+            for (int u = 0; u < U; ++u) {
+                const uint32_t at = ring + stage * R::STAGE;
+                KTile<FMT, D> kt;
+                kt.load(at + 16 * u * RB + KTile<FMT, D>::at(g8, c4), at + R::ROWS + 16 * u * MB + KTile<FMT, D>::meta_at(g8));
+                if (u == U - 1) {
+                    __syncwarp();            // the stage has been read
+                    fetch();
+                }
+                float sum[2] = {0.0f, 0.0f};
+                auto columns = [&](int n) {
+                    float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        uint32_t a0, a1, a2, a3;
+                        key_frag<T, FMT, D>(cd, kt.k[0], kt.s[0], i, a0, a2);
+                        key_frag<T, FMT, D>(cd, kt.k[1], kt.s[1], i, a1, a3);
+                        mma16816<T>(sc, a0, a1, a2, a3, col.q[i][0], col.q[i][1]);
+                    }
+                    float w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = ex2(fmaf(sc[i], a.scale, -col.lse[i & 1]));
+                    if (j0 + KEYS - 1 > s.pos0) {        // some row may be before some key
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (s.pos0 + (8 * n + 2 * c4 + (i & 1)) / a.G < j0 + 16 * u + key_of(g8) + 8 * (i >> 1)) w[i] = 0.0f;
+                    }
+                    // a column that is no row has q = 0, which a key that is not finite would turn into no number
+                    const bool l0 = n == 0 ? live[0] : 8 * n + 2 * c4 < rows, l1 = n == 0 ? live[1] : 8 * n + 2 * c4 + 1 < rows;
+                    sum[0] += (l0 ? w[0] : 0.0f) + (l1 ? w[1] : 0.0f);
+                    sum[1] += (l0 ? w[2] : 0.0f) + (l1 ? w[3] : 0.0f);
+                };
+                if (there >> u & 1u) {
+                    if (rows <= 8) columns(0);
+                    else
+#pragma unroll 1
+                        for (int n = j0 > s.pos0 ? (j0 - s.pos0) * a.G / 8 : 0; 8 * n < rows; ++n) {     // from the first row that sees the first key on
+                            if (n != 0 || !first_columns) col.load(a, s, p.h, n, rows, g8, c4);
+                            first_columns = n == 0;
+                            columns(n);
+                        }
+                }
+                const float x = (odd ? sum[1] : sum[0]) + __shfl_xor_sync(0xffffffffu, odd ? sum[0] : sum[1], 1);
+                if (u == 0) y[0] = x;
+                else y[U - 1] = x;
+            }
             if (++stage == STAGES) {
                 stage = 0;
                 phase ^= 1;
             }
-            float sum[2] = {0.0f, 0.0f};
-            auto columns = [&](int n) {
-                float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    uint32_t a0, a1, a2, a3;
-                    key_frag<T, FMT, D>(cd, kt.k[0], kt.s[0], i, a0, a2);
-                    key_frag<T, FMT, D>(cd, kt.k[1], kt.s[1], i, a1, a3);
-                    mma16816<T>(sc, a0, a1, a2, a3, col.q[i][0], col.q[i][1]);
-                }
-                float w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = ex2(fmaf(sc[i], a.scale, -col.lse[i & 1]));
-                if (j0 + 15 > s.pos0) {      // some row may be before some key
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (s.pos0 + (8 * n + 2 * c4 + (i & 1)) / a.G < j0 + key_of(g8) + 8 * (i >> 1)) w[i] = 0.0f;
-                }
-                // a column that is no row has q = 0, which a key that is not finite would turn into no number
-                const bool l0 = n == 0 ? live[0] : 8 * n + 2 * c4 < rows, l1 = n == 0 ? live[1] : 8 * n + 2 * c4 + 1 < rows;
-                sum[0] += (l0 ? w[0] : 0.0f) + (l1 ? w[1] : 0.0f);
-                sum[1] += (l0 ? w[2] : 0.0f) + (l1 ? w[3] : 0.0f);
-            };
-            if (there) {
-                if (rows <= 8) columns(0);
-                else
-#pragma unroll 1
-                    for (int n = j0 > s.pos0 ? (j0 - s.pos0) * a.G / 8 : 0; 8 * n < rows; ++n) {     // from the first row that sees the first key on
-                        if (n != 0 || !first_columns) col.load(a, s, p.h, n, rows, g8, c4);
-                        first_columns = n == 0;
-                        columns(n);
-                    }
-            }
-            // four lanes' sums of two keys: a lane pair exchanges one for the other
-            float x = c4 & 1 ? sum[1] : sum[0];
-            x += __shfl_xor_sync(0xffffffffu, c4 & 1 ? sum[0] : sum[1], 1);
-            x += __shfl_xor_sync(0xffffffffu, x, 2);
+            // ... and pairs of pairs
+            float x = (high ? y[U - 1] : y[0]) + __shfl_xor_sync(0xffffffffu, high ? y[0] : y[U - 1], 2);
+            if (!(there >> (c4 >> 1) & 1u)) x = 0.0f;            // its page is none
             if (j0 + jl < put_to) out[j0] = fmaf(decay, had[0], x);
         }
         left -= run;
         p.k += run - 1;
-        if (left > 0) wg_next(p, a);
+        if (left > 0) wg_next<KEYS>(p, a);
     }
     for (; !ok && under_way > 0; --under_way) {              // copies in flight end before the block does
         bar_drain(bars + 8 * stage, phase);
@@ -274,7 +294,7 @@ int launch_few(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
     using R = WgRing<FMT, D>;
     SC_CHECK(cudaFuncSetAttribute(k_weigh_few<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::BYTES));
     // no more blocks than there can be groups of keys for: sequences times heads times the table's groups
-    const long long most = (long long)a.sq.n_seqs * a.pc.heads * (((long long)a.sq.width << a.pc.page_shift) >> 4);
+    const long long most = (long long)a.sq.n_seqs * a.pc.heads * ((((long long)a.sq.width << a.pc.page_shift) + wg_keys<FMT, D>() - 1) / wg_keys<FMT, D>());
     const int blocks = (int)max(1ll, min((most + WG_WARPS - 1) / WG_WARPS, (long long)c->sm_count * WG_BLOCKS));
     SC_CHECK(pt_launch(k_weigh_few<T, FMT, D>, dim3((unsigned)blocks), WG_THREADS, R::BYTES, st, a));
     c->launches++;
