@@ -119,7 +119,8 @@ struct Columns {
     }
 };
 
-template <typename T, int FMT, int D>
+// NT: column tiles that stay in registers.
+template <typename T, int FMT, int D, int NT>
 __global__ void __launch_bounds__(WG_THREADS, WG_BLOCKS)
 k_weigh_few(WgArgs a) {
     using R = WgRing<FMT, D>;
@@ -202,10 +203,11 @@ k_weigh_few(WgArgs a) {
         auto load_had = [&](int k) { return KEYS * k + jl < had_to && k < p.k + run ? in[KEYS * k] : 0.0f; };
         if (lane == 0 && p.k == 0 && (s.cut || s.len > a.w_stride)) atomicMin(a.status, SALICACHE_E_CAPACITY);
         float had[3] = {0.0f, load_had(p.k), load_had(p.k + 1)};
-        Columns<FMT, D> col;
-        if (rows > 0) col.load(a, s, p.h, 0, rows, g8, c4);
-        bool first_columns = true;           // `col` holds column tile 0
-        const bool live[2] = {2 * c4 < rows, 2 * c4 + 1 < rows};
+        Columns<FMT, D> col[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            if (8 * n < rows) col[n].load(a, s, p.h, n, rows, g8, c4);
+        bool first_columns = true;           // `col[0]` holds column tile 0
 #pragma unroll 1
         for (int t = 0; t < run; ++t) {
             const int j0 = (p.k + t) * KEYS;
@@ -229,36 +231,38 @@ k_weigh_few(WgArgs a) {
                     fetch();
                 }
                 float sum[2] = {0.0f, 0.0f};
-                auto columns = [&](int n) {
+                auto columns = [&](const Columns<FMT, D>& x, int n) {
                     float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
                         uint32_t a0, a1, a2, a3;
                         key_frag<T, FMT, D>(cd, kt.k[0], kt.s[0], i, a0, a2);
                         key_frag<T, FMT, D>(cd, kt.k[1], kt.s[1], i, a1, a3);
-                        mma16816<T>(sc, a0, a1, a2, a3, col.q[i][0], col.q[i][1]);
+                        mma16816<T>(sc, a0, a1, a2, a3, x.q[i][0], x.q[i][1]);
                     }
                     float w[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = ex2(fmaf(sc[i], a.scale, -col.lse[i & 1]));
+                    for (int i = 0; i < 4; ++i) w[i] = ex2(fmaf(sc[i], a.scale, -x.lse[i & 1]));
                     if (j0 + KEYS - 1 > s.pos0) {        // some row may be before some key
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             if (s.pos0 + (8 * n + 2 * c4 + (i & 1)) / a.G < j0 + 16 * u + key_of(g8) + 8 * (i >> 1)) w[i] = 0.0f;
                     }
                     // a column that is no row has q = 0, which a key that is not finite would turn into no number
-                    const bool l0 = n == 0 ? live[0] : 8 * n + 2 * c4 < rows, l1 = n == 0 ? live[1] : 8 * n + 2 * c4 + 1 < rows;
+                    const bool l0 = 8 * n + 2 * c4 < rows, l1 = 8 * n + 2 * c4 + 1 < rows;
                     sum[0] += (l0 ? w[0] : 0.0f) + (l1 ? w[1] : 0.0f);
                     sum[1] += (l0 ? w[2] : 0.0f) + (l1 ? w[3] : 0.0f);
                 };
                 if (there >> u & 1u) {
-                    if (rows <= 8) columns(0);
-                    else
+                    if (rows <= 8 * NT) {
+                        columns(col[0], 0);
+                        if (NT > 1 && rows > 8) columns(col[NT - 1], NT - 1);
+                    } else
 #pragma unroll 1
                         for (int n = j0 > s.pos0 ? (j0 - s.pos0) * a.G / 8 : 0; 8 * n < rows; ++n) {     // from the first row that sees the first key on
-                            if (n != 0 || !first_columns) col.load(a, s, p.h, n, rows, g8, c4);
+                            if (n != 0 || !first_columns) col[0].load(a, s, p.h, n, rows, g8, c4);
                             first_columns = n == 0;
-                            columns(n);
+                            columns(col[0], n);
                         }
                 }
                 const float x = (odd ? sum[1] : sum[0]) + __shfl_xor_sync(0xffffffffu, odd ? sum[0] : sum[1], 1);
@@ -289,23 +293,27 @@ k_weigh_few(WgArgs a) {
     if (threadIdx.x == 0 && *gave_up) atomicMin(a.status, SC_GAVE_UP);
 }
 
-template <typename T, int FMT, int D>
+template <typename T, int FMT, int D, int NT>
 int launch_few(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
     using R = WgRing<FMT, D>;
-    SC_CHECK(cudaFuncSetAttribute(k_weigh_few<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::BYTES));
+    SC_CHECK(cudaFuncSetAttribute(k_weigh_few<T, FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::BYTES));
     // no more blocks than there can be groups of keys for: sequences times heads times the table's groups
     const long long most = (long long)a.sq.n_seqs * a.pc.heads * ((((long long)a.sq.width << a.pc.page_shift) + wg_keys<FMT, D>() - 1) / wg_keys<FMT, D>());
     const int blocks = (int)max(1ll, min((most + WG_WARPS - 1) / WG_WARPS, (long long)c->sm_count * WG_BLOCKS));
-    SC_CHECK(pt_launch(k_weigh_few<T, FMT, D>, dim3((unsigned)blocks), WG_THREADS, R::BYTES, st, a));
+    SC_CHECK(pt_launch(k_weigh_few<T, FMT, D, NT>, dim3((unsigned)blocks), WG_THREADS, R::BYTES, st, a));
     c->launches++;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;
 }
+template <typename T, int FMT, int D>
+int few_columns(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
+    return (long long)a.sq.n_rows * a.G > 8ll * a.sq.n_seqs ? launch_few<T, FMT, D, 2>(c, a, st) : launch_few<T, FMT, D, 1>(c, a, st);
+}
 template <typename T, int D>
 int few_format(salicache_ctx* c, const WgArgs& a, int format, cudaStream_t st) {
-    if (format == SALICACHE_FP16) return launch_few<T, PF_16, D>(c, a, st);
-    if (format == SALICACHE_INT8) return launch_few<T, PF_I8, D>(c, a, st);
-    return launch_few<T, PF_I4, D>(c, a, st);
+    if (format == SALICACHE_FP16) return few_columns<T, PF_16, D>(c, a, st);
+    if (format == SALICACHE_INT8) return few_columns<T, PF_I8, D>(c, a, st);
+    return few_columns<T, PF_I4, D>(c, a, st);
 }
 
 }  // namespace

@@ -13,6 +13,8 @@ struct WgArgs {
     float scale, decay;                      // scale * log2(e)
     int* status;
     int wait_limit;                          // tries before a wait between a block's roles is given up
+    int tok;                                 // many rows: tokens of a tile of rows, and 2^38 / tok
+    uint64_t per_tok;
     float* part;                             // [2 * blocks][keys of a tile]: sums of a tile's rows so far, tail after head records of a block
     int4* head;                              // [2 * blocks]: per block: head record (0 none, 1 the tile goes on, 2 it ends), tail record
                                              // (0, 1), its sequence, its head; then its tile of keys, -, -, -

@@ -37,17 +37,16 @@ struct WmWalk {
     int b, h, kt, k;                         // sequence, head, tile of keys, unit within the item
     PgSeq s;
 };
-// The tiles of rows of an item.
-struct WmRows {
-    int R, HR;                               // tiles of the sequence, rows of one (whole tokens)
-    __device__ __forceinline__ WmRows(const PgSeq& s, int G) : R((s.n + 128 / G - 1) / (128 / G)), HR(128 / G * G) {}
-};
-// First tile of rows that sees some key from j0 on.
-__device__ __forceinline__ int wm_first(const PgSeq& s, int G, int j0) { return max(0, j0 - s.pos0) / (128 / G); }
+// Tiles of the sequence's rows, and the first one that sees some key from j0 on.  A tile has `tok` whole tokens, by which a
+// product with 2^38 / tok rounded up divides: x is at most a call's tokens, below 2^30 / G, and tok = 128 / G rounded down, so
+// that the product fits and is less than x / 2^38, which is less than 1 / tok, too large.
+__device__ __forceinline__ int wm_by_tok(int x, const WgArgs& a) { return (int)((uint64_t)x * a.per_tok >> 38); }
+__device__ __forceinline__ int wm_rows(const PgSeq& s, const WgArgs& a) { return wm_by_tok(s.n + a.tok - 1, a); }
+__device__ __forceinline__ int wm_first(const PgSeq& s, const WgArgs& a, int j0) { return wm_by_tok(max(0, j0 - s.pos0), a); }
 __device__ __forceinline__ int wm_items(const PgSeq& s, const WgArgs& a) { return (wg_held(s, a) + WM_KEYS - 1) / WM_KEYS; }
 // Units of an item: its fixed cost and its tiles, one at least (a sequence without rows has its weights copied).
-__device__ __forceinline__ int wm_units(const PgSeq& s, int G, int kt) {
-    return WM_ITEM + max(1, WmRows(s, G).R - wm_first(s, G, kt * WM_KEYS));
+__device__ __forceinline__ int wm_units(const PgSeq& s, const WgArgs& a, int kt) {
+    return WM_ITEM + max(1, wm_rows(s, a) - wm_first(s, a, kt * WM_KEYS));
 }
 // Items at the front that all rows see.
 __device__ __forceinline__ int wm_whole(const PgSeq& s, const WgArgs& a) {
@@ -57,17 +56,17 @@ __device__ __forceinline__ int wm_whole(const PgSeq& s, const WgArgs& a) {
 __device__ __forceinline__ long long wm_per_head(const WgArgs& a, const PgSeq& s) {
     constexpr int ALONE = 2;
     const int lane = threadIdx.x & 31, n = wm_items(s, a), whole = wm_whole(s, a);
-    long long w = whole > 0 ? (long long)whole * wm_units(s, a.G, 0) : 0;
+    long long w = whole > 0 ? (long long)whole * wm_units(s, a, 0) : 0;
     if (n - whole <= ALONE)
 #pragma unroll 1
-        for (int kt = whole; kt < n; ++kt) w += wm_units(s, a.G, kt);
+        for (int kt = whole; kt < n; ++kt) w += wm_units(s, a, kt);
     for (uint32_t many = __ballot_sync(0xffffffffu, n - whole > ALONE); many; many &= many - 1) {
         const int from = __ffs(many) - 1;
         const PgSeq o = pt_seq_of(s, from);
         long long x = 0;
 #pragma unroll 1
         for (int kt = __shfl_sync(0xffffffffu, whole, from) + lane; kt < __shfl_sync(0xffffffffu, n, from) + lane; kt += 32)
-            if (kt < wm_items(o, a)) x += wm_units(o, a.G, kt);
+            if (kt < wm_items(o, a)) x += wm_units(o, a, kt);
 #pragma unroll
         for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
         if (lane == from) w += x;
@@ -104,7 +103,7 @@ __device__ __noinline__ WmWalk wm_start(const WgArgs& a, int block, int blocks) 
         const long long at = __shfl_sync(0xffffffffu, beg - (incl - n), from), per = __shfl_sync(0xffffffffu, n, from) / a.pc.heads;
         w.h = (int)(at / per);
         long long rem = at - w.h * per;
-        const int items = wm_items(w.s, a), whole = wm_whole(w.s, a), each = wm_units(w.s, a.G, 0);
+        const int items = wm_items(w.s, a), whole = wm_whole(w.s, a), each = wm_units(w.s, a, 0);
         if (rem < (long long)whole * each) {
             w.kt = (int)(rem / each);
             w.k = (int)(rem - (long long)w.kt * each);
@@ -113,7 +112,7 @@ __device__ __noinline__ WmWalk wm_start(const WgArgs& a, int block, int blocks) 
         rem -= (long long)whole * each;
 #pragma unroll 1
         for (int k0 = whole;; k0 += 32) {
-            const int u = k0 + lane < items ? wm_units(w.s, a.G, k0 + lane) : 0;
+            const int u = k0 + lane < items ? wm_units(w.s, a, k0 + lane) : 0;
             const long long upto = pt_scan(u);
             const uint32_t in = __ballot_sync(0xffffffffu, rem >= upto - u && rem < upto);
             if (in || k0 + 32 >= items) {
@@ -149,7 +148,7 @@ struct WmSeg {
     __device__ __forceinline__ WmSeg(const WgArgs& a, const WmWalk& w) {
         j0 = w.kt * WM_KEYS;
         held = wg_held(w.s, a);
-        const int f = wm_first(w.s, a.G, j0), n = WmRows(w.s, a.G).R - f, units = WM_ITEM + max(1, n);
+        const int f = wm_first(w.s, a, j0), n = wm_rows(w.s, a) - f, units = WM_ITEM + max(1, n);
         k0 = w.k;
         k1 = (int)min((long long)units, k0 + w.left);
         const int t0 = max(0, k0 - WM_ITEM), t1 = max(0, k1 - WM_ITEM);
@@ -253,7 +252,7 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // rows of a tile that no copy fills (128 is no multiple of G) are zeros
-    const int HR = 128 / a.G * a.G;
+    const int HR = a.tok * a.G;
     for (int i = tid; i < WM_Q * (128 - HR) * (D / 8); i += WM_THREADS) {
         const int c = i % (D / 8), r = i / (D / 8) % (128 - HR), q = i / (D / 8) / (128 - HR);
         sts16(base + SM::Q + q * SM::TILE + swz(HR + r, c), 0u, 0u, 0u, 0u);
@@ -383,14 +382,39 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
         if (FMT != PF_16) {
             constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>(), LPR = RB / 16, RPP = 32 / LPR, P = 16 / RPP;
             static_assert(P >= 1, "16 keys at a time");
+            constexpr int BATCH = FMT == PF_I4 ? 4 : 2;          // groups of 16 keys under way at a time, as the registers allow
             const Codes<T> cd;
             const int lw = wid - 16, c = lane % LPR;
             uint32_t n_item = 0;
+            int pid16 = w.left > 0 ? WmSeg(a, w).page_of(a, w, lane) : -2;
             while (w.left > 0) {
                 const WmSeg g(a, w);
+                // the next item's pages are looked up meanwhile
+                WmWalk wn = w;
+                wn.left -= g.k1 - g.k0;
+                if (wn.left > 0) wn = wm_after(a, wn);
+                const int pid16n = wn.left > 0 ? WmSeg(a, wn).page_of(a, wn, lane) : -2;
                 if (g.tiles > 0) {
                     const uint32_t kb = n_item % WM_K;
-                    const int pid16 = g.page_of(a, w, lane);
+                    uint4 words[BATCH][P];
+                    uint32_t meta[BATCH][P];
+                    int pid[BATCH];
+                    auto load = [&](int grp0) {
+#pragma unroll
+                        for (int e = 0; e < BATCH; ++e) {
+                            pid[e] = __shfl_sync(0xffffffffu, pid16, lw * 4 + grp0 + e);
+                            const size_t slot = pg_slot(a.pc, max(pid[e], 0), 0, w.h, (g.j0 + lw * 64 + (grp0 + e) * 16) & ((1 << a.pc.page_shift) - 1));
+                            if (pid[e] >= 0)
+#pragma unroll
+                                for (int p = 0; p < P; ++p) {
+                                    const int r = p * RPP + lane / LPR;
+                                    words[e][p] = __ldcs(reinterpret_cast<const uint4*>(a.pc.data + (slot + r) * RB) + c);
+                                    const uint8_t* m = a.pc.scale + (slot + r) * MB;
+                                    meta[e][p] = FMT == PF_I8 ? *reinterpret_cast<const uint16_t*>(m) : *reinterpret_cast<const uint32_t*>(m);
+                                }
+                        }
+                    };
+                    load(0);                 // before there is a place for them
                     if (n_item >= WM_K && !wait(bars.k_empty[kb], (n_item / WM_K - 1) & 1)) break;
                     if (lw == 0) {
                         const uint32_t there = __ballot_sync(0xffffffffu, pid16 >= 0), bad = __ballot_sync(0xffffffffu, pid16 == -1);
@@ -402,44 +426,36 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                     const uint32_t dst = base + SM::K + kb * 2 * SM::TILE + (lw >> 1) * SM::TILE;
 #pragma unroll
                     for (int grp = 0; grp < 4; ++grp) {
-                        const int pid = __shfl_sync(0xffffffffu, pid16, lw * 4 + grp);
-                        if (pid < 0) continue;                   // what lies there is not looked at
-                        const size_t slot = pg_slot(a.pc, pid, 0, w.h, (g.j0 + lw * 64 + grp * 16) & ((1 << a.pc.page_shift) - 1));
-                        uint4 words[P];
-                        uint32_t meta[P];
+                        const int e = grp % BATCH;
+                        if (pid[e] >= 0)                         // what lies in no page is not looked at
 #pragma unroll
-                        for (int p = 0; p < P; ++p) {
-                            const int r = p * RPP + lane / LPR;
-                            words[p] = __ldcs(reinterpret_cast<const uint4*>(a.pc.data + (slot + r) * RB) + c);
-                            const uint8_t* m = a.pc.scale + (slot + r) * MB;
-                            meta[p] = FMT == PF_I8 ? *reinterpret_cast<const uint16_t*>(m) : *reinterpret_cast<const uint32_t*>(m);
-                        }
+                            for (int p = 0; p < P; ++p) {
+                                const int row = (lw & 1) * 64 + grp * 16 + p * RPP + lane / LPR;
+                                const uint32_t s2 = dup_lo(meta[e][p]), z2 = dup_hi(meta[e][p]), w4[4] = {words[e][p].x, words[e][p].y, words[e][p].z, words[e][p].w};
+                                if (FMT == PF_I8) {
 #pragma unroll
-                        for (int p = 0; p < P; ++p) {
-                            const int row = (lw & 1) * 64 + grp * 16 + p * RPP + lane / LPR;
-                            const uint32_t s2 = dup_lo(meta[p]), z2 = dup_hi(meta[p]), w4[4] = {words[p].x, words[p].y, words[p].z, words[p].w};
-                            if (FMT == PF_I8) {
+                                    for (int i = 0; i < 2; ++i)
+                                        sts16(dst + swz(row, 2 * c + i), mul2<T>(cd.bytes(w4[2 * i], 0x5140), s2), mul2<T>(cd.bytes(w4[2 * i], 0x5342), s2),
+                                              mul2<T>(cd.bytes(w4[2 * i + 1], 0x5140), s2), mul2<T>(cd.bytes(w4[2 * i + 1], 0x5342), s2));
+                                } else {
 #pragma unroll
-                                for (int i = 0; i < 2; ++i)
-                                    sts16(dst + swz(row, 2 * c + i), mul2<T>(cd.bytes(w4[2 * i], 0x5140), s2), mul2<T>(cd.bytes(w4[2 * i], 0x5342), s2),
-                                          mul2<T>(cd.bytes(w4[2 * i + 1], 0x5140), s2), mul2<T>(cd.bytes(w4[2 * i + 1], 0x5342), s2));
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {                    // elements 0 4, 1 5, 2 6, 3 7 in their words: put in order
-                                    const uint32_t y = w4[i] >> 8, e04 = fma2<T>(cd.nib_lo(w4[i]), s2, z2), e15 = fma2<T>(cd.nib_hi(w4[i]), s2, z2);
-                                    const uint32_t e26 = fma2<T>(cd.nib_lo(y), s2, z2), e37 = fma2<T>(cd.nib_hi(y), s2, z2);
-                                    sts16(dst + swz(row, 4 * c + i), __byte_perm(e04, e15, 0x5410), __byte_perm(e26, e37, 0x5410),
-                                          __byte_perm(e04, e15, 0x7632), __byte_perm(e26, e37, 0x7632));
+                                    for (int i = 0; i < 4; ++i) {                // elements 0 4, 1 5, 2 6, 3 7 in their words: put in order
+                                        const uint32_t y = w4[i] >> 8, e04 = fma2<T>(cd.nib_lo(w4[i]), s2, z2), e15 = fma2<T>(cd.nib_hi(w4[i]), s2, z2);
+                                        const uint32_t e26 = fma2<T>(cd.nib_lo(y), s2, z2), e37 = fma2<T>(cd.nib_hi(y), s2, z2);
+                                        sts16(dst + swz(row, 4 * c + i), __byte_perm(e04, e15, 0x5410), __byte_perm(e26, e37, 0x5410),
+                                              __byte_perm(e04, e15, 0x7632), __byte_perm(e26, e37, 0x7632));
+                                    }
                                 }
                             }
-                        }
+                        if (e == BATCH - 1 && grp < 3) load(grp + 1);
                     }
                     fence_async();
                     __syncwarp();
                     if (lane == 0) bar_arrive(smem_u32(&bars.k_full[kb]));
                     ++n_item;
                 }
-                next(g);
+                w = wn;
+                pid16 = pid16n;
             }
         }
     } else {
@@ -542,7 +558,7 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                     if (lane == 0) {
                         bar_expect(bar, (uint32_t)(HR * D * 2));
                         for (int x = 0; x < D; x += 64)
-                            tensor_copy3(base + SM::Q + st * SM::TILE + x * 256, &q_map, x, w.h * a.G, w.s.row0 + (g.rt + t) * (128 / a.G), bar);
+                            tensor_copy3(base + SM::Q + st * SM::TILE + x * 256, &q_map, x, w.h * a.G, w.s.row0 + (g.rt + t) * a.tok, bar);
                     }
                     __syncwarp();
                     // the next item's keys, once the rows' ring has gone past the item before, whose keys they replace
@@ -581,7 +597,7 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
             while (w.left > 0 && ok) {
                 const WmSeg g(a, w);
                 for (int t = 0; t < g.tiles; ++t, ++n) {
-                    const float* p = a.lse + (long long)(w.s.row0 + (g.rt + t) * (128 / a.G)) * Hq + w.h * a.G;
+                    const float* p = a.lse + (long long)(w.s.row0 + (g.rt + t) * a.tok) * Hq + w.h * a.G;
                     const int cols = min(HR, w.s.n * a.G - (g.rt + t) * HR);
                     float l[4];
 #pragma unroll
@@ -636,6 +652,8 @@ int launch_many(salicache_ctx* c, WgArgs a, char* work, cudaStream_t st) {
     if (FMT == PF_16 && !page_map(&map, a.pc, D, bf16)) return SALICACHE_E_CUDA;
     SC_CHECK(cudaFuncSetAttribute(k_weigh_many<T, FMT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
     const int blocks = min(c->sm_count, PT_MAX_BLOCKS);
+    a.tok = 128 / a.G;
+    a.per_tok = ((1ull << 38) + a.tok - 1) / a.tok;
     a.part = reinterpret_cast<float*>(work);
     a.head = reinterpret_cast<int4*>(a.part + (size_t)2 * blocks * WM_KEYS);
     SC_CHECK(pt_launch(k_weigh_many<T, FMT, D>, dim3(blocks), wm_threads<FMT>(), BYTES, st, a, map, q_map, blocks));
