@@ -1,12 +1,12 @@
 // Eviction from the paged cache: which positions a budget keeps, and moving them together.
 //
 // Selection.  Of every (sequence, key/value head) the first `sinks` and the last `recent` positions stay, and the heaviest of
-// those between.  One block per (sequence, head) finds the weight of the last one that fits by its bits, eight at a time from
-// the top (floats become unsigned numbers in the same order), counting in shared memory; then it writes the positions above
-// that weight, and the lowest ones at it, in ascending order: every warp has a stretch of positions, whose counts are summed
-// before the second look.
+// those between.  One block per (sequence, head) finds the weight of the last one that fits by its bits, 11, 11 and 10 of them
+// from the top (floats become unsigned numbers in the same order), counting in shared memory, where the keys stay too; then it
+// writes the positions above that weight, and the lowest ones at it, in ascending order: every warp has a stretch of positions,
+// whose counts are summed before the second look.
 //
-// Moving.  A block has the rows that 128 entries of a list name, K and V of one head, 16 bytes a lane.  Into other pages all
+// Moving.  A block has the rows that a tile of a list's entries names, K and V of one head, 16 bytes a lane.  Into other pages all
 // tiles of a list move at once.  In place one block takes a list's tiles in turn, and reads a tile before it writes it: entry
 // k of an ascending list is at least first + k, so what a tile writes lies below all that later tiles read.
 #include "paged_async.cuh"
@@ -23,75 +23,106 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+constexpr int SH_BINS = 2048, SH_KEYS = 53 * 1024;               // keys that shared memory holds at most
+
+// `held`: keys of a list that the block's shared memory holds; those behind are read again in every pass.
 __global__ void __launch_bounds__(SH_THREADS)
 k_select_heavy(const float* weight, long long stride, int heads, const int* len_, int budget, int sinks, int recent, int* keep, int* kept,
-               int* status) {
-    __shared__ uint32_t hist[256], warp_sum[SH_WARPS][2];
+               int* status, int held) {
+    extern __shared__ uint32_t keys[];
+    __shared__ uint32_t hist[SH_BINS], warp_sum[SH_WARPS][2];
     __shared__ uint32_t s_digit, s_left;
-    const int b = blockIdx.x / heads, h = blockIdx.x % heads, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int b = blockIdx.x / heads, h = blockIdx.x % heads, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const uint32_t before = (1u << lane) - 1u;
     grid_wait();
     grid_release();
     int len = max(len_[b], 0);
     if (len > stride) {
         len = (int)stride;
-        if (threadIdx.x == 0) atomicMin(status, SALICACHE_E_CAPACITY);
+        if (tid == 0) atomicMin(status, SALICACHE_E_CAPACITY);
     }
     const float* w = weight + (size_t)blockIdx.x * stride;
     int* out = keep + (size_t)blockIdx.x * budget;
-    if (h == 0 && threadIdx.x == 0) kept[b] = min(len, budget);
+    if (h == 0 && tid == 0) kept[b] = min(len, budget);
     if (len <= budget) {
-        for (int i = threadIdx.x; i < budget; i += SH_THREADS) out[i] = i < len ? i : -1;
+        for (int i = tid; i < budget; i += SH_THREADS) out[i] = i < len ? i : -1;
         return;
     }
-    for (int i = threadIdx.x; i < sinks; i += SH_THREADS) out[i] = i;
-    for (int i = threadIdx.x; i < recent; i += SH_THREADS) out[budget - recent + i] = len - recent + i;
-    const int lo = sinks, hi = len - recent, take = budget - sinks - recent;
+    for (int i = tid; i < sinks; i += SH_THREADS) out[i] = i;
+    for (int i = tid; i < recent; i += SH_THREADS) out[budget - recent + i] = len - recent + i;
+    const int n = len - recent - sinks, take = budget - sinks - recent;      // of positions sinks .. sinks + n - 1, in this order
     if (take == 0) return;
-    // the take-th heaviest of [lo, hi): its key's bits from the top
+    w += sinks;
+    auto key = [&](int i) -> uint32_t { return i < held ? keys[i] : weight_key(w[i]); };
+    // the take-th heaviest: its key's bits from the top, 11, 11 and 10 of them
     uint32_t prefix = 0, left = (uint32_t)take;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+        for (int i = tid; i < SH_BINS; i += SH_THREADS) hist[i] = 0;
         __syncthreads();
-        for (int i = lo + threadIdx.x; i < hi; i += SH_THREADS) {
-            const uint32_t k = weight_key(w[i]);
-            if (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[k >> shift & 255u], 1u);
-        }
-        __syncthreads();
-        if (wid == 0) {                      // from the top: lane l has digits 255 - 8 l .. 248 - 8 l
-            uint32_t c[8], sum = 0;
+        if (pass == 0) {
+            constexpr int E = 8;             // loads under way
+            for (int i0 = wid * 32; i0 < n; i0 += E * SH_THREADS) {
+                uint32_t k[E];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += c[i] = hist[255 - 8 * lane - i];
-            uint32_t incl = sum;
+                for (int e = 0; e < E; ++e) {
+                    const int i = i0 + e * SH_THREADS + lane;
+                    k[e] = i < n ? weight_key(w[i]) : 0u;
+                }
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += t;
-            }
-            uint32_t above = incl - sum;
-            if (above < left && incl >= left) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (above < left && above + c[i] >= left) {
-                        s_digit = 255 - 8 * lane - i;
-                        s_left = left - above;
+                for (int e = 0; e < E; ++e) {
+                    const int i = i0 + e * SH_THREADS + lane;
+                    if (i < n) {
+                        if (i < held) keys[i] = k[e];
+                        atomicAdd(&hist[k[e] >> shift], 1u);
                     }
-                    above += c[i];
                 }
             }
+        } else {
+            auto count = [&](uint32_t k) {
+                if (k >> (shift + bits) == prefix >> (shift + bits)) atomicAdd(&hist[k >> shift & ((1u << bits) - 1u)], 1u);
+            };
+#pragma unroll 8
+            for (int i = tid; i < min(n, held); i += SH_THREADS) count(keys[i]);
+            for (int i = (held - tid + SH_THREADS - 1) / SH_THREADS * SH_THREADS + tid; i < n; i += SH_THREADS) count(weight_key(w[i]));
+        }
+        __syncthreads();
+        // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t
+        const uint32_t c0 = hist[SH_BINS - 1 - 2 * tid], c1 = hist[SH_BINS - 2 - 2 * tid];
+        uint32_t incl = c0 + c1;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        if (lane == 31) warp_sum[wid][0] = incl;
+        __syncthreads();
+        incl += __reduce_add_sync(0xffffffffu, lane < wid ? warp_sum[lane][0] : 0u);
+        const uint32_t above = incl - c0 - c1;
+        if (above < left && incl >= left) {
+            const bool second = above + c0 < left;
+            s_digit = SH_BINS - 1 - 2 * tid - second;
+            s_left = left - above - (second ? c0 : 0u);
         }
         __syncthreads();
         prefix |= s_digit << shift;
         left = s_left;
-        __syncthreads();
     }
-    // positions above `prefix`, and the first `left` at it
-    const int seg = ((hi - lo + SH_WARPS - 1) / SH_WARPS + 31) / 32 * 32, a = min(hi, lo + wid * seg), e = min(hi, a + seg);
+    // positions above `prefix`, and the first `left` at it: a stretch for every warp, counted, then written
+    const int seg = ((n + SH_WARPS - 1) / SH_WARPS + 31) / 32 * 32, a = min(n, wid * seg), e = min(n, a + seg);
     uint32_t n_above = 0, n_equal = 0;
-    for (int i = a + lane; i < e; i += 32) {
-        const uint32_t k = weight_key(w[i]);
-        n_above += k > prefix;
-        n_equal += k == prefix;
-    }
+    if (e <= held) {
+#pragma unroll 8
+        for (int i = a + lane; i < e; i += 32) {
+            n_above += keys[i] > prefix;
+            n_equal += keys[i] == prefix;
+        }
+    } else
+        for (int i = a + lane; i < e; i += 32) {
+            n_above += key(i) > prefix;
+            n_equal += key(i) == prefix;
+        }
     n_above = __reduce_add_sync(0xffffffffu, n_above);
     n_equal = __reduce_add_sync(0xffffffffu, n_equal);
     if (lane == 0) {
@@ -99,22 +130,35 @@ k_select_heavy(const float* weight, long long stride, int heads, const int* len_
         warp_sum[wid][1] = n_equal;
     }
     __syncthreads();
-    uint32_t above = lane < wid ? warp_sum[lane][0] : 0u, equal = lane < wid ? warp_sum[lane][1] : 0u;
-    above = __reduce_add_sync(0xffffffffu, above);
-    equal = __reduce_add_sync(0xffffffffu, equal);
-    for (int i0 = a; i0 < e; i0 += 32) {
-        const int i = i0 + lane;
-        const uint32_t k = i < e ? weight_key(w[i]) : 0u;
-        const uint32_t is_above = __ballot_sync(0xffffffffu, i < e && k > prefix), is_equal = __ballot_sync(0xffffffffu, i < e && k == prefix);
-        const uint32_t before = (1u << lane) - 1u, eq = equal + __popc(is_equal & before);
-        const bool mine = is_above >> lane & 1u || (is_equal >> lane & 1u && eq < left);
-        if (mine) out[sinks + above + __popc(is_above & before) + min(eq, left)] = i;
-        above += __popc(is_above);
-        equal += __popc(is_equal);
+    uint32_t above = __reduce_add_sync(0xffffffffu, lane < wid ? warp_sum[lane][0] : 0u);
+    uint32_t equal = __reduce_add_sync(0xffffffffu, lane < wid ? warp_sum[lane][1] : 0u);
+    constexpr int E = 4;                     // times 32 positions at a time
+    for (int i0 = a; i0 < e; i0 += 32 * E) {
+        uint32_t is_above[E], is_equal[E];
+#pragma unroll
+        for (int x = 0; x < E; ++x) {
+            const int i = i0 + 32 * x + lane;
+            const uint32_t k = i < e ? key(i) : 0u;
+            is_above[x] = __ballot_sync(0xffffffffu, i < e && k > prefix);
+            is_equal[x] = __ballot_sync(0xffffffffu, i < e && k == prefix);
+        }
+#pragma unroll
+        for (int x = 0; x < E; ++x) {
+            const uint32_t eq = equal + __popc(is_equal[x] & before);
+            const bool mine = is_above[x] >> lane & 1u || (is_equal[x] >> lane & 1u && eq < left);
+            if (mine) out[sinks + above + __popc(is_above[x] & before) + min(eq, left)] = sinks + i0 + 32 * x + lane;
+            above += __popc(is_above[x]);
+            equal += __popc(is_equal[x]);
+        }
     }
 }
 
-constexpr int KP_THREADS = 256, KP_TILE = 128;
+constexpr int KP_THREADS = 256;
+// Rows of a tile: eight 16-byte pieces a thread, K and V (twice as many, 128 rows of 512 bytes, take a quarter longer); in place,
+// where tiles follow one another, sixteen.
+template <int FMT, int D, bool IN_PLACE> __host__ __device__ constexpr int kp_tile() {
+    return (IN_PLACE ? 16 : 8) * KP_THREADS / (2 * (pg_row_bytes<FMT, D>() / 16));
+}
 
 struct KpArgs {
     PgCache pc;
@@ -155,7 +199,8 @@ template <int FMT, int D, bool IN_PLACE>
 __global__ void __launch_bounds__(KP_THREADS)
 k_paged_keep(KpArgs a, int row_blocks) {
     constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>(), LPR = RB / 16, PIECES = 2 * LPR;
-    constexpr int EACH = KP_TILE * PIECES / KP_THREADS;          // 16-byte pieces of a thread
+    constexpr int KP_TILE = kp_tile<FMT, D, IN_PLACE>(), EACH = KP_TILE * PIECES / KP_THREADS;      // 16-byte pieces of a thread
+    constexpr int METAS = MB > 0 ? (2 * KP_TILE + KP_THREADS - 1) / KP_THREADS : 1;                 // scales of a thread
     __shared__ long long src[KP_TILE], dst[KP_TILE];             // slots of K, or -1
     const int b = blockIdx.y / a.pc.heads, h = blockIdx.y % a.pc.heads;
     grid_wait();
@@ -172,8 +217,8 @@ k_paged_keep(KpArgs a, int row_blocks) {
     const int mask = (1 << a.pc.page_shift) - 1;
     const size_t v_step = (size_t)a.pc.heads << a.pc.page_shift;         // slots from K to V
     for (int k0 = blockIdx.x * KP_TILE; k0 < n; k0 += row_blocks * KP_TILE) {
-        if (threadIdx.x < KP_TILE) {
-            const int k = k0 + threadIdx.x;
+        for (int i = threadIdx.x; i < KP_TILE; i += KP_THREADS) {
+            const int k = k0 + i;
             long long s = -1, d = -1;
             if (k < n) {
                 const int e = list[k];
@@ -189,22 +234,25 @@ k_paged_keep(KpArgs a, int row_blocks) {
                 if (s < 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
                 else if (s == d) s = -1;                         // stays where it is
             }
-            src[threadIdx.x] = s;
-            dst[threadIdx.x] = d;
+            src[i] = s;
+            dst[i] = d;
         }
         __syncthreads();
         uint4 v[EACH];
-        uint32_t meta = 0;
-        const int mk = threadIdx.x >> 1, mkv = threadIdx.x & 1;  // a scale per thread
-        static_assert(KP_THREADS == 2 * KP_TILE, "a scale per thread");
+        uint32_t meta[METAS];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int p = i * KP_THREADS + threadIdx.x, k = p / PIECES, kv = p / LPR & 1, c = p % LPR;
             if (src[k] >= 0) v[i] = __ldcs(reinterpret_cast<const uint4*>(a.pc.data + (src[k] + kv * v_step) * RB) + c);
         }
-        if (MB > 0 && src[mk] >= 0) {
-            const uint8_t* at = a.pc.scale + (src[mk] + mkv * v_step) * MB;
-            meta = MB == 2 ? *reinterpret_cast<const uint16_t*>(at) : *reinterpret_cast<const uint32_t*>(at);
+#pragma unroll
+        for (int i = 0; i < METAS; ++i) {
+            const int p = i * KP_THREADS + threadIdx.x, k = p >> 1;
+            meta[i] = 0;
+            if (MB > 0 && k < KP_TILE && src[k] >= 0) {
+                const uint8_t* at = a.pc.scale + (src[k] + (p & 1) * v_step) * MB;
+                meta[i] = MB == 2 ? *reinterpret_cast<const uint16_t*>(at) : *reinterpret_cast<const uint32_t*>(at);
+            }
         }
         if (IN_PLACE) __syncthreads();                           // all of the tile is read
 #pragma unroll
@@ -212,10 +260,14 @@ k_paged_keep(KpArgs a, int row_blocks) {
             const int p = i * KP_THREADS + threadIdx.x, k = p / PIECES, kv = p / LPR & 1, c = p % LPR;
             if (src[k] >= 0) __stcs(reinterpret_cast<uint4*>(a.pc.data + (dst[k] + kv * v_step) * RB) + c, v[i]);
         }
-        if (MB > 0 && src[mk] >= 0) {
-            uint8_t* at = a.pc.scale + (dst[mk] + mkv * v_step) * MB;
-            if (MB == 2) *reinterpret_cast<uint16_t*>(at) = (uint16_t)meta;
-            else *reinterpret_cast<uint32_t*>(at) = meta;
+#pragma unroll
+        for (int i = 0; i < METAS; ++i) {
+            const int p = i * KP_THREADS + threadIdx.x, k = p >> 1;
+            if (MB > 0 && k < KP_TILE && src[k] >= 0) {
+                uint8_t* at = a.pc.scale + (dst[k] + (p & 1) * v_step) * MB;
+                if (MB == 2) *reinterpret_cast<uint16_t*>(at) = (uint16_t)meta[i];
+                else *reinterpret_cast<uint32_t*>(at) = meta[i];
+            }
         }
         __syncthreads();                                         // the slots are used up
     }
@@ -223,7 +275,8 @@ k_paged_keep(KpArgs a, int row_blocks) {
 
 template <int FMT, int D, bool IN_PLACE>
 int launch_keep(salicache_ctx* c, const KpArgs& a, cudaStream_t st) {
-    const int tiles = (a.keep_width + KP_TILE - 1) / KP_TILE, lists = a.from.n_seqs * a.pc.heads;
+    constexpr int TILE = kp_tile<FMT, D, IN_PLACE>();
+    const int tiles = (a.keep_width + TILE - 1) / TILE, lists = a.from.n_seqs * a.pc.heads;
     const int row_blocks = IN_PLACE ? 1 : tiles;
     const dim3 grid((unsigned)(row_blocks + (a.w_in ? 1 : 0)), (unsigned)lists);
     SC_CHECK(pt_launch(k_paged_keep<FMT, D, IN_PLACE>, grid, KP_THREADS, 0, st, a, row_blocks));
@@ -246,8 +299,10 @@ int keep_format(salicache_ctx* c, const KpArgs& a, int format, bool in_place, cu
 
 int sc_select_heavy(salicache_ctx* c, const float* d_weight, int64_t weight_stride, int heads, int n_seqs, const int32_t* d_len,
                     int budget, int sinks, int recent, int32_t* d_keep, int32_t* d_kept, cudaStream_t st) {
-    SC_CHECK(pt_launch(k_select_heavy, dim3((unsigned)(n_seqs * heads)), SH_THREADS, 0, st, d_weight, (long long)weight_stride, heads,
-                       (const int*)d_len, budget, sinks, recent, (int*)d_keep, (int*)d_kept, c->d_status));
+    const int held = (int)min(weight_stride, (int64_t)SH_KEYS);
+    SC_CHECK(cudaFuncSetAttribute(k_select_heavy, cudaFuncAttributeMaxDynamicSharedMemorySize, SH_KEYS * 4));
+    SC_CHECK(pt_launch(k_select_heavy, dim3((unsigned)(n_seqs * heads)), SH_THREADS, (size_t)held * 4, st, d_weight, (long long)weight_stride, heads,
+                       (const int*)d_len, budget, sinks, recent, (int*)d_keep, (int*)d_kept, c->d_status, held));
     c->launches++;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;
