@@ -23,16 +23,36 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-constexpr int SH_BINS = 2048, SH_KEYS = 53 * 1024;               // keys that shared memory holds at most
+constexpr int SH_BINS = 2048, SH_KEYS = 49 * 1024;               // keys that shared memory holds at most
 
-// `held`: keys of a list that the block's shared memory holds; those behind are read again in every pass.
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A word of another block's shared memory.
+__device__ __forceinline__ uint32_t ld_peer(const uint32_t* p, uint32_t rank) {
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// A block per (sequence, head), or a cluster of two with half of the positions each.  `held`: keys of a part that the block's
+// shared memory holds; those behind are read again in every pass.
+template <int BLOCKS>
 __global__ void __launch_bounds__(SH_THREADS)
 k_select_heavy(const float* weight, long long stride, int heads, const int* len_, int budget, int sinks, int recent, int* keep, int* kept,
                int* status, int held) {
     extern __shared__ uint32_t keys[];
-    __shared__ uint32_t hist[SH_BINS], warp_sum[SH_WARPS][2];
+    __shared__ uint32_t hist[3][SH_BINS], warp_sum[SH_WARPS][2], part_sum[2];
     __shared__ uint32_t s_digit, s_left;
-    const int b = blockIdx.x / heads, h = blockIdx.x % heads, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const int rank = BLOCKS > 1 ? (int)cluster_rank() : 0;
+    const int list = blockIdx.x / BLOCKS, b = list / heads, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const uint32_t before = (1u << lane) - 1u;
     grid_wait();
     grid_release();
@@ -41,26 +61,33 @@ k_select_heavy(const float* weight, long long stride, int heads, const int* len_
         len = (int)stride;
         if (tid == 0) atomicMin(status, SALICACHE_E_CAPACITY);
     }
-    const float* w = weight + (size_t)blockIdx.x * stride;
-    int* out = keep + (size_t)blockIdx.x * budget;
-    if (h == 0 && tid == 0) kept[b] = min(len, budget);
-    if (len <= budget) {
-        for (int i = tid; i < budget; i += SH_THREADS) out[i] = i < len ? i : -1;
+    int* out = keep + (size_t)list * budget;
+    if (list % heads == 0 && rank == 0 && tid == 0) kept[b] = min(len, budget);
+    constexpr int each = BLOCKS * SH_THREADS;
+    const int me = rank * SH_THREADS + tid;
+    auto sync_all = [&]() {
+        if (BLOCKS > 1) cluster_sync();
+        else __syncthreads();
+    };
+    if (len <= budget) {                     // the same for all blocks of the cluster, as is what follows
+        for (int i = me; i < budget; i += each) out[i] = i < len ? i : -1;
         return;
     }
-    for (int i = tid; i < sinks; i += SH_THREADS) out[i] = i;
-    for (int i = tid; i < recent; i += SH_THREADS) out[budget - recent + i] = len - recent + i;
-    const int n = len - recent - sinks, take = budget - sinks - recent;      // of positions sinks .. sinks + n - 1, in this order
+    for (int i = me; i < sinks; i += each) out[i] = i;
+    for (int i = me; i < recent; i += each) out[budget - recent + i] = len - recent + i;
+    const int take = budget - sinks - recent, all = len - recent - sinks;
     if (take == 0) return;
-    w += sinks;
+    // of positions sinks .. sinks + all - 1 this block has n from `from` on
+    const int part = ((all + BLOCKS - 1) / BLOCKS + 31) / 32 * 32, from = min(all, rank * part), n = min(part, all - from);
+    const float* w = weight + (size_t)list * stride + sinks + from;
     auto key = [&](int i) -> uint32_t { return i < held ? keys[i] : weight_key(w[i]); };
+    for (int i = tid; i < 3 * SH_BINS; i += SH_THREADS) hist[0][i] = 0;
+    __syncthreads();
     // the take-th heaviest: its key's bits from the top, 11, 11 and 10 of them
     uint32_t prefix = 0, left = (uint32_t)take;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int i = tid; i < SH_BINS; i += SH_THREADS) hist[i] = 0;
-        __syncthreads();
         if (pass == 0) {
             constexpr int E = 8;             // loads under way
             for (int i0 = wid * 32; i0 < n; i0 += E * SH_THREADS) {
@@ -75,21 +102,25 @@ k_select_heavy(const float* weight, long long stride, int heads, const int* len_
                     const int i = i0 + e * SH_THREADS + lane;
                     if (i < n) {
                         if (i < held) keys[i] = k[e];
-                        atomicAdd(&hist[k[e] >> shift], 1u);
+                        atomicAdd(&hist[0][k[e] >> shift], 1u);
                     }
                 }
             }
         } else {
             auto count = [&](uint32_t k) {
-                if (k >> (shift + bits) == prefix >> (shift + bits)) atomicAdd(&hist[k >> shift & ((1u << bits) - 1u)], 1u);
+                if (k >> (shift + bits) == prefix >> (shift + bits)) atomicAdd(&hist[pass][k >> shift & ((1u << bits) - 1u)], 1u);
             };
 #pragma unroll 8
             for (int i = tid; i < min(n, held); i += SH_THREADS) count(keys[i]);
             for (int i = (held - tid + SH_THREADS - 1) / SH_THREADS * SH_THREADS + tid; i < n; i += SH_THREADS) count(weight_key(w[i]));
         }
-        __syncthreads();
-        // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t
-        const uint32_t c0 = hist[SH_BINS - 1 - 2 * tid], c1 = hist[SH_BINS - 2 - 2 * tid];
+        sync_all();
+        // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t of all blocks
+        uint32_t c0 = hist[pass][SH_BINS - 1 - 2 * tid], c1 = hist[pass][SH_BINS - 2 - 2 * tid];
+        if (BLOCKS > 1) {
+            c0 += ld_peer(&hist[pass][SH_BINS - 1 - 2 * tid], rank ^ 1);
+            c1 += ld_peer(&hist[pass][SH_BINS - 2 - 2 * tid], rank ^ 1);
+        }
         uint32_t incl = c0 + c1;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -125,13 +156,27 @@ k_select_heavy(const float* weight, long long stride, int heads, const int* len_
         }
     n_above = __reduce_add_sync(0xffffffffu, n_above);
     n_equal = __reduce_add_sync(0xffffffffu, n_equal);
+    __syncthreads();                         // the sums of the last scan have been read
     if (lane == 0) {
         warp_sum[wid][0] = n_above;
         warp_sum[wid][1] = n_equal;
     }
     __syncthreads();
+    if (wid == 0) {
+        const uint32_t x = __reduce_add_sync(0xffffffffu, warp_sum[lane][0]), y = __reduce_add_sync(0xffffffffu, warp_sum[lane][1]);
+        if (lane == 0) {
+            part_sum[0] = x;
+            part_sum[1] = y;
+        }
+    }
     uint32_t above = __reduce_add_sync(0xffffffffu, lane < wid ? warp_sum[lane][0] : 0u);
     uint32_t equal = __reduce_add_sync(0xffffffffu, lane < wid ? warp_sum[lane][1] : 0u);
+    sync_all();
+    for (int r = 0; r < rank; ++r) {
+        above += ld_peer(&part_sum[0], r);
+        equal += ld_peer(&part_sum[1], r);
+    }
+    sync_all();                              // nobody reads another block's memory any more
     constexpr int E = 4;                     // times 32 positions at a time
     for (int i0 = a; i0 < e; i0 += 32 * E) {
         uint32_t is_above[E], is_equal[E];
@@ -146,7 +191,7 @@ k_select_heavy(const float* weight, long long stride, int heads, const int* len_
         for (int x = 0; x < E; ++x) {
             const uint32_t eq = equal + __popc(is_equal[x] & before);
             const bool mine = is_above[x] >> lane & 1u || (is_equal[x] >> lane & 1u && eq < left);
-            if (mine) out[sinks + above + __popc(is_above[x] & before) + min(eq, left)] = sinks + i0 + 32 * x + lane;
+            if (mine) out[sinks + above + __popc(is_above[x] & before) + min(eq, left)] = sinks + from + i0 + 32 * x + lane;
             above += __popc(is_above[x]);
             equal += __popc(is_equal[x]);
         }
@@ -299,10 +344,27 @@ int keep_format(salicache_ctx* c, const KpArgs& a, int format, bool in_place, cu
 
 int sc_select_heavy(salicache_ctx* c, const float* d_weight, int64_t weight_stride, int heads, int n_seqs, const int32_t* d_len,
                     int budget, int sinks, int recent, int32_t* d_keep, int32_t* d_kept, cudaStream_t st) {
-    const int held = (int)min(weight_stride, (int64_t)SH_KEYS);
-    SC_CHECK(cudaFuncSetAttribute(k_select_heavy, cudaFuncAttributeMaxDynamicSharedMemorySize, SH_KEYS * 4));
-    SC_CHECK(pt_launch(k_select_heavy, dim3((unsigned)(n_seqs * heads)), SH_THREADS, (size_t)held * 4, st, d_weight, (long long)weight_stride, heads,
-                       (const int*)d_len, budget, sinks, recent, (int*)d_keep, (int*)d_kept, c->d_status, held));
+    // Two blocks where every one finds an SM and has 4096 positions at least: 32 lists of 32768 17.6 us instead of 22.6, while
+    // a cluster's launch costs short lists 2 us.  (Clusters of four: 21 us; not all of them find their place at once.)
+    const int blocks = (long long)n_seqs * heads * 2 <= c->sm_count && weight_stride >= 2 * 4096 ? 2 : 1;
+    const int held = (int)min((weight_stride + blocks - 1) / blocks + 32, (int64_t)SH_KEYS);
+    auto kernel = blocks == 2 ? k_select_heavy<2> : k_select_heavy<1>;
+    SC_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SH_KEYS * 4));
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(n_seqs * heads * blocks));
+    cfg.blockDim = dim3(SH_THREADS);
+    cfg.dynamicSmemBytes = (size_t)held * 4;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = blocks;
+    SC_CHECK(cudaLaunchKernelEx(&cfg, kernel, d_weight, (long long)weight_stride, heads, (const int*)d_len, budget, sinks, recent,
+                                (int*)d_keep, (int*)d_kept, c->d_status, held));
     c->launches++;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;
