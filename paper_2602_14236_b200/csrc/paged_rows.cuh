@@ -19,39 +19,43 @@ struct RowMap {
     int slot[ROWS];       // -2: the row belongs to no sequence
 };
 
-// Sequence of row r = number of sequences that end at or before it (d_row_start is non-decreasing).
+// Sequence of row r = number of sequences that end at or before it (d_row_start is non-decreasing).  A warp has ROWS / WARPS
+// rows, whose look-ups go side by side: three dependent loads for all of them (one row after the other: 10.6 us instead of
+// 7.5 for writing prompts of 5864 rows).
 template <int ROWS>
 __device__ __forceinline__ void map_rows(RowMap<ROWS>& m, const PgSeqs& sq, const PgCache& pc, int r0, int* status) {
-    constexpr int WARPS = PM_THREADS / 32;
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    for (int i = wid; i < ROWS; i += WARPS) {
-        const int r = r0 + i;
-        int b = 0;
-        for (int base = 0; base < sq.n_seqs; base += 32) {
-            const int k = base + lane;
-            const bool before = k < sq.n_seqs && sq.start[k + 1] <= r;
-            b += __popc(__ballot_sync(0xffffffffu, before));
+    constexpr int WARPS = PM_THREADS / 32, EACH = ROWS / WARPS;
+    static_assert(EACH >= 1 && EACH * WARPS == ROWS, "rows of a warp");
+    const int lane = threadIdx.x & 31, i0 = (threadIdx.x >> 5) * EACH;
+    int b = 0;                               // of this lane's row, i0 + lane
+    for (int base = 0; base < sq.n_seqs; base += 32) {
+        const int k = base + lane, end = k < sq.n_seqs ? sq.start[k + 1] : 0;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int n = __popc(__ballot_sync(0xffffffffu, k < sq.n_seqs && end <= r0 + i0 + e));
+            if (lane == e) b += n;
         }
-        if (lane == 0) {
-            int pid = -1, slot = -2;
-            if (r < sq.n_rows && b < sq.n_seqs) {
-                const PgSeq s = pg_seq(sq, pc, b);
-                const int pos = s.pos0 + (r - s.row0);
-                if (r >= s.row0 && r < s.row0 + s.n) {
-                    slot = -1;
-                    if (pos >= 0) {
-                        if (pos < s.len) pid = sq.table[(size_t)b * sq.width + (pos >> pc.page_shift)];
-                        if (pid >= 0 && pid < pc.n_pages) slot = pos & ((1 << pc.page_shift) - 1);
-                        else {
-                            pid = -1;
-                            atomicMin(status, SALICACHE_E_CAPACITY);
-                        }
+    }
+    if (lane < EACH) {
+        const int i = i0 + lane, r = r0 + i;
+        int pid = -1, slot = -2;
+        if (r < sq.n_rows && b < sq.n_seqs) {
+            const PgSeq s = pg_seq(sq, pc, b);
+            const int pos = s.pos0 + (r - s.row0);
+            if (r >= s.row0 && r < s.row0 + s.n) {
+                slot = -1;
+                if (pos >= 0) {
+                    if (pos < s.len) pid = sq.table[(size_t)b * sq.width + (pos >> pc.page_shift)];
+                    if (pid >= 0 && pid < pc.n_pages) slot = pos & ((1 << pc.page_shift) - 1);
+                    else {
+                        pid = -1;
+                        atomicMin(status, SALICACHE_E_CAPACITY);
                     }
                 }
             }
-            m.pid[i] = pid;
-            m.slot[i] = slot;
         }
+        m.pid[i] = pid;
+        m.slot[i] = slot;
     }
 }
 
