@@ -26,7 +26,7 @@ namespace {
 constexpr int WM_KEYS = 256, WM_K = 2, WM_Q = 3;
 // Which of eight columns take their exponentials on the FMA pipe instead of the special-function unit.
 #ifndef WM_POLY
-#define WM_POLY 0x11
+#define WM_POLY 0x01
 #endif
 // An item's fixed cost (its keys) in tiles' time.
 constexpr int WM_ITEM = 2;
