@@ -523,7 +523,8 @@ typedef struct salicache_rotary {
  *            the positions that the sequences' tables go by (the visual tokens of a frame share their position in time)
  *   d_q      DEVICE [n_rows] rows of [heads * q_per_kv][head_dim], q_stride elements from row to row (>= the row's width, a
  *            multiple of 8), or NULL: no q, and q_per_kv, q_stride, d_q_out and q_out_stride are not looked at
- *   d_q_out  the turned rows, q_out_stride elements apart; may be d_q with the same stride, else the two do not overlap.
+ *   d_q_out  the turned rows, q_out_stride elements apart; may be d_q with the same stride, else the two do not overlap, and
+ *            in no case are they rows of d_K or d_V.
  *            Rows of no sequence are left as they are; rows in no page are turned all the same.
  * pages, seqs, d_K, d_V, strides and errors as for salicache_paged_write; q_per_kv 1 .. 64.  E_NULL also for d_pos and
  * rotary, E_PARAM for what the struct does not allow, E_ALIGN for d_pos off a 4-byte boundary.
@@ -567,7 +568,7 @@ SALICACHE_API int salicache_paged_attend_tree(salicache_ctx* ctx, const salicach
  *   d_weight_out  the same shape, written below d_len[b]; may be d_weight_in, else the two do not overlap
  *   decay         0 .. 1: 1 adds up over all calls, less forgets older ones
  * Positions in no page gain nothing (deferred E_CAPACITY); positions at or past weight_stride are left out (deferred
- * E_CAPACITY).  To weigh by the last m rows of a prompt only, let d_row_start name those m: the positions before them then
+ * E_CAPACITY).  A position's sum below 1e-33 may count as 0.  To weigh by the last m rows of a prompt only, let d_row_start name those m: the positions before them then
  * have to hold their weights, or zeros.  A row's -infinity in d_lse (it sees nothing) counts as no row.
  * q, pages, seqs, d_work and errors as for salicache_paged_attend; E_PARAM also for a decay outside [0, 1], E_SHAPE for
  * weight_stride < 1.

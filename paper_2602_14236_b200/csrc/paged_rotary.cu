@@ -192,9 +192,9 @@ int sc_paged_write_rotary(salicache_ctx* c, const salicache_pages* pg, const sal
     a.rt.n_axes = rotary->n_axes;
     for (int i = 0; i < rotary->pairs; ++i) {
         // whole turns go; what is left of a double has 53 bits, of which the fraction loses none above 2^-62 turns
-        const long double turns = (long double)rotary->freq[i] / 6.283185307179586476925286766559005768L, part = turns - floorl(turns);
-        const long double scaled = roundl(part * 0x1p64L);
-        a.rt.f[i] = ((scaled >= 0x1p64L ? 0ull : (uint64_t)scaled) & ~3ull) | rotary->axis[i];
+        long double part = (long double)rotary->freq[i] * 0.159154943091895335768883763372514362L;
+        if (!(part >= 0.0L && part < 1.0L)) part -= floorl(part);
+        a.rt.f[i] = ((part < 1.0L ? (uint64_t)(part * 0x1p64L) : 0ull) & ~3ull) | rotary->axis[i];
     }
     a.pos = d_pos;
     a.q = (const uint16_t*)d_q;

@@ -169,15 +169,15 @@ struct WmSeg {
 
 // 2^x without the special-function unit, to 2.2e-7: x = n + f, n the nearest integer, which 1.5 * 2^23 + x holds in its low bits;
 // a polynomial of degree 5 for 2^f on [-1/2, 1/2] (least largest relative error, by the Remez exchange); n goes into the
-// exponent.  Below -126 the result is some number below 2^-126; above 127 it is not right.
+// exponent.  Below -126 the result is some number below 2^-126, from 128 on infinity; what is no number stays none.
 __device__ __forceinline__ float ex2_fma(float x) {
-    const float y = fmaxf(x, -127.0f), t = y + 12582912.0f, f = y - (t - 12582912.0f);
+    const float y = fminf(fmaxf(x, -127.0f), 128.0f), t = y + 12582912.0f, f = y - (t - 12582912.0f);
     float p = fmaf(0x1.5c08e6p-10f, f, 0x1.3d0c52p-7f);
     p = fmaf(p, f, 0x1.c6b6e4p-5f);
     p = fmaf(p, f, 0x1.ebf918p-3f);
     p = fmaf(p, f, 0x1.62e428p-1f);
     p = fmaf(p, f, 0x1.000002p+0f);
-    return __uint_as_float((__float_as_uint(t) << 23) + __float_as_uint(p));
+    return x == x ? __uint_as_float((__float_as_uint(t) << 23) + __float_as_uint(p)) : x;
 }
 
 __device__ __forceinline__ uint64_t pair2(float lo, float hi) {
