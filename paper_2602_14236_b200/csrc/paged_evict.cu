@@ -349,7 +349,8 @@ int sc_select_heavy(salicache_ctx* c, const float* d_weight, int64_t weight_stri
     const int blocks = (long long)n_seqs * heads * 2 <= c->sm_count && weight_stride >= 2 * 4096 ? 2 : 1;
     const int held = (int)min((weight_stride + blocks - 1) / blocks + 32, (int64_t)SH_KEYS);
     auto kernel = blocks == 2 ? k_select_heavy<2> : k_select_heavy<1>;
-    SC_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SH_KEYS * 4));
+    // 48 KB, of which the counts take half, need no leave
+    if (held > 5 * 1024) SC_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SH_KEYS * 4));
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at[2]{};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
