@@ -4,11 +4,14 @@
 // those between.  One block per (sequence, head) finds the weight of the last one that fits by its bits, 11, 11 and 10 of them
 // from the top (floats become unsigned numbers in the same order), counting in shared memory, where the keys stay too; then it
 // writes the positions above that weight, and the lowest ones at it, in ascending order: every warp has a stretch of positions,
-// whose counts are summed before the second look.
+// whose counts are summed before the second look.  Bound by the latency of its passes: 24 lists of 640 positions 5.2 us, 64 of
+// up to 8640 9.8 us, 32 of up to 32768 17 us (a third of it the first look, at 50 bytes a clock and with counts that meet).
 //
 // Moving.  A block has the rows that a tile of a list's entries names, K and V of one head, 16 bytes a lane.  Into other pages all
 // tiles of a list move at once.  In place one block takes a list's tiles in turn, and reads a tile before it writes it: entry
 // k of an ascending list is at least first + k, so what a tile writes lies below all that later tiles read.
+// Bound by memory: 32768 rows of 8 heads x 128 in 16 bits, 268 MB: 45 to 49 us = 5.5 to 6.0 TB/s, 0.86 to 0.93 of the copy
+// bandwidth; 31127 rows of INT4 codes, 68 MB: 14 us.
 #include "paged_async.cuh"
 #include "paged.cuh"
 

@@ -14,6 +14,14 @@
 //   5      one thread issues the matrix instructions; one warp feeds K of 16-bit pages and the rows of q by tensor copies, another
 //          one the rows' sums
 // K is double-buffered, and read once per item; the rows of q come once per tile, from the L2.
+//
+// Measured: a prompt of 8192 rows, 32 query and 8 key/value heads x 128: 290 us, 330 us once the clocks have settled under load,
+// = 830 to 950 TFLOP/s of the products.  A tile takes 2200 clocks: 2048 its 32768 exponentials would take on the special-function unit
+// alone (69 % of it used, an eighth of them being elsewhere), 1024 the products (39 % of the tensor pipe).  Tried: 8 warps for the
+// weights, which wait for the tensor memory at the same time (361 us with three stages of rows, 513 with two), two keys a thread
+// (424), both halves of the warps on every tile (368).  A sequence's few rows over a long cache (64 to 256 of them over 8000
+// positions) cost an item's fixed 3 us, over codes 5, per 256 keys.
+//
 // An item that the ends of blocks' stretches cut leaves partial sums, which a second kernel adds in the order of the blocks.
 #include <math.h>
 #include <type_traits>

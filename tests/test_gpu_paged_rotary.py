@@ -1,9 +1,9 @@
 """GPU tests of rows that are turned by their positions on their way into the pages, against a plain form with 64-bit angles.
 
-Bounds: the angle is right to 2^-25 of half a turn (its 32-bit fraction goes through binary32), 2^-32 turns (what is cut off)
-and cosine and sine to 2 units in the last place, 2^-23, so that both are off by at most pi 2^-25 + 2^-23 + 2^-29 < 2.2e-7;
-one product and one fused step in binary32 add 2^-23 (|a| + |b|): together 3.4e-7 (|a| + |b|), and then the rounding to the
-16-bit type, half a step of the value, or of f16's subnormals."""
+Bounds: the angle is right to 2^-27 half turns (within a quarter of a half turn it goes through binary32) and 2^-32 turns (what
+is cut off), cosine and sine to 2 units in the last place, 2^-23, so that both are off by at most pi 2^-27 + pi 2^-31 + 2^-23 <
+1.5e-7; one product and one fused step in binary32 add 2^-23 (|a| + |b|): together 2.7e-7 (|a| + |b|), and then the rounding to
+the 16-bit type, half a step of the value, or of f16's subnormals."""
 import numpy as np
 import pytest
 
@@ -33,7 +33,7 @@ def turned(x, pos, freq, axis, pairing, t):
     a, b = x[..., one], x[..., two]
     y, tol = x.copy(), np.zeros_like(x)
     y[..., one], y[..., two] = a * np.cos(phi) - b * np.sin(phi), b * np.cos(phi) + a * np.sin(phi)
-    off = 3.4e-7 * (np.abs(a) + np.abs(b))
+    off = 2.7e-7 * (np.abs(a) + np.abs(b))
     for s in (one, two):
         tol[..., s] = off + pu.eps(t) / 2 * (np.abs(y[..., s]) + off) + (2.0 ** -25 if pu.eps(t) < 2e-3 else 0.0)
     return y, tol
