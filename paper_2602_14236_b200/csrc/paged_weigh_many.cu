@@ -20,7 +20,8 @@
 // alone (69 % of it used, an eighth of them being elsewhere), 1024 the products (39 % of the tensor pipe).  Tried: 8 warps for the
 // weights, which wait for the tensor memory at the same time (361 us with three stages of rows, 513 with two), two keys a thread
 // (424), both halves of the warps on every tile (368).  A sequence's few rows over a long cache (64 to 256 of them over 8000
-// positions) cost an item's fixed 3 us, over codes 5, per 256 keys.
+// positions) cost an item's fixed time per 256 keys: 2.7 us over 16-bit pages, 4.5 over codes, of which each role's walk and waits are more
+// than half.
 //
 // An item that the ends of blocks' stretches cut leaves partial sums, which a second kernel adds in the order of the blocks.
 #include <math.h>
@@ -43,6 +44,7 @@ struct WmWalk {
     long long left;                          // units still to do
     int b, h, kt, k;                         // sequence, head, tile of keys, unit within the item
     PgSeq s;
+    int held, rows;                          // its positions with a weight, and tiles of rows
 };
 // Tiles of the sequence's rows, and the first one that sees some key from j0 on.  A tile has `tok` whole tokens, by which a
 // product with 2^38 / tok rounded up divides: x is at most a call's tokens, below 2^30 / G, and tok = 128 / G rounded down, so
@@ -80,6 +82,10 @@ __device__ __forceinline__ long long wm_per_head(const WgArgs& a, const PgSeq& s
     }
     return w;
 }
+__device__ __forceinline__ void wm_enter(WmWalk& w, const WgArgs& a) {
+    w.held = wg_held(w.s, a);
+    w.rows = wm_rows(w.s, a);
+}
 // Where the block starts; the same for every thread, each warp for itself.
 __device__ __noinline__ WmWalk wm_start(const WgArgs& a, int block, int blocks) {
     const int lane = threadIdx.x & 31;
@@ -105,6 +111,7 @@ __device__ __noinline__ WmWalk wm_start(const WgArgs& a, int block, int blocks) 
         if (!hit) continue;
         const int from = __ffs(hit) - 1;
         w.s = pt_seq_of(s, from);
+        wm_enter(w, a);
         w.b = b0 + from;
         w.left = end - beg;
         const long long at = __shfl_sync(0xffffffffu, beg - (incl - n), from), per = __shfl_sync(0xffffffffu, n, from) / a.pc.heads;
@@ -134,9 +141,8 @@ __device__ __noinline__ WmWalk wm_start(const WgArgs& a, int block, int blocks) 
     w.left = 0;
     return w;
 }
+// On to another head.
 __device__ __noinline__ WmWalk wm_after(const WgArgs& a, WmWalk w) {
-    w.k = 0;
-    if (++w.kt < wm_items(w.s, a)) return w;
     w.kt = 0;
     if (++w.h < a.pc.heads) return w;
     w.h = 0;
@@ -145,17 +151,23 @@ __device__ __noinline__ WmWalk wm_after(const WgArgs& a, WmWalk w) {
         if (++w.b >= a.sq.n_seqs) return w;  // cannot happen while units are left
         w.s = pg_seq(a.sq, a.pc, w.b);
     } while (wm_items(w.s, a) == 0);
+    wm_enter(w, a);
     return w;
+}
+// On to the next item.  The keys after these of the same head need no more than their number: every role walks for itself, and over
+// few rows that is what an item's time goes into (four rows over INT4 pages 137 us with all of it in the function above, 117 so).
+__device__ __forceinline__ void wm_next(WmWalk& w, const WgArgs& a) {
+    w.k = 0;
+    if ((++w.kt) * WM_KEYS >= w.held) w = wm_after(a, w);
 }
 
 // A block's share of one item.
 struct WmSeg {
-    int k0, k1, tiles, rt, j0, held;         // units [k0, k1); tiles of rows from rt on; first key; positions with a weight
+    int k0, k1, tiles, rt, j0;               // units [k0, k1); tiles of rows from rt on; first key
     bool first, last, real;                  // the item begins, ends here; some of its tiles are here
     __device__ __forceinline__ WmSeg(const WgArgs& a, const WmWalk& w) {
         j0 = w.kt * WM_KEYS;
-        held = wg_held(w.s, a);
-        const int f = wm_first(w.s, a, j0), n = wm_rows(w.s, a) - f, units = WM_ITEM + max(1, n);
+        const int f = j0 <= w.s.pos0 ? 0 : wm_first(w.s, a, j0), n = w.rows - f, units = WM_ITEM + max(1, n);
         k0 = w.k;
         k1 = (int)min((long long)units, k0 + w.left);
         const int t0 = max(0, k0 - WM_ITEM), t1 = max(0, k1 - WM_ITEM);
@@ -168,7 +180,7 @@ struct WmSeg {
     // Page of keys 16 grp .. of the item: -2 there are none (or grp > 15), -1 there is no such page.
     __device__ __forceinline__ int page_of(const WgArgs& a, const WmWalk& w, int grp) const {
         const int j = j0 + grp * 16;
-        if (grp > 15 || j >= held) return -2;
+        if (grp > 15 || j >= w.held) return -2;
         const int p = a.sq.table[(size_t)w.b * a.sq.width + (j >> a.pc.page_shift)];
         return p >= 0 && p < a.pc.n_pages ? p : -1;
     }
@@ -277,7 +289,7 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
     auto wait = [&](uint64_t& bar, uint32_t parity) -> bool { return warp_wait_far(smem_u32(&bar), parity, a.wait_limit, gave_up); };
     auto next = [&](const WmSeg& g) {
         w.left -= g.k1 - g.k0;
-        if (w.left > 0) w = wm_after(a, w);
+        if (w.left > 0) wm_next(w, a);
     };
 
     if (wid < 16) {
@@ -286,15 +298,17 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
         const uint32_t S = tmem + 256 * part + 128 * half + ((uint32_t)((wid & 3) * 32) << 16);
         const ulonglong2* const ls = reinterpret_cast<const ulonglong2*>(mem + SM::LSE) + 32 * part;
         float* const other = reinterpret_cast<float*>(mem + SM::OTHER) + key;
-        uint32_t n = 0, n_item = 0;              // tiles, items with tiles so far
+        uint32_t n = 0, n_item = 0, n_two = 0;   // tiles, items with tiles, with two or more of them so far
         bool ok = true;
         while (w.left > 0 && ok) {
             const WmSeg g(a, w);
             if (tid == 0 && (w.s.cut || w.s.len > a.w_stride)) atomicMin(a.status, SALICACHE_E_CAPACITY);
             const int j = g.j0 + key;
             float sum = 0.0f;
-            const bool mine = j < g.held;
-            const float had = part == 0 && mine && g.first && g.last ? wg_had(a, w.s, w.b, w.h, j) : 0.0f;
+            const bool mine = j < w.held;
+            const bool writes = g.tiles > 0 ? (int)((n + g.tiles - 1) & 1) == part : part == 0;        // the group that has the last tile
+            if (writes && mine && a.in)      // what the key had is looked at when the tiles are through: no register holds it until then
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(a.in + ((size_t)w.b * a.pc.heads + w.h) * a.w_stride + j));
             for (int t = 0; t < g.tiles; ++t, ++n) {
                 if ((int)(n & 1) != part) continue;
                 if (!(wait(bars.l_full[part], n >> 1 & 1) && wait(bars.s_full[part][half], n >> 1 & 1))) {
@@ -349,29 +363,33 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                 sum += top < 128.0f ? s_lo + s_hi : top == top ? INFINITY : top;
             }
             if (!ok) break;
+            const float had = writes && mine && g.first && g.last ? wg_had(a, w.s, w.b, w.h, j) : 0.0f;
             if (g.tiles > 0) {
-                // the odd and the even tiles come together
-                if (part == 1) {
-                    if (n_item > 0 && !wait(bars.o_empty, (n_item - 1) & 1)) break;
-                    *other = sum;
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(smem_u32(&bars.o_full));
-                } else {
-                    if (!wait(bars.o_full, n_item & 1)) break;
-                    sum += *other;
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(smem_u32(&bars.o_empty));
-                    // what lies in no page is not a weight, nor is what is left of exponentials of minus infinity
-                    if (!(*(volatile uint32_t*)&bars.pages[n_item & 7] >> (key >> 4) & 1u) || sum < 1e-33f) sum = 0.0f;
+                // the even and the odd tiles come together where the last one was; the other group has been done before it
+                if (g.tiles > 1) {
+                    if (!writes) {
+                        if (n_two > 0 && !wait(bars.o_empty, (n_two - 1) & 1)) break;
+                        *other = sum;
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_u32(&bars.o_full));
+                    } else {
+                        if (!wait(bars.o_full, n_two & 1)) break;
+                        sum += *other;
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_u32(&bars.o_empty));
+                    }
+                    ++n_two;
                 }
+                // what lies in no page is not a weight, nor is what is left of exponentials of minus infinity
+                if (writes && (!(*(volatile uint32_t*)&bars.pages[n_item & 7] >> (key >> 4) & 1u) || sum < 1e-33f)) sum = 0.0f;
                 ++n_item;
             }
-            if (g.real && part == 0) {
+            if (g.real && writes) {
                 if (g.first && g.last) {
                     if (mine) wg_put(a, w.s, w.b, w.h, j, had, sum);
                 } else {
                     a.part[(2 * (size_t)blockIdx.x + (g.first ? 1 : 0)) * WM_KEYS + key] = sum;
-                    if (tid == 0) {
+                    if (key == 0) {
                         if (g.first) {
                             bars.hd[0].y = 1;
                             bars.hd[0].z = w.b;
@@ -382,10 +400,6 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                 }
             }
             next(g);
-        }
-        if (tid == 0) {
-            a.head[2 * blockIdx.x] = bars.hd[0];
-            a.head[2 * blockIdx.x + 1] = bars.hd[1];
         }
     } else if (wid < LAST) {
         // ---------------- codes to operands: 64 keys a warp
@@ -402,7 +416,7 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                 // the next item's pages are looked up meanwhile
                 WmWalk wn = w;
                 wn.left -= g.k1 - g.k0;
-                if (wn.left > 0) wn = wm_after(a, wn);
+                if (wn.left > 0) wm_next(wn, a);
                 const int pid16n = wn.left > 0 ? WmSeg(a, wn).page_of(a, wn, lane) : -2;
                 if (g.tiles > 0) {
                     const uint32_t kb = n_item % WM_K;
@@ -478,7 +492,7 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
             while (w.left > 0 && ok) {
                 const WmSeg g(a, w);
                 const uint32_t kb = n_item % WM_K;
-                const int halves = g.held - g.j0 > 128 ? 2 : 1;
+                const int halves = w.held - g.j0 > 128 ? 2 : 1;
                 if (g.tiles > 0) ok = wait(bars.k_full[kb], n_item / WM_K & 1);
                 for (int t = 0; t < g.tiles && ok; ++t, ++n) {
                     const uint32_t buf = n & 1, st = n % WM_Q;
@@ -558,7 +572,7 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
                 const WmSeg g(a, w);
                 WmWalk wn = w;
                 wn.left -= g.k1 - g.k0;
-                if (wn.left > 0) wn = wm_after(a, wn);
+                if (wn.left > 0) wm_next(wn, a);
                 for (int t = 0; t < g.tiles; ++t, ++n) {
                     const uint32_t st = n % WM_Q, bar = smem_u32(&bars.q_full[st]);
                     if (n >= WM_Q && !wait(bars.q_empty[st], (n / WM_Q - 1) & 1)) {
@@ -631,7 +645,11 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
     }
     tc_before();
     join_roles();
-    if (tid == 0 && *gave_up) atomicMin(a.status, SC_GAVE_UP);
+    if (tid == 0) {
+        a.head[2 * blockIdx.x] = bars.hd[0];
+        a.head[2 * blockIdx.x + 1] = bars.hd[1];
+        if (*gave_up) atomicMin(a.status, SC_GAVE_UP);
+    }
     if (wid == LAST) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
