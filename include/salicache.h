@@ -544,10 +544,11 @@ SALICACHE_API int salicache_paged_write_rotary(salicache_ctx* ctx, const salicac
  * sees under salicache_paged_attend's rule: the number of its bits is its depth in the tree.  The window does not bound
  * what the bits name.  Bits past the sequence's rows mean nothing; rows past 64 * tree_words are named by none.
  *   d_tree   DEVICE u64 [n_rows][tree_words], 8-byte aligned; tree_words 1 .. 16
- * A chain of at most 64 * tree_words rows (row i has bits 0 .. i) without a window gives what salicache_paged_attend gives,
- * bit for bit.  V is finite at all of the call's own positions, and from d_len - n - window + 1 on under a window, whether
- * or not a bit names them; those positions' pages count as touched.  All other arguments, the workspace, the waits and the
- * errors are those of salicache_paged_attend; E_PARAM also for tree_words, E_NULL and E_ALIGN for d_tree.
+ * A chain of at most 64 * tree_words rows (row i has bits 0 .. i) without a window gives what salicache_paged_attend gives, but
+ * for the order in which the parts of a long cache are added up.  V is finite at all of the call's own positions, and from
+ * d_len - n - window + 1 on under a window, whether or not a bit names them; those positions' pages count as touched.  All
+ * other arguments, the workspace, the waits and the errors are those of salicache_paged_attend; E_PARAM also for tree_words,
+ * E_NULL and E_ALIGN for d_tree.
  */
 SALICACHE_API int salicache_paged_attend_tree(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,
                                               const uint64_t* d_tree, int tree_words, const void* d_q, int64_t q_stride,

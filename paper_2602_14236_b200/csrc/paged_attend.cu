@@ -116,6 +116,9 @@ __global__ void __launch_bounds__(ST_THREADS, StSmem<FMT, D, NT>::BLOCKS)
 k_paged_step(PtArgs a, int blocks) {
     using SM = StSmem<FMT, D, NT>;
     constexpr int RT = 8 * NT, KS = D / 16, VS = D / 16, STAGES = SM::STAGES;
+    // Drafts are ragged: beside a long sequence stand short ones, whose items are their fixed cost and little more (one stream of 22478
+    // INT8 positions and five of up to 1231, 16 x 2 heads, 2 to 13 nodes: 66 us, 98 with the cost that single tokens have).
+    constexpr int ITEM = TREE && NT == 2 && FMT == PF_I8 ? 5 : SM::ITEM;
     static_assert(STAGES >= 2, "ring");
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ uint64_t full[STAGES], empty[STAGES], q_full[2], q_empty[2];
@@ -123,7 +126,7 @@ k_paged_step(PtArgs a, int blocks) {
     __shared__ float2 sh_stat[ST_WARPS][ST_ROUND];
     __shared__ PtShared sh_plan;
     __shared__ int sh_gave_up;
-    using Seg = PtSeg<SM::ITEM>;
+    using Seg = PtSeg<ITEM>;
     const uint32_t q_ring = smem_u32(ring) + STAGES * SM::STAGE + SM::ACC;
     float (*sh_acc)[ST_ROUND][D + 4] = reinterpret_cast<float (*)[ST_ROUND][D + 4]>(ring + STAGES * SM::STAGE);
     volatile int* gave_up = &sh_gave_up;
@@ -143,7 +146,7 @@ k_paged_step(PtArgs a, int blocks) {
     }
     grid_wait();
     grid_release();
-    const PtPlace start = pt_start<ST_THREADS, SM::ITEM>(a, c, blocks, sh_plan);
+    const PtPlace start = pt_start<ST_THREADS, ITEM>(a, c, blocks, sh_plan);
     PtWalk w = start.w;
     PgSeq s = start.s;
     __syncthreads();
