@@ -6,13 +6,15 @@
 // and nothing to be joined.  Only K is read.
 //
 // This file's kernel, for few rows per sequence: a warp has 16 keys of one head as the long side of m16n8k16 matrix
-// instructions, rows of q are the columns, 8 at a time.  A lane sums its columns' weights, four lanes join at the end.  Every
+// instructions, rows of q are the columns, 8 at a time (more than 16 only where a batch of as many rows as sequences has them in
+// one).  A lane sums its columns' weights, four lanes join at the end.  Every
 // warp has a ring of its own in shared memory, which its first lanes fill by bulk copies of 16 keys' rows and scales.  All
 // groups of keys stand in one line, of which every warp takes an equal stretch, so that the lengths on the device decide the
 // split, and warps never wait for one another.
 // Measured, 16 sequences of 8000 positions, 8 heads x 128, one token and four query heads a group (four tokens): 16-bit pages 52 us
 // (58) = 5.1 TB/s, bound by memory; INT8 36 us (44), INT4 36 us (45), bound by issue slots: some 320 instructions go into 16 INT4
 // keys of a head, 112 of them turn codes into numbers.
+#include <limits.h>
 #include <math.h>
 
 #include "paged_frags.cuh"
@@ -142,6 +144,8 @@ k_weigh_few(WgArgs a) {
     }
     grid_wait();
     grid_release();
+    static_assert(WG_THREADS == WM_KEYS, "a thread per key of a tile that is joined");
+    if ((int)blockIdx.x < a.join) wg_join(a);
     long long left;
     WgPlace p = wg_start<KEYS>(a, blockIdx.x * WG_WARPS + wid, gridDim.x * WG_WARPS, left);
     __syncthreads();
@@ -302,7 +306,7 @@ int launch_few(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
     SC_CHECK(cudaFuncSetAttribute(k_weigh_few<T, FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::BYTES));
     // no more blocks than there can be groups of keys for: sequences times heads times the table's groups
     const long long most = (long long)a.sq.n_seqs * a.pc.heads * ((((long long)a.sq.width << a.pc.page_shift) + wg_keys<FMT, D>() - 1) / wg_keys<FMT, D>());
-    const int blocks = (int)max(1ll, min((most + WG_WARPS - 1) / WG_WARPS, (long long)c->sm_count * WG_BLOCKS));
+    const int blocks = max(a.join, (int)max(1ll, min((most + WG_WARPS - 1) / WG_WARPS, (long long)c->sm_count * WG_BLOCKS)));
     SC_CHECK(pt_launch(k_weigh_few<T, FMT, D, NT>, dim3((unsigned)blocks), WG_THREADS, R::BYTES, st, a));
     c->launches++;
     SC_CHECK(cudaGetLastError());
@@ -310,7 +314,8 @@ int launch_few(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
 }
 template <typename T, int FMT, int D>
 int few_columns(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
-    return (long long)a.sq.n_rows * a.G > 8ll * a.sq.n_seqs ? launch_few<T, FMT, D, 2>(c, a, st) : launch_few<T, FMT, D, 1>(c, a, st);
+    const bool one = (long long)a.sq.n_rows * a.G <= 8 || (a.G <= 8 && a.sq.n_rows <= a.sq.n_seqs);      // single tokens
+    return one ? launch_few<T, FMT, D, 1>(c, a, st) : launch_few<T, FMT, D, 2>(c, a, st);
 }
 template <typename T, int D>
 int few_format(salicache_ctx* c, const WgArgs& a, int format, cudaStream_t st) {
@@ -338,7 +343,22 @@ int sc_paged_weigh(salicache_ctx* c, const salicache_pages* pg, const salicache_
     a.decay = decay;
     a.status = c->d_status;
     a.wait_limit = c->paged_wait;
-    if ((long long)sq->n_rows * q_per_kv > 16ll * sq->n_seqs) return sc_weigh_many(c, a, pg, (char*)d_work, st);
+    // Rows of q per sequence up to which reading the keys is the work: what two tiles of columns hold.  (16 sequences of 8000 positions, 16
+    // rows each, this kernel against the other: 16-bit pages 58 / 74 us, INT8 44 / 129, INT4 45 / 117; 32 rows 179 / 75, 174 / 129,
+    // 296 / 117.)  Only the device knows how many a sequence has, so each kernel takes its own ones and a batch that may have both
+    // kinds gets both launches, some 5 us more where it turns out not to: single tokens beside a prompt are the usual batch, and
+    // either kernel takes many times as long over the other's.
+    constexpr int FEW = 16;
+    const long long rows = (long long)sq->n_rows * q_per_kv;
+    const bool few = sq->n_seqs > 1 || rows <= FEW, many = rows > FEW && (sq->n_rows > sq->n_seqs || q_per_kv > FEW);
+    a.rows_over = few ? FEW : -1;
+    a.rows_to = INT_MAX;
+    if (many) {
+        const int rc = sc_weigh_many(c, a, pg, (char*)d_work, !few, st);
+        if (rc != SALICACHE_OK || !few) return rc;
+    }
+    a.rows_over = -1;
+    a.rows_to = many ? FEW : INT_MAX;
     if (pg->dtype == SALICACHE_F16)
         return pg->head_dim == 128 ? few_format<TypeF16, 128>(c, a, pg->format, st) : few_format<TypeF16, 64>(c, a, pg->format, st);
     return pg->head_dim == 128 ? few_format<TypeBF16, 128>(c, a, pg->format, st) : few_format<TypeBF16, 64>(c, a, pg->format, st);

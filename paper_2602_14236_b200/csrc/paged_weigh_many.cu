@@ -32,7 +32,7 @@
 
 namespace {
 
-constexpr int WM_KEYS = 256, WM_K = 2, WM_Q = 3;
+constexpr int WM_K = 2, WM_Q = 3;
 // Which of eight columns take their exponentials on the FMA pipe instead of the special-function unit.  A prompt of 8192 rows with
 // none, one, two of them: 314, 290, 298 us; one call after the other, until the clocks have settled: 339, 330, 343.
 constexpr uint32_t WM_POLY = 0x01;
@@ -656,23 +656,14 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
     }
 }
 
-// Joins split items: block c that item whose tail block c of the first kernel left; a thread per key.
 __global__ void __launch_bounds__(WM_KEYS)
-k_weigh_join(WgArgs a, int blocks) {
-    __shared__ int list[PT_MAX_BLOCKS + 1];
+k_weigh_join(WgArgs a) {
     grid_wait();
-    const int4 hd = a.head[2 * blockIdx.x];
-    if (hd.y == 0) return;
-    const int b = hd.z, h = hd.w, j = a.head[2 * blockIdx.x + 1].x * WM_KEYS + threadIdx.x;
-    const int n = pt_records([&](int c) { return a.head[2 * c].x; }, blockIdx.x, blocks, list);
-    const PgSeq s = pg_seq(a.sq, a.pc, b);
-    float sum = 0.0f;
-    for (int i = 0; i < n; ++i) sum += a.part[(size_t)list[i] * WM_KEYS + threadIdx.x];
-    if (j < wg_held(s, a)) wg_put(a, s, b, h, j, wg_had(a, s, b, h, j), sum);
+    wg_join(a);
 }
 
 template <typename T, int FMT, int D>
-int launch_many(salicache_ctx* c, WgArgs a, char* work, cudaStream_t st) {
+int launch_many(salicache_ctx* c, WgArgs& a, char* work, bool join, cudaStream_t st) {
     constexpr int BYTES = WmSmem<D>::BYTES;
     CUtensorMap map{}, q_map{};
     const bool bf16 = T::ONE == TypeBF16::ONE;
@@ -685,22 +676,26 @@ int launch_many(salicache_ctx* c, WgArgs a, char* work, cudaStream_t st) {
     a.part = reinterpret_cast<float*>(work);
     a.head = reinterpret_cast<int4*>(a.part + (size_t)2 * blocks * WM_KEYS);
     SC_CHECK(pt_launch(k_weigh_many<T, FMT, D>, dim3(blocks), wm_threads<FMT>(), BYTES, st, a, map, q_map, blocks));
-    SC_CHECK(pt_launch(k_weigh_join, dim3(blocks), WM_KEYS, 0, st, a, blocks));
-    c->launches += 2;
+    a.join = blocks;
+    c->launches++;
+    if (join) {
+        SC_CHECK(pt_launch(k_weigh_join, dim3(blocks), WM_KEYS, 0, st, a));
+        c->launches++;
+    }
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;
 }
 template <typename T, int D>
-int many_format(salicache_ctx* c, const WgArgs& a, int format, char* work, cudaStream_t st) {
-    if (format == SALICACHE_FP16) return launch_many<T, PF_16, D>(c, a, work, st);
-    if (format == SALICACHE_INT8) return launch_many<T, PF_I8, D>(c, a, work, st);
-    return launch_many<T, PF_I4, D>(c, a, work, st);
+int many_format(salicache_ctx* c, WgArgs& a, int format, char* work, bool join, cudaStream_t st) {
+    if (format == SALICACHE_FP16) return launch_many<T, PF_16, D>(c, a, work, join, st);
+    if (format == SALICACHE_INT8) return launch_many<T, PF_I8, D>(c, a, work, join, st);
+    return launch_many<T, PF_I4, D>(c, a, work, join, st);
 }
 
 }  // namespace
 
-int sc_weigh_many(salicache_ctx* c, const WgArgs& a, const salicache_pages* pg, char* work, cudaStream_t st) {
+int sc_weigh_many(salicache_ctx* c, WgArgs& a, const salicache_pages* pg, char* work, bool join, cudaStream_t st) {
     if (pg->dtype == SALICACHE_F16)
-        return pg->head_dim == 128 ? many_format<TypeF16, 128>(c, a, pg->format, work, st) : many_format<TypeF16, 64>(c, a, pg->format, work, st);
-    return pg->head_dim == 128 ? many_format<TypeBF16, 128>(c, a, pg->format, work, st) : many_format<TypeBF16, 64>(c, a, pg->format, work, st);
+        return pg->head_dim == 128 ? many_format<TypeF16, 128>(c, a, pg->format, work, join, st) : many_format<TypeF16, 64>(c, a, pg->format, work, join, st);
+    return pg->head_dim == 128 ? many_format<TypeBF16, 128>(c, a, pg->format, work, join, st) : many_format<TypeBF16, 64>(c, a, pg->format, work, join, st);
 }

@@ -161,6 +161,21 @@ def test_many_sequences(ctx, fmt, news):
     run(ctx, pu.World(5, fmt, _t("f16"), 1, 64, 16, lens, news), 2)
 
 
+@pytest.mark.parametrize("fmt", ["fp16", "int8", "int4"])
+@pytest.mark.parametrize("heads,G,D,page,lens,news", [
+    (2, 4, 128, 32, [300, 900, 17, 40, 700, 33, 5], [1, 400, 1, 0, 5, 33, 4]),       # single tokens, drafts and prompts
+    (1, 2, 64, 16, [300] * 40, [1] * 20 + [200] + [1] * 19),
+    (1, 1, 128, 64, [90, 500, 64], [0, 3, 0]),                                       # as many rows as sequences, all in one
+    (1, 2, 64, 16, [200, 300, 50, 70], [0, 0, 4, 0]),
+    (1, 40, 64, 16, [200, 30], [1, 1]),                                              # many query heads
+    (1, 12, 64, 16, [200, 30, 60], [2, 1, 0]),
+])
+def test_batches_of_every_kind(ctx, fmt, heads, G, D, page, lens, news):
+    w = pu.World(6, fmt, _t("f16"), heads, D, page, lens, news)
+    run(ctx, w, G)
+    run(ctx, w, G, decay=0.5, alias=True)
+
+
 @pytest.mark.parametrize("layout", [0, 2, 4, 6])
 def test_the_same_bits_on_every_call(ctx, layout):
     import torch
