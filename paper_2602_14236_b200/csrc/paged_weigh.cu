@@ -346,8 +346,10 @@ int sc_paged_weigh(salicache_ctx* c, const salicache_pages* pg, const salicache_
     // Rows of q per sequence up to which reading the keys is the work: what two tiles of columns hold.  (16 sequences of 8000 positions, 16
     // rows each, this kernel against the other: 16-bit pages 58 / 74 us, INT8 44 / 129, INT4 45 / 117; 32 rows 179 / 75, 174 / 129,
     // 296 / 117.)  Only the device knows how many a sequence has, so each kernel takes its own ones and a batch that may have both
-    // kinds gets both launches, some 5 us more where it turns out not to: single tokens beside a prompt are the usual batch, and
-    // either kernel takes many times as long over the other's.
+    // kinds gets both launches: single tokens beside a prompt are the usual batch, and either kernel takes many times as long over
+    // the other's.  (31 single tokens over 8000 INT4 positions and a prompt of 4096: 162 us, 318 in the other kernel alone; 63 over
+    // 4000 INT8 positions and 193 rows over 16000: 131, in this one alone 5098.)  A batch without long sequences pays 12 us for the
+    // launch that finds none (16 of four tokens, 16-bit pages: 64 us, 52).
     constexpr int FEW = 16;
     const long long rows = (long long)sq->n_rows * q_per_kv;
     const bool few = sq->n_seqs > 1 || rows <= FEW, many = rows > FEW && (sq->n_rows > sq->n_seqs || q_per_kv > FEW);

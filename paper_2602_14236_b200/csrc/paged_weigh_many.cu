@@ -23,7 +23,8 @@
 // positions) cost an item's fixed time per 256 keys: 2.7 us over 16-bit pages, 4.5 over codes, of which each role's walk and waits are more
 // than half.
 //
-// An item that the ends of blocks' stretches cut leaves partial sums, which a second kernel adds in the order of the blocks.
+// An item that the ends of blocks' stretches cut leaves partial sums, which the next launch adds in the order of the blocks: that
+// of the few-row kernel, where the batch may have such sequences, or one for this alone.
 #include <math.h>
 #include <type_traits>
 
