@@ -36,6 +36,8 @@ struct WgRing {
     static constexpr int BYTES = WG_WARPS * STAGES * STAGE;
 };
 
+// Positions of a sequence that have a weight; none, if the sequence is the other kernel's.
+__device__ __forceinline__ int wf_held(const PgSeq& s, const WgArgs& a) { return s.n * a.G <= a.rows_to ? wg_held(s, a) : 0; }
 // A group of KEYS keys: its sequence, head and first position.
 struct WgPlace {
     int b, h, k, groups;                     // the k-th of `groups`
@@ -45,7 +47,7 @@ struct WgPlace {
 template <int KEYS>
 __device__ __forceinline__ void wg_enter(WgPlace& p, const WgArgs& a) {
     p.s = pg_seq(a.sq, a.pc, p.b);
-    p.held = wg_held(p.s, a);
+    p.held = wf_held(p.s, a);
     p.groups = (p.held + KEYS - 1) / KEYS;
 }
 template <int KEYS>
@@ -64,7 +66,7 @@ template <int KEYS>
 __device__ __forceinline__ WgPlace wg_start(const WgArgs& a, int warp, int warps, long long& left) {
     const int lane = threadIdx.x & 31;
     auto units = [&](int b) -> long long {
-        return b < a.sq.n_seqs ? (long long)((wg_held(pg_seq(a.sq, a.pc, b), a) + KEYS - 1) / KEYS) * a.pc.heads : 0ll;
+        return b < a.sq.n_seqs ? (long long)((wf_held(pg_seq(a.sq, a.pc, b), a) + KEYS - 1) / KEYS) * a.pc.heads : 0ll;
     };
     long long total = 0;
     const long long mine = units(lane);
@@ -144,8 +146,6 @@ k_weigh_few(WgArgs a) {
     }
     grid_wait();
     grid_release();
-    static_assert(WG_THREADS == WM_KEYS, "a thread per key of a tile that is joined");
-    if ((int)blockIdx.x < a.join) wg_join(a);
     long long left;
     WgPlace p = wg_start<KEYS>(a, blockIdx.x * WG_WARPS + wid, gridDim.x * WG_WARPS, left);
     __syncthreads();
@@ -306,7 +306,7 @@ int launch_few(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
     SC_CHECK(cudaFuncSetAttribute(k_weigh_few<T, FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::BYTES));
     // no more blocks than there can be groups of keys for: sequences times heads times the table's groups
     const long long most = (long long)a.sq.n_seqs * a.pc.heads * ((((long long)a.sq.width << a.pc.page_shift) + wg_keys<FMT, D>() - 1) / wg_keys<FMT, D>());
-    const int blocks = max(a.join, (int)max(1ll, min((most + WG_WARPS - 1) / WG_WARPS, (long long)c->sm_count * WG_BLOCKS)));
+    const int blocks = (int)max(1ll, min((most + WG_WARPS - 1) / WG_WARPS, (long long)c->sm_count * WG_BLOCKS));
     SC_CHECK(pt_launch(k_weigh_few<T, FMT, D, NT>, dim3((unsigned)blocks), WG_THREADS, R::BYTES, st, a));
     c->launches++;
     SC_CHECK(cudaGetLastError());
@@ -347,21 +347,16 @@ int sc_paged_weigh(salicache_ctx* c, const salicache_pages* pg, const salicache_
     // rows each, this kernel against the other: 16-bit pages 58 / 74 us, INT8 44 / 129, INT4 45 / 117; 32 rows 179 / 75, 174 / 129,
     // 296 / 117.)  Only the device knows how many a sequence has, so each kernel takes its own ones and a batch that may have both
     // kinds gets both launches: single tokens beside a prompt are the usual batch, and either kernel takes many times as long over
-    // the other's.  (31 single tokens over 8000 INT4 positions and a prompt of 4096: 162 us, 318 in the other kernel alone; 63 over
-    // 4000 INT8 positions and 193 rows over 16000: 131, in this one alone 5098.)  A batch without long sequences pays 12 us for the
-    // launch that finds none (16 of four tokens, 16-bit pages: 64 us, 52).
-    constexpr int FEW = 16;
-    const long long rows = (long long)sq->n_rows * q_per_kv;
-    const bool few = sq->n_seqs > 1 || rows <= FEW, many = rows > FEW && (sq->n_rows > sq->n_seqs || q_per_kv > FEW);
-    a.rows_over = few ? FEW : -1;
-    a.rows_to = INT_MAX;
-    if (many) {
-        const int rc = sc_weigh_many(c, a, pg, (char*)d_work, !few, st);
-        if (rc != SALICACHE_OK || !few) return rc;
-    }
-    a.rows_over = -1;
-    a.rows_to = many ? FEW : INT_MAX;
+    // the other's.  (31 single tokens over 8000 INT4 positions and a prompt of 4096: 158 us, 318 in the other kernel alone; 63 over
+    // 4000 INT8 positions and 193 rows over 16000: 128, in this one alone 5098.)  A batch without long sequences pays 5 us for
+    // launches that find none (16 of four tokens, 16-bit pages: 57 us, 52).  This kernel goes first: the other one cannot start beside its
+    // rings, and after it, doing the join as well, it added 20 us to a prompt of 8192 rows (313, 290).
+    const bool many = (long long)sq->n_rows * q_per_kv > WG_FEW && (sq->n_rows > sq->n_seqs || q_per_kv > WG_FEW);
+    a.rows_to = many ? WG_FEW : INT_MAX;
+    int rc;
     if (pg->dtype == SALICACHE_F16)
-        return pg->head_dim == 128 ? few_format<TypeF16, 128>(c, a, pg->format, st) : few_format<TypeF16, 64>(c, a, pg->format, st);
-    return pg->head_dim == 128 ? few_format<TypeBF16, 128>(c, a, pg->format, st) : few_format<TypeBF16, 64>(c, a, pg->format, st);
+        rc = pg->head_dim == 128 ? few_format<TypeF16, 128>(c, a, pg->format, st) : few_format<TypeF16, 64>(c, a, pg->format, st);
+    else
+        rc = pg->head_dim == 128 ? few_format<TypeBF16, 128>(c, a, pg->format, st) : few_format<TypeBF16, 64>(c, a, pg->format, st);
+    return rc == SALICACHE_OK && many ? sc_weigh_many(c, a, pg, (char*)d_work, st) : rc;
 }

@@ -23,8 +23,8 @@
 // positions) cost an item's fixed time per 256 keys: 2.7 us over 16-bit pages, 4.5 over codes, of which each role's walk and waits are more
 // than half.
 //
-// An item that the ends of blocks' stretches cut leaves partial sums, which the next launch adds in the order of the blocks: that
-// of the few-row kernel, where the batch may have such sequences, or one for this alone.
+// An item that the ends of blocks' stretches cut leaves partial sums, which a second kernel adds in the
+// order of the blocks.
 #include <math.h>
 #include <type_traits>
 
@@ -33,7 +33,7 @@
 
 namespace {
 
-constexpr int WM_K = 2, WM_Q = 3;
+constexpr int WM_KEYS = 256, WM_K = 2, WM_Q = 3;
 // Which of eight columns take their exponentials on the FMA pipe instead of the special-function unit.  A prompt of 8192 rows with
 // none, one, two of them: 314, 290, 298 us; one call after the other, until the clocks have settled: 339, 330, 343.
 constexpr uint32_t WM_POLY = 0x01;
@@ -53,7 +53,9 @@ struct WmWalk {
 __device__ __forceinline__ int wm_by_tok(int x, const WgArgs& a) { return (int)((uint64_t)x * a.per_tok >> 38); }
 __device__ __forceinline__ int wm_rows(const PgSeq& s, const WgArgs& a) { return wm_by_tok(s.n + a.tok - 1, a); }
 __device__ __forceinline__ int wm_first(const PgSeq& s, const WgArgs& a, int j0) { return wm_by_tok(max(0, j0 - s.pos0), a); }
-__device__ __forceinline__ int wm_items(const PgSeq& s, const WgArgs& a) { return (wg_held(s, a) + WM_KEYS - 1) / WM_KEYS; }
+// Its positions with a weight; none, if the sequence is the other kernel's.
+__device__ __forceinline__ int wm_held(const PgSeq& s, const WgArgs& a) { return s.n * a.G > WG_FEW ? wg_held(s, a) : 0; }
+__device__ __forceinline__ int wm_items(const PgSeq& s, const WgArgs& a) { return (wm_held(s, a) + WM_KEYS - 1) / WM_KEYS; }
 // Units of an item: its fixed cost and its tiles, one at least (a sequence without rows has its weights copied).
 __device__ __forceinline__ int wm_units(const PgSeq& s, const WgArgs& a, int kt) {
     return WM_ITEM + max(1, wm_rows(s, a) - wm_first(s, a, kt * WM_KEYS));
@@ -84,7 +86,7 @@ __device__ __forceinline__ long long wm_per_head(const WgArgs& a, const PgSeq& s
     return w;
 }
 __device__ __forceinline__ void wm_enter(WmWalk& w, const WgArgs& a) {
-    w.held = wg_held(w.s, a);
+    w.held = wm_held(w.s, a);
     w.rows = wm_rows(w.s, a);
 }
 // Where the block starts; the same for every thread, each warp for itself.
@@ -238,7 +240,7 @@ template <int FMT> __host__ __device__ constexpr int wm_threads() { return FMT =
 
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(wm_threads<FMT>(), 1)
-k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map, int blocks) {
+k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map, int blocks) {
     using SM = WmSmem<D>;
     constexpr int WM_THREADS = wm_threads<FMT>(), LAST = WM_THREADS / 32 - 4;           // first warp of the last group
     extern __shared__ __align__(1024) uint8_t mem[];         // the swizzle's atoms; there is no room to align by hand
@@ -657,14 +659,23 @@ k_weigh_many(WgArgs a, const __grid_constant__ CUtensorMap map, const __grid_con
     }
 }
 
+// Joins split items: block c that item whose tail block c of the first kernel left; a thread per key.
 __global__ void __launch_bounds__(WM_KEYS)
-k_weigh_join(WgArgs a) {
+k_weigh_join(WgArgs a, int blocks) {
+    __shared__ int list[PT_MAX_BLOCKS + 1];
     grid_wait();
-    wg_join(a);
+    const int4 hd = a.head[2 * blockIdx.x];
+    if (hd.y == 0) return;
+    const int b = hd.z, h = hd.w, j = a.head[2 * blockIdx.x + 1].x * WM_KEYS + threadIdx.x;
+    const int n = pt_records([&](int c) { return a.head[2 * c].x; }, blockIdx.x, blocks, list);
+    const PgSeq s = pg_seq(a.sq, a.pc, b);
+    float sum = 0.0f;
+    for (int i = 0; i < n; ++i) sum += a.part[(size_t)list[i] * WM_KEYS + threadIdx.x];
+    if (j < wm_held(s, a)) wg_put(a, s, b, h, j, wg_had(a, s, b, h, j), sum);
 }
 
 template <typename T, int FMT, int D>
-int launch_many(salicache_ctx* c, WgArgs& a, char* work, bool join, cudaStream_t st) {
+int launch_many(salicache_ctx* c, WgArgs a, char* work, cudaStream_t st) {
     constexpr int BYTES = WmSmem<D>::BYTES;
     CUtensorMap map{}, q_map{};
     const bool bf16 = T::ONE == TypeBF16::ONE;
@@ -677,26 +688,22 @@ int launch_many(salicache_ctx* c, WgArgs& a, char* work, bool join, cudaStream_t
     a.part = reinterpret_cast<float*>(work);
     a.head = reinterpret_cast<int4*>(a.part + (size_t)2 * blocks * WM_KEYS);
     SC_CHECK(pt_launch(k_weigh_many<T, FMT, D>, dim3(blocks), wm_threads<FMT>(), BYTES, st, a, map, q_map, blocks));
-    a.join = blocks;
-    c->launches++;
-    if (join) {
-        SC_CHECK(pt_launch(k_weigh_join, dim3(blocks), WM_KEYS, 0, st, a));
-        c->launches++;
-    }
+    SC_CHECK(pt_launch(k_weigh_join, dim3(blocks), WM_KEYS, 0, st, a, blocks));
+    c->launches += 2;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;
 }
 template <typename T, int D>
-int many_format(salicache_ctx* c, WgArgs& a, int format, char* work, bool join, cudaStream_t st) {
-    if (format == SALICACHE_FP16) return launch_many<T, PF_16, D>(c, a, work, join, st);
-    if (format == SALICACHE_INT8) return launch_many<T, PF_I8, D>(c, a, work, join, st);
-    return launch_many<T, PF_I4, D>(c, a, work, join, st);
+int many_format(salicache_ctx* c, const WgArgs& a, int format, char* work, cudaStream_t st) {
+    if (format == SALICACHE_FP16) return launch_many<T, PF_16, D>(c, a, work, st);
+    if (format == SALICACHE_INT8) return launch_many<T, PF_I8, D>(c, a, work, st);
+    return launch_many<T, PF_I4, D>(c, a, work, st);
 }
 
 }  // namespace
 
-int sc_weigh_many(salicache_ctx* c, WgArgs& a, const salicache_pages* pg, char* work, bool join, cudaStream_t st) {
+int sc_weigh_many(salicache_ctx* c, const WgArgs& a, const salicache_pages* pg, char* work, cudaStream_t st) {
     if (pg->dtype == SALICACHE_F16)
-        return pg->head_dim == 128 ? many_format<TypeF16, 128>(c, a, pg->format, work, join, st) : many_format<TypeF16, 64>(c, a, pg->format, work, join, st);
-    return pg->head_dim == 128 ? many_format<TypeBF16, 128>(c, a, pg->format, work, join, st) : many_format<TypeBF16, 64>(c, a, pg->format, work, join, st);
+        return pg->head_dim == 128 ? many_format<TypeF16, 128>(c, a, pg->format, work, st) : many_format<TypeF16, 64>(c, a, pg->format, work, st);
+    return pg->head_dim == 128 ? many_format<TypeBF16, 128>(c, a, pg->format, work, st) : many_format<TypeBF16, 64>(c, a, pg->format, work, st);
 }
