@@ -219,33 +219,45 @@ struct KpArgs {
     int* status;
 };
 
-// Weights of one list in tiles of 16 entries a thread, read before they are written, so that they may move in place.
-__device__ void keep_weights(const KpArgs& a, int b, int h, int n, int len, const int* list) {
-    constexpr int E = 16;
+// The pages that position e of sequence b comes from and position t goes to; false: one of them is in no page.
+__device__ __forceinline__ bool kp_pages(const KpArgs& a, int b, int len, int e, long long t, int& from, int& to) {
+    const bool held = e >= 0 && e < len && t < min((long long)a.to.width << a.pc.page_shift, 1ll << 30);
+    from = held ? a.from.table[(size_t)b * a.from.width + (e >> a.pc.page_shift)] : -1;
+    to = held ? a.to.table[(size_t)b * a.to.width + (t >> a.pc.page_shift)] : -1;
+    return from >= 0 && from < a.pc.n_pages && to >= 0 && to < a.pc.n_pages;
+}
+
+// Weights of one list, each where its row moves, in tiles of 8 entries a thread, of which block `first_tile` of `blocks` takes its own.  A
+// tile is read before it is written: one block moves a list's weights in place.
+constexpr int KW_EACH = 8, KW_TILE = KW_EACH * KP_THREADS;
+__device__ void keep_weights(const KpArgs& a, int b, int h, int n, int len, const int* list, int first_tile, int blocks) {
     const long long first = a.first ? max(a.first[b], 0) : 0;
     const size_t row = ((size_t)b * a.pc.heads + h) * a.w_stride;
-    for (int k0 = 0; k0 < n; k0 += E * KP_THREADS) {
-        int src[E];
-        float w[E];
+    for (int k0 = first_tile * KW_TILE; k0 < n; k0 += blocks * KW_TILE) {
+        int src[KW_EACH], p[KW_EACH], q[KW_EACH];
+        float w[KW_EACH];
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
+        for (int i = 0; i < KW_EACH; ++i) {
             const int k = k0 + i * KP_THREADS + threadIdx.x;
             src[i] = k < n ? list[k] : -1;
-            if (src[i] < 0 || src[i] >= len || src[i] >= a.w_stride || first + k >= a.w_stride) src[i] = -1;
+            if (src[i] >= a.w_stride || first + k >= a.w_stride) src[i] = -1;
         }
 #pragma unroll
-        for (int i = 0; i < E; ++i) w[i] = src[i] >= 0 ? a.w_in[row + src[i]] : 0.0f;
+        for (int i = 0; i < KW_EACH; ++i)
+            if (!kp_pages(a, b, len, src[i], first + k0 + i * KP_THREADS + threadIdx.x, p[i], q[i])) src[i] = -1;
+#pragma unroll
+        for (int i = 0; i < KW_EACH; ++i) w[i] = src[i] >= 0 ? a.w_in[row + src[i]] : 0.0f;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < E; ++i)
+        for (int i = 0; i < KW_EACH; ++i)
             if (src[i] >= 0) a.w_out[row + first + k0 + i * KP_THREADS + threadIdx.x] = w[i];
     }
 }
 
-// grid.y: (sequence, head); grid.x: a list's tiles (one block for all of them in place), and one more for the weights.
+// grid.y: (sequence, head); grid.x: blocks for the weights, if they move, then a list's tiles (one block for all of them in place).
 template <int FMT, int D, bool IN_PLACE>
 __global__ void __launch_bounds__(KP_THREADS)
-k_paged_keep(KpArgs a, int row_blocks) {
+k_paged_keep(KpArgs a, int weight_blocks, int row_blocks) {
     constexpr int RB = pg_row_bytes<FMT, D>(), MB = pg_meta_bytes<FMT>(), LPR = RB / 16, PIECES = 2 * LPR;
     constexpr int KP_TILE = kp_tile<FMT, D, IN_PLACE>(), EACH = KP_TILE * PIECES / KP_THREADS;      // 16-byte pieces of a thread
     constexpr int METAS = MB > 0 ? (2 * KP_TILE + KP_THREADS - 1) / KP_THREADS : 1;                 // scales of a thread
@@ -257,27 +269,24 @@ k_paged_keep(KpArgs a, int row_blocks) {
     const long long cap = min((long long)a.from.width << a.pc.page_shift, 1ll << 30);
     const int len = (int)min((long long)max(a.from.len[b], 0), cap);
     const int* list = a.keep + ((size_t)b * a.keep_heads + (a.keep_heads > 1 ? h : 0)) * a.keep_width;
-    if ((int)blockIdx.x == row_blocks) {
-        keep_weights(a, b, h, n, len, list);
+    if ((int)blockIdx.x < weight_blocks) {
+        keep_weights(a, b, h, n, len, list, blockIdx.x, weight_blocks);
         return;
     }
-    const long long to_cap = min((long long)a.to.width << a.pc.page_shift, 1ll << 30), first = a.first ? max(a.first[b], 0) : 0;
+    const long long first = a.first ? max(a.first[b], 0) : 0;
     const int mask = (1 << a.pc.page_shift) - 1;
     const size_t v_step = (size_t)a.pc.heads << a.pc.page_shift;         // slots from K to V
-    for (int k0 = blockIdx.x * KP_TILE; k0 < n; k0 += row_blocks * KP_TILE) {
+    for (int k0 = ((int)blockIdx.x - weight_blocks) * KP_TILE; k0 < n; k0 += row_blocks * KP_TILE) {
         for (int i = threadIdx.x; i < KP_TILE; i += KP_THREADS) {
             const int k = k0 + i;
             long long s = -1, d = -1;
             if (k < n) {
                 const int e = list[k];
                 const long long t = first + k;
-                if (e >= 0 && e < len && t < to_cap) {
-                    const int p = a.from.table[(size_t)b * a.from.width + (e >> a.pc.page_shift)];
-                    const int q = a.to.table[(size_t)b * a.to.width + (t >> a.pc.page_shift)];
-                    if (p >= 0 && p < a.pc.n_pages && q >= 0 && q < a.pc.n_pages) {
-                        s = (long long)pg_slot(a.pc, p, 0, h, e & mask);
-                        d = (long long)pg_slot(a.pc, q, 0, h, (int)t & mask);
-                    }
+                int p, q;
+                if (kp_pages(a, b, len, e, t, p, q)) {
+                    s = (long long)pg_slot(a.pc, p, 0, h, e & mask);
+                    d = (long long)pg_slot(a.pc, q, 0, h, (int)t & mask);
                 }
                 if (s < 0) atomicMin(a.status, SALICACHE_E_CAPACITY);
                 else if (s == d) s = -1;                         // stays where it is
@@ -326,8 +335,9 @@ int launch_keep(salicache_ctx* c, const KpArgs& a, cudaStream_t st) {
     constexpr int TILE = kp_tile<FMT, D, IN_PLACE>();
     const int tiles = (a.keep_width + TILE - 1) / TILE, lists = a.from.n_seqs * a.pc.heads;
     const int row_blocks = IN_PLACE ? 1 : tiles;
-    const dim3 grid((unsigned)(row_blocks + (a.w_in ? 1 : 0)), (unsigned)lists);
-    SC_CHECK(pt_launch(k_paged_keep<FMT, D, IN_PLACE>, grid, KP_THREADS, 0, st, a, row_blocks));
+    const int weight_blocks = !a.w_in ? 0 : a.w_in == a.w_out ? 1 : (a.keep_width + KW_TILE - 1) / KW_TILE;
+    const dim3 grid((unsigned)(weight_blocks + row_blocks), (unsigned)lists);
+    SC_CHECK(pt_launch(k_paged_keep<FMT, D, IN_PLACE>, grid, KP_THREADS, 0, st, a, weight_blocks, row_blocks));
     c->launches++;
     SC_CHECK(cudaGetLastError());
     return SALICACHE_OK;
