@@ -98,7 +98,7 @@ __device__ __forceinline__ WgPlace wg_start(const WgArgs& a, int warp, int warps
 template <int FMT, int D>
 struct Columns {
     uint32_t q[D / 16][2];
-    float lse[2];                            // of rows 8 n + 2 c4 and the next; +inf for what is no row
+    float lse[2];                            // of rows 8 n + 2 c4 and the next; WG_NONE for what is no row
     __device__ __forceinline__ void load(const WgArgs& a, const PgSeq& s, int h, int n, int rows, int g8, int c4) {
         const int rr = 8 * n + g8;
         const uint16_t* src = a.q + (long long)(s.row0 + rr / a.G) * a.q_stride + (long long)(h * a.G + rr % a.G) * D;
@@ -117,10 +117,10 @@ struct Columns {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = 8 * n + 2 * c4 + i;
-            lse[i] = INFINITY;
+            lse[i] = WG_NONE;
             if (r < rows) {
                 const float x = __ldg(a.lse + (long long)(s.row0 + r / a.G) * (a.pc.heads * a.G) + h * a.G + r % a.G);
-                lse[i] = x == -INFINITY ? INFINITY : x * PT_LOG2E;
+                lse[i] = x == -INFINITY ? WG_NONE : x * PT_LOG2E;
             }
         }
     }
@@ -255,8 +255,9 @@ k_weigh_few(WgArgs a) {
                         for (int i = 0; i < 4; ++i)
                             if (s.pos0 + (8 * n + 2 * c4 + (i & 1)) / a.G < j0 + 16 * u + key_of(g8) + 8 * (i >> 1)) w[i] = 0.0f;
                     }
-                    // a column that is no row has q = 0, which a key that is not finite would turn into no number
-                    const bool l0 = 8 * n + 2 * c4 < rows, l1 = 8 * n + 2 * c4 + 1 < rows;
+                    // what is no row gives nothing, whatever its score: q is 0 behind the last row, which a key that is not finite would
+                    // turn into no number, and anything in a row that sees nothing
+                    const bool l0 = x.lse[0] != WG_NONE, l1 = x.lse[1] != WG_NONE;
                     sum[0] += (l0 ? w[0] : 0.0f) + (l1 ? w[1] : 0.0f);
                     sum[1] += (l0 ? w[2] : 0.0f) + (l1 ? w[3] : 0.0f);
                 };

@@ -3,6 +3,7 @@
 #include "paged_plan.cuh"
 
 constexpr int WG_FEW = 16;                   // rows of q of a sequence up to which it is the other kernel's
+constexpr float WG_NONE = 3.4028235e38f;     // the sum of a row that counts as none: finite, so that it is not taken for a row's own infinity
 struct WgArgs {
     PgCache pc;
     PgSeqs sq;
