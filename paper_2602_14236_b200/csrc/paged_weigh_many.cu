@@ -34,9 +34,10 @@
 namespace {
 
 constexpr int WM_KEYS = 256, WM_K = 2, WM_Q = 3;
-// Which of eight columns take their exponentials on the FMA pipe instead of the special-function unit.  A prompt of 8192 rows with
-// none, one, two of them: 314, 290, 298 us; one call after the other, until the clocks have settled: 339, 330, 343.
-constexpr uint32_t WM_POLY = 0x01;
+// The pairs of columns of which the first takes its exponentials on the FMA pipe instead of the special-function unit: one column in
+// eight.  A prompt of 8192 rows with none, one, two of eight: 314, 290, 298 us; one call after the other, until the clocks have settled:
+// 339, 330, 343.
+__device__ __forceinline__ constexpr bool WM_POLY(int pair) { return (pair & 3) == 0; }
 // An item's fixed cost (its keys) in tiles' time.
 constexpr int WM_ITEM = 2;
 
@@ -225,6 +226,8 @@ struct WmBars {
     int4 hd[2];                              // what the block says of its records
     uint32_t tmem;
     int gave_up;
+    uint32_t counts[2][4];                   // even and odd tiles: bit c set: column c is a row, and one that counts
+    int all[2];                              // ... which all but those behind the last whole token are
     uint32_t pages[8];                       // per item with tiles (in turn): bit g set: the page of keys 16 g .. 16 g + 15 exists
 };
 template <int D>
@@ -319,15 +322,18 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
                     break;
                 }
                 tc_after();
-                // columns that see this key: rows from its own on, up to the last one
-                const int r0 = (g.rt + t) * HR, c_hi = min(HR, w.s.n * a.G - r0);
-                const bool whole = c_hi == HR && (long long)(g.j0 + half * 128 + 127 - w.s.pos0) * a.G <= r0;
-                const int c_lo = max(0, min(128, max(0, j - w.s.pos0) * a.G - r0));
-                uint64_t acc[2] = {0ull, 0ull};
+                const int r0 = (g.rt + t) * HR;
+                const bool whole = HR >= 112 && *(volatile int*)&bars.all[part] && (long long)(g.j0 + half * 128 + 127 - w.s.pos0) * a.G <= r0;
+                const int c_lo = max(0, min(128, max(0, j - w.s.pos0) * a.G - r0));          // rows before this column do not see the key
+                // A column that is no row has the sum WG_NONE, which leaves nothing of a finite score, and is masked where it may meet
+                // another one: the zeros behind a tile's rows under a key that is not finite, a row that counts as none.  `whole` tiles have
+                // the former among the last 16 columns and none of the latter.  (Masks in all columns of tiles with zeros: 5 % of their
+                // time; masks in 16 columns of all: 2 %; the zeros' tiles in a third copy of this code: 1 %, but 5 % of 64 rows a sequence.)
+                uint64_t acc[2] = {0ull, 0ull};  // the first one's lower half has the polynomial's columns alone
                 float top = -INFINITY;
                 const uint64_t scale2 = pair2(a.scale, a.scale);
-                auto columns = [&](auto masked_) {
-                    constexpr bool MASKED = decltype(masked_)::value;
+                auto columns = [&](auto whole_) {
+                    constexpr bool WHOLE = decltype(whole_)::value;
                     uint32_t x[2][16];
                     tc_ld16(x[0], S);
                     tc_wait_ld16(x[0]);
@@ -335,7 +341,9 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
                     for (int c = 0; c < 8; ++c) {
                         if (c < 7) tc_ld16(x[(c + 1) & 1], S + 16 * (c + 1));
                         const uint32_t(&y)[16] = x[c & 1];
-                        const uint32_t sees = MASKED ? below(c_hi - 16 * c) & ~below(c_lo - 16 * c) : 0u;
+                        const bool MASKED = !WHOLE || c == 7;
+                        uint32_t sees = MASKED ? *(volatile uint32_t*)&bars.counts[part][c >> 1] >> (16 * (c & 1)) : 0u;
+                        if (!WHOLE) sees &= ~below(c_lo - 16 * c);
                         ulonglong2 l[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) l[i] = ls[4 * c + i];
@@ -347,23 +355,25 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             float lo, hi;
-                            split2(fma2x(pair2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), scale2, i & 1 ? l[i >> 1].y : l[i >> 1].x), lo, hi);
-                            lo = !MASKED && (WM_POLY >> (2 * (i & 3)) & 1) ? ex2_fma(lo, top) : ex2(lo);
-                            hi = !MASKED && (WM_POLY >> (2 * (i & 3) + 1) & 1) ? ex2_fma(hi, top) : ex2(hi);
+                            const uint64_t minus = i & 1 ? l[i >> 1].y : l[i >> 1].x;
+                            split2(fma2x(pair2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), scale2, minus), lo, hi);
+                            lo = !MASKED && WM_POLY(i) ? ex2_fma(lo, top) : ex2(lo);
+                            hi = ex2(hi);
                             if (MASKED) {
                                 lo = sees & 1u << (2 * i) ? lo : 0.0f;
                                 hi = sees & 2u << (2 * i) ? hi : 0.0f;
                             }
-                            acc[i & 1] = add2x(acc[i & 1], pair2(lo, hi));
+                            acc[!WM_POLY(i)] = add2x(acc[!WM_POLY(i)], pair2(lo, hi));
                         }
                         if (c < 7) tc_wait_ld16(x[(c + 1) & 1]);
                     }
                 };
-                if (whole) columns(std::false_type{});
-                else columns(std::true_type{});
-                float s_lo, s_hi;
-                split2(add2x(acc[0], acc[1]), s_lo, s_hi);
-                sum += top < 128.0f ? s_lo + s_hi : top == top ? INFINITY : top;
+                if (whole) columns(std::true_type{});
+                else columns(std::false_type{});
+                float s[4];
+                split2(acc[0], s[0], s[1]);
+                split2(acc[1], s[2], s[3]);
+                sum += (top < 128.0f ? s[0] : top == top ? INFINITY : top) + ((s[1] + s[2]) + s[3]);
             }
             if (!ok) break;
             const float had = writes && mine && g.first && g.last ? wg_had(a, w.s, w.b, w.h, j) : 0.0f;
@@ -614,7 +624,7 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
             return;
         }
         if (wid == LAST + 2) {
-            // ---------------- the rows' sums: minus their logarithms, in powers of two; -inf for what is no row.  A lane has four columns
+            // ---------------- the rows' sums: minus their logarithms, in powers of two; -WG_NONE for what is none.  A lane has four columns
             const int Hq = a.pc.heads * a.G;
             int off[4];
 #pragma unroll
@@ -627,17 +637,24 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
                     const float* p = a.lse + (long long)(w.s.row0 + (g.rt + t) * a.tok) * Hq + w.h * a.G;
                     const int cols = min(HR, w.s.n * a.G - (g.rt + t) * HR);
                     float l[4];
+                    uint32_t there = 0;          // this lane's columns that count
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float y = 4 * lane + i < cols ? __ldg(p + off[i]) : -INFINITY;
-                        l[i] = y == -INFINITY ? y : -y * PT_LOG2E;
+                        l[i] = y == -INFINITY ? -WG_NONE : -y * PT_LOG2E;
+                        there |= (y == -INFINITY ? 0u : 1u << i) << 4 * (lane & 7);
                     }
+                    const bool all = __reduce_add_sync(0xffffffffu, __popc(there)) == HR;
+#pragma unroll
+                    for (int d = 1; d < 8; d <<= 1) there |= __shfl_xor_sync(0xffffffffu, there, d);
                     // who frees tile n - 2 has read its sums
                     if (n >= 2 && !(wait(bars.s_free[n & 1][0], (n / 2 - 1) & 1) && wait(bars.s_free[n & 1][1], (n / 2 - 1) & 1))) {
                         ok = false;
                         break;
                     }
                     reinterpret_cast<float4*>(mem + SM::LSE)[(n & 1) * 32 + lane] = make_float4(l[0], l[1], l[2], l[3]);
+                    if ((lane & 7) == 0) *(volatile uint32_t*)&bars.counts[n & 1][lane >> 3] = there;
+                    if (lane == 0) *(volatile int*)&bars.all[n & 1] = all;
                     __syncwarp();
                     if (lane == 0) bar_arrive(smem_u32(&bars.l_full[n & 1]));
                 }
