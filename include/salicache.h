@@ -583,13 +583,13 @@ SALICACHE_API int salicache_paged_weigh(salicache_ctx* ctx, const salicache_page
  * The positions that a budget keeps, for every sequence b and key/value head h: all of them while d_len[b] <= budget; else
  * the first `sinks`, the last `recent`, and of the rest the budget - sinks - recent heaviest, equal weights by the lower
  * position.  A weight that is not a number counts as less than all others.
- *   d_weight  DEVICE f32 [n_seqs][heads][weight_stride], weight_stride >= d_len[b] (positions past it count as not held:
- *             d_len is taken as weight_stride, deferred E_CAPACITY)
+ *   d_weight  DEVICE f32 [n_seqs][heads][weight_stride], weight_stride >= d_len[b] (positions past it, or from 2^30 on, count as not
+ *             held: d_len is taken as weight_stride or 2^30, deferred E_CAPACITY)
  *   d_len     DEVICE i32 [n_seqs]
  *   d_keep    DEVICE i32 [n_seqs][heads][budget], written: ascending positions, -1 behind the last
  *   d_kept    DEVICE i32 [n_seqs], written: min(d_len[b], budget), which is the sequence's length after
  *             salicache_paged_keep
- * sinks + recent <= budget, all of them >= 0, budget >= 1 (E_PARAM); heads 1 .. 256, n_seqs >= 0, n_seqs * heads below 2^16 (E_SHAPE).
+ * sinks + recent <= budget, all of them >= 0, budget 1 .. 2^30 (E_PARAM); heads 1 .. 256, n_seqs >= 0, n_seqs * heads below 2^16 (E_SHAPE).
  * Errors: E_NULL, E_ALIGN (4 bytes), E_PARAM, E_SHAPE, E_CUDA.
  */
 SALICACHE_API int salicache_select_heavy(salicache_ctx* ctx, const float* d_weight, int64_t weight_stride, int heads, int n_seqs,
@@ -613,7 +613,7 @@ SALICACHE_API int salicache_select_heavy(salicache_ctx* ctx, const float* d_weig
  * Entries outside [0, d_len[b]), and rows whose source or destination is in no page (past the table, an entry outside
  * [0, n_pages)), are not moved (deferred E_CAPACITY); the destination, and the weight there, stays as it is.  A weight at or
  * past weight_stride is not moved.
- * Errors: as for salicache_paged_write; E_SHAPE also for keep_heads, keep_width < 0, another n_seqs in to_or_null, n_seqs *
+ * Errors: as for salicache_paged_write; E_SHAPE also for keep_heads, keep_width below 0 or above 2^30, another n_seqs in to_or_null, n_seqs *
  * heads at or past 2^16, weight_stride < 1 with weights; E_PARAM when the two tables are one; E_NULL for one of the weights.
  */
 SALICACHE_API int salicache_paged_keep(salicache_ctx* ctx, const salicache_pages* pages, const salicache_seqs* seqs,

@@ -590,7 +590,7 @@ int salicache_select_heavy(salicache_ctx* c, const float* d_weight, int64_t weig
                            int budget, int sinks, int recent, int32_t* d_keep, int32_t* d_kept, void* cuda_stream) {
     Range range__("salicache_select_heavy");
     if (!d_weight || !d_len || !d_keep || !d_kept) return SALICACHE_E_NULL;
-    if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return SALICACHE_E_PARAM;
+    if (budget < 1 || budget > 1 << 30 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return SALICACHE_E_PARAM;
     if (heads < 1 || heads > 256 || n_seqs < 0 || (int64_t)n_seqs * heads >= (1 << 16) || weight_stride < 1) return SALICACHE_E_SHAPE;
     if ((reinterpret_cast<uintptr_t>(d_weight) | reinterpret_cast<uintptr_t>(d_len) | reinterpret_cast<uintptr_t>(d_keep) |
          reinterpret_cast<uintptr_t>(d_kept)) & 3u)
@@ -611,7 +611,7 @@ int salicache_paged_keep(salicache_ctx* c, const salicache_pages* pages, const s
     if (rc == SALICACHE_OK && to) rc = check_seqs(to);
     if (rc != SALICACHE_OK) return rc;
     if (!d_keep || !d_kept || !d_weight_in != !d_weight_out) return SALICACHE_E_NULL;
-    if ((keep_heads != 1 && keep_heads != pages->heads) || keep_width < 0 || (to && to->n_seqs != seqs->n_seqs) ||
+    if ((keep_heads != 1 && keep_heads != pages->heads) || keep_width < 0 || keep_width > 1 << 30 || (to && to->n_seqs != seqs->n_seqs) ||
         (int64_t)seqs->n_seqs * pages->heads >= (1 << 16) || (d_weight_in && weight_stride < 1))
         return SALICACHE_E_SHAPE;
     if (to && to->n_seqs > 0 && to->d_table == seqs->d_table) return SALICACHE_E_PARAM;

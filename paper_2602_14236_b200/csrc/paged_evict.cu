@@ -60,8 +60,9 @@ k_select_heavy(const float* weight, long long stride, int heads, const int* len_
     grid_wait();
     grid_release();
     int len = max(len_[b], 0);
-    if (len > stride) {
-        len = (int)stride;
+    const long long most = min(stride, 1ll << 30);       // sums of positions and strides of the loops below stay within 32 bits
+    if (len > most) {
+        len = (int)most;
         if (tid == 0) atomicMin(status, SALICACHE_E_CAPACITY);
     }
     int* out = keep + (size_t)list * budget;
