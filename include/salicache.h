@@ -420,7 +420,8 @@ typedef struct salicache_pages {
  * Positions at or past table_width * page (or 2^30), and positions whose table entry lies outside [0, n_pages), are in no page: a
  * call that has to touch one records E_CAPACITY in the status word and treats it as stated with the call.  Table entries
  * of positions that no row has to touch are never used: they may be stale.
- * The offsets are read on the device: calls can be captured and replayed with other lengths of the same n_rows. */
+ * The offsets are read on the device: calls can be captured and replayed with other lengths of the same n_rows.
+ * An array that has no elements in a call (no rows, no sequences, no entries of a list) may be NULL, as an empty tensor's address is. */
 typedef struct salicache_seqs {
     int32_t n_seqs, table_width;
     int32_t n_rows;                /* rows in the caller's arrays                */

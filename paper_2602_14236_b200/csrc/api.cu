@@ -432,9 +432,9 @@ static int check_seqs(const salicache_seqs* q) {
     return SALICACHE_OK;
 }
 
-// Rows of `width` elements `stride` apart.
-static int check_rows(const void* p, int64_t stride, int64_t width) {
-    if (!p) return SALICACHE_E_NULL;
+// Rows of `width` elements `stride` apart; no rows need no address.
+static int check_rows(const salicache_seqs* q, const void* p, int64_t stride, int64_t width) {
+    if (!p && q->n_rows > 0) return SALICACHE_E_NULL;
     if (stride < width || stride % 8 != 0) return SALICACHE_E_SHAPE;
     return aligned16(p) ? SALICACHE_OK : SALICACHE_E_ALIGN;
 }
@@ -450,8 +450,8 @@ static int paged_move(salicache_ctx* c, const salicache_pages* pg, const salicac
                       int64_t k_stride, int64_t v_stride, bool write, void* cuda_stream) {
     int rc = check_pages(pg);
     if (rc == SALICACHE_OK) rc = check_seqs(sq);
-    if (rc == SALICACHE_OK) rc = check_rows(d_K, k_stride, (int64_t)pg->heads * pg->head_dim);
-    if (rc == SALICACHE_OK) rc = check_rows(d_V, v_stride, (int64_t)pg->heads * pg->head_dim);
+    if (rc == SALICACHE_OK) rc = check_rows(sq, d_K, k_stride, (int64_t)pg->heads * pg->head_dim);
+    if (rc == SALICACHE_OK) rc = check_rows(sq, d_V, v_stride, (int64_t)pg->heads * pg->head_dim);
     if (rc == SALICACHE_OK) rc = check_device(c);
     if (rc != SALICACHE_OK) return rc;
     if (sq->n_seqs == 0 || sq->n_rows == 0) return SALICACHE_OK;
@@ -470,8 +470,8 @@ int salicache_paged_read(salicache_ctx* c, const salicache_pages* pages, const s
     return paged_move(c, pages, seqs, d_K_out, d_V_out, k_stride, v_stride, false, cuda_stream);
 }
 
-static int check_rotary(const salicache_rotary* r, const int32_t* d_pos, int head_dim) {
-    if (!r || !d_pos) return SALICACHE_E_NULL;
+static int check_rotary(const salicache_rotary* r, const int32_t* d_pos, int n_rows, int head_dim) {
+    if (!r || (!d_pos && n_rows > 0)) return SALICACHE_E_NULL;
     if (r->pairs < 8 || r->pairs % 8 != 0 || 2 * r->pairs > head_dim || r->n_axes < 1 || r->n_axes > 4) return SALICACHE_E_PARAM;
     if (r->pairing != SALICACHE_HALVES && r->pairing != SALICACHE_NEIGHBOURS) return SALICACHE_E_PARAM;
     for (int i = 0; i < r->pairs; ++i)
@@ -486,17 +486,17 @@ int salicache_paged_write_rotary(salicache_ctx* c, const salicache_pages* pages,
     Range range__("salicache_paged_write_rotary");
     int rc = check_pages(pages);
     if (rc == SALICACHE_OK) rc = check_seqs(seqs);
-    if (rc == SALICACHE_OK) rc = check_rotary(rotary, d_pos, pages->head_dim);
+    if (rc == SALICACHE_OK) rc = check_rotary(rotary, d_pos, seqs->n_rows, pages->head_dim);
     if (rc != SALICACHE_OK) return rc;
     const int64_t width = (int64_t)pages->heads * pages->head_dim;
     if (d_q) {
         if (q_per_kv < 1 || q_per_kv > 64) return SALICACHE_E_PARAM;
-        rc = check_rows(d_q, q_stride, width * q_per_kv);
-        if (rc == SALICACHE_OK) rc = check_rows(d_q_out, q_out_stride, width * q_per_kv);
+        rc = check_rows(seqs, d_q, q_stride, width * q_per_kv);
+        if (rc == SALICACHE_OK) rc = check_rows(seqs, d_q_out, q_out_stride, width * q_per_kv);
         if (rc == SALICACHE_OK && d_q == d_q_out && q_stride != q_out_stride) rc = SALICACHE_E_SHAPE;
     }
-    if (rc == SALICACHE_OK) rc = check_rows(d_K, k_stride, width);
-    if (rc == SALICACHE_OK) rc = check_rows(d_V, v_stride, width);
+    if (rc == SALICACHE_OK) rc = check_rows(seqs, d_K, k_stride, width);
+    if (rc == SALICACHE_OK) rc = check_rows(seqs, d_V, v_stride, width);
     if (rc == SALICACHE_OK) rc = check_device(c);
     if (rc != SALICACHE_OK) return rc;
     if (seqs->n_seqs == 0 || seqs->n_rows == 0) return SALICACHE_OK;
@@ -530,8 +530,8 @@ static int check_attend(const salicache_pages* pages, const salicache_seqs* seqs
         return SALICACHE_E_PARAM;
     if ((int64_t)seqs->n_rows * q_per_kv >= (1ll << 30)) return SALICACHE_E_SHAPE;
     const int64_t width = (int64_t)pages->heads * q_per_kv * pages->head_dim;
-    rc = check_rows(d_q, q_stride, width);
-    if (rc == SALICACHE_OK) rc = check_rows(d_out, out_stride, width);
+    rc = check_rows(seqs, d_q, q_stride, width);
+    if (rc == SALICACHE_OK) rc = check_rows(seqs, d_out, out_stride, width);
     if (rc == SALICACHE_OK && !d_work) rc = SALICACHE_E_NULL;
     if (rc == SALICACHE_OK && (!aligned16(d_work) || (reinterpret_cast<uintptr_t>(d_lse) & 3u))) rc = SALICACHE_E_ALIGN;
     return rc;
@@ -556,7 +556,7 @@ int salicache_paged_attend_tree(salicache_ctx* c, const salicache_pages* pages, 
                                 void* cuda_stream) {
     Range range__("salicache_paged_attend_tree");
     int rc = check_attend(pages, seqs, d_q, q_stride, q_per_kv, softmax_scale, window, sinks, d_out, out_stride, d_lse, d_work);
-    if (rc == SALICACHE_OK && !d_tree) rc = SALICACHE_E_NULL;
+    if (rc == SALICACHE_OK && !d_tree && seqs->n_rows > 0) rc = SALICACHE_E_NULL;
     if (rc == SALICACHE_OK && (tree_words < 1 || tree_words > 16)) rc = SALICACHE_E_PARAM;
     if (rc == SALICACHE_OK && (reinterpret_cast<uintptr_t>(d_tree) & 7u)) rc = SALICACHE_E_ALIGN;
     if (rc == SALICACHE_OK) rc = check_device(c);
@@ -573,7 +573,7 @@ int salicache_paged_weigh(salicache_ctx* c, const salicache_pages* pages, const 
     Range range__("salicache_paged_weigh");
     // no output rows here: the rows of q stand in for them
     int rc = check_attend(pages, seqs, d_q, q_stride, q_per_kv, softmax_scale, 0, 0, const_cast<void*>(d_q), q_stride, d_lse, d_work);
-    if (rc == SALICACHE_OK && (!d_lse || !d_weight_out)) rc = SALICACHE_E_NULL;
+    if (rc == SALICACHE_OK && ((!d_lse && seqs->n_rows > 0) || (!d_weight_out && seqs->n_seqs > 0))) rc = SALICACHE_E_NULL;
     if (rc == SALICACHE_OK && !(decay >= 0.0f && decay <= 1.0f)) rc = SALICACHE_E_PARAM;
     if (rc == SALICACHE_OK && weight_stride < 1) rc = SALICACHE_E_SHAPE;
     if (rc == SALICACHE_OK && ((reinterpret_cast<uintptr_t>(d_weight_in) | reinterpret_cast<uintptr_t>(d_weight_out)) & 3u))
@@ -589,7 +589,7 @@ int salicache_paged_weigh(salicache_ctx* c, const salicache_pages* pages, const 
 int salicache_select_heavy(salicache_ctx* c, const float* d_weight, int64_t weight_stride, int heads, int n_seqs, const int32_t* d_len,
                            int budget, int sinks, int recent, int32_t* d_keep, int32_t* d_kept, void* cuda_stream) {
     Range range__("salicache_select_heavy");
-    if (!d_weight || !d_len || !d_keep || !d_kept) return SALICACHE_E_NULL;
+    if (n_seqs > 0 && (!d_weight || !d_len || !d_keep || !d_kept)) return SALICACHE_E_NULL;
     if (budget < 1 || budget > 1 << 30 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return SALICACHE_E_PARAM;
     if (heads < 1 || heads > 256 || n_seqs < 0 || (int64_t)n_seqs * heads >= (1 << 16) || weight_stride < 1) return SALICACHE_E_SHAPE;
     if ((reinterpret_cast<uintptr_t>(d_weight) | reinterpret_cast<uintptr_t>(d_len) | reinterpret_cast<uintptr_t>(d_keep) |
@@ -610,7 +610,7 @@ int salicache_paged_keep(salicache_ctx* c, const salicache_pages* pages, const s
     if (rc == SALICACHE_OK) rc = check_seqs(seqs);
     if (rc == SALICACHE_OK && to) rc = check_seqs(to);
     if (rc != SALICACHE_OK) return rc;
-    if (!d_keep || !d_kept || !d_weight_in != !d_weight_out) return SALICACHE_E_NULL;
+    if ((seqs->n_seqs > 0 && ((!d_keep && keep_width > 0) || !d_kept)) || !d_weight_in != !d_weight_out) return SALICACHE_E_NULL;
     if ((keep_heads != 1 && keep_heads != pages->heads) || keep_width < 0 || keep_width > 1 << 30 || (to && to->n_seqs != seqs->n_seqs) ||
         (int64_t)seqs->n_seqs * pages->heads >= (1 << 16) || (d_weight_in && weight_stride < 1))
         return SALICACHE_E_SHAPE;
