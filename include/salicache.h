@@ -601,12 +601,12 @@ SALICACHE_API int salicache_select_heavy(salicache_ctx* ctx, const float* d_weig
  * Moves the kept positions together: position first + k of sequence b gets what position d_keep[b][h][k] holds, K, V and
  * scales bit for bit, for k < d_kept[b], per key/value head.  After an eviction the lists are salicache_select_heavy's; after
  * a draft has been verified, the positions of the accepted path, the same for all heads.
- *   seqs       where the rows are: n_seqs, d_len, d_table, table_width (the row offsets are not used)
+ *   seqs       where the rows are: n_seqs, d_len, d_table, table_width (the row offsets are not used and may be NULL)
  *   d_keep     DEVICE i32 [n_seqs][keep_heads][keep_width]; keep_heads is the pages' heads, or 1: one list for all heads
  *   d_first    DEVICE i32 [n_seqs] (not negative), or NULL: 0
  *   d_kept     DEVICE i32 [n_seqs]; more than keep_width counts as keep_width, less than 0 as 0
  *   to_or_null where they go: n_seqs, d_table and table_width of other pages of the same array (its d_len and row offsets
- *              are not used).  No page may be among both the sources and the destinations, nor twice among the destinations.
+ *              are not used and may be NULL).  No page may be among both the sources and the destinations, nor twice among the destinations.
  *              NULL: in place.  The lists are then strictly ascending with d_keep[b][h][k] >= first + k, and no page that
  *              is written belongs to two sequences: rows of shared prefixes are not to be moved in place.
  *   d_weight_in, d_weight_out  DEVICE f32 [n_seqs][heads][weight_stride], both or neither: the weights move along; the two

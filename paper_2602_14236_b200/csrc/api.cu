@@ -422,10 +422,11 @@ static int check_pages(const salicache_pages* p) {
     return SALICACHE_OK;
 }
 
-static int check_seqs(const salicache_seqs* q) {
+// `rows`, `len`: whether the call looks at the row offsets and at the lengths.
+static int check_seqs(const salicache_seqs* q, bool rows = true, bool len = true) {
     if (!q) return SALICACHE_E_NULL;
     if (q->n_seqs < 0 || q->n_rows < 0 || q->table_width < 1) return SALICACHE_E_SHAPE;
-    if (q->n_seqs > 0 && (!q->d_row_start || !q->d_len || !q->d_table)) return SALICACHE_E_NULL;
+    if (q->n_seqs > 0 && ((rows && !q->d_row_start) || (len && !q->d_len) || !q->d_table)) return SALICACHE_E_NULL;
     if ((reinterpret_cast<uintptr_t>(q->d_row_start) | reinterpret_cast<uintptr_t>(q->d_len) |
          reinterpret_cast<uintptr_t>(q->d_table)) & 3u)
         return SALICACHE_E_ALIGN;
@@ -607,8 +608,8 @@ int salicache_paged_keep(salicache_ctx* c, const salicache_pages* pages, const s
                          const float* d_weight_in, float* d_weight_out, int64_t weight_stride, void* cuda_stream) {
     Range range__("salicache_paged_keep");
     int rc = check_pages(pages);
-    if (rc == SALICACHE_OK) rc = check_seqs(seqs);
-    if (rc == SALICACHE_OK && to) rc = check_seqs(to);
+    if (rc == SALICACHE_OK) rc = check_seqs(seqs, false);
+    if (rc == SALICACHE_OK && to) rc = check_seqs(to, false, false);
     if (rc != SALICACHE_OK) return rc;
     if ((seqs->n_seqs > 0 && ((!d_keep && keep_width > 0) || !d_kept)) || !d_weight_in != !d_weight_out) return SALICACHE_E_NULL;
     if ((keep_heads != 1 && keep_heads != pages->heads) || keep_width < 0 || keep_width > 1 << 30 || (to && to->n_seqs != seqs->n_seqs) ||

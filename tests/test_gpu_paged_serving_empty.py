@@ -56,3 +56,19 @@ def test_no_sequences_and_no_entries(ctx):
     one = sc.Seqs(torch.zeros(2, dtype=i32, device="cuda"), torch.full((1,), 9, dtype=i32, device="cuda"), torch.zeros((1, 3), dtype=i32, device="cuda"), 0)
     sc.salicache_paged_keep(ctx, pages.c, one.c, torch.empty((1, 1, 0), dtype=i32, device="cuda"), 1, 0, None, torch.zeros(1, dtype=i32, device="cuda"), None)
     assert ctx.launch_count() == n and sc.salicache_poll_status(ctx) == 0
+
+
+def test_moving_without_the_offsets_that_it_does_not_use(ctx):
+    import torch
+    w = pu.World(3, "fp16", torch.float16, 2, 64, 16, [100], [0], spare=8)
+    pages, seqs = w.device()
+    free = np.setdiff1d(np.arange(w.n_pages), w.table[0])
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(torch.int32).cuda()
+    keep, kept, table = i32(np.arange(0, 100, 3)[None, None]), i32(np.array([34])), i32(free[None, :3])
+    source = sc.SeqsC(1, w.width, 0, None, seqs.length.data_ptr(), seqs.table.data_ptr())
+    target = sc.SeqsC(1, 3, 0, None, None, table.data_ptr())
+    sc.salicache_paged_keep(ctx, pages.c, source, keep, 1, 34, None, kept, target)
+    assert sc.salicache_poll_status(ctx) == 0
+    raw = pages.data.cpu()
+    for k, j in enumerate(range(0, 100, 3)):
+        assert torch.equal(raw[free[k // 16], :, :, k % 16], raw[w.table[0, j // 16], :, :, j % 16])

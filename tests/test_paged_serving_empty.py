@@ -28,6 +28,13 @@ def test_no_entries_need_no_address():
     assert _keep(keep=None, kw=1, kh=3) == sc.E_NULL
 
 
+def test_offsets_that_moving_does_not_use_may_be_missing():
+    assert _keep(seqs=_seqs(d_row_start=None), kh=3) == sc.E_SHAPE
+    assert _keep(to=_seqs(d_row_start=None, d_len=None, d_table=2 * A), kh=3) == sc.E_SHAPE
+    assert _keep(seqs=_seqs(d_row_start=None), to=_seqs(d_row_start=None, d_len=None, d_table=2 * A), first=A + 2) == sc.E_ALIGN
+    assert _keep(to=_seqs(d_table=None), kh=3) == sc.E_NULL
+
+
 @pytest.mark.parametrize("call", [_write, _tree, _weigh])
 def test_rows_that_belong_to_nobody_still_need_one(call):
     assert call(seqs=_seqs(n_seqs=0, n_rows=3), q=None, **({} if call is not _write else dict(k=None))) == sc.E_NULL
