@@ -503,9 +503,9 @@ SALICACHE_API int salicache_paged_wait_limit(salicache_ctx* ctx, int tries);
  * (2 i, 2 i + 1) with SALICACHE_NEIGHBOURS, and pair i is turned by position[axis[i]] * freq[i] radians:
  *   first' = first cos - second sin,  second' = second cos + first sin
  * The other dimensions stay.  A position has 1 .. 4 axes (one: plain rotary positions; time, height and width: the visual
- * tokens of images and video), and freq may be any finite numbers, scaled for long contexts or not; negated ones turn back.
- * The angle is reduced exactly, whatever the position: the kernel multiplies it with freq / 2 pi as a 64-bit fraction of a
- * turn, modulo one.  Cosine, sine and products are binary32, the result is rounded to the 16-bit type.
+ * tokens of images and video), and freq may be any numbers up to 2^64 in magnitude, scaled for long contexts or not; negated ones
+ * turn back.  freq / 2 pi is reduced to a fraction of a turn that is right to 2^-62, whatever the frequency, and the kernel's product
+ * of it and the position, modulo one, is exact.  Cosine, sine and products are binary32, the result is rounded to the 16-bit type.
  * HOST memory, read during the call. */
 #define SALICACHE_HALVES     0
 #define SALICACHE_NEIGHBOURS 1

@@ -476,7 +476,7 @@ static int check_rotary(const salicache_rotary* r, const int32_t* d_pos, int n_r
     if (r->pairs < 8 || r->pairs % 8 != 0 || 2 * r->pairs > head_dim || r->n_axes < 1 || r->n_axes > 4) return SALICACHE_E_PARAM;
     if (r->pairing != SALICACHE_HALVES && r->pairing != SALICACHE_NEIGHBOURS) return SALICACHE_E_PARAM;
     for (int i = 0; i < r->pairs; ++i)
-        if (!isfinite(r->freq[i]) || r->axis[i] >= r->n_axes) return SALICACHE_E_PARAM;
+        if (!(fabs(r->freq[i]) <= 0x1p64) || r->axis[i] >= r->n_axes) return SALICACHE_E_PARAM;
     return reinterpret_cast<uintptr_t>(d_pos) & 3u ? SALICACHE_E_ALIGN : SALICACHE_OK;
 }
 

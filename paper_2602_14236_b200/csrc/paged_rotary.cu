@@ -145,6 +145,28 @@ k_paged_write_rotary(PgCache pc, PgSeqs sq, const __grid_constant__ RtTurns rt, 
     }
 }
 
+// freq / 2 pi modulo one as a fraction of 2^64, for frequencies up to 2^64: the frequency's 53 bits times 192 of 1 / 2 pi (from
+// Machin's formula for pi), of which the whole turns fall off.  What is cut off is below 2^-64 turns, 2^-62 with the axis in the
+// last two bits.
+uint64_t turns_per_position(double freq) {
+    static const uint64_t INV[3] = {0x36d8a5664f10e410ull, 0x7f09d5f47d4d3770ull, 0x28be60db9391054aull};    // least first
+    int e;
+    const uint64_t m = (uint64_t)ldexp(frexp(fabs(freq), &e), 53);
+    uint64_t p[5] = {};                      // freq = m 2^(e - 53), freq / 2 pi = p 2^(e - 53 - 192)
+    unsigned __int128 carry = 0;
+    for (int i = 0; i < 3; ++i) {
+        carry += (unsigned __int128)m * INV[i];
+        p[i] = (uint64_t)carry;
+        carry >>= 64;
+    }
+    p[3] = (uint64_t)carry;
+    const int shift = 128 + 53 - e;          // at least 116
+    if (shift >= 256) return 0;
+    const int w = shift / 64, off = shift % 64;
+    const uint64_t f = off ? p[w] >> off | p[w + 1] << (64 - off) : p[w];
+    return freq < 0 ? 0 - f : f;
+}
+
 struct RtCall {
     PgCache pc;
     PgSeqs sq;
@@ -197,12 +219,7 @@ int sc_paged_write_rotary(salicache_ctx* c, const salicache_pages* pg, const sal
     a.sq = pg_seqs(sq);
     a.rt.pairs = rotary->pairs;
     a.rt.n_axes = rotary->n_axes;
-    for (int i = 0; i < rotary->pairs; ++i) {
-        // whole turns go; what is left of a double has 53 bits, of which the fraction loses none above 2^-62 turns
-        long double part = (long double)rotary->freq[i] * 0.159154943091895335768883763372514362L;
-        if (!(part >= 0.0L && part < 1.0L)) part -= floorl(part);
-        a.rt.f[i] = ((part < 1.0L ? (uint64_t)(part * 0x1p64L) : 0ull) & ~3ull) | rotary->axis[i];
-    }
+    for (int i = 0; i < rotary->pairs; ++i) a.rt.f[i] = (turns_per_position(rotary->freq[i]) & ~3ull) | rotary->axis[i];
     a.pos = d_pos;
     a.q = (const uint16_t*)d_q;
     a.q_out = (uint16_t*)d_q_out;
