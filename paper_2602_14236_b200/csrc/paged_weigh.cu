@@ -6,9 +6,8 @@
 // and nothing to be joined.  Only K is read.
 //
 // This file's kernel, for few rows per sequence: a warp has 16 keys of one head as the long side of m16n8k16 matrix
-// instructions, rows of q are the columns, 8 at a time (more than 16 only where a batch of as many rows as sequences has them in
-// one).  A lane sums its columns' weights, four lanes join at the end.  Every
-// warp has a ring of its own in shared memory, which its first lanes fill by bulk copies of 16 keys' rows and scales.  All
+// instructions, rows of q are the columns, 8 at a time, 16 at most.  A lane sums its columns' weights, four lanes join at the
+// end.  Every warp has a ring of its own in shared memory, which its first lanes fill by bulk copies of 16 keys' rows and scales.  All
 // groups of keys stand in one line, of which every warp takes an equal stretch, so that the lengths on the device decide the
 // split, and warps never wait for one another.
 // Measured, 16 sequences of 8000 positions, 8 heads x 128, one token and four query heads a group (four tokens): 16-bit pages 52 us
@@ -148,6 +147,12 @@ k_weigh_few(WgArgs a) {
     grid_release();
     long long left;
     WgPlace p = wg_start<KEYS>(a, blockIdx.x * WG_WARPS + wid, gridDim.x * WG_WARPS, left);
+    if (a.some && blockIdx.x == 0 && wid == 0) {
+        bool some = false;
+        for (int b = lane; b < a.sq.n_seqs; b += 32) some = some || pg_seq(a.sq, a.pc, b).n * a.G > a.rows_to;
+        some = __any_sync(0xffffffffu, some);
+        if (lane == 0) *a.some = some;
+    }
     __syncthreads();
     const uint32_t ring = smem_u32(rings) + wid * STAGES * R::STAGE, bars = smem_u32(&full[wid][0]);
 
@@ -262,12 +267,12 @@ k_weigh_few(WgArgs a) {
                     sum[1] += (l0 ? w[2] : 0.0f) + (l1 ? w[3] : 0.0f);
                 };
                 if (there >> u & 1u) {
-                    if (rows <= 8 * NT) {
+                    if (NT > 1 || rows <= 8) {
                         columns(col[0], 0);
                         if (NT > 1 && rows > 8) columns(col[NT - 1], NT - 1);
                     } else
 #pragma unroll 1
-                        for (int n = j0 > s.pos0 ? (j0 - s.pos0) * a.G / 8 : 0; 8 * n < rows; ++n) {     // from the first row that sees the first key on
+                        for (int n = 0; n < 2; ++n) {
                             if (n != 0 || !first_columns) col[0].load(a, s, p.h, n, rows, g8, c4);
                             first_columns = n == 0;
                             columns(col[0], n);
@@ -315,7 +320,7 @@ int launch_few(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
 }
 template <typename T, int FMT, int D>
 int few_columns(salicache_ctx* c, const WgArgs& a, cudaStream_t st) {
-    const bool one = (long long)a.sq.n_rows * a.G <= 8 || (a.G <= 8 && a.sq.n_rows <= a.sq.n_seqs);      // single tokens
+    const bool one = (long long)a.sq.n_rows * a.G <= 8 || (a.G <= 8 && a.sq.n_rows == a.sq.n_seqs);      // single tokens
     return one ? launch_few<T, FMT, D, 1>(c, a, st) : launch_few<T, FMT, D, 2>(c, a, st);
 }
 template <typename T, int D>
@@ -344,16 +349,20 @@ int sc_paged_weigh(salicache_ctx* c, const salicache_pages* pg, const salicache_
     a.decay = decay;
     a.status = c->d_status;
     a.wait_limit = c->paged_wait;
-    // Rows of q per sequence up to which reading the keys is the work: what two tiles of columns hold.  (16 sequences of 8000 positions, 16
+    // Rows of q of a sequence up to which reading the keys is the work: what two tiles of columns hold.  (16 sequences of 8000 positions, 16
     // rows each, this kernel against the other: 16-bit pages 58 / 74 us, INT8 44 / 129, INT4 45 / 117; 32 rows 179 / 75, 174 / 129,
     // 296 / 117.)  Only the device knows how many a sequence has, so each kernel takes its own ones and a batch that may have both
     // kinds gets both launches: single tokens beside a prompt are the usual batch, and either kernel takes many times as long over
     // the other's.  (31 single tokens over 8000 INT4 positions and a prompt of 4096: 158 us, 318 in the other kernel alone; 63 over
-    // 4000 INT8 positions and 193 rows over 16000: 128, in this one alone 5098.)  A batch without long sequences pays 5 us for
-    // launches that find none (16 of four tokens, 16-bit pages: 57 us, 52).  This kernel goes first: the other one cannot start beside its
-    // rings, and after it, doing the join as well, it added 20 us to a prompt of 8192 rows (313, 290).
-    const bool many = (long long)sq->n_rows * q_per_kv > WG_FEW && (sq->n_rows > sq->n_seqs || q_per_kv > WG_FEW);
+    // 4000 INT8 positions and 193 rows over 16000: 128, in this one alone 5098.)  How many rows there are for a sequence on average says
+    // nothing about that: of 256 slots one may have a chunk of 200 rows while the others are idle (16000 INT4 positions: 83 us, in this
+    // kernel alone 1702).  This kernel goes first and tells the others whether there is such a sequence; a batch without one pays 2 to 3 us
+    // for two launches that return at once (16 single tokens over 8000 INT4 positions 46 us, 43; 256 over 2000 134, 131; 5 to 13 us where
+    // they look for themselves).  The other one cannot start beside this one's rings, and after it, doing the join as well, this one added
+    // 20 us to a prompt of 8192 rows (313, 290).
+    const bool many = (long long)sq->n_rows * q_per_kv > WG_FEW;
     a.rows_to = many ? WG_FEW : INT_MAX;
+    a.some = many ? reinterpret_cast<int*>(d_work) : nullptr;
     int rc;
     if (pg->dtype == SALICACHE_F16)
         rc = pg->head_dim == 128 ? few_format<TypeF16, 128>(c, a, pg->format, st) : few_format<TypeF16, 64>(c, a, pg->format, st);

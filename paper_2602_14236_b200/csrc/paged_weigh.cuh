@@ -19,6 +19,7 @@ struct WgArgs {
     int tok;                                 // many rows: tokens of a tile of rows, and 2^38 / tok
     uint64_t per_tok;
     float* part;                             // [2 * blocks][keys of a tile]: sums of a tile's rows so far, tail after head records of a block
+    int* some;                               // whether a sequence of many rows is in the batch: the kernel for few rows tells
     int4* head;                              // [2 * blocks]: per block: head record (0 none, 1 the tile goes on, 2 it ends), tail record
                                              // (0, 1), its sequence, its head; then its tile of keys, -, -, -
 };

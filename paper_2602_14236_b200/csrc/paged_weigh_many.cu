@@ -251,6 +251,9 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
     WmBars& bars = *reinterpret_cast<WmBars*>(mem + SM::BARS);
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
     volatile int* gave_up = &bars.gave_up;
+    grid_wait();
+    grid_release();
+    if (!*a.some) return;
     if (tid == 0) {
         for (int i = 0; i < WM_K; ++i) {
             bar_init(smem_u32(&bars.k_full[i]), FMT == PF_16 ? 1 : 4);       // the feeder, or the warps of group 2
@@ -285,8 +288,6 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
         sts16(base + SM::Q + q * SM::TILE + swz(HR + r, c), 0u, 0u, 0u, 0u);
     }
     fence_async();
-    grid_wait();
-    grid_release();
     tc_before();
     WmWalk w = wm_start(a, blockIdx.x, blocks);
     __syncthreads();
@@ -681,6 +682,7 @@ __global__ void __launch_bounds__(WM_KEYS)
 k_weigh_join(WgArgs a, int blocks) {
     __shared__ int list[PT_MAX_BLOCKS + 1];
     grid_wait();
+    if (!*a.some) return;
     const int4 hd = a.head[2 * blockIdx.x];
     if (hd.y == 0) return;
     const int b = hd.z, h = hd.w, j = a.head[2 * blockIdx.x + 1].x * WM_KEYS + threadIdx.x;
@@ -702,7 +704,7 @@ int launch_many(salicache_ctx* c, WgArgs a, char* work, cudaStream_t st) {
     const int blocks = min(c->sm_count, PT_MAX_BLOCKS);
     a.tok = 128 / a.G;
     a.per_tok = ((1ull << 38) + a.tok - 1) / a.tok;
-    a.part = reinterpret_cast<float*>(work);
+    a.part = reinterpret_cast<float*>(work + 16);        // behind a.some
     a.head = reinterpret_cast<int4*>(a.part + (size_t)2 * blocks * WM_KEYS);
     SC_CHECK(pt_launch(k_weigh_many<T, FMT, D>, dim3(blocks), wm_threads<FMT>(), BYTES, st, a, map, q_map, blocks));
     SC_CHECK(pt_launch(k_weigh_join, dim3(blocks), WM_KEYS, 0, st, a, blocks));
