@@ -116,9 +116,12 @@ __global__ void __launch_bounds__(ST_THREADS, StSmem<FMT, D, NT>::BLOCKS)
 k_paged_step(PtArgs a, int blocks) {
     using SM = StSmem<FMT, D, NT>;
     constexpr int RT = 8 * NT, KS = D / 16, VS = D / 16, STAGES = SM::STAGES;
-    // Drafts are ragged: beside a long sequence stand short ones, whose items are their fixed cost and little more (one stream of 22478
-    // INT8 positions and five of up to 1231, 16 x 2 heads, 2 to 13 nodes: 66 us, 98 with the cost that single tokens have).
-    constexpr int ITEM = TREE && NT == 2 && FMT == PF_I8 ? 5 : SM::ITEM;
+    // An item of two column tiles has a higher fixed cost than a single token's, and drafts are ragged: beside a long sequence stand short
+    // ones, whose items are that cost and little more.  One stream of 22478 positions and five of up to 1231, 16 x 2 heads, 2 to 13
+    // nodes, with an item at 2, 3, 5, 8 tiles: INT8 185, 140, 120, 124 us, INT4 171, 128, 116, 118; 16 streams of 8000 and four nodes
+    // each: INT8 153, 153, 157, 161, INT4 146, 147, 151, 155.  With one column tile (two nodes over 16-bit pages): 16000 positions beside
+    // 31 times 200: 40, 42, 46, 52; the five ragged ones 85, 85, 81, 83.
+    constexpr int ITEM = TREE && NT == 2 ? 5 : SM::ITEM;
     static_assert(STAGES >= 2, "ring");
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ uint64_t full[STAGES], empty[STAGES], q_full[2], q_empty[2];
