@@ -1,5 +1,5 @@
 // Fifth-generation tensor cores (tcgen05), tensor memory and tensor copies, for operand tiles of 128 rows of 16-bit elements in
-// the 128-byte swizzle.  Shared by the attention of many rows (paged_chunk.cu) and the weights of many rows (paged_weigh.cu).
+// the 128-byte swizzle.  Shared by the attention of many rows (paged_chunk.cu) and the weights of many rows (paged_weigh_many.cu).
 #pragma once
 #include <cuda.h>
 
@@ -71,14 +71,6 @@ __device__ __forceinline__ void tc_wait_ld(uint32_t* r) {
 }
 __device__ __forceinline__ void tc_wait_ld16(uint32_t* r) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-                 :
-                 : "memory");
-}
-// More registers that a wait just before has brought.
-__device__ __forceinline__ void tc_landed16(uint32_t* r) {
-    asm volatile(""
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
                    "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
                  :

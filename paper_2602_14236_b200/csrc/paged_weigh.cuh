@@ -26,13 +26,13 @@ struct WgArgs {
 
 // Positions of a sequence that have a weight.
 __device__ __forceinline__ int wg_held(const PgSeq& s, const WgArgs& a) { return (int)min((long long)s.len, a.w_stride); }
-// What position j of (sequence b, head h) had before, of which decay is left.
+// What position j of (sequence b, head h), which has rows in the call, had before, of which decay is left.
 __device__ __forceinline__ float wg_had(const WgArgs& a, const PgSeq& s, int b, int h, int j) {
-    if (!a.in || (s.n > 0 && j >= s.pos0)) return 0.0f;
+    if (!a.in || j >= s.pos0) return 0.0f;
     return a.in[((size_t)b * a.pc.heads + h) * a.w_stride + j];
 }
-__device__ __forceinline__ void wg_put(const WgArgs& a, const PgSeq& s, int b, int h, int j, float had, float sum) {
-    a.out[((size_t)b * a.pc.heads + h) * a.w_stride + j] = fmaf(s.n > 0 ? a.decay : 1.0f, had, sum);
+__device__ __forceinline__ void wg_put(const WgArgs& a, int b, int h, int j, float had, float sum) {
+    a.out[((size_t)b * a.pc.heads + h) * a.w_stride + j] = fmaf(a.decay, had, sum);
 }
 
 // paged_weigh_many.cu

@@ -57,13 +57,13 @@ __device__ __forceinline__ int wm_first(const PgSeq& s, const WgArgs& a, int j0)
 // Its positions with a weight; none, if the sequence is the other kernel's.
 __device__ __forceinline__ int wm_held(const PgSeq& s, const WgArgs& a) { return s.n * a.G > WG_FEW ? wg_held(s, a) : 0; }
 __device__ __forceinline__ int wm_items(const PgSeq& s, const WgArgs& a) { return (wm_held(s, a) + WM_KEYS - 1) / WM_KEYS; }
-// Units of an item: its fixed cost and its tiles, one at least (a sequence without rows has its weights copied).
+// Units of an item: its fixed cost and its tiles, of which there are some, since the last row sees every position.
 __device__ __forceinline__ int wm_units(const PgSeq& s, const WgArgs& a, int kt) {
-    return WM_ITEM + max(1, wm_rows(s, a) - wm_first(s, a, kt * WM_KEYS));
+    return WM_ITEM + wm_rows(s, a) - wm_first(s, a, kt * WM_KEYS);
 }
 // Items at the front that all rows see.
 __device__ __forceinline__ int wm_whole(const PgSeq& s, const WgArgs& a) {
-    return s.n == 0 ? wm_items(s, a) : min(wm_items(s, a), s.pos0 >= 0 ? s.pos0 / WM_KEYS + 1 : 0);
+    return min(wm_items(s, a), s.pos0 >= 0 ? s.pos0 / WM_KEYS + 1 : 0);
 }
 // Units of one head of the sequence that each lane of a warp has; the warp sums the items of long ones together.
 __device__ __forceinline__ long long wm_per_head(const WgArgs& a, const PgSeq& s) {
@@ -168,17 +168,16 @@ __device__ __forceinline__ void wm_next(WmWalk& w, const WgArgs& a) {
 // A block's share of one item.
 struct WmSeg {
     int k0, k1, tiles, rt, j0;               // units [k0, k1); tiles of rows from rt on; first key
-    bool first, last, real;                  // the item begins, ends here; some of its tiles are here
+    bool first, last;                        // the item begins, ends here
     __device__ __forceinline__ WmSeg(const WgArgs& a, const WmWalk& w) {
         j0 = w.kt * WM_KEYS;
-        const int f = j0 <= w.s.pos0 ? 0 : wm_first(w.s, a, j0), n = w.rows - f, units = WM_ITEM + max(1, n);
+        const int f = j0 <= w.s.pos0 ? 0 : wm_first(w.s, a, j0), units = WM_ITEM + w.rows - f;
         k0 = w.k;
         k1 = (int)min((long long)units, k0 + w.left);
         const int t0 = max(0, k0 - WM_ITEM), t1 = max(0, k1 - WM_ITEM);
         first = t0 == 0;
         last = k1 == units;
-        real = t1 > t0;
-        tiles = w.s.n == 0 ? 0 : t1 - t0;
+        tiles = t1 - t0;
         rt = f + t0;
     }
     // Page of keys 16 grp .. of the item: -2 there are none (or grp > 15), -1 there is no such page.
@@ -256,7 +255,7 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
     if (!*a.some) return;
     if (tid == 0) {
         for (int i = 0; i < WM_K; ++i) {
-            bar_init(smem_u32(&bars.k_full[i]), FMT == PF_16 ? 1 : 4);       // the feeder, or the warps of group 2
+            bar_init(smem_u32(&bars.k_full[i]), FMT == PF_16 ? 1 : 4);       // the feeder, or the warps of group 4
             bar_init(smem_u32(&bars.k_empty[i]), 1);
         }
         for (int i = 0; i < WM_Q; ++i) {
@@ -313,7 +312,7 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
             const int j = g.j0 + key;
             float sum = 0.0f;
             const bool mine = j < w.held;
-            const bool writes = g.tiles > 0 ? (int)((n + g.tiles - 1) & 1) == part : part == 0;        // the group that has the last tile
+            const bool writes = g.tiles > 0 && (int)((n + g.tiles - 1) & 1) == part;       // the group that has the last tile
             if (writes && mine && a.in)      // what the key had is looked at when the tiles are through: no register holds it until then
                 asm volatile("prefetch.global.L2 [%0];" ::"l"(a.in + ((size_t)w.b * a.pc.heads + w.h) * a.w_stride + j));
             for (int t = 0; t < g.tiles; ++t, ++n) {
@@ -398,9 +397,9 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
                 if (writes && (!(*(volatile uint32_t*)&bars.pages[n_item & 7] >> (key >> 4) & 1u) || sum < 1e-33f)) sum = 0.0f;
                 ++n_item;
             }
-            if (g.real && writes) {
+            if (writes) {
                 if (g.first && g.last) {
-                    if (mine) wg_put(a, w.s, w.b, w.h, j, had, sum);
+                    if (mine) wg_put(a, w.b, w.h, j, had, sum);
                 } else {
                     a.part[(2 * (size_t)blockIdx.x + (g.first ? 1 : 0)) * WM_KEYS + key] = sum;
                     if (key == 0) {
@@ -551,7 +550,7 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
             bool ok = true;
             const int per_page = 1 << a.pc.page_shift;
             if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
-            // the keys of an item, those of 16-bit pages: group 2 brings the others
+            // the keys of an item, those of 16-bit pages: group 4 brings the others
             auto feed_keys = [&](const WmWalk& x, const WmSeg& g) -> bool {
                 const uint32_t kb = n_item % WM_K, bar = smem_u32(&bars.k_full[kb]);
                 const int pid16 = g.page_of(a, x, lane);
@@ -690,7 +689,7 @@ k_weigh_join(WgArgs a, int blocks) {
     const PgSeq s = pg_seq(a.sq, a.pc, b);
     float sum = 0.0f;
     for (int i = 0; i < n; ++i) sum += a.part[(size_t)list[i] * WM_KEYS + threadIdx.x];
-    if (j < wm_held(s, a)) wg_put(a, s, b, h, j, wg_had(a, s, b, h, j), sum);
+    if (j < wm_held(s, a)) wg_put(a, b, h, j, wg_had(a, s, b, h, j), sum);
 }
 
 template <typename T, int FMT, int D>
