@@ -327,8 +327,9 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
                 const int c_lo = max(0, min(128, max(0, j - w.s.pos0) * a.G - r0));          // rows before this column do not see the key
                 // A column that is no row has the sum WG_NONE, which leaves nothing of a finite score, and is masked where it may meet
                 // another one: the zeros behind a tile's rows under a key that is not finite, a row that counts as none.  `whole` tiles have
-                // the former among the last 16 columns and none of the latter.  (Masks in all columns of tiles with zeros: 5 % of their
-                // time; masks in 16 columns of all: 2 %; the zeros' tiles in a third copy of this code: 1 %, but 5 % of 64 rows a sequence.)
+                // the former, where 128 is no multiple of G, among the last 16 columns, and none of the latter.  (The last 16 columns masked
+                // in every tile: a prompt of 8192 rows 308 us instead of 298.  Such tiles in a third copy of this code: 5 % more for
+                // 64 rows a sequence, whose time goes into walks and waits.)
                 uint64_t acc[2] = {0ull, 0ull};  // the first one's lower half has the polynomial's columns alone
                 float top = -INFINITY;
                 const uint64_t scale2 = pair2(a.scale, a.scale);
@@ -341,30 +342,34 @@ k_weigh_many(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorM
                     for (int c = 0; c < 8; ++c) {
                         if (c < 7) tc_ld16(x[(c + 1) & 1], S + 16 * (c + 1));
                         const uint32_t(&y)[16] = x[c & 1];
-                        const bool MASKED = !WHOLE || c == 7;
-                        uint32_t sees = MASKED ? *(volatile uint32_t*)&bars.counts[part][c >> 1] >> (16 * (c & 1)) : 0u;
-                        if (!WHOLE) sees &= ~below(c_lo - 16 * c);
                         ulonglong2 l[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) l[i] = ls[4 * c + i];
-                        if (c == 7) {            // the scores and their rows' sums are in registers
-                            tc_before();
-                            __syncwarp();
-                            if (lane == 0) bar_arrive(smem_u32(&bars.s_free[part][half]));
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float lo, hi;
-                            const uint64_t minus = i & 1 ? l[i >> 1].y : l[i >> 1].x;
-                            split2(fma2x(pair2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), scale2, minus), lo, hi);
-                            lo = !MASKED && WM_POLY(i) ? ex2_fma(lo, top) : ex2(lo);
-                            hi = ex2(hi);
-                            if (MASKED) {
-                                lo = sees & 1u << (2 * i) ? lo : 0.0f;
-                                hi = sees & 2u << (2 * i) ? hi : 0.0f;
+                        auto sixteen = [&](auto masked_) {
+                            constexpr bool MASKED = decltype(masked_)::value;
+                            uint32_t sees = MASKED ? *(volatile uint32_t*)&bars.counts[part][c >> 1] >> (16 * (c & 1)) : 0u;
+                            if (!WHOLE) sees &= ~below(c_lo - 16 * c);
+                            if (c == 7) {        // the scores and their rows' sums are in registers
+                                tc_before();
+                                __syncwarp();
+                                if (lane == 0) bar_arrive(smem_u32(&bars.s_free[part][half]));
                             }
-                            acc[!WM_POLY(i)] = add2x(acc[!WM_POLY(i)], pair2(lo, hi));
-                        }
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                float lo, hi;
+                                const uint64_t minus = i & 1 ? l[i >> 1].y : l[i >> 1].x;
+                                split2(fma2x(pair2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), scale2, minus), lo, hi);
+                                lo = !MASKED && WM_POLY(i) ? ex2_fma(lo, top) : ex2(lo);
+                                hi = ex2(hi);
+                                if (MASKED) {
+                                    lo = sees & 1u << (2 * i) ? lo : 0.0f;
+                                    hi = sees & 2u << (2 * i) ? hi : 0.0f;
+                                }
+                                acc[!WM_POLY(i)] = add2x(acc[!WM_POLY(i)], pair2(lo, hi));
+                            }
+                        };
+                        if (WHOLE && (c < 7 || HR == 128)) sixteen(std::false_type{});
+                        else sixteen(std::true_type{});
                         if (c < 7) tc_wait_ld16(x[(c + 1) & 1]);
                     }
                 };
