@@ -5,7 +5,8 @@
 // halves of 128 = the lanes of tensor memory; scores S = Q K^T and sums O += P V of both halves stand in all 512 columns.
 // Roles by warp group:
 //   0, 1   one thread per row of half 0 / 1: maximum over the row's 128 scores, weights, row sum; P overwrites S as the
-//          16-bit operand of the second product, handed on in two parts; also the output
+//          16-bit operand of the second product, handed on in two parts; also the output.  The row sum is of the unrounded
+//          weights, in binary32; what P's rounding adds to the output's own is in paged_attend.cu
 //   2      codes from a ring of raw stages to 16-bit operands; of 16-bit pages only the V tiles that hold positions no
 //          row sees, which become zeros whatever the page holds there
 //   3      one thread issues the matrix instructions; one warp feeds the rings with bulk copies, a lane per page: tensor

@@ -10,8 +10,9 @@
 // Moving.  A block has the rows that a tile of a list's entries names, K and V of one head, 16 bytes a lane.  Into other pages all
 // tiles of a list move at once.  In place one block takes a list's tiles in turn, and reads a tile before it writes it: entry
 // k of an ascending list is at least first + k, so what a tile writes lies below all that later tiles read.
-// Bound by memory: 32768 rows of 8 heads x 128 in 16 bits, 268 MB: 45 to 49 us = 5.5 to 6.0 TB/s, 0.86 to 0.93 of the copy
-// bandwidth; 31127 rows of INT4 codes, 68 MB: 14 us.
+// Into other pages bound by memory: 32768 rows of 8 heads x 128 in 16 bits, 268 MB: 45 to 47 us = 5.7 to 6.0 TB/s, 0.89 to 0.93 of the
+// copy bandwidth; 31127 rows of INT4 codes, 68 MB: 14 us.  In place, where a block per list has one tile after the other under way: 163
+// and 32 us.
 #include "paged_async.cuh"
 #include "paged.cuh"
 

@@ -14,7 +14,8 @@
 // for 8 elements.
 // Measured: four frames (11520 rows of 32 query and 8 key/value heads x 128) into INT4 pages, 248 MB: 47 to 49 us = 5.2 TB/s = 0.80
 // of the copy bandwidth, 65 % of the issue slots used (K and V alone take 19, of which the turning 5); prompts of 5864 rows of 12
-// heads x 64, 54 MB: 13 us, of which a third is look-ups and angles before the first row; a token each of 32 streams 4.2 us.
+// heads x 64, 54 MB: 13 us (11 with the rows in the L2 from the pass before, as the variants below were timed), of which a third is
+// look-ups and angles before the first row; a token each of 32 streams 4.2 us in a graph.
 #include <math.h>
 
 #include "paged_async.cuh"
@@ -190,7 +191,7 @@ int launch_rotary(salicache_ctx* c, const RtCall& a, cudaStream_t st) {
     while (per > PM_AHEAD && tiles * (shares(pairs, per) + shares(a.q_heads, per)) < 3ll * c->sm_count) per = (per + 1) / 2;
     per = (per + PM_AHEAD - 1) / PM_AHEAD * PM_AHEAD;
     const int kv_shares = shares(pairs, per), all = kv_shares + shares(a.q_heads, per);
-    const dim3 grid((unsigned)(tiles * all));            // below 2^30 rows / 16 tiles times 256 shares
+    const dim3 grid((unsigned)(tiles * all));            // below 2^28: a tile has 16 rows at least, and many tiles have two shares each
     SC_CHECK(pt_launch(k_paged_write_rotary<T, FMT, D, HALVES>, grid, PM_THREADS, 0, st, a.pc, a.sq, a.rt, a.pos, a.q, a.q_out, a.K, a.V, a.qs,
                        a.qos, a.ks, a.vs, a.q_heads, all, kv_shares, per, c->d_status));
     c->launches++;

@@ -10,9 +10,10 @@
 // end.  Every warp has a ring of its own in shared memory, which its first lanes fill by bulk copies of 16 keys' rows and scales.  All
 // groups of keys stand in one line, of which every warp takes an equal stretch, so that the lengths on the device decide the
 // split, and warps never wait for one another.
-// Measured, 16 sequences of 8000 positions, 8 heads x 128, one token and four query heads a group (four tokens): 16-bit pages 52 us
-// (58) = 5.1 TB/s, bound by memory; INT8 36 us (44), INT4 36 us (45), bound by issue slots: some 320 instructions go into 16 INT4
-// keys of a head, 112 of them turn codes into numbers.
+// Measured, 16 sequences of 8000 positions, 8 heads x 128, one token and four query heads a group (four tokens), with the launches of
+// the other kernel, which return at once: 16-bit pages 55 us (55) = 4.9 TB/s, bound by memory; INT8 39 us (45), INT4 38 us (47), bound
+// by neither memory nor issue slots alone: some 320 instructions go into 16 INT4 keys of a head, 112 of them turn codes into numbers,
+// and take 64 % of the issue slots; the rest is fixed latencies of one chain of products after the other.
 #include <limits.h>
 #include <math.h>
 

@@ -15,8 +15,8 @@
 //          one the rows' sums
 // K is double-buffered, and read once per item; the rows of q come once per tile, from the L2.
 //
-// Measured: a prompt of 8192 rows, 32 query and 8 key/value heads x 128: 290 us, 330 us once the clocks have settled under load,
-// = 830 to 950 TFLOP/s of the products.  A tile takes 2200 clocks: 2048 its 32768 exponentials would take on the special-function unit
+// Measured: a prompt of 8192 rows, 32 query and 8 key/value heads x 128: 298 us, 333 us once the clocks have settled under load,
+// = 825 to 925 TFLOP/s of the products.  A tile takes 2200 clocks: 2048 its 32768 exponentials would take on the special-function unit
 // alone (69 % of it used, an eighth of them being elsewhere), 1024 the products (39 % of the tensor pipe).  Tried: 8 warps for the
 // weights, which wait for the tensor memory at the same time (361 us with three stages of rows, 513 with two), two keys a thread
 // (424), both halves of the warps on every tile (368).  A sequence's few rows over a long cache (64 to 256 of them over 8000
@@ -35,8 +35,8 @@ namespace {
 
 constexpr int WM_KEYS = 256, WM_K = 2, WM_Q = 3;
 // The pairs of columns of which the first takes its exponentials on the FMA pipe instead of the special-function unit: one column in
-// eight.  A prompt of 8192 rows with none, one, two of eight: 314, 290, 298 us; one call after the other, until the clocks have settled:
-// 339, 330, 343.
+// eight.  A prompt of 8192 rows with none, one, two of eight, before the last columns' masks: 314, 290, 298 us; one call after the other,
+// until the clocks have settled: 339, 330, 343.
 __device__ __forceinline__ constexpr bool WM_POLY(int pair) { return (pair & 3) == 0; }
 // An item's fixed cost (its keys) in tiles' time.
 constexpr int WM_ITEM = 2;
