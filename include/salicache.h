@@ -571,7 +571,7 @@ SALICACHE_API int salicache_paged_attend_tree(salicache_ctx* ctx, const salicach
  *   decay         0 .. 1: 1 adds up over all calls, less forgets older ones
  * Positions in no page gain nothing (deferred E_CAPACITY); positions at or past weight_stride are left out (deferred
  * E_CAPACITY).  A position's sum below 1e-33 may count as 0.  To weigh by the last m rows of a prompt only, let d_row_start name those m: the positions before them then
- * have to hold their weights, or zeros.  A row's -infinity in d_lse (it sees nothing) counts as no row.
+ * have to hold their weights, or zeros.  A row's -infinity in d_lse (it sees nothing) counts as no row, whatever its q holds.
  * q, pages, seqs, d_work and errors as for salicache_paged_attend; E_PARAM also for a decay outside [0, 1], E_SHAPE for
  * weight_stride < 1.
  */
